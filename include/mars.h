@@ -378,6 +378,104 @@ MARS_API mars_status_t mars_profile_read(mars_model_t *model, double *ms_per_cla
  * of distinct experts selected per layer; valid after the step's stream is synchronised. */
 MARS_API const int32_t *mars_active_experts_device(const mars_model_t *model);
 
+/* ---- operators of the policy update ------------------------------------------------------------
+ * The step above rolls out and scores; these calls are what a trainer needs next to it: the
+ * log-probability of known tokens WITH its gradient (Eq. 3 differentiates log pi_theta(o_t | q, o_<t)),
+ * the products of the mixture's experts with their two gradients, and the norm over all gradients with
+ * clipping.  They work on plain device tensors, need no model and no cache, upload nothing and wait for
+ * nothing, so they may be captured into a CUDA graph (a captured call replays on the pointers it was given; two
+ * graphs that are replayed at the same time need a handle each).
+ *
+ * mars_update_t holds the workspace of the first two groups: `hidden` x `vocab` is the lm_head, max_tokens
+ * the largest number of rows of a log-prob call.  hidden = vocab = max_tokens = 0 makes a handle for the
+ * expert products alone.  hidden: a multiple of 8, at least 8; vocab >= 1.  Workspace: 256-byte aligned device
+ * memory of the device that is current at creation (the handle's device; calls made while another device is
+ * current switch to it and back), its content private between calls.  One call at a time per handle, on the
+ * GPU as well: calls on several streams are to be ordered by the caller.  mars_update_poll_status works as
+ * mars_poll_status (MARS_OK, MARS_ERR_BAD_TOKEN, MARS_ERR_TIMEOUT). */
+typedef struct mars_update mars_update_t;
+enum { MARS_F32 = 0, MARS_BF16 = 1, MARS_F16 = 2 };
+MARS_API size_t mars_update_workspace_bytes(int32_t hidden, int32_t vocab, int32_t max_tokens);
+MARS_API mars_status_t mars_update_create(int32_t hidden, int32_t vocab, int32_t max_tokens, void *workspace,
+                                          size_t workspace_bytes, mars_update_t **out);
+MARS_API mars_status_t mars_update_free(mars_update_t *update);
+MARS_API mars_status_t mars_update_poll_status(mars_update_t *update);
+
+/* mars_logprob: for every row i of `hidden` (bf16 [n_tokens][ld_hidden], the final normalised hidden states; the
+ * first `hidden` elements of a row count),
+ *   out_logprobs[i] = log softmax(lm_head hidden_i / temperature)[targets[i]],
+ *   out_lse[i]      = log sum_v exp((lm_head hidden_i)_v / temperature)          (what the gradient needs)
+ * in fp32, over the full vocabulary and without ever holding the logits; both are 0 where targets[i] < 0
+ * (prompt and padding rows: their hidden states are not read and may hold anything).  A target >= vocab counts as
+ * < 0 and is reported by mars_update_poll_status.
+ *
+ * mars_logprob_grad: with the same hidden, lm_head, targets and temperature, the lse of mars_logprob and
+ * d_logprobs[i] = d loss / d logp_i (fp32; for Eq. 3 the clipped importance ratio times the advantage):
+ *   d_hidden[i]  = d_logprobs[i] / temperature (lm_head[targets[i]] - sum_v p_iv lm_head[v])      bf16
+ *   d_lm_head[v] = sum_i d_logprobs[i] / temperature ([v = targets[i]] - p_iv) hidden_i           bf16 or fp32
+ * The vocabulary is worked off in pieces; the probabilities of a piece are computed again from hidden and
+ * lse.  Rows without a target and rows with d_logprobs = 0 take no part: their d_hidden is 0, whatever
+ * their hidden states hold.  accumulate_d_lm_head != 0 adds to what d_lm_head holds (micro-batches); the sum is
+ * formed in fp32 and rounded once to the type of d_lm_head.  Precision: d loss / d logit is rounded to bf16
+ * (relative 2^-8, independent per entry) before the two products, which accumulate in fp32.
+ * n_tokens = 0 is allowed (d_lm_head is then zeroed, or left when it accumulates).  Row strides are in elements
+ * and multiples of 8; matrices are 16-byte aligned, d_hidden [n_tokens][ld_d_hidden].  Outputs must not overlap inputs.
+ * The same call on the same inputs gives the same bits. */
+MARS_API mars_status_t mars_logprob(mars_update_t *update, void *cuda_stream, int32_t n_tokens, const void *hidden,
+                                    int64_t ld_hidden, const void *lm_head, const int32_t *targets, float temperature,
+                                    float *out_logprobs, float *out_lse);
+MARS_API mars_status_t mars_logprob_grad(mars_update_t *update, void *cuda_stream, int32_t n_tokens, const void *hidden,
+                                         int64_t ld_hidden, const void *lm_head, const int32_t *targets, float temperature,
+                                         const float *lse, const float *d_logprobs, void *d_hidden, int64_t ld_d_hidden,
+                                         void *d_lm_head, int32_t d_lm_head_type, int32_t accumulate_d_lm_head);
+
+/* Products of the mixture's experts: rows that are sorted by expert (the expert slots of a token permutation,
+ * see expert_off in mars_debug_t), expert e owning rows expert_off[e] .. expert_off[e + 1] - 1:
+ *   mars_expert_matmul      y_r  = w_e x_r           x [n_rows][ld_x], w [n_experts][d_out][d_in], y [n_rows][ld_y]
+ *   mars_expert_matmul_dx   dx_r = w_e^T dy_r
+ *   mars_expert_matmul_dw   dw_e = sum_r dy_r x_r^T  dw [n_experts][d_out][d_in], 0 for an expert without rows
+ * x, w, dy are bf16, sums fp32; y, dx, dw are bf16 (rounded once) or fp32; accumulate != 0 adds to what dw holds.
+ * expert_off: DEVICE int32 [n_experts + 1], read on the device (no host copy, capturable).  Rows outside
+ * [expert_off[0], expert_off[n_experts]) are not touched; their inputs may hold anything, and so may the rows
+ * of other experts: nothing crosses a group's border.  Offsets are clamped to [0, n_rows] and a decreasing
+ * offset counts as equal to the largest before it.  n_rows = 0 is allowed.  1 <= n_experts <= 1024; d_in, d_out and
+ * row strides multiples of 8; matrices 16-byte aligned; outputs must not overlap inputs.  Same bits on every call. */
+MARS_API mars_status_t mars_expert_matmul(mars_update_t *update, void *cuda_stream, int32_t n_experts, int32_t n_rows,
+                                          int32_t d_in, int32_t d_out, const void *x, int64_t ld_x, const int32_t *expert_off,
+                                          const void *w, void *y, int64_t ld_y, int32_t y_type);
+MARS_API mars_status_t mars_expert_matmul_dx(mars_update_t *update, void *cuda_stream, int32_t n_experts, int32_t n_rows,
+                                             int32_t d_in, int32_t d_out, const void *dy, int64_t ld_dy,
+                                             const int32_t *expert_off, const void *w, void *dx, int64_t ld_dx,
+                                             int32_t dx_type);
+MARS_API mars_status_t mars_expert_matmul_dw(mars_update_t *update, void *cuda_stream, int32_t n_experts, int32_t n_rows,
+                                             int32_t d_in, int32_t d_out, const void *dy, int64_t ld_dy, const void *x,
+                                             int64_t ld_x, const int32_t *expert_off, void *dw, int32_t dw_type,
+                                             int32_t accumulate);
+
+/* Gradient lists.  mars_grads_create records n_tensors (grad, out, numel, type) entries; the pointers are borrowed
+ * for the lifetime of the handle, the table is copied into `workspace` (device memory, 256-byte aligned,
+ * mars_grads_bytes(n_tensors)) before the call returns.  type: MARS_F32, MARS_BF16 or MARS_F16, of grad and out
+ * alike; any element-aligned address (places in a flat buffer); numel 0 is allowed.  out = grad scales in place,
+ * another out leaves the gradients as they are; an out that overlaps anything but its own grad in full is refused.
+ *   mars_grads_norm   *out_norm = sqrt of the sum of all squares (device fp32), summed in fp32 / fp64
+ *   mars_grads_clip   the same, and out_t = grad_t min(1, max_norm / (norm + 1e-6)), rounded once to its type.
+ * max_norm >= 0.  A NaN norm makes every out NaN; an infinite one makes finite values 0.  Where nothing has to be
+ * scaled, tensors in place are not touched.  One call at a time per handle; same bits on every call. */
+typedef struct {
+    const void *grad;
+    void *out;
+    int64_t numel;
+    int32_t type;
+    int32_t reserved;
+} mars_grad_t;
+typedef struct mars_grads mars_grads_t;
+MARS_API size_t mars_grads_bytes(int32_t n_tensors);
+MARS_API mars_status_t mars_grads_create(const mars_grad_t *tensors /*host*/, int32_t n_tensors, void *workspace,
+                                         size_t workspace_bytes, mars_grads_t **out);
+MARS_API mars_status_t mars_grads_free(mars_grads_t *grads);
+MARS_API mars_status_t mars_grads_norm(mars_grads_t *grads, void *cuda_stream, float *out_norm);
+MARS_API mars_status_t mars_grads_clip(mars_grads_t *grads, void *cuda_stream, float max_norm, float *out_norm);
+
 MARS_API int32_t mars_last_cuda_error(void);
 MARS_API const char *mars_status_string(mars_status_t status);
 MARS_API const char *mars_version(void);

@@ -65,6 +65,10 @@ class mars_step_info_t(ctypes.Structure):
                 ("kv_tokens_streamed", c_int64)]
 
 
+class mars_grad_t(ctypes.Structure):
+    _fields_ = [("grad", c_void_p), ("out", c_void_p), ("numel", c_int64), ("type", c_int32), ("reserved", c_int32)]
+
+
 # name -> (restype, argtypes); mirrors include/mars.h one to one
 SIGNATURES = {
     "mars_workspace_bytes": (c_size_t, [POINTER(mars_config_t), c_int32, c_int32]),
@@ -111,6 +115,25 @@ SIGNATURES = {
     "mars_profile_read": (c_int32, [c_void_p, POINTER(ctypes.c_double), POINTER(c_int64)]),
     "mars_last_step_info": (c_int32, [c_void_p, POINTER(mars_step_info_t)]),
     "mars_active_experts_device": (c_void_p, [c_void_p]),
+    "mars_update_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32]),
+    "mars_update_create": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_size_t, POINTER(c_void_p)]),
+    "mars_update_free": (c_int32, [c_void_p]),
+    "mars_update_poll_status": (c_int32, [c_void_p]),
+    "mars_logprob": (c_int32, [c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_void_p,
+                               c_void_p]),
+    "mars_logprob_grad": (c_int32, [c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_void_p,
+                                    c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_int32]),
+    "mars_expert_matmul": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p,
+                                     c_void_p, c_void_p, c_int64, c_int32]),
+    "mars_expert_matmul_dx": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p,
+                                        c_void_p, c_void_p, c_int64, c_int32]),
+    "mars_expert_matmul_dw": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p,
+                                        c_int64, c_void_p, c_void_p, c_int32, c_int32]),
+    "mars_grads_bytes": (c_size_t, [c_int32]),
+    "mars_grads_create": (c_int32, [POINTER(mars_grad_t), c_int32, c_void_p, c_size_t, POINTER(c_void_p)]),
+    "mars_grads_free": (c_int32, [c_void_p]),
+    "mars_grads_norm": (c_int32, [c_void_p, c_void_p, c_void_p]),
+    "mars_grads_clip": (c_int32, [c_void_p, c_void_p, c_float, c_void_p]),
     "mars_last_cuda_error": (c_int32, []),
     "mars_status_string": (c_char_p, [c_int32]),
     "mars_version": (c_char_p, []),
@@ -410,3 +433,191 @@ def mars_decode_step_static(model_shape: dict, weights: dict, max_pos: int, k_po
                                              page_size, _ptr(block_table), block_table.shape[1], lens,
                                              _stream_handle(stream), n, _ptr(in_tokens), byref(sampling),
                                              _ptr(out_tokens), _ptr(out_logprobs))
+
+
+# ------------------------------------------------------------------------- operators of the policy update
+
+MARS_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _want(t: torch.Tensor, name: str, dtypes, dev: torch.device, *shape, rows: bool = False):
+    """Raises ValueError unless `t` has one of the dtypes and the shape, lies on the handle's device and is
+    contiguous (rows: its rows are, with any row stride)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected {tuple(str(d) for d in dtypes)} {shape}, got "
+                         f"{getattr(t, 'dtype', type(t))} {tuple(getattr(t, 'shape', ()))}")
+    if t.device != dev:
+        raise ValueError(f"{name}: on {t.device}, the handle on {dev}")
+    ok = t.is_contiguous() or (rows and t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1) and
+                               t.stride(0) >= t.shape[1])
+    if not ok:
+        raise ValueError(f"{name}: strides {t.stride()} are not supported")
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+class Update:
+    """mars_update_create / mars_update_free: the handle of the log-prob and expert-product calls.  hidden, vocab:
+    shape of the lm_head; max_tokens: largest number of rows of a log-prob call (all 0: expert products only)."""
+
+    def __init__(self, hidden: int = 0, vocab: int = 0, max_tokens: int = 0, device="cuda"):
+        self.hidden, self.vocab, self.max_tokens = hidden, vocab, max_tokens
+        nbytes = lib().mars_update_workspace_bytes(hidden, vocab, max_tokens)
+        if nbytes == 0:
+            raise MarsError(2, "mars_update_workspace_bytes")
+        with torch.cuda.device(torch.device(device)):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+            self.device = self.workspace.device
+            torch.cuda.current_stream().synchronize()      # the memory may still be in use by an earlier owner's kernels
+            handle = c_void_p()
+            _check(lib().mars_update_create(hidden, vocab, max_tokens, _ptr(self.workspace), nbytes, byref(handle)),
+                   "mars_update_create")
+        self.handle = handle
+
+    def poll_status(self) -> int:
+        return lib().mars_update_poll_status(self.handle)
+
+    def _stream(self, stream) -> c_void_p:
+        return c_void_p((stream if stream is not None else torch.cuda.current_stream(self.device)).cuda_stream)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().mars_update_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def mars_logprob(update: Update, hidden: torch.Tensor, lm_head: torch.Tensor, targets: torch.Tensor, temperature: float,
+                 out_logprobs: torch.Tensor, out_lse: torch.Tensor, stream=None) -> int:
+    """Log-probs of `targets` (int32 [n], < 0 = none) given hidden states (bf16 [n, hidden], any row stride); returns
+    the status code."""
+    n, dev = hidden.shape[0], update.device
+    _want(hidden, "hidden", (torch.bfloat16,), dev, n, update.hidden, rows=True)
+    _want(lm_head, "lm_head", (torch.bfloat16,), dev, update.vocab, update.hidden)
+    _want(targets, "targets", (torch.int32,), dev, n)
+    _want(out_logprobs, "out_logprobs", (torch.float32,), dev, n)
+    _want(out_lse, "out_lse", (torch.float32,), dev, n)
+    return lib().mars_logprob(update.handle, update._stream(stream), n, _ptr(hidden), _ld(hidden), _ptr(lm_head),
+                              _ptr(targets), float(temperature), _ptr(out_logprobs), _ptr(out_lse))
+
+
+def mars_logprob_grad(update: Update, hidden: torch.Tensor, lm_head: torch.Tensor, targets: torch.Tensor, temperature: float,
+                      lse: torch.Tensor, d_logprobs: torch.Tensor, d_hidden: torch.Tensor, d_lm_head: torch.Tensor,
+                      accumulate: bool = False, stream=None) -> int:
+    """d_hidden (bf16) and d_lm_head (bf16 or fp32) of sum_i d_logprobs[i] logp_i, `lse` from mars_logprob; returns the
+    status code.  accumulate: add to d_lm_head."""
+    n, dev = hidden.shape[0], update.device
+    _want(hidden, "hidden", (torch.bfloat16,), dev, n, update.hidden, rows=True)
+    _want(lm_head, "lm_head", (torch.bfloat16,), dev, update.vocab, update.hidden)
+    _want(targets, "targets", (torch.int32,), dev, n)
+    _want(lse, "lse", (torch.float32,), dev, n)
+    _want(d_logprobs, "d_logprobs", (torch.float32,), dev, n)
+    _want(d_hidden, "d_hidden", (torch.bfloat16,), dev, n, update.hidden, rows=True)
+    _want(d_lm_head, "d_lm_head", (torch.bfloat16, torch.float32), dev, update.vocab, update.hidden)
+    return lib().mars_logprob_grad(update.handle, update._stream(stream), n, _ptr(hidden), _ld(hidden), _ptr(lm_head),
+                                   _ptr(targets), float(temperature), _ptr(lse), _ptr(d_logprobs), _ptr(d_hidden),
+                                   _ld(d_hidden), _ptr(d_lm_head), MARS_TYPES[d_lm_head.dtype], int(bool(accumulate)))
+
+
+def _expert_shapes(update: Update, w: torch.Tensor, expert_off: torch.Tensor, name: str, dtypes):
+    if not isinstance(w, torch.Tensor) or w.dim() != 3:
+        raise ValueError(f"{name}: expected [experts, d_out, d_in]")
+    E, d_out, d_in = w.shape
+    _want(w, name, dtypes, update.device, E, d_out, d_in)
+    _want(expert_off, "expert_off", (torch.int32,), update.device, E + 1)
+    return E, d_out, d_in
+
+
+def mars_expert_matmul(update: Update, x: torch.Tensor, expert_off: torch.Tensor, w: torch.Tensor, y: torch.Tensor,
+                       stream=None) -> int:
+    """y[r] = w[e] x[r] for the rows r of expert e (expert_off: int32 [experts + 1] on the device); returns the status code."""
+    E, d_out, d_in = _expert_shapes(update, w, expert_off, "w", (torch.bfloat16,))
+    rows, out = x.shape[0], (torch.bfloat16, torch.float32)
+    _want(x, "x", (torch.bfloat16,), update.device, rows, d_in, rows=True)
+    _want(y, "y", out, update.device, rows, d_out, rows=True)
+    return lib().mars_expert_matmul(update.handle, update._stream(stream), E, rows, d_in, d_out, _ptr(x), _ld(x),
+                                    _ptr(expert_off), _ptr(w), _ptr(y), _ld(y), MARS_TYPES[y.dtype])
+
+
+def mars_expert_matmul_dx(update: Update, dy: torch.Tensor, expert_off: torch.Tensor, w: torch.Tensor, dx: torch.Tensor,
+                          stream=None) -> int:
+    """dx[r] = w[e]^T dy[r]: the gradient of mars_expert_matmul to its rows; returns the status code."""
+    E, d_out, d_in = _expert_shapes(update, w, expert_off, "w", (torch.bfloat16,))
+    rows, out = dy.shape[0], (torch.bfloat16, torch.float32)
+    _want(dy, "dy", (torch.bfloat16,), update.device, rows, d_out, rows=True)
+    _want(dx, "dx", out, update.device, rows, d_in, rows=True)
+    return lib().mars_expert_matmul_dx(update.handle, update._stream(stream), E, rows, d_in, d_out, _ptr(dy), _ld(dy),
+                                       _ptr(expert_off), _ptr(w), _ptr(dx), _ld(dx), MARS_TYPES[dx.dtype])
+
+
+def mars_expert_matmul_dw(update: Update, dy: torch.Tensor, x: torch.Tensor, expert_off: torch.Tensor, dw: torch.Tensor,
+                          accumulate: bool = False, stream=None) -> int:
+    """dw[e] = sum over the rows of expert e of dy[r] x[r]^T (added to dw if accumulate); returns the status code."""
+    E, d_out, d_in = _expert_shapes(update, dw, expert_off, "dw", (torch.bfloat16, torch.float32))
+    rows = x.shape[0]
+    _want(dy, "dy", (torch.bfloat16,), update.device, rows, d_out, rows=True)
+    _want(x, "x", (torch.bfloat16,), update.device, rows, d_in, rows=True)
+    return lib().mars_expert_matmul_dw(update.handle, update._stream(stream), E, rows, d_in, d_out, _ptr(dy), _ld(dy),
+                                       _ptr(x), _ld(x), _ptr(expert_off), _ptr(dw), MARS_TYPES[dw.dtype],
+                                       int(bool(accumulate)))
+
+
+class GradList:
+    """mars_grads_create / mars_grads_free over contiguous CUDA tensors (fp32, bf16 or fp16).  outs: where the
+    clipped gradients go, one tensor of the same type and size per gradient; None = in place."""
+
+    def __init__(self, grads, outs=None):
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if not grads or len(outs) != len(grads):
+            raise ValueError("grads and outs: the same number of tensors, at least one")
+        dev = grads[0].device
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            _want(g, f"grads[{i}]", tuple(MARS_TYPES), dev, *g.shape)
+            _want(o, f"outs[{i}]", (g.dtype,), dev, *g.shape)
+        if dev.type != "cuda":
+            raise ValueError("grads: expected CUDA tensors")
+        self._keep = (grads, outs)
+        table = (mars_grad_t * len(grads))()
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            table[i] = mars_grad_t(g.data_ptr(), o.data_ptr(), g.numel(), MARS_TYPES[g.dtype], 0)
+        nbytes = lib().mars_grads_bytes(len(grads))
+        with torch.cuda.device(dev):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            self.device = self.workspace.device
+            torch.cuda.current_stream().synchronize()
+            handle = c_void_p()
+            _check(lib().mars_grads_create(table, len(grads), _ptr(self.workspace), nbytes, byref(handle)), "mars_grads_create")
+        self.handle = handle
+
+    _stream = Update._stream
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().mars_grads_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def mars_grads_norm(grads: GradList, out_norm: torch.Tensor, stream=None) -> int:
+    """out_norm[0] = the 2-norm over all gradients of the list; returns the status code."""
+    _want(out_norm, "out_norm", (torch.float32,), grads.device, 1)
+    return lib().mars_grads_norm(grads.handle, grads._stream(stream), _ptr(out_norm))
+
+
+def mars_grads_clip(grads: GradList, max_norm: float, out_norm: torch.Tensor, stream=None) -> int:
+    """The norm, and every gradient scaled by min(1, max_norm / (norm + 1e-6)) into its out; returns the status code."""
+    _want(out_norm, "out_norm", (torch.float32,), grads.device, 1)
+    return lib().mars_grads_clip(grads.handle, grads._stream(stream), float(max_norm), _ptr(out_norm))

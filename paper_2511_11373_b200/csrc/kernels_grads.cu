@@ -1,0 +1,237 @@
+// The norm over all gradients of a list of tensors, and the list scaled down to a largest norm.
+//   norm = sqrt(sum_t sum_i t_i^2),   out_t = t min(1, max_norm / (norm + 1e-6))
+// Bound by HBM: the list is read once for the norm and, because no output may be written before the norm is
+// known, once more for the outputs.  The list is cut into chunks of kChunkBytes of a tensor's own memory; blocks
+// take chunks round robin, so one launch covers tensors of any number and size.  Squares are added in fp32 over
+// at most a chunk's share of one thread and in fp64 beyond; a chunk whose fp32 sum overflowed, or is so small
+// that squares were lost below the smallest fp32 number, is summed again in fp64.  All sums run in a fixed
+// order: the same list gives the same bits on every call.
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "update.h"
+
+namespace mars {
+
+namespace {
+constexpr int kChunkBytes = 32768, kThreads = 256;
+constexpr int kBlocksPerSm = 8;
+
+__host__ __device__ constexpr int elem_bytes(int type) { return type == 0 ? 4 : 2; }     // MARS_F32, MARS_BF16, MARS_F16
+
+__device__ __forceinline__ void unpack(uint4 v, int type, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if (type == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
+    } else if (type == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            f[2 * i] = t.x; f[2 * i + 1] = t.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[i] = __uint_as_float(w[i]); f[i + 4] = 0.f; }
+    }
+}
+__device__ __forceinline__ float load_one(const unsigned char* p, int type) {
+    if (type == 0) return *reinterpret_cast<const float*>(p);
+    if (type == 1) return __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(p));
+    return __half2float(*reinterpret_cast<const __half*>(p));
+}
+__device__ __forceinline__ void store_one(unsigned char* p, int type, float v) {
+    if (type == 0) *reinterpret_cast<float*>(p) = v;
+    else if (type == 1) *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(v);
+    else *reinterpret_cast<__half*>(p) = __float2half_rn(v);
+}
+
+// A chunk is what lies between two multiples of kChunkBytes of the tensor's memory, counted from its address
+// rounded down to 16 bytes: inside a chunk 16-byte loads are aligned, and only its ends can be ragged.
+struct Chunk {
+    const unsigned char *src, *lo, *hi;    // lo..hi: whole 16-byte pieces
+    unsigned char* dst;
+    int64_t begin, end;                    // bytes of the tensor covered, [begin, end)
+    int type;
+};
+
+__device__ __forceinline__ int find_tensor(const GradEntry* table, int n, int64_t chunk) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (table[mid].first_chunk <= chunk) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+__device__ __forceinline__ Chunk chunk_at(const GradEntry* table, int n, int64_t chunk) {
+    const GradEntry g = table[find_tensor(table, n, chunk)];
+    Chunk c;
+    c.type = g.type;
+    c.src = reinterpret_cast<const unsigned char*>(g.src);
+    c.dst = reinterpret_cast<unsigned char*>(g.dst);
+    const int64_t shift = (int64_t)((uintptr_t)g.src & 15), bytes = g.numel * elem_bytes(g.type);
+    const int64_t k = chunk - g.first_chunk;
+    c.begin = max((int64_t)0, k * kChunkBytes - shift);
+    c.end = min(bytes, (k + 1) * kChunkBytes - shift);
+    uintptr_t a = ((uintptr_t)c.src + c.begin + 15) & ~(uintptr_t)15, b = ((uintptr_t)c.src + c.end) & ~(uintptr_t)15;
+    if (b < a) b = a;
+    c.lo = reinterpret_cast<const unsigned char*>(a);
+    c.hi = reinterpret_cast<const unsigned char*>(b);
+    return c;
+}
+// Elements before the first and behind the last whole piece, by index 0 .. ragged() - 1 (at most 14).
+__device__ __forceinline__ int ragged_head(const Chunk& c) {
+    const int64_t h = min((int64_t)(c.lo - c.src), c.end) - c.begin;
+    return (int)(h / elem_bytes(c.type));
+}
+__device__ __forceinline__ int ragged_tail(const Chunk& c) {
+    const int64_t from = max((int64_t)(c.hi - c.src), c.begin + (int64_t)ragged_head(c) * elem_bytes(c.type));
+    return from < c.end ? (int)((c.end - from) / elem_bytes(c.type)) : 0;
+}
+__device__ __forceinline__ int64_t ragged_offset(const Chunk& c, int i, int head, int tail) {
+    const int eb = elem_bytes(c.type);
+    return i < head ? c.begin + (int64_t)i * eb : c.end - (int64_t)(tail - (i - head)) * eb;
+}
+
+__device__ __forceinline__ double block_sum_double(double v, double* scratch) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if (lane == 0) scratch[warp] = v;
+    __syncthreads();
+    double t = 0.;
+    for (int i = 0; i < (int)(blockDim.x >> 5); ++i) t += scratch[i];
+    return t;
+}
+
+__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const GradEntry* table, int n, int64_t n_chunks, double* partials,
+                                                             int32_t* ticket, float max_norm, float* norm_out, float* scale) {
+    __shared__ double scratch[kThreads / 32];
+    __shared__ int last;
+    pdl_wait();
+    double total = 0.;
+    for (int64_t chunk = blockIdx.x; chunk < n_chunks; chunk += gridDim.x) {
+        const Chunk c = chunk_at(table, n, chunk);
+        const int pieces = (int)((c.hi - c.lo) >> 4);
+        float sum = 0.f;
+        uint32_t seen = 0;
+        for (int i = threadIdx.x; i < pieces; i += kThreads) {
+            const uint4 v = ldg_stream(c.lo + (size_t)i * 16);
+            float f[8];
+            unpack(v, c.type, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(f[j], f[j], sum);
+            seen |= v.x | v.y | v.z | v.w;
+        }
+        const int head = ragged_head(c), tail = ragged_tail(c);
+        if (threadIdx.x < head + tail) {
+            const float f = load_one(c.src + ragged_offset(c, threadIdx.x, head, tail), c.type);
+            sum = fmaf(f, f, sum);
+            seen |= f != 0.f;
+        }
+        // squares of one thread that left the range of fp32: again in fp64 (an infinity or a NaN in the tensor
+        // comes out the same)
+        if (!(sum < 1e37f) || (sum < 1e-20f && (seen & (c.type == 0 ? 0x7fffffffu : 0x7fff7fffu)))) {
+            double d = 0.;
+            for (int i = threadIdx.x; i < pieces; i += kThreads) {
+                float f[8];
+                unpack(*reinterpret_cast<const uint4*>(c.lo + (size_t)i * 16), c.type, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d = fma((double)f[j], (double)f[j], d);
+            }
+            if (threadIdx.x < head + tail) {
+                const double f = load_one(c.src + ragged_offset(c, threadIdx.x, head, tail), c.type);
+                d = fma(f, f, d);
+            }
+            total += d;
+        } else {
+            total += sum;
+        }
+    }
+    total = block_sum_double(total, scratch);
+    if (threadIdx.x == 0) {
+        partials[blockIdx.x] = total;
+        __threadfence();
+        last = atomicAdd(ticket, 1) == (int)gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double t = 0.;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) t += __ldcg(partials + i);
+    t = block_sum_double(t, scratch);
+    if (threadIdx.x == 0) {
+        *ticket = 0;
+        const double norm = sqrt(t);
+        *norm_out = (float)norm;
+        if (scale) {
+            const double s = (double)max_norm / (norm + 1e-6);
+            *scale = s < 1. ? (float)s : (s >= 1. ? 1.f : __int_as_float(0x7fffffff));      // a NaN norm gives NaN
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const GradEntry* table, int n, int64_t n_chunks, const float* scale) {
+    pdl_wait();
+    const float s = *scale;
+    for (int64_t chunk = blockIdx.x; chunk < n_chunks; chunk += gridDim.x) {
+        const Chunk c = chunk_at(table, n, n_chunks - 1 - chunk);       // from the end: what the norm read last is in L2
+        if (s == 1.f && c.src == c.dst) continue;
+        const int pieces = (int)((c.hi - c.lo) >> 4), eb = elem_bytes(c.type);
+        const bool vec = (((uintptr_t)c.dst ^ (uintptr_t)c.src) & 15) == 0;
+        for (int i = threadIdx.x; i < pieces; i += kThreads) {
+            const int64_t at = (c.lo - c.src) + (int64_t)i * 16;
+            float f[8];
+            unpack(*reinterpret_cast<const uint4*>(c.src + at), c.type, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] *= s;
+            if (vec) {
+                uint4 o;
+                if (c.type == 0) {
+                    o = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                } else if (c.type == 1) {
+                    o = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+                } else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const __half2 h = __floats2half2_rn(f[2 * q], f[2 * q + 1]);
+                        w[q] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                    o = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                *reinterpret_cast<uint4*>(c.dst + at) = o;
+            } else {
+                for (int j = 0; j < 16 / eb; ++j) store_one(c.dst + at + j * eb, c.type, f[j]);
+            }
+        }
+        const int head = ragged_head(c), tail = ragged_tail(c);
+        if (threadIdx.x < head + tail) {
+            const int64_t at = ragged_offset(c, threadIdx.x, head, tail);
+            store_one(c.dst + at, c.type, load_one(c.src + at, c.type) * s);
+        }
+    }
+}
+}  // namespace
+
+int64_t grad_chunks(const void* src, int64_t numel, int type) {
+    const int64_t bytes = (int64_t)((uintptr_t)src & 15) + numel * elem_bytes(type);
+    return numel ? (bytes + kChunkBytes - 1) / kChunkBytes : 0;
+}
+int grad_blocks(int sms) { return sms * kBlocksPerSm; }
+
+cudaError_t launch_grad_norm(const GradEntry* table, int n_tensors, int64_t n_chunks, double* partials, int32_t* ticket,
+                             float max_norm, float* norm_out, float* scale, int blocks, cudaStream_t st) {
+    const int grid = (int)(n_chunks < 1 ? 1 : n_chunks < blocks ? n_chunks : blocks);
+    return launch_chained(grad_norm_kernel, dim3(grid), dim3(kThreads), 0, st, table, n_tensors, n_chunks, partials, ticket,
+                          max_norm, norm_out, scale);
+}
+cudaError_t launch_grad_scale(const GradEntry* table, int n_tensors, int64_t n_chunks, const float* scale, int blocks,
+                              cudaStream_t st) {
+    const int grid = (int)(n_chunks < 1 ? 1 : n_chunks < blocks ? n_chunks : blocks);
+    return launch_chained(grad_scale_kernel, dim3(grid), dim3(kThreads), 0, st, table, n_tensors, n_chunks, scale);
+}
+
+}  // namespace mars

@@ -4,12 +4,14 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 #include <new>
 #include <vector>
 
 #include "../../include/mars.h"
+#include "api_common.h"
 #include "kernels.h"
 
 namespace mars {
@@ -22,16 +24,7 @@ cudaError_t init_fattn_kernels();
 
 using namespace mars;
 
-static thread_local int32_t g_last_cuda_error = 0;
-
-#define CUDA_TRY(expr)                                   \
-    do {                                                 \
-        cudaError_t _e = (expr);                         \
-        if (_e != cudaSuccess) {                         \
-            g_last_cuda_error = (int32_t)_e;             \
-            return MARS_ERR_CUDA;                        \
-        }                                                \
-    } while (0)
+thread_local int32_t mars::g_last_cuda_error = 0;
 
 namespace {
 
@@ -41,8 +34,6 @@ constexpr int kUmmaMinTokens = 64;  // calls with more token rows take the tenso
 constexpr int kSharedRows = 4;      // decode rows per work item of the shared-prefix attention kernel on mma.sync
 constexpr int kSharedItemWords = 36; // capacity per shared item: the tcgen05 kernel's items hold 16 rows
 constexpr int kMinSharedTokens = 128;  // shorter common prefixes are read per row as usual
-
-size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 struct Caps {
     int n_tok;     // token rows per call
@@ -147,12 +138,16 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-static mars_status_t make_tiled_map(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims,
-                                    const cuuint64_t* strides_bytes, const cuuint32_t* box) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
-    if (!fn || qres != cudaDriverEntryPointSuccess) return MARS_ERR_UNSUPPORTED;
+mars_status_t mars::make_tiled_map(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims,
+                                   const cuuint64_t* strides_bytes, const cuuint32_t* box) {
+    static std::atomic<void*> known{nullptr};      // looked up once per process
+    void* fn = known.load(std::memory_order_relaxed);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult qres;
+        CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
+        if (!fn || qres != cudaDriverEntryPointSuccess) return MARS_ERR_UNSUPPORTED;
+        known.store(fn, std::memory_order_relaxed);
+    }
     const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
     CUresult r = ((EncodeTiledFn)fn)(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims,
                                      strides_bytes, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
