@@ -54,26 +54,76 @@ __device__ __forceinline__ void mb_expect(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void mb_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+// Bounded wait: at most kSpin polls and about two seconds.  CLUSTER: acquires plain writes of the other CTA too
+// (a copy's or an MMA's arrival needs no such scope).
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mb_wait(uint64_t* bar, uint32_t parity) {
+    uint64_t begin = 0;
     for (uint32_t i = 0; i < kSpin; ++i) {
         uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+        if (CLUSTER)
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+        else
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
         if (ok) return true;
+        if ((i & 1023) == 1023) {
+            uint64_t t;
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+            if (!begin) begin = t;
+            else if (t - begin > 2000000000ull) return false;
+        }
     }
     return false;
 }
-__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+// Address of the same shared-memory object in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
 }
-__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-        ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
+__device__ __forceinline__ void mb_arrive_at(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// One lane of a converged warp.  The loops around it stay warp-uniform, so that the compiler keeps stage
+// counters, addresses and descriptors in uniform registers, which the copy and MMA instructions take: with the
+// whole loop under `if (lane == 0)` an MMA cost its issuing lane about twice its time on the tensor cores.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// CG = 2: the barrier may be the other CTA's (`bar`: cluster address).
+template <int CG>
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint32_t bar) {
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
+    if (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+            ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+            ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 // Shared-memory matrix descriptor (version 1, 128-byte swizzle).  K-major: rows of 128 B, groups of 8 rows 1024 B
 // apart (stride offset), the leading offset unused.  MN-major: a row of 128 B holds 64 consecutive columns of one
@@ -94,16 +144,29 @@ template <int CG, bool A_MN, bool B_MN>
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
                             ((uint32_t)(kTileN >> 3) << 17) | ((uint32_t)(Cfg<CG>::kTileM >> 4) << 24);
 
+template <int CG>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-        ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate), "r"(0u)
-        : "memory");
+    if (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
 }
+// Arrives on the barrier (of both CTAs, at the same place, for a pair) once the MMAs issued so far are done.
+template <int CG>
 __device__ __forceinline__ void commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    if (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
     uint32_t r[32];
@@ -378,108 +441,166 @@ contract_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)up_raw + 1023) & ~(uintptr_t)1023);
     int* off = reinterpret_cast<int*>(smem + C::kStages * C::kStageBytes);
     int* first = off + kUpMaxExperts + 1;
-    __shared__ __align__(8) uint64_t full[C::kStages], empty[C::kStages], acc_full[2], acc_empty[2];
+    __shared__ __align__(8) uint64_t full[C::kStages], empty[C::kStages], tail[C::kStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int dead;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0;      // place in the pair; rank 0 leads
+    const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+    // a stage of kGroupK is full after two arrivals: the leader's own two, or one of each CTA that cleared rows
+    constexpr int kFullCount = SCHED == kGroupK ? 2 : 1;
 
     if (tid == 0) {
-        for (int i = 0; i < C::kStages; ++i) { mb_init(&full[i], 1); mb_init(&empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mb_init(&acc_full[i], 1); mb_init(&acc_empty[i], 4); }
+        for (int i = 0; i < C::kStages; ++i) { mb_init(&full[i], kFullCount); mb_init(&empty[i], 1); mb_init(&tail[i], 1); }
+        for (int i = 0; i < 2; ++i) { mb_init(&acc_full[i], 1); mb_init(&acc_empty[i], 4 * CG); }
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)),
-                     "r"(2 * kTileN));
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2 * kTileN));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2 * kTileN));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     pdl_wait();
     if (SCHED != kDense && warp == 3) load_groups<C::kTileM>(p, off, first, (p.n + kTileN - 1) / kTileN, lane);
-    __syncthreads();
+    __syncwarp();
+    if (CG == 2) cluster_sync(); else __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_d = tmem_slot;
     const TileMap<CG, SCHED> map(p, off, first);
+    const uint32_t ring = smem_u32(smem);
 
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t it = 0, waited = 0;
-            for (int tile = blockIdx.x; tile < map.count && !dead; tile += gridDim.x) {
-                const Tile t = map.at(tile);
-                const int nk = (t.k_len + kStageK - 1) / kStageK;
-                for (int ks = 0; ks < nk && !dead; ++ks, ++it) {
-                    const int s = it % C::kStages;
-                    if (!mb_wait(&empty[s], ((it / C::kStages) & 1) ^ 1)) { dead = 1; atomicOr(p.err, kErrTimeout); break; }
-                    const uint32_t sa = smem_u32(smem + (size_t)s * C::kStageBytes), sb = sa + C::kABytes;
-                    const int k = t.k0 + ks * kStageK;
-                    mb_expect(&full[s], C::kStageBytes);
+        const bool elected = elect_one();
+        uint32_t it = 0;
+        int s = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int tile = worker; ok && tile < map.count; tile += workers) {
+            const Tile t = map.at(tile);
+            const int nk = (t.k_len + kStageK - 1) / kStageK;
+            const int a_row = t.a_row + rank * 128, b_col = t.b_col + rank * C::kBRows;
+            for (int ks = 0; ks < nk; ++ks) {
+                ok = !dead && mb_wait(&empty[s], phase ^ 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t sa = ring + (uint32_t)s * C::kStageBytes, sb = sa + C::kABytes;
+                const int k = t.k0 + ks * kStageK;
+                const bool ragged = SCHED == kGroupK && (t.k_len - ks * kStageK) < kStageK && t.k_len % 16;
+                // a ragged stage is reported by warp 1 once it has cleared rows, any other by the copies to the leader
+                const uint32_t bar = ragged ? (CG == 2 ? in_cta(&tail[s], rank) : smem_u32(&tail[s]))
+                                            : (CG == 2 ? in_cta(&full[s], 0) : smem_u32(&full[s]));
+                if (elected) {
+                    if (ragged) {
+                        mb_expect(&tail[s], C::kStageBytes);
+                    } else if (rank == 0) {
+                        if (kFullCount == 2) mb_arrive(&full[s]);
+                        mb_expect(&full[s], CG * C::kStageBytes);
+                    }
                     if (A_MN) {
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) tma_2d(sa + b * kMnBox, &tm_a, t.a_row + b * 64, k, &full[s]);
+                        for (int b = 0; b < 2; ++b) tma_2d<CG>(sa + b * kMnBox, &tm_a, a_row + b * 64, k, bar);
                     } else {
-                        tma_2d(sa, &tm_a, k, t.a_row, &full[s]);
+                        tma_2d<CG>(sa, &tm_a, k, a_row, bar);
                     }
                     if (B_MN) {
 #pragma unroll
                         for (int b = 0; b < C::kBRows / 64; ++b) {
-                            if (SCHED == kGroupRows) tma_3d(sb + b * kMnBox, &tm_b, t.b_col + b * 64, k, t.expert, &full[s]);
-                            else tma_2d(sb + b * kMnBox, &tm_b, t.b_col + b * 64, k, &full[s]);
+                            if (SCHED == kGroupRows) tma_3d<CG>(sb + b * kMnBox, &tm_b, b_col + b * 64, k, t.expert, bar);
+                            else tma_2d<CG>(sb + b * kMnBox, &tm_b, b_col + b * 64, k, bar);
                         }
                     } else {
 #pragma unroll
                         for (int b = 0; b < C::kBRows / 128; ++b) {
-                            if (SCHED == kGroupRows) tma_3d(sb + b * 16384, &tm_b, k, t.b_col + b * 128, t.expert, &full[s]);
-                            else tma_2d(sb + b * 16384, &tm_b, k, t.b_col + b * 128, &full[s]);
+                            if (SCHED == kGroupRows) tma_3d<CG>(sb + b * 16384, &tm_b, k, b_col + b * 128, t.expert, bar);
+                            else tma_2d<CG>(sb + b * 16384, &tm_b, k, b_col + b * 128, bar);
                         }
                     }
                 }
+                __syncwarp();
+                ++it;
+                if (++s == C::kStages) { s = 0; phase ^= 1; }
             }
-            if (dead)      // copies in flight must land before the shared memory is given up
-                for (waited = it > C::kStages ? it - C::kStages : 0; waited < it; ++waited)
-                    mb_wait(&full[waited % C::kStages], (waited / C::kStages) & 1);
+        }
+        // Copies in flight must land before the shared memory is given up: the stages' release says so in the
+        // regular case (the last accumulator is waited for); after a wait that gave up they are waited for here.
+        if (!ok && lane == 0) {
+            dead = 1;
+            atomicOr(p.err, kErrTimeout);
+            if (rank == 0)
+                for (uint32_t w = it > C::kStages ? it - C::kStages : 0; w < it; ++w) mb_wait(&full[w % C::kStages], (w / C::kStages) & 1);
         }
     } else if (warp == 1) {
-        // kGroupK: the whole warp walks along (it clears rows); otherwise one lane does
-        if (SCHED == kGroupK || lane == 0) {
-            const auto all = [](bool ok) { return SCHED == kGroupK ? __all_sync(0xffffffffu, ok) != 0 : ok; };
-            uint32_t it = 0;
-            int local = 0;
+        // the leader's warp issues the MMAs; for kGroupK the other CTA's walks along to clear rows of its own half
+        if (SCHED == kGroupK || rank == 0) {
+            const bool elected = elect_one();
+            uint32_t tails = 0;                               // parity of every stage's tail barrier
+            int s = 0, local = 0;
+            uint32_t phase = 0;
             bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < map.count; tile += gridDim.x) {
+            const uint64_t desc_a = smem_desc<A_MN>(ring), desc_b = smem_desc<B_MN>(ring + C::kABytes);
+            for (int tile = worker; ok && tile < map.count; tile += workers) {
                 const Tile t = map.at(tile);
                 const int nk = (t.k_len + kStageK - 1) / kStageK;
                 if (nk <= 0) continue;                        // nothing to contract: the epilogue writes zeros
                 const int buf = local & 1;
-                ok = all(!dead && mb_wait(&acc_empty[buf], ((local >> 1) & 1) ^ 1));
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t acc = tmem_d + (uint32_t)(buf * kTileN);
-                for (int ks = 0; ok && ks < nk; ++ks, ++it) {
-                    const int s = it % C::kStages;
-                    ok = all(!dead && mb_wait(&full[s], (it / C::kStages) & 1));
-                    if (!ok) break;
+                if (rank == 0) {
+                    ok = !dead && mb_wait<CG == 2>(&acc_empty[buf], ((local >> 1) & 1) ^ 1);
+                    ok = __all_sync(0xffffffffu, ok);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    unsigned char* st = smem + (size_t)s * C::kStageBytes;
-                    const int left = min(kStageK, t.k_len - ks * kStageK), steps = (left + 15) / 16;
-                    if (SCHED == kGroupK && left % 16) {      // rows behind the group's end, up to the step's 16
+                }
+                const uint32_t acc = tmem_d + (uint32_t)(buf * kTileN);
+                for (int ks = 0; ok && ks < nk; ++ks) {
+                    const int left = t.k_len - ks * kStageK;
+                    const int steps = left >= kStageK ? 4 : (left + 15) / 16;
+                    if (SCHED == kGroupK && left < kStageK && left % 16) {
+                        ok = !dead && mb_wait(&tail[s], (tails >> s) & 1);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        tails ^= 1u << s;
                         constexpr int kBoxes = (C::kABytes + C::kBBytes) / kMnBox;
-                        const int n_rows = steps * 16 - left;
+                        unsigned char* st = smem + (size_t)s * C::kStageBytes;
+                        const int n_rows = steps * 16 - left;     // rows behind the group's end, up to the step's 16
                         for (int i = lane; i < n_rows * kBoxes * 8; i += 32) {
                             const int piece = i & 7, row = left + (i >> 3) % n_rows, box = (i >> 3) / n_rows;
                             *reinterpret_cast<uint4*>(st + (size_t)box * kMnBox + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
                         }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        asm volatile("fence.proxy.async;" ::: "memory");
+                        __syncwarp();
+                        if (elected) {
+                            if (CG == 1) { mb_arrive(&full[s]); mb_arrive(&full[s]); }
+                            else mb_arrive_at(in_cta(&full[s], 0));
+                        }
                         __syncwarp();
                     }
-                    if (lane == 0) {
-                        const uint64_t da = smem_desc<A_MN>(smem_u32(st)), db = smem_desc<B_MN>(smem_u32(st) + C::kABytes);
-                        for (int kk = 0; kk < steps; ++kk)
-                            mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, kIdesc<CG, A_MN, B_MN>, (ks | kk) != 0);
-                        commit(&empty[s]);
+                    if (rank == 0) {
+                        ok = !dead && mb_wait<CG == 2 && SCHED == kGroupK>(&full[s], phase);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t da = desc_a + (uint64_t)(s * (C::kStageBytes >> 4)), db = desc_b + (uint64_t)(s * (C::kStageBytes >> 4));
+                        if (elected) {
+                            if (steps == 4) {
+#pragma unroll
+                                for (int kk = 0; kk < 4; ++kk)
+                                    mma_f16<CG>(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, kIdesc<CG, A_MN, B_MN>, kk == 0 ? ks != 0 : 1u);
+                            } else {
+                                for (int kk = 0; kk < steps; ++kk)
+                                    mma_f16<CG>(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, kIdesc<CG, A_MN, B_MN>, (ks | kk) != 0);
+                            }
+                            commit<CG>(&empty[s]);
+                            if (ks == nk - 1) commit<CG>(&acc_full[buf]);
+                        }
+                        __syncwarp();
                     }
+                    if (++s == C::kStages) { s = 0; phase ^= 1; }
                 }
-                if (ok && lane == 0) commit(&acc_full[buf]);
                 ++local;
             }
             if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
@@ -487,8 +608,9 @@ contract_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
     } else {
         const int quarter = warp & 3, row = quarter * 32 + lane;
         int local = 0;
-        for (int tile = blockIdx.x; tile < map.count; tile += gridDim.x) {
-            const Tile t = map.at(tile);
+        for (int tile = worker; tile < map.count; tile += workers) {
+            Tile t = map.at(tile);
+            if (CG == 2) { t.a_row += rank * 128; t.m_valid -= rank * 128; t.out += (int64_t)rank * 128 * p.e.ld; }
             if (t.k_len <= 0) {
                 if (EPI == kStore && !p.e.accumulate) store_tile(p.e, t, row, 0, true);
                 continue;
@@ -504,26 +626,44 @@ contract_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
             else store_tile(p.e, t, row, taddr, false);
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mb_arrive(&acc_empty[buf]);
+            if (lane == 0) {
+                if (CG == 1) mb_arrive(&acc_empty[buf]);
+                else mb_arrive_at(in_cta(&acc_empty[buf], 0));
+            }
             ++local;
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
-    __syncthreads();
+    // neither CTA of a pair leaves while the other may still signal its barriers or read its operands
+    __syncwarp();
+    if (CG == 2) cluster_sync(); else __syncthreads();
     if (warp == 2) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"(2 * kTileN));
+        if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"(2 * kTileN));
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"(2 * kTileN));
     }
 }
 
-constexpr int kCG = 1;
+constexpr int kCG = 2;
 
 template <bool A_MN, bool B_MN, int SCHED, int EPI>
 cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const UpParams& p, int64_t tiles, int sms, cudaStream_t st) {
     const int64_t want = tiles < 1 ? 1 : tiles;
-    const int grid = (int)(want < sms / kCG ? want : sms / kCG) * kCG;
-    return launch_chained(contract_kernel<kCG, A_MN, B_MN, SCHED, EPI>, dim3(grid), dim3(kThreads),
-                          Cfg<kCG>::smem_bytes(SCHED != kDense), st, a, b, p);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(want < sms / kCG ? want : sms / kCG) * kCG);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Cfg<kCG>::smem_bytes(SCHED != kDense);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCG;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, contract_kernel<kCG, A_MN, B_MN, SCHED, EPI>, a, b, p);
 }
 template <bool A_MN, bool B_MN, int SCHED, int EPI>
 cudaError_t init_one() {
