@@ -1,19 +1,25 @@
-// Contractions of the policy update on the 5th-generation tensor cores (tcgen05 + TMEM):
-//   log-prob of known tokens      logits = h W^T, softmax statistics in the epilogue        (K-major x K-major)
-//   its gradient, per piece       d = g/T ([v = t] - softmax) from the logits again          (K-major x K-major)
-//                                 d_hidden += d W_piece                                      (K-major x MN-major)
-//                                 d_lm_head_piece = d^T h                                    (MN-major x MN-major)
-//   expert products               y_e = x_e w_e^T, dx_e = dy_e w_e, dw_e = dy_e^T x_e        (the same three forms)
-// One persistent kernel template serves all of them.  A CTA walks 128 x 256 output tiles:
-//   warp 0 (one lane)  TMA producer, 64 contraction indexes per stage, 128-byte swizzle, mbarrier ring that
-//                      runs on across tiles;
-//   warp 1             one lane issues tcgen05.mma (K 16) into one of two TMEM accumulators;
-//   warps 2..5         epilogue of the previous tile (a thread owns a row of it) while the next is computed.
-// A K-major operand is a [rows][k] matrix (boxes of 128 rows x 64 k), an MN-major one a [k][columns] matrix
-// (boxes of 64 k x 64 columns), so no transposed copy of anything is made.  Ragged groups: rows of a tile
-// behind the group's end are computed and not stored; in dw_e, where the rows are the contraction, the stage
-// that holds the end has the rows behind it cleared in shared memory (they belong to the next expert and may
-// hold anything, NaN included), in whole steps of 16 the rest is not issued at all.
+// Contractions of the policy update on the 5th-generation tensor cores (tcgen05 + TMEM), all of the form
+// C[n][m] = sum_k A(m, k) B(n, k) with the axis that is contiguous in the output on M (the TMEM lanes):
+//   log-prob of known tokens    logits: A = lm_head (M vocabulary), B = hidden rows; softmax statistics in the epilogue
+//   its gradient, per piece     d = g/T ([v = t] - softmax): the same contraction again, d stored as bf16
+//                               d_hidden += W_piece^T d: A = lm_head (M hidden, MN-major), B = d
+//                               d_lm_head_piece = d^T h: A = hidden rows (M hidden, MN-major), B = d (MN-major)
+//   expert products             y: A = w_e, B = x;   dx: A = w_e (MN-major), B = dy;   dw_e: A = x, B = dy (both MN-major)
+// One persistent kernel template serves all of them.  A pair of CTAs (cta_group::2) works on one tile of 256 x
+// up to 256: each CTA holds 128 rows of A and half of B's rows, its tensor core reads the other half from its
+// peer, so a 64-deep stage brings 32 KB into each SM where single-CTA 128 x 256 tiles bring 48 (those ran at the
+// 11.5 TB/s that the L2 delivers: 758 us against 665 us for 131072 expert rows x 2048 -> 1536).
+// The N width of a tile is a multiple of 32 chosen from the rows there are (one width for all tiles of a group,
+// rows / ceil(rows / 256) rounded up): tokens sit on N, so ragged groups and short calls cost what they hold (a
+// group of 4 rows a 32-wide tile, 300 rows two of 160), and a call of few rows is a plain stream of the weights.
+//   warp 0      TMA producer, 64 contraction indexes per stage, 128-byte swizzle, 6-stage mbarrier ring that
+//               runs on across tiles;
+//   warp 1      of the leading CTA: issues tcgen05.mma (M 256, K 16) into one of two TMEM accumulators;
+//   warps 2..9  epilogue of the previous tile (a thread owns one M index, half of the columns) meanwhile.
+// A K-major operand is a [rows][k] matrix, an MN-major one a [k][columns] matrix (boxes of 64 k x 64 columns),
+// so no transposed copy of anything is made.  Ragged groups: N rows of a tile behind the group's end are
+// computed and not stored; in dw_e, where the rows are the contraction, the stage that holds the end has the
+// rows behind it cleared in shared memory (they belong to the next expert and may hold anything, NaN included).
 // Every wait is bounded; one that gives up sets the status word, the CTA stops issuing, waits for its copies
 // in flight, frees its TMEM and returns.
 #include "common.cuh"
@@ -24,23 +30,19 @@ namespace mars {
 
 namespace {
 
-constexpr int kTileN = 256, kStageK = 64, kThreads = 192;
+constexpr int kTileM = 256, kTileN = 256, kStageK = 64;
+constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
 constexpr uint32_t kSpin = 1u << 22;
 constexpr int kMnBox = 64 * kStageK * 2;                     // 8 KB: 64 contraction rows of 128 B
-
-template <int CG>
-struct Cfg {
-    static constexpr int kTileM = 128 * CG;
-    static constexpr int kBRows = kTileN / CG;               // B columns held by one CTA
-    static constexpr int kABytes = 128 * kStageK * 2;
-    static constexpr int kBBytes = kBRows * kStageK * 2;
-    static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = CG == 1 ? 4 : 6;          // 192 KB of ring
-    static constexpr int kGroupWords = 2 * (kUpMaxExperts + 1);
-    static constexpr size_t smem_bytes(bool groups) {
-        return (size_t)kStages * kStageBytes + 1024 + (groups ? kGroupWords * 4 : 0);
-    }
-};
+constexpr int kABytes = 128 * kStageK * 2;                   // one CTA's half of a tile's A rows
+constexpr int kBBytes = 128 * kStageK * 2;                   // room for one CTA's half of the widest tile's B rows
+constexpr int kStageBytes = kABytes + kBBytes;
+constexpr int kStages = 6;                                   // 192 KB of ring (3 stages: 10 % slower)
+constexpr int kGroupWords = 2 * (kUpMaxExperts + 1);
+constexpr int kEpiBytes = 2 * 4 * kTileN * 8;                // statistics of two tiles, or the tokens' values of a chunk per warp
+constexpr size_t smem_bytes(bool groups) {
+    return (size_t)kStages * kStageBytes + kEpiBytes + 1024 + (groups ? kGroupWords * 4 : 0);
+}
 
 enum Sched { kDense, kGroupRows, kGroupK };
 enum Epi { kStats, kDlogits, kStore };
@@ -78,10 +80,16 @@ __device__ __forceinline__ bool mb_wait(uint64_t* bar, uint32_t parity) {
             uint64_t t;
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
             if (!begin) begin = t;
-            else if (t - begin > 2000000000ull) return false;
+            else if ((int64_t)(t - begin) > 2000000000ll) return false;
         }
     }
     return false;
+}
+// The same for a whole warp: every lane polls for itself, all go on together or none does.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const volatile int& dead) {
+    const bool ok = !dead && mb_wait<CLUSTER>(bar, parity);
+    return __all_sync(0xffffffffu, ok) != 0;
 }
 // Address of the same shared-memory object in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t rank) {
@@ -104,26 +112,15 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// CG = 2: the barrier may be the other CTA's (`bar`: cluster address).
-template <int CG>
+// The barrier (`bar`: cluster address) may be the other CTA's.
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint32_t bar) {
-    if (CG == 1)
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                     ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(bar) : "memory");
-    else
-        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                     ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(bar) : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-template <int CG>
 __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
-    if (CG == 1)
-        asm volatile(
-            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-            ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-            ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"((uint64_t)tm), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 // Shared-memory matrix descriptor (version 1, 128-byte swizzle).  K-major: rows of 128 B, groups of 8 rows 1024 B
 // apart (stride offset), the leading offset unused.  MN-major: a row of 128 B holds 64 consecutive columns of one
@@ -139,34 +136,22 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
 }
 template <bool MN> constexpr uint32_t kDescStep = MN ? 16 * 128 / 16 : 32 / 16;    // 16 contraction indexes, in 16 bytes
 
-// fp32 accumulator, bf16 operands, bit 15 / 16: A / B is MN-major
-template <int CG, bool A_MN, bool B_MN>
+// fp32 accumulator, bf16 operands, bit 15 / 16: A / B is MN-major; the N width is added per tile
+template <bool A_MN, bool B_MN>
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
-                            ((uint32_t)(kTileN >> 3) << 17) | ((uint32_t)(Cfg<CG>::kTileM >> 4) << 24);
+                            ((uint32_t)(kTileM >> 4) << 24);
 
-template <int CG>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
-    if (CG == 1)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "setp.ne.b32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-            ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "setp.ne.b32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-            ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
 }
-// Arrives on the barrier (of both CTAs, at the same place, for a pair) once the MMAs issued so far are done.
-template <int CG>
+// Arrives on the barrier, of both CTAs at the same place, once the MMAs issued so far are done.
 __device__ __forceinline__ void commit(uint64_t* bar) {
-    if (CG == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
     uint32_t r[32];
@@ -191,91 +176,85 @@ __device__ __forceinline__ float exp2_approx(float x) {
 
 // One output tile and its contraction.
 struct Tile {
-    int a_row, b_col;         // first row / column in the operands' coordinates
-    int m_valid, n_valid;     // rows / columns that exist
+    int a_row, b_row;         // first M / N index in the operands' coordinates
+    int m_valid, n_valid;     // M / N indexes that exist
+    int width;                // N width of the MMA, a multiple of 32
     int k0, k_len;            // contraction range
     int expert;               // third coordinate of the expert stack
-    int col_tile;
+    int m_tile;
     int64_t out;              // element offset of the tile's corner in the output
 };
 
+__device__ __forceinline__ int tile_width(int n, int tiles) { return ((n + tiles - 1) / tiles + 31) & ~31; }
+
 // The tiles of a call, numbered the same way in every role.  `off`, `first`: group bounds and the number of
 // tiles before each group, in shared memory.
-template <int CG, int SCHED>
+template <int SCHED>
 struct TileMap {
     const UpParams& p;
     const int* off;
     const int* first;
-    int m, k, tiles_m, tiles_n, count;
+    int n, k, tiles_m, tiles_n, width, count;
 
     __device__ __forceinline__ TileMap(const UpParams& q, const int* o, const int* f) : p(q), off(o), first(f) {
-        constexpr int TM = Cfg<CG>::kTileM;
-        tiles_n = (p.n + kTileN - 1) / kTileN;
-        m = p.m; k = p.k;
+        n = p.n; k = p.k;
         if (SCHED == kDense) {
-            if (p.m_live) m = *p.m_live;
+            if (p.n_live) n = *p.n_live;
             if (p.k_live) k = *p.k_live;
-            tiles_m = (m + TM - 1) / TM;
-            count = tiles_m * tiles_n * p.splits;
-        } else if (SCHED == kGroupRows) {
-            tiles_m = 0;
-            count = first[p.experts];
-        } else {
-            tiles_m = (m + TM - 1) / TM;
-            count = p.experts * tiles_m * tiles_n;
         }
+        tiles_m = (p.m + kTileM - 1) / kTileM;
+        tiles_n = (n + kTileN - 1) / kTileN;
+        width = tiles_n > 0 ? tile_width(n, tiles_n) : 32;
+        count = SCHED == kGroupRows ? first[p.experts] : tiles_m * tiles_n * (SCHED == kGroupK ? p.experts : p.splits);
     }
     __device__ __forceinline__ Tile at(int t) const {
-        constexpr int TM = Cfg<CG>::kTileM;
         Tile r;
-        int tm;
-        if (SCHED == kDense) {                       // rows fastest: neighbours share the columns' operand in L2
-            const int per = tiles_m * tiles_n, split = t / per, u = t - split * per;
-            r.col_tile = u / tiles_m;
-            tm = u - r.col_tile * tiles_m;
-            const int stages = (k + kStageK - 1) / kStageK;
-            const int s0 = (int)((int64_t)stages * split / p.splits), s1 = (int)((int64_t)stages * (split + 1) / p.splits);
-            r.k0 = s0 * kStageK;
-            r.k_len = min(k, s1 * kStageK) - r.k0;
-            r.expert = 0;
-            r.a_row = tm * TM;
-            r.m_valid = m - r.a_row;
-            r.out = (int64_t)split * p.e.split_stride + (int64_t)r.a_row * p.e.ld;
-        } else if (SCHED == kGroupRows) {
-            int lo = 0, hi = p.experts - 1;          // the last group whose first tile is <= t and that has tiles
+        int tn;
+        if (SCHED == kGroupRows) {
+            int lo = 0, hi = p.experts - 1;          // the last group whose first tile is <= t: it has tiles
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
                 if (first[mid] <= t) lo = mid; else hi = mid - 1;
             }
-            const int rows = off[lo + 1] - off[lo], per = (rows + TM - 1) / TM, u = t - first[lo];
-            r.col_tile = u / per;
-            tm = u - r.col_tile * per;
+            const int rows = off[lo + 1] - off[lo], per = (rows + kTileN - 1) / kTileN, u = t - first[lo];
+            r.m_tile = u / per;                      // rows fastest: neighbours share the weights
+            tn = u - r.m_tile * per;
+            r.width = tile_width(rows, per);
             r.k0 = 0; r.k_len = k; r.expert = lo;
-            r.a_row = off[lo] + tm * TM;
-            r.m_valid = rows - tm * TM;
-            r.out = (int64_t)r.a_row * p.e.ld;
+            r.b_row = off[lo] + tn * r.width;
+            r.n_valid = min(r.width, rows - tn * r.width);
+            r.out = (int64_t)r.b_row * p.e.ld;
         } else {
-            const int per = tiles_m * tiles_n, e = t / per, u = t - e * per;
-            r.col_tile = u / tiles_m;
-            tm = u - r.col_tile * tiles_m;
-            r.expert = e;
-            r.k0 = off[e];
-            r.k_len = off[e + 1] - off[e];
-            r.a_row = tm * TM;
-            r.m_valid = m - r.a_row;
-            r.out = ((int64_t)e * m + r.a_row) * p.e.ld;
+            const int per = tiles_m * tiles_n, group = t / per, u = t - group * per;
+            if (SCHED == kGroupK || p.m_fastest) { tn = u / tiles_m; r.m_tile = u - tn * tiles_m; }
+            else { r.m_tile = u / tiles_n; tn = u - r.m_tile * tiles_n; }
+            r.width = width;
+            r.b_row = tn * width;
+            r.n_valid = min(width, n - r.b_row);
+            if (SCHED == kGroupK) {
+                r.expert = group;
+                r.k0 = off[group];
+                r.k_len = off[group + 1] - off[group];
+                r.out = ((int64_t)group * n + r.b_row) * p.e.ld;
+            } else {
+                const int stages = (k + kStageK - 1) / kStageK;
+                const int s0 = (int)((int64_t)stages * group / p.splits), s1 = (int)((int64_t)stages * (group + 1) / p.splits);
+                r.expert = 0;
+                r.k0 = s0 * kStageK;
+                r.k_len = min(k, s1 * kStageK) - r.k0;
+                r.out = (int64_t)group * p.e.split_stride + (int64_t)r.b_row * p.e.ld;
+            }
         }
-        r.b_col = r.col_tile * kTileN;
-        r.n_valid = min(kTileN, p.n - r.b_col);
-        r.out += r.b_col;
+        r.a_row = r.m_tile * kTileM;
+        r.m_valid = p.m - r.a_row;
+        r.out += r.a_row;
         return r;
     }
 };
 
 // Group bounds in shared memory: clamped to [0, rows] and made non-decreasing, so that no offset array leads
 // outside the operands; first[e] = tiles of the groups before e.  One warp.
-template <int TM>
-__device__ __forceinline__ void load_groups(const UpParams& p, int* off, int* first, int tiles_n, int lane) {
+__device__ __forceinline__ void load_groups(const UpParams& p, int* off, int* first, int tiles_m, int lane) {
     const int E = p.experts, per = (E + 1 + 31) / 32, b = min(lane * per, E + 1), e = min(b + per, E + 1);
     int top = 0;
     for (int i = b; i < e; ++i) {
@@ -293,7 +272,7 @@ __device__ __forceinline__ void load_groups(const UpParams& p, int* off, int* fi
     for (int i = b; i < e; ++i) off[i] = max(off[i], before);
     __syncwarp();
     int sum = 0;
-    for (int i = b; i < min(e, E); ++i) sum += (off[i + 1] - off[i] + TM - 1) / TM * tiles_n;
+    for (int i = b; i < min(e, E); ++i) sum += (off[i + 1] - off[i] + kTileN - 1) / kTileN * tiles_m;
     int pre = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -303,19 +282,27 @@ __device__ __forceinline__ void load_groups(const UpParams& p, int* off, int* fi
     pre -= sum;
     for (int i = b; i < e; ++i) {
         first[i] = pre;
-        if (i < E) pre += (off[i + 1] - off[i] + TM - 1) / TM * tiles_n;
+        if (i < E) pre += (off[i + 1] - off[i] + kTileN - 1) / kTileN * tiles_m;
     }
     __syncwarp();
 }
 
 // ---------------------------------------------------------------------------------------- epilogues
-// `taddr`: this thread's lane of the accumulator, column 0.  row: row of the tile.
+// `taddr`: this thread's lane of the accumulator, column 0; ch: its M index in the tile; c0 .. c1: its warp's columns.
+
+// Two columns of a warp (32 M indexes each) as packed pairs: even lanes get (m, m + 1) of column j, odd lanes of
+// column j + 1, so that a store instruction writes 64 contiguous bytes for each of two output rows.
+__device__ __forceinline__ uint32_t pair_columns(float a, float b, bool odd) {
+    const float got = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+    return odd ? pack_bf16(got, b) : pack_bf16(a, got);
+}
 
 // Store the tile: bf16 (rounded once from the fp32 accumulator) or fp32, optionally on top of what is there.
-__device__ __forceinline__ void store_tile(const UpEpilogue& e, const Tile& t, int row, uint32_t taddr, bool zero) {
-    const bool live = row < t.m_valid;
+__device__ __forceinline__ void store_tile(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1, uint32_t taddr, bool zero) {
+    const bool live = ch < t.m_valid, odd = ch & 1;
+    const int end = min(c1, t.n_valid);
 #pragma unroll 1
-    for (int c = 0; c < t.n_valid; c += 32) {
+    for (int c = c0; c < end; c += 32) {
         float v[32];
         if (zero) {
 #pragma unroll
@@ -323,157 +310,177 @@ __device__ __forceinline__ void store_tile(const UpEpilogue& e, const Tile& t, i
         } else {
             tmem_ld32(taddr + c, v);
         }
-        if (!live) continue;
-        const int64_t at = t.out + (int64_t)row * e.ld + c;
+        const int left = end - c;
         if (e.out_f32) {
-            float* dst = reinterpret_cast<float*>(e.out) + at;
+            float* dst = reinterpret_cast<float*>(e.out) + t.out + (int64_t)c * e.ld + ch;
+            if (e.accumulate) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 4)
-                if (c + j < t.n_valid) {
-                    float4 w = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                    if (e.accumulate) {
-                        const float4 o = *reinterpret_cast<const float4*>(dst + j);
-                        w.x += o.x; w.y += o.y; w.z += o.z; w.w += o.w;
-                    }
-                    *reinterpret_cast<float4*>(dst + j) = w;
-                }
+                for (int j = 0; j < 32; ++j)
+                    if (live && j < left) v[j] += dst[(int64_t)j * e.ld];
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (live && j < left) dst[(int64_t)j * e.ld] = v[j];
         } else {
-            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(e.out) + at;
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(e.out) + t.out + (int64_t)(c + odd) * e.ld + (ch - odd);
+            uint32_t old[16];
+            if (e.accumulate) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 8)
-                if (c + j < t.n_valid) {
-                    if (e.accumulate) {
-                        const uint4 o = *reinterpret_cast<const uint4*>(dst + j);
-                        const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
+                for (int j = 0; j < 32; j += 2)
+                    if (live && j + odd < left) old[j / 2] = *reinterpret_cast<const uint32_t*>(dst + (int64_t)j * e.ld);
+            }
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) { v[j + 2 * q] += bf16_lo(ow[q]); v[j + 2 * q + 1] += bf16_hi(ow[q]); }
-                    }
-                    *reinterpret_cast<uint4*>(dst + j) =
-                        make_uint4(pack_bf16(v[j], v[j + 1]), pack_bf16(v[j + 2], v[j + 3]), pack_bf16(v[j + 4], v[j + 5]),
-                                   pack_bf16(v[j + 6], v[j + 7]));
+            for (int j = 0; j < 32; j += 2) {
+                uint32_t w;
+                if (e.accumulate) {          // added in fp32, rounded once
+                    const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
+                    w = live && j + odd < left ? pack_bf16((odd ? got : v[j]) + bf16_lo(old[j / 2]), (odd ? v[j + 1] : got) + bf16_hi(old[j / 2])) : 0u;
+                } else {
+                    w = pair_columns(v[j], v[j + 1], odd);
+                }
+                if (live && j + odd < left) *reinterpret_cast<uint32_t*>(dst + (int64_t)j * e.ld) = w;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ float redux_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// Softmax statistics of the tile's vocabulary entries for every token, the token's own target left out (its
+// logit is computed apart, in fp32): the largest logit M (before the temperature) and sum exp((logit - M) / T).
+// Differences are taken before the scaling, so the exponents carry no rounding of large values.  A warp holds 32
+// entries x 32 tokens at a time: the maximum of a token is one redux, the sums of 32 tokens take 31 exchanges
+// (halving the number of columns a lane holds each time), after which lane l has token l's; the four warps of
+// a column half meet in shared memory.
+__device__ __forceinline__ void stats_tile(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1, uint32_t taddr, float2* meet,
+                                           int quarter, int half, int lane, int slot, int slots, const int* n_live) {
+    const bool live = ch < t.m_valid;
+    const int v_row = t.a_row + ch, end = min(c1, t.n_valid);
+    const float scale = e.inv_temp * 1.4426950408889634f;
+#pragma unroll 1
+    for (int c = c0; c < end; c += 32) {
+        float v[32];
+        tmem_ld32(taddr + c, v);
+        const int tok = t.b_row + c + lane;
+        const int tgt = tok < *n_live ? e.target[tok] : -1;
+        float mine = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const int tj = __shfl_sync(0xffffffffu, tgt, j);
+            if (!live || tj == v_row) v[j] = -INFINITY;
+            const float m = redux_max(v[j]);
+            if (lane == j) mine = m;
+            v[j] = exp2_approx((v[j] - (m == -INFINITY ? 0.f : m)) * scale);       // nothing but -inf: all terms are 0
+        }
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) {
+            const bool up = lane & o;
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (j < o) {
+                    const float give = up ? v[j] : v[j + o], keep = up ? v[j + o] : v[j];
+                    v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
                 }
         }
+        meet[quarter * kTileN + c + lane] = make_float2(mine, v[0]);
+    }
+    __syncwarp();
+    asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+    const int col = c0 + quarter * 32 + lane;
+    if (col < end) {
+        float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mx = fmaxf(mx, meet[q * kTileN + col].x);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float2 s = meet[q * kTileN + col];
+            sum += s.y * exp2_approx((s.x - ref) * scale);
+        }
+        e.stats[(int64_t)(t.b_row + col) * slots + slot] = make_float2(mx, sum);
     }
 }
 
-// Softmax statistics of the tile's columns: the largest logit M (before the temperature) and
-// sum exp((logit - M) / T), one pass with a running maximum; differences are taken before the scaling, so the
-// exponents carry no rounding of large values.  The row's own target logit is stored on the way.
-__device__ __forceinline__ void stats_tile(const UpEpilogue& e, const Tile& t, int row, uint32_t taddr, int tiles_n) {
-    const bool live = row < t.m_valid;
-    const int r = t.a_row + row;
-    const int tgt = live ? e.target[r] - t.b_col : -1;        // column of the target, if it is in this tile
+// Gradient of the logits: d = w ([v = t] - p), p = exp(z - lse), w = g / T, rounded to bf16 (relative 2^-8 at
+// most, independent from entry to entry) because it is an operand of two tensor-core products; for calls of few
+// rows, which are streams of the lm_head anyway, what the rounding took off is stored as a second bf16 row.  The
+// target's own value w (1 - p) comes from its fp32 logit: no cancellation where p is close to 1.  Tokens and
+// entries behind the end are written as zeros: they are contraction indexes of those products.
+__device__ __forceinline__ void dlogits_tile(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1, uint32_t taddr, float4* tokens,
+                                             int lane, const int* n_live) {
+    const int v_row = e.v0 + t.a_row + ch, end = min(c1, t.width);
+    const bool live = v_row < e.vocab, odd = ch & 1;
     const float scale = e.inv_temp * 1.4426950408889634f;
-    float mx = -INFINITY, sum = 0.f, zt = 0.f;
 #pragma unroll 1
-    for (int c = 0; c < t.n_valid; c += 32) {
+    for (int c = c0; c < end; c += 32) {
+        const int tok = t.b_row + c + lane;
+        float4 mine = make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
+        if (tok < *n_live) mine = make_float4(e.lse[tok] * -1.4426950408889634f, -e.weight[tok], __int_as_float(e.target[tok]), e.target_d[tok]);
+        __syncwarp();
+        tokens[lane] = mine;
         float v[32];
         tmem_ld32(taddr + c, v);
-        if (!live) continue;
-        const int left = t.n_valid - c;
-        float nm = mx;
+        __syncwarp();
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-            if (j >= left) v[j] = -INFINITY;
-            nm = fmaxf(nm, v[j]);
+            const float4 k = tokens[j];
+            const float d = k.y * exp2_approx(fmaf(v[j], scale, k.x));
+            v[j] = !live ? 0.f : __float_as_int(k.z) == v_row ? k.w : d;
         }
-        const float ref = nm == -INFINITY ? 0.f : nm;          // nothing but -inf so far: all terms are 0
-        float add = 0.f;
+        __nv_bfloat16* dst = e.dlogits + (int64_t)(t.b_row + c + odd) * e.ld + (t.a_row + ch - odd);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) add += exp2_approx((v[j] - ref) * scale);
-        sum = sum * exp2_approx((mx - ref) * scale) + add;
-        mx = nm;
-        if (tgt >= c && tgt < c + 32) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (c + j == tgt) zt = v[j];
+        for (int j = 0; j < 32; j += 2) {
+            const uint32_t w = pair_columns(v[j], v[j + 1], odd);
+            *reinterpret_cast<uint32_t*>(dst + (int64_t)j * e.ld) = w;
+            if (e.lo_rows) {
+                const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
+                *reinterpret_cast<uint32_t*>(dst + (int64_t)(j + e.lo_rows) * e.ld) =
+                    pack_bf16((odd ? got : v[j]) - bf16_lo(w), (odd ? v[j + 1] : got) - bf16_hi(w));
+            }
         }
-    }
-    if (!live) return;
-    e.stats[(int64_t)r * tiles_n + t.col_tile] = make_float2(mx, sum);
-    if (tgt >= 0 && tgt < t.n_valid) e.target_logit[r] = zt;
-}
-
-// Gradient of the logits: d = w ([v = t] - p), p = exp(z - lse), w = g / T, rounded once to bf16 (relative
-// 2^-8 at most, independent from entry to entry) because it is an operand of two tensor-core products.
-// The target's own 1 - p is -expm1(z - lse): no cancellation where p is close to 1.  Rows and columns behind
-// the end are written as zeros: they are contraction indexes of those products.
-__device__ __forceinline__ void dlogits_tile(const UpEpilogue& e, const Tile& t, int row, uint32_t taddr) {
-    const bool live = row < t.m_valid;
-    const int r = t.a_row + row;
-    const int tgt = live ? e.target[r] - e.v0 - t.b_col : -1;
-    const float w = live ? e.weight[r] : 0.f, lse = live ? e.lse[r] : 0.f;
-    const float scale = e.inv_temp * 1.4426950408889634f, shift = -lse * 1.4426950408889634f;
-    const int left0 = e.vocab - e.v0 - t.b_col;
-    __nv_bfloat16* dst = e.dlogits + (int64_t)r * e.ld + t.b_col;
-#pragma unroll 1
-    for (int c = 0; c < t.n_valid; c += 32) {
-        float v[32];
-        tmem_ld32(taddr + c, v);
-        const int left = left0 - c;
-        const bool own = tgt >= c && tgt < c + 32;
-        float dt = 0.f;
-        if (own) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (c + j == tgt) dt = v[j];
-            dt = -w * expm1f(fmaf(dt, e.inv_temp, -lse));
-        }
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float d = -w * exp2_approx(fmaf(v[j], scale, shift));
-            v[j] = live && j < left ? (own && c + j == tgt ? dt : d) : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < 32; j += 8)
-            *reinterpret_cast<uint4*>(dst + c + j) =
-                make_uint4(pack_bf16(v[j], v[j + 1]), pack_bf16(v[j + 2], v[j + 3]), pack_bf16(v[j + 4], v[j + 5]),
-                           pack_bf16(v[j + 6], v[j + 7]));
     }
 }
 
-template <int CG, bool A_MN, bool B_MN, int SCHED, int EPI>
-__global__ void __launch_bounds__(kThreads, 1)
-contract_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
-                const __grid_constant__ UpParams p) {
-    using C = Cfg<CG>;
+template <bool A_MN, bool B_MN, int SCHED, int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpParams p) {
     extern __shared__ unsigned char up_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)up_raw + 1023) & ~(uintptr_t)1023);
-    int* off = reinterpret_cast<int*>(smem + C::kStages * C::kStageBytes);
+    unsigned char* epi = smem + kStages * kStageBytes;
+    int* off = reinterpret_cast<int*>(epi + kEpiBytes);
     int* first = off + kUpMaxExperts + 1;
-    __shared__ __align__(8) uint64_t full[C::kStages], empty[C::kStages], tail[C::kStages], acc_full[2], acc_empty[2];
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], tail[kStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int dead;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0;      // place in the pair; rank 0 leads
-    const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+    const int rank = (int)(blockIdx.x & 1);                    // place in the pair; rank 0 leads
+    const int worker = blockIdx.x / 2, workers = gridDim.x / 2;
     // a stage of kGroupK is full after two arrivals: the leader's own two, or one of each CTA that cleared rows
     constexpr int kFullCount = SCHED == kGroupK ? 2 : 1;
 
     if (tid == 0) {
-        for (int i = 0; i < C::kStages; ++i) { mb_init(&full[i], kFullCount); mb_init(&empty[i], 1); mb_init(&tail[i], 1); }
-        for (int i = 0; i < 2; ++i) { mb_init(&acc_full[i], 1); mb_init(&acc_empty[i], 4 * CG); }
+        for (int i = 0; i < kStages; ++i) { mb_init(&full[i], kFullCount); mb_init(&empty[i], 1); mb_init(&tail[i], 1); }
+        for (int i = 0; i < 2; ++i) { mb_init(&acc_full[i], 1); mb_init(&acc_empty[i], 2 * kEpiWarps); }
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 2) {
-        if (CG == 1) {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2 * kTileN));
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2 * kTileN));
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-        }
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2 * kTileN));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     pdl_wait();
-    if (SCHED != kDense && warp == 3) load_groups<C::kTileM>(p, off, first, (p.n + kTileN - 1) / kTileN, lane);
+    if (SCHED != kDense && warp == 3) load_groups(p, off, first, (p.m + kTileM - 1) / kTileM, lane);
     __syncwarp();
-    if (CG == 2) cluster_sync(); else __syncthreads();
+    cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_d = tmem_slot;
-    const TileMap<CG, SCHED> map(p, off, first);
+    const TileMap<SCHED> map(p, off, first);
     const uint32_t ring = smem_u32(smem);
 
     if (warp == 0) {
@@ -485,56 +492,57 @@ contract_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
         for (int tile = worker; ok && tile < map.count; tile += workers) {
             const Tile t = map.at(tile);
             const int nk = (t.k_len + kStageK - 1) / kStageK;
-            const int a_row = t.a_row + rank * 128, b_col = t.b_col + rank * C::kBRows;
+            const int half = t.width / 2, a_row = t.a_row + rank * 128, b_row = t.b_row + rank * half;
+            // B, K-major: one box of 16, 32, 64 or 128 rows holds the half; MN-major: one or two boxes of 64 columns
+            const int box = half <= 16 ? 0 : half <= 32 ? 1 : half <= 64 ? 2 : 3;
+            const uint32_t b_bytes = B_MN ? (uint32_t)((half + 63) / 64 * kMnBox) : (uint32_t)(16 << box) * 128u;
+            const CUtensorMap* tm_b = &maps.b[B_MN ? 0 : box];
             for (int ks = 0; ks < nk; ++ks) {
-                ok = !dead && mb_wait(&empty[s], phase ^ 1);
-                ok = __all_sync(0xffffffffu, ok);
+                ok = warp_wait(&empty[s], phase ^ 1, dead);
                 if (!ok) break;
-                const uint32_t sa = ring + (uint32_t)s * C::kStageBytes, sb = sa + C::kABytes;
+                const uint32_t sa = ring + (uint32_t)s * kStageBytes, sb = sa + kABytes;
                 const int k = t.k0 + ks * kStageK;
                 const bool ragged = SCHED == kGroupK && (t.k_len - ks * kStageK) < kStageK && t.k_len % 16;
                 // a ragged stage is reported by warp 1 once it has cleared rows, any other by the copies to the leader
-                const uint32_t bar = ragged ? (CG == 2 ? in_cta(&tail[s], rank) : smem_u32(&tail[s]))
-                                            : (CG == 2 ? in_cta(&full[s], 0) : smem_u32(&full[s]));
+                const uint32_t bar = ragged ? in_cta(&tail[s], rank) : in_cta(&full[s], 0);
                 if (elected) {
                     if (ragged) {
-                        mb_expect(&tail[s], C::kStageBytes);
+                        mb_expect(&tail[s], kABytes + b_bytes);
                     } else if (rank == 0) {
                         if (kFullCount == 2) mb_arrive(&full[s]);
-                        mb_expect(&full[s], CG * C::kStageBytes);
+                        mb_expect(&full[s], 2 * (kABytes + b_bytes));
                     }
                     if (A_MN) {
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) tma_2d<CG>(sa + b * kMnBox, &tm_a, a_row + b * 64, k, bar);
+                        for (int b = 0; b < 2; ++b) {
+                            if (SCHED == kGroupRows) tma_3d(sa + b * kMnBox, &maps.a, a_row + b * 64, k, t.expert, bar);
+                            else tma_2d(sa + b * kMnBox, &maps.a, a_row + b * 64, k, bar);
+                        }
                     } else {
-                        tma_2d<CG>(sa, &tm_a, k, a_row, bar);
+                        if (SCHED == kGroupRows) tma_3d(sa, &maps.a, k, a_row, t.expert, bar);
+                        else tma_2d(sa, &maps.a, k, a_row, bar);
                     }
                     if (B_MN) {
-#pragma unroll
-                        for (int b = 0; b < C::kBRows / 64; ++b) {
-                            if (SCHED == kGroupRows) tma_3d<CG>(sb + b * kMnBox, &tm_b, b_col + b * 64, k, t.expert, bar);
-                            else tma_2d<CG>(sb + b * kMnBox, &tm_b, b_col + b * 64, k, bar);
-                        }
+                        tma_2d(sb, tm_b, b_row, k, bar);
+                        if (half > 64) tma_2d(sb + kMnBox, tm_b, b_row + 64, k, bar);
                     } else {
-#pragma unroll
-                        for (int b = 0; b < C::kBRows / 128; ++b) {
-                            if (SCHED == kGroupRows) tma_3d<CG>(sb + b * 16384, &tm_b, k, b_col + b * 128, t.expert, bar);
-                            else tma_2d<CG>(sb + b * 16384, &tm_b, k, b_col + b * 128, bar);
-                        }
+                        tma_2d(sb, tm_b, k, b_row, bar);
                     }
                 }
                 __syncwarp();
                 ++it;
-                if (++s == C::kStages) { s = 0; phase ^= 1; }
+                if (++s == kStages) { s = 0; phase ^= 1; }
             }
         }
-        // Copies in flight must land before the shared memory is given up: the stages' release says so in the
-        // regular case (the last accumulator is waited for); after a wait that gave up they are waited for here.
-        if (!ok && lane == 0) {
-            dead = 1;
-            atomicOr(p.err, kErrTimeout);
+        // The last stages' release is waited for as well: it says that the copies into them and the MMAs on them are
+        // done, and it is a signal from the leader's MMAs into this CTA's shared memory, which must not be given up
+        // before (the epilogue's accumulator signal is another one and need not come later).  After a wait that
+        // gave up the copies in flight are waited for instead.
+        for (uint32_t w = it > kStages ? it - kStages : 0; ok && w < it; ++w) ok = warp_wait(&empty[w % kStages], (w / kStages) & 1, dead);
+        if (!ok) {
+            if (lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
             if (rank == 0)
-                for (uint32_t w = it > C::kStages ? it - C::kStages : 0; w < it; ++w) mb_wait(&full[w % C::kStages], (w / C::kStages) & 1);
+                for (uint32_t w = it > kStages ? it - kStages : 0; w < it; ++w) mb_wait(&full[w % kStages], (w / kStages) & 1);
         }
     } else if (warp == 1) {
         // the leader's warp issues the MMAs; for kGroupK the other CTA's walks along to clear rows of its own half
@@ -544,177 +552,173 @@ contract_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
             int s = 0, local = 0;
             uint32_t phase = 0;
             bool ok = true;
-            const uint64_t desc_a = smem_desc<A_MN>(ring), desc_b = smem_desc<B_MN>(ring + C::kABytes);
+            const uint64_t desc_a = smem_desc<A_MN>(ring), desc_b = smem_desc<B_MN>(ring + kABytes);
             for (int tile = worker; ok && tile < map.count; tile += workers) {
                 const Tile t = map.at(tile);
                 const int nk = (t.k_len + kStageK - 1) / kStageK;
                 if (nk <= 0) continue;                        // nothing to contract: the epilogue writes zeros
                 const int buf = local & 1;
                 if (rank == 0) {
-                    ok = !dead && mb_wait<CG == 2>(&acc_empty[buf], ((local >> 1) & 1) ^ 1);
-                    ok = __all_sync(0xffffffffu, ok);
+                    ok = warp_wait<true>(&acc_empty[buf], ((local >> 1) & 1) ^ 1, dead);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 }
                 const uint32_t acc = tmem_d + (uint32_t)(buf * kTileN);
+                const uint32_t idesc = kIdesc<A_MN, B_MN> | ((uint32_t)(t.width >> 3) << 17);
                 for (int ks = 0; ok && ks < nk; ++ks) {
                     const int left = t.k_len - ks * kStageK;
                     const int steps = left >= kStageK ? 4 : (left + 15) / 16;
                     if (SCHED == kGroupK && left < kStageK && left % 16) {
-                        ok = !dead && mb_wait(&tail[s], (tails >> s) & 1);
-                        ok = __all_sync(0xffffffffu, ok);
+                        ok = warp_wait(&tail[s], (tails >> s) & 1, dead);
                         if (!ok) break;
                         tails ^= 1u << s;
-                        constexpr int kBoxes = (C::kABytes + C::kBBytes) / kMnBox;
-                        unsigned char* st = smem + (size_t)s * C::kStageBytes;
+                        unsigned char* st = smem + (size_t)s * kStageBytes;
                         const int n_rows = steps * 16 - left;     // rows behind the group's end, up to the step's 16
-                        for (int i = lane; i < n_rows * kBoxes * 8; i += 32) {
+                        const int boxes = 2 + (t.width / 2 + 63) / 64;
+                        for (int i = lane; i < n_rows * boxes * 8; i += 32) {
                             const int piece = i & 7, row = left + (i >> 3) % n_rows, box = (i >> 3) / n_rows;
                             *reinterpret_cast<uint4*>(st + (size_t)box * kMnBox + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
                         }
                         asm volatile("fence.proxy.async;" ::: "memory");
                         __syncwarp();
-                        if (elected) {
-                            if (CG == 1) { mb_arrive(&full[s]); mb_arrive(&full[s]); }
-                            else mb_arrive_at(in_cta(&full[s], 0));
-                        }
+                        if (elected) mb_arrive_at(in_cta(&full[s], 0));
                         __syncwarp();
                     }
                     if (rank == 0) {
-                        ok = !dead && mb_wait<CG == 2 && SCHED == kGroupK>(&full[s], phase);
-                        ok = __all_sync(0xffffffffu, ok);
+                        ok = warp_wait<SCHED == kGroupK>(&full[s], phase, dead);
                         if (!ok) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint64_t da = desc_a + (uint64_t)(s * (C::kStageBytes >> 4)), db = desc_b + (uint64_t)(s * (C::kStageBytes >> 4));
+                        const uint64_t da = desc_a + (uint64_t)(s * (kStageBytes >> 4)), db = desc_b + (uint64_t)(s * (kStageBytes >> 4));
                         if (elected) {
                             if (steps == 4) {
 #pragma unroll
                                 for (int kk = 0; kk < 4; ++kk)
-                                    mma_f16<CG>(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, kIdesc<CG, A_MN, B_MN>, kk == 0 ? ks != 0 : 1u);
+                                    mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, kk == 0 ? ks != 0 : 1u);
                             } else {
                                 for (int kk = 0; kk < steps; ++kk)
-                                    mma_f16<CG>(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, kIdesc<CG, A_MN, B_MN>, (ks | kk) != 0);
+                                    mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, (ks | kk) != 0);
                             }
-                            commit<CG>(&empty[s]);
-                            if (ks == nk - 1) commit<CG>(&acc_full[buf]);
+                            commit(&empty[s]);
+                            if (ks == nk - 1) commit(&acc_full[buf]);
                         }
                         __syncwarp();
                     }
-                    if (++s == C::kStages) { s = 0; phase ^= 1; }
+                    if (++s == kStages) { s = 0; phase ^= 1; }
                 }
                 ++local;
             }
             if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
         }
     } else {
-        const int quarter = warp & 3, row = quarter * 32 + lane;
+        // a warp may touch the TMEM lanes 32 (warp % 4) .. + 31; the first four warps take the left half of the columns
+        const int quarter = warp & 3, half = (warp - 2) >> 2, ch = rank * 128 + quarter * 32 + lane;
         int local = 0;
-        for (int tile = worker; tile < map.count; tile += workers) {
-            Tile t = map.at(tile);
-            if (CG == 2) { t.a_row += rank * 128; t.m_valid -= rank * 128; t.out += (int64_t)rank * 128 * p.e.ld; }
+        bool ok = true;
+        for (int tile = worker; ok && tile < map.count; tile += workers) {
+            const Tile t = map.at(tile);
+            const int mid = ((t.width / 2 + 31) & ~31), c0 = half ? mid : 0, c1 = half ? t.width : mid;
             if (t.k_len <= 0) {
-                if (EPI == kStore && !p.e.accumulate) store_tile(p.e, t, row, 0, true);
+                if (EPI == kStore && !p.e.accumulate) store_tile(p.e, t, ch, c0, c1, 0, true);
                 continue;
             }
             const int buf = local & 1;
-            if (lane == 0 && !dead && !mb_wait(&acc_full[buf], (local >> 1) & 1)) { dead = 1; atomicOr(p.err, kErrTimeout); }
-            __syncwarp();
-            if (!__all_sync(0xffffffffu, !dead)) break;
+            if (EPI == kStats) {
+                ok = warp_wait(&acc_full[buf], (local >> 1) & 1, dead);
+            } else {
+                if (lane == 0) ok = !dead && mb_wait(&acc_full[buf], (local >> 1) & 1);
+                __syncwarp();
+                ok = __all_sync(0xffffffffu, ok) != 0;
+            }
+            if (EPI == kStats) {          // the warps of a column half meet on a barrier: all of them go on, or none
+                uint32_t all_ok;
+                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                             : "=r"(all_ok) : "r"((uint32_t)ok), "r"(1 + half) : "memory");
+                ok = all_ok != 0;
+            }
+            if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t taddr = tmem_d + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kTileN);
-            if (EPI == kStats) stats_tile(p.e, t, row, taddr, map.tiles_n);
-            else if (EPI == kDlogits) dlogits_tile(p.e, t, row, taddr);
-            else store_tile(p.e, t, row, taddr, false);
+            if (EPI == kStats)
+                stats_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float2*>(epi) + buf * 4 * kTileN, quarter, half, lane,
+                           t.m_tile * 2 + rank, map.tiles_m * 2, p.n_live);
+            else if (EPI == kDlogits)
+                dlogits_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float4*>(epi) + (warp - 2) * 32, lane, p.e.n_live);
+            else
+                store_tile(p.e, t, ch, c0, c1, taddr, false);
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) {
-                if (CG == 1) mb_arrive(&acc_empty[buf]);
-                else mb_arrive_at(in_cta(&acc_empty[buf], 0));
-            }
+            if (lane == 0) mb_arrive_at(in_cta(&acc_empty[buf], 0));
             ++local;
         }
+        if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
-    // neither CTA of a pair leaves while the other may still signal its barriers or read its operands
+    // neither CTA of a pair leaves while the other may still signal its barriers or read its operands; after a wait
+    // that gave up, what is in flight (copies, MMAs and their signals: microseconds) gets two milliseconds to land
     __syncwarp();
-    if (CG == 2) cluster_sync(); else __syncthreads();
+    if (__any_sync(0xffffffffu, dead))
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    __syncwarp();
+    cluster_sync();
     if (warp == 2) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"(2 * kTileN));
-        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"(2 * kTileN));
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"(2 * kTileN));
     }
 }
 
-constexpr int kCG = 2;
-
 template <bool A_MN, bool B_MN, int SCHED, int EPI>
-cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const UpParams& p, int64_t tiles, int sms, cudaStream_t st) {
-    const int64_t want = tiles < 1 ? 1 : tiles;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(want < sms / kCG ? want : sms / kCG) * kCG);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Cfg<kCG>::smem_bytes(SCHED != kDense);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = kCG;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, contract_kernel<kCG, A_MN, B_MN, SCHED, EPI>, a, b, p);
+cudaError_t launch(const UpMaps& m, const UpParams& p, int64_t tiles, int sms, cudaStream_t st) {
+    const int64_t want = tiles < 1 ? 1 : tiles, pairs = sms / 2;
+    return launch_chained(contract_kernel<A_MN, B_MN, SCHED, EPI>, dim3((unsigned)(want < pairs ? want : pairs) * 2), dim3(kThreads),
+                          smem_bytes(SCHED != kDense), st, m, p);
 }
 template <bool A_MN, bool B_MN, int SCHED, int EPI>
 cudaError_t init_one() {
-    return cudaFuncSetAttribute(contract_kernel<kCG, A_MN, B_MN, SCHED, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)Cfg<kCG>::smem_bytes(SCHED != kDense));
+    return cudaFuncSetAttribute(contract_kernel<A_MN, B_MN, SCHED, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)smem_bytes(SCHED != kDense));
 }
-int64_t tiles_of(int64_t m, int64_t n) {
-    return ((m + Cfg<kCG>::kTileM - 1) / Cfg<kCG>::kTileM) * ((n + kTileN - 1) / kTileN);
-}
+int64_t tiles_of(int64_t m, int64_t n) { return ((m + kTileM - 1) / kTileM) * ((n + kTileN - 1) / kTileN); }
 }  // namespace
 
 cudaError_t init_update_kernels() {
     cudaError_t e = init_one<false, false, kDense, kStats>();
     if (e == cudaSuccess) e = init_one<false, false, kDense, kDlogits>();
-    if (e == cudaSuccess) e = init_one<false, true, kDense, kStore>();
+    if (e == cudaSuccess) e = init_one<true, false, kDense, kStore>();
     if (e == cudaSuccess) e = init_one<true, true, kDense, kStore>();
     if (e == cudaSuccess) e = init_one<false, false, kGroupRows, kStore>();
-    if (e == cudaSuccess) e = init_one<false, true, kGroupRows, kStore>();
+    if (e == cudaSuccess) e = init_one<true, false, kGroupRows, kStore>();
     if (e == cudaSuccess) e = init_one<true, true, kGroupK, kStore>();
     return e;
 }
 
-cudaError_t launch_logit_stats(const CUtensorMap& h, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<false, false, kDense, kStats>(h, w, p, tiles_of(p.m, p.n), sms, st);
+cudaError_t launch_logit_stats(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    return launch<false, false, kDense, kStats>(m, p, tiles_of(p.m, p.n), sms, st);
 }
-cudaError_t launch_dlogits(const CUtensorMap& h, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<false, false, kDense, kDlogits>(h, w, p, tiles_of(p.m, p.n), sms, st);
+cudaError_t launch_dlogits(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    return launch<false, false, kDense, kDlogits>(m, p, tiles_of(p.m, p.n), sms, st);
 }
-cudaError_t launch_dhidden(const CUtensorMap& d, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<false, true, kDense, kStore>(d, w, p, tiles_of(p.m, p.n) * p.splits, sms, st);
+cudaError_t launch_dhidden(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    return launch<true, false, kDense, kStore>(m, p, tiles_of(p.m, p.n) * p.splits, sms, st);
 }
-cudaError_t launch_dhead(const CUtensorMap& d, const CUtensorMap& h, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<true, true, kDense, kStore>(d, h, p, tiles_of(p.m, p.n), sms, st);
+cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    return launch<true, true, kDense, kStore>(m, p, tiles_of(p.m, p.n), sms, st);
 }
-cudaError_t launch_expert_fwd(const CUtensorMap& x, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<false, false, kGroupRows, kStore>(x, w, p, sms, sms, st);
+cudaError_t launch_expert_fwd(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    return launch<false, false, kGroupRows, kStore>(m, p, sms, sms, st);
 }
-cudaError_t launch_expert_dx(const CUtensorMap& dy, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<false, true, kGroupRows, kStore>(dy, w, p, sms, sms, st);
+cudaError_t launch_expert_dx(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    return launch<true, false, kGroupRows, kStore>(m, p, sms, sms, st);
 }
-cudaError_t launch_expert_dw(const CUtensorMap& dy, const CUtensorMap& x, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<true, true, kGroupK, kStore>(dy, x, p, tiles_of(p.m, p.n) * p.experts, sms, st);
+cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    return launch<true, true, kGroupK, kStore>(m, p, tiles_of(p.m, p.n) * p.experts, sms, st);
 }
 
 // Parts of the d_hidden contraction (over the vocabulary piece, `stages` stages of 64): few rows give few output
-// tiles, and a piece is long, so it is cut until the tiles fill the SMs' rounds; at least 8 stages remain.
+// tiles, and a piece is long, so it is cut until the tiles fill the pairs' rounds; at least 8 stages remain.
 int dhidden_splits(int rows, int hidden, int stages, int sms) {
-    const int64_t tiles = tiles_of(rows, hidden), slots = sms / kCG;
+    const int64_t tiles = tiles_of(hidden, rows), slots = sms / 2;
     int best = 1;
     double best_fill = 0.;
-    for (int s = 1; s <= 16 && (s == 1 || stages / s >= 8); ++s) {
+    for (int s = 1; s <= 64 && (s == 1 || stages / s >= 8); ++s) {
         const int64_t units = tiles * s, rounds = (units + slots - 1) / slots;
         const double fill = (double)units / (double)(rounds * slots) - 0.01 * s;     // a part more costs its output's traffic
         if (fill > best_fill) { best_fill = fill; best = s; }
@@ -726,8 +730,10 @@ int dhidden_splits(int rows, int hidden, int stages, int sms) {
 
 constexpr int kLiveRowsPerBlock = 8, kLiveThreads = 256;
 
-// Copies the live rows side by side.  Every block counts the live rows before its own range (targets and
-// weights are a few bytes per row and sit in L2), so one launch does the whole compaction, in order.
+// Copies the live rows side by side and takes each one's target logit as an fp32 dot product (the tensor cores'
+// sums drop low bits on the way, always towards zero; a target that leads its row carries that error into its own
+// log-prob in full).  Every block counts the live rows before its own range (targets and weights are a few bytes
+// per row and sit in L2), so one launch does the whole compaction, in order.
 __global__ void __launch_bounds__(kLiveThreads) live_rows_kernel(LiveRows a) {
     __shared__ int counts[kLiveThreads / 32];
     __shared__ int place[kLiveRowsPerBlock];
@@ -752,6 +758,7 @@ __global__ void __launch_bounds__(kLiveThreads) live_rows_kernel(LiveRows a) {
         if (blockIdx.x == gridDim.x - 1) *a.n_live = at;
     }
     __syncthreads();
+    const int pieces = a.H / 8;
     for (int i = row0 + warp; i < end; i += kLiveThreads / 32) {      // a warp copies a row
         const int to = place[i - row0];
         if (to < 0) {
@@ -760,24 +767,48 @@ __global__ void __launch_bounds__(kLiveThreads) live_rows_kernel(LiveRows a) {
                 if (a.targets[i] >= a.vocab) atomicOr(a.err, kErrBadToken);
             }
             if (a.d_hidden)
-                for (int j = lane; j < a.H / 8; j += 32)
+                for (int j = lane; j < pieces; j += 32)
                     reinterpret_cast<uint4*>(a.d_hidden + (int64_t)i * a.ld_d)[j] = make_uint4(0, 0, 0, 0);
             continue;
         }
+        const int tgt = a.targets[i];
         const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (int64_t)i * a.ld);
+        const uint4* head = reinterpret_cast<const uint4*>(a.lm_head + (int64_t)tgt * a.H);
         uint4* dst = reinterpret_cast<uint4*>(a.rows + (int64_t)to * a.H);
-        for (int j = lane; j < a.H / 8; j += 32) dst[j] = src[j];
+        uint4* dst2 = a.lo_rows ? dst + (int64_t)a.lo_rows * pieces : nullptr;
+        float dot = 0.f;
+        for (int j = lane; j < pieces; j += 32) {
+            const uint4 x = src[j], w = head[j];
+            dst[j] = x;
+            if (dst2) dst2[j] = x;
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                dot = fmaf(bf16_lo(xs[q]), bf16_lo(ws[q]), dot);
+                dot = fmaf(bf16_hi(xs[q]), bf16_hi(ws[q]), dot);
+            }
+        }
+        dot = warp_sum(dot);
         if (lane == 0) {
             a.src[to] = i;
-            a.target[to] = a.targets[i];
-            if (a.weight) { a.scaled[to] = a.weight[i] * a.inv_temp; a.lse[to] = a.lse_in[i]; }
+            a.target[to] = tgt;
+            a.target_logit[to] = dot;
+            if (a.weight) {
+                const float w = a.weight[i] * a.inv_temp, l = a.lse_in[i];
+                a.scaled[to] = w;
+                a.lse[to] = l;
+                a.target_d[to] = -w * expm1f(fmaf(dot, a.inv_temp, -l));
+            }
         }
     }
-    if (blockIdx.x == gridDim.x - 1) {       // zero rows up to the tile: contraction indexes of d_lm_head
-        const int total = counts[0], pad = (total + kUpTile - 1) / kUpTile * kUpTile;
-        const int64_t n = (int64_t)(pad - total) * (a.H / 8);
+    if (blockIdx.x == gridDim.x - 1) {       // zero rows behind the end: contraction indexes of d_lm_head
+        const int total = counts[0], pad = a.lo_rows ? a.lo_rows : (total + kUpTile - 1) / kUpTile * kUpTile;
+        const int64_t n = (int64_t)(pad - total) * pieces;
         uint4* dst = reinterpret_cast<uint4*>(a.rows + (int64_t)total * a.H);
-        for (int64_t j = tid; j < n; j += kLiveThreads) dst[j] = make_uint4(0, 0, 0, 0);
+        for (int64_t j = tid; j < n; j += kLiveThreads) {
+            dst[j] = make_uint4(0, 0, 0, 0);
+            if (a.lo_rows) dst[j + (int64_t)a.lo_rows * pieces] = make_uint4(0, 0, 0, 0);
+        }
     }
 }
 
@@ -786,39 +817,52 @@ cudaError_t launch_live_rows(const LiveRows& r, cudaStream_t st) {
     return launch_chained(live_rows_kernel, dim3(blocks < 1 ? 1 : blocks), dim3(kLiveThreads), 0, st, r);
 }
 
-// One warp joins the column tiles' (largest logit, sum) of a row: lse = M / T + log sum, logp = (z_t - M) / T - log sum.
-__global__ void __launch_bounds__(256) logprob_finish_kernel(const float2* stats, int tiles, int tiles_ld, const float* zt,
-                                                             const int32_t* src, const int32_t* n_live, float inv_temp,
-                                                             float* logp, float* lse) {
+// One warp joins a row's (largest logit, sum of the others' exp) of all column tiles with its target's logit z:
+// l = log(exp(z / T) + sum), logp = z / T - l, both taken from the larger of z and the maximum; where the target leads,
+// logp = -log1p(sum exp(M - z)) keeps its relative accuracy down to probabilities next to 1.
+__global__ void __launch_bounds__(256) logprob_finish_kernel(const float2* stats, int tiles, const float* zt, const int32_t* src,
+                                                             const int32_t* n_live, float inv_temp, float* logp, float* lse) {
     pdl_wait();
     const int r = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (r >= *n_live) return;
-    const float2* row = stats + (int64_t)r * tiles_ld;
+    const float2* row = stats + (int64_t)r * tiles;
     const float scale = inv_temp * 1.4426950408889634f;
     float mx = -INFINITY;
     for (int i = lane; i < tiles; i += 32) mx = fmaxf(mx, row[i].x);
     mx = warp_max(mx);
+    const float ref = mx == -INFINITY ? 0.f : mx;
     float sum = 0.f;
     for (int i = lane; i < tiles; i += 32) {
         const float2 v = row[i];
-        sum += v.y * exp2_approx((v.x - mx) * scale);
+        sum += v.y * exp2_approx((v.x - ref) * scale);
     }
     sum = warp_sum(sum);
     if (lane == 0) {
-        const float l = logf(sum);
-        lse[src[r]] = fmaf(mx, inv_temp, l);
-        logp[src[r]] = (zt[r] - mx) * inv_temp - l;
+        const float z = zt[r];
+        float l, lp;
+        if (z >= ref || mx == -INFINITY) {
+            const float x = log1pf(sum * exp2_approx((mx - z) * scale));
+            l = fmaf(z, inv_temp, x);
+            lp = -x;
+        } else {
+            const float x = logf(sum + exp2_approx((z - mx) * scale));
+            l = fmaf(mx, inv_temp, x);
+            lp = (z - mx) * inv_temp - x;
+        }
+        lse[src[r]] = l;
+        logp[src[r]] = lp;
     }
 }
 
-cudaError_t launch_logprob_finish(const float2* stats, int tiles, int tiles_ld, const float* target_logit, const int32_t* src,
+cudaError_t launch_logprob_finish(const float2* stats, int tiles, const float* target_logit, const int32_t* src,
                                   const int32_t* n_live, int n, float inv_temp, float* logp, float* lse, cudaStream_t st) {
-    return launch_chained(logprob_finish_kernel, dim3((n + 7) / 8), dim3(256), 0, st, stats, tiles, tiles_ld, target_logit, src,
-                          n_live, inv_temp, logp, lse);
+    return launch_chained(logprob_finish_kernel, dim3((n + 7) / 8), dim3(256), 0, st, stats, tiles, target_logit, src, n_live,
+                          inv_temp, logp, lse);
 }
 
-// d_hidden of the live rows: the splits' fp32 parts added in order, rounded once, scattered to the original rows.
-__global__ void __launch_bounds__(256) dhidden_finish_kernel(const float* parts, int splits, int64_t split_stride,
+// d_hidden of the live rows: the splits' fp32 parts (and the second bf16 rows' share, lo_rows further) added in
+// order, rounded once, scattered to the original rows.
+__global__ void __launch_bounds__(256) dhidden_finish_kernel(const float* parts, int splits, int64_t split_stride, int lo_rows,
                                                              const int32_t* src, const int32_t* n_live, int H,
                                                              __nv_bfloat16* out, int64_t ld) {
     pdl_wait();
@@ -827,18 +871,19 @@ __global__ void __launch_bounds__(256) dhidden_finish_kernel(const float* parts,
     const float* p = parts + (int64_t)r * H;
     __nv_bfloat16* dst = out + (int64_t)src[r] * ld;
     for (int j = threadIdx.x * 4; j < H; j += 1024) {
-        float4 v = *reinterpret_cast<const float4*>(p + j);
-        for (int s = 1; s < splits; ++s) {
-            const float4 w = *reinterpret_cast<const float4*>(p + s * split_stride + j);
-            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-        }
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < splits; ++s)
+            for (int o = 0; o <= lo_rows; o += lo_rows ? lo_rows : 1) {
+                const float4 w = *reinterpret_cast<const float4*>(p + s * split_stride + (int64_t)o * H + j);
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+            }
         *reinterpret_cast<uint2*>(dst + j) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
     }
 }
 
-cudaError_t launch_dhidden_finish(const float* parts, int splits, int64_t split_stride, const int32_t* src,
+cudaError_t launch_dhidden_finish(const float* parts, int splits, int64_t split_stride, int lo_rows, const int32_t* src,
                                   const int32_t* n_live, int n, int H, __nv_bfloat16* d_hidden, int64_t ld, cudaStream_t st) {
-    return launch_chained(dhidden_finish_kernel, dim3(n), dim3(256), 0, st, parts, splits, split_stride, src, n_live, H,
+    return launch_chained(dhidden_finish_kernel, dim3(n), dim3(256), 0, st, parts, splits, split_stride, lo_rows, src, n_live, H,
                           d_hidden, ld);
 }
 

@@ -11,30 +11,41 @@ namespace mars {
 constexpr int kUpTile = 256;        // rows / columns by which workspace rows and vocabulary pieces are padded
 constexpr int kUpMaxExperts = 1024;
 
-// What the epilogue of a contraction does with its accumulator tile (row = TMEM lane).
+constexpr int kUpLoRows = 128;      // calls of at most this many rows keep d as two bf16 rows (see dlogits_tile)
+
+// Tensor maps of a contraction's operands (bf16, 128-byte swizzle).  K-major: boxes of 64 contraction indexes x 128
+// rows for A, x 16 << i rows for b[i]; MN-major: boxes of 64 contraction indexes x 64 columns (b[0] alone).
+struct UpMaps {
+    CUtensorMap a, b[4];
+};
+
+// What the epilogue of a contraction does with its accumulator tile (M index = TMEM lane).
 struct UpEpilogue {
-    // store: out[row][col], fp32 or bf16, optionally added to what is there
+    // store: out[n][m], fp32 or bf16, optionally added to what is there
     void* out;
-    int64_t ld;               // elements between rows of out
+    int64_t ld;               // elements between N rows of out (or of dlogits)
     int64_t split_stride;     // elements between the outputs of two splits of the contraction
     int out_f32, accumulate;
     // log-prob rows (compact, live rows only)
     const int32_t* target;    // vocabulary entry of every row
     const float* lse;         // log sum exp of every row (gradient)
     const float* weight;      // d loss / d logp / T of every row (gradient)
+    const float* target_d;    // gradient of the target's own logit
+    const int32_t* n_live;    // rows that exist (gradient)
     float inv_temp;
-    float2* stats;            // [row][tiles_n]: (largest logit, sum of exp((logit - largest) / T)) of a column tile
-    float* target_logit;      // [row]
+    float2* stats;            // [row][2 tiles_m]: (largest logit, sum of exp((logit - largest) / T)) of 128 entries
     __nv_bfloat16* dlogits;   // [row][ld] of one vocabulary piece
+    int lo_rows;              // not 0: distance of the second row that holds what the rounding took off
     int v0, vocab;            // first vocabulary entry of the piece, size of the vocabulary
 };
 
-// One contraction (or a family of them, one for each expert): C[m, n] = sum_k A(m, k) B(n, k).
+// One contraction (or a family of them, one for each expert): C[n][m] = sum_k A(m, k) B(n, k).
 struct UpParams {
-    int m, n, k;              // extents; for expert products see below
-    const int32_t* m_live;    // device counts that replace m / k where not null (live rows of a log-prob call)
+    int m, n, k;
+    const int32_t* n_live;    // device counts that replace n / k where not null (live rows of a log-prob call)
     const int32_t* k_live;
     int splits;               // the contraction is cut into this many parts with outputs of their own
+    int m_fastest;            // order of the tiles: neighbours share B, or A
     const int32_t* expert_off;   // [experts + 1], device: groups of rows (expert products)
     int experts, rows;        // rows: extent of the row axis that the offsets refer to
     int32_t* err;
@@ -43,37 +54,38 @@ struct UpParams {
 
 cudaError_t init_update_kernels();
 
-// tensor maps: K-major operands have boxes of 64 x 128 rows, MN-major operands boxes of 64 x 64 rows
-cudaError_t launch_logit_stats(const CUtensorMap& h, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st);
-cudaError_t launch_dlogits(const CUtensorMap& h, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st);
-cudaError_t launch_dhidden(const CUtensorMap& d, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st);
-cudaError_t launch_dhead(const CUtensorMap& d, const CUtensorMap& h, const UpParams& p, int sms, cudaStream_t st);
-cudaError_t launch_expert_fwd(const CUtensorMap& x, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st);
-cudaError_t launch_expert_dx(const CUtensorMap& dy, const CUtensorMap& w, const UpParams& p, int sms, cudaStream_t st);
-cudaError_t launch_expert_dw(const CUtensorMap& dy, const CUtensorMap& x, const UpParams& p, int sms, cudaStream_t st);
+cudaError_t launch_logit_stats(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);    // a = lm_head, b = rows
+cudaError_t launch_dlogits(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);        // a = lm_head, b = rows
+cudaError_t launch_dhidden(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);        // a = lm_head (MN), b = dlogits
+cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);          // a = rows (MN), b = dlogits (MN)
+cudaError_t launch_expert_fwd(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);     // a = w, b = x
+cudaError_t launch_expert_dx(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);      // a = w (MN), b = dy
+cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);      // a = x (MN), b = dy (MN)
 int dhidden_splits(int rows, int hidden, int stages, int sms);
 
 // Live rows of a log-prob call: those with a target (and, for the gradient, a non-zero weight).
 struct LiveRows {
     const __nv_bfloat16* hidden;   // [n][ld]
     int64_t ld;
+    const __nv_bfloat16* lm_head;  // [vocab][H]
     const int32_t* targets;
     const float* weight;           // null: forward
     const float* lse_in;           // gradient: [n]
     int n, H, vocab;
     float inv_temp;
     __nv_bfloat16* rows;           // [padded][H] compact copies, zeroed behind the last one up to a multiple of kUpTile
+    int lo_rows;                   // not 0: a second copy this many rows further, both zeroed up to there
     int32_t *src, *target, *n_live;   // compact: original row, target
-    float *lse, *scaled;           // compact: lse, weight / T
+    float *target_logit, *lse, *scaled, *target_d;   // compact: logit of the target, lse, weight / T, d of the target's logit
     float *logp_out, *lse_out;     // forward: 0 for rows without a target
     __nv_bfloat16* d_hidden;       // gradient: zeroed for rows that are not live
     int64_t ld_d;
     int32_t* err;
 };
 cudaError_t launch_live_rows(const LiveRows& r, cudaStream_t st);
-cudaError_t launch_logprob_finish(const float2* stats, int tiles, int tiles_ld, const float* target_logit, const int32_t* src,
+cudaError_t launch_logprob_finish(const float2* stats, int tiles, const float* target_logit, const int32_t* src,
                                   const int32_t* n_live, int n, float inv_temp, float* logp, float* lse, cudaStream_t st);
-cudaError_t launch_dhidden_finish(const float* parts, int splits, int64_t split_stride, const int32_t* src,
+cudaError_t launch_dhidden_finish(const float* parts, int splits, int64_t split_stride, int lo_rows, const int32_t* src,
                                   const int32_t* n_live, int n, int H, __nv_bfloat16* d_hidden, int64_t ld, cudaStream_t st);
 
 // Gradient lists.

@@ -60,17 +60,23 @@ size_t span(int64_t rows, int64_t ld, int64_t cols, size_t elem) {
 bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 bool aligned4(const void* p) { return (uintptr_t)p % 4 == 0; }
 
-// K-major operand: rows of `inner` contraction indexes; boxes of 64 x 128 rows.
-mars_status_t map_k(CUtensorMap* tm, const void* p, uint64_t inner, uint64_t rows, uint64_t ld) {
+// K-major operand: `rows` rows of `inner` contraction indexes; boxes of 64 x box_rows.
+mars_status_t map_k(CUtensorMap* tm, const void* p, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_rows = 128) {
     const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
-    const cuuint32_t box[2] = {64u, 128u};
+    const cuuint32_t box[2] = {64u, box_rows};
     return make_tiled_map(tm, p, 2, dims, strides, box);
+}
+// The rows of a K-major B operand in boxes of 16, 32, 64 and 128.
+mars_status_t map_rows(UpMaps* m, const void* p, uint64_t inner, uint64_t rows, uint64_t ld) {
+    for (int i = 0; i < 4; ++i) {
+        const mars_status_t s = map_k(&m->b[i], p, inner, rows, ld, 16u << i);
+        if (s != MARS_OK) return s;
+    }
+    return MARS_OK;
 }
 // MN-major operand: `rows` contraction indexes of `inner` columns; boxes of 64 x 64.
 mars_status_t map_mn(CUtensorMap* tm, const void* p, uint64_t inner, uint64_t rows, uint64_t ld) {
-    const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
-    const cuuint32_t box[2] = {64u, 64u};
-    return make_tiled_map(tm, p, 2, dims, strides, box);
+    return map_k(tm, p, inner, rows, ld, 64u);
 }
 // Stack of expert matrices [experts][rows][inner]: the third coordinate keeps a box inside its expert.
 mars_status_t map_stack(CUtensorMap* tm, const void* p, uint64_t inner, uint64_t rows, uint64_t experts, uint32_t box_rows) {
@@ -110,7 +116,7 @@ struct mars_update {
     __nv_bfloat16 *rows, *dlogits;
     float* parts;
     float2* stats;
-    float *target_logit, *lse, *scaled;
+    float *target_logit, *lse, *scaled, *target_d;
     int32_t *src, *target, *n_live;
     cudaStream_t last_stream;
 };
@@ -139,9 +145,10 @@ size_t carve_update(const Layout& l, unsigned char* base, mars_update* u) {
         t.target_logit = (float*)take(R * 4);
         t.lse = (float*)take(R * 4);
         t.scaled = (float*)take(R * 4);
+        t.target_d = (float*)take(R * 4);
         t.rows = (__nv_bfloat16*)take(R * l.H * 2);
         // the forward's statistics and the gradient's pieces are never alive together
-        const size_t stats = R * tiles * 8, grads = align_up(R * l.piece * 2, 256) + (size_t)l.splits * R * l.H * 4;
+        const size_t stats = R * tiles * 16, grads = align_up(R * l.piece * 2, 256) + (size_t)l.splits * R * l.H * 4;
         unsigned char* shared = take(std::max(stats, grads));
         t.stats = (float2*)shared;
         t.dlogits = (__nv_bfloat16*)shared;
@@ -149,7 +156,7 @@ size_t carve_update(const Layout& l, unsigned char* base, mars_update* u) {
     }
     if (u) {
         u->err = t.err; u->n_live = t.n_live; u->src = t.src; u->target = t.target; u->target_logit = t.target_logit;
-        u->lse = t.lse; u->scaled = t.scaled; u->rows = t.rows; u->stats = t.stats; u->dlogits = t.dlogits; u->parts = t.parts;
+        u->lse = t.lse; u->scaled = t.scaled; u->target_d = t.target_d; u->rows = t.rows; u->stats = t.stats; u->dlogits = t.dlogits; u->parts = t.parts;
     }
     return at;
 }
@@ -240,23 +247,22 @@ mars_status_t mars_logprob(mars_update_t* u, void* cuda_stream, int32_t n, const
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    CUtensorMap tm_h, tm_w;
-    RUN(map_k(&tm_h, u->rows, l.H, l.rows, l.H));
-    RUN(map_k(&tm_w, lm_head, l.H, l.V, l.H));
+    UpMaps maps{};
+    RUN(map_k(&maps.a, lm_head, l.H, l.V, l.H));
+    RUN(map_rows(&maps, u->rows, l.H, l.rows, l.H));
     u->last_stream = st;
 
     LiveRows r{};
-    r.hidden = (const __nv_bfloat16*)hidden; r.ld = ld; r.targets = targets;
+    r.hidden = (const __nv_bfloat16*)hidden; r.ld = ld; r.lm_head = (const __nv_bfloat16*)lm_head; r.targets = targets;
     r.n = n; r.H = l.H; r.vocab = l.V; r.inv_temp = 1.f / temperature;
-    r.rows = u->rows; r.src = u->src; r.target = u->target; r.n_live = u->n_live;
+    r.rows = u->rows; r.src = u->src; r.target = u->target; r.n_live = u->n_live; r.target_logit = u->target_logit;
     r.logp_out = out_logprobs; r.lse_out = out_lse; r.err = u->err;
     RUN(launched(launch_live_rows(r, st)));
     UpParams p{};
-    p.m = n; p.n = l.V; p.k = l.H; p.m_live = u->n_live; p.splits = 1; p.err = u->err;
-    p.e.target = u->target; p.e.inv_temp = 1.f / temperature; p.e.stats = u->stats; p.e.target_logit = u->target_logit;
-    RUN(launched(launch_logit_stats(tm_h, tm_w, p, u->sms, st)));
-    const int tiles = (l.V + 255) / 256;
-    return launched(launch_logprob_finish(u->stats, tiles, tiles, u->target_logit, u->src, u->n_live, n, 1.f / temperature,
+    p.m = l.V; p.n = n; p.k = l.H; p.n_live = u->n_live; p.splits = 1; p.err = u->err;
+    p.e.target = u->target; p.e.inv_temp = 1.f / temperature; p.e.stats = u->stats;
+    RUN(launched(launch_logit_stats(maps, p, u->sms, st)));
+    return launched(launch_logprob_finish(u->stats, (l.V + 255) / 256 * 2, u->target_logit, u->src, u->n_live, n, 1.f / temperature,
                                           out_logprobs, out_lse, st));
 }
 
@@ -283,16 +289,20 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
         if (!accumulate) CUDA_TRY(cudaMemsetAsync(d_lm_head, 0, ow, st));
         return MARS_OK;
     }
-    CUtensorMap tm_h, tm_h_mn, tm_w, tm_w_mn, tm_d, tm_d_mn;
-    RUN(map_k(&tm_h, u->rows, l.H, l.rows, l.H));
-    RUN(map_mn(&tm_h_mn, u->rows, l.H, l.rows, l.H));
-    RUN(map_k(&tm_d, u->dlogits, l.piece, l.rows, l.piece));
-    RUN(map_mn(&tm_d_mn, u->dlogits, l.piece, l.rows, l.piece));
+    // few rows: d as two bf16 rows each, the second ones behind the first; counts are then the padded ones
+    const int lo = n <= kUpLoRows ? (int)align_up((size_t)n, 32) : 0;
+    UpMaps logits{}, dhidden{}, dhead{};
+    RUN(map_rows(&logits, u->rows, l.H, l.rows, l.H));
+    RUN(map_rows(&dhidden, u->dlogits, l.piece, l.rows, l.piece));
+    RUN(map_mn(&dhead.a, u->rows, l.H, l.rows, l.H));
+    RUN(map_mn(&dhead.b[0], u->dlogits, l.piece, l.rows, l.piece));
 
     LiveRows r{};
-    r.hidden = (const __nv_bfloat16*)hidden; r.ld = ld; r.targets = targets; r.weight = d_logprobs; r.lse_in = lse;
+    r.hidden = (const __nv_bfloat16*)hidden; r.ld = ld; r.lm_head = (const __nv_bfloat16*)lm_head; r.targets = targets;
+    r.weight = d_logprobs; r.lse_in = lse;
     r.n = n; r.H = l.H; r.vocab = l.V; r.inv_temp = 1.f / temperature;
-    r.rows = u->rows; r.src = u->src; r.target = u->target; r.n_live = u->n_live; r.lse = u->lse; r.scaled = u->scaled;
+    r.rows = u->rows; r.lo_rows = lo; r.src = u->src; r.target = u->target; r.n_live = u->n_live;
+    r.target_logit = u->target_logit; r.lse = u->lse; r.scaled = u->scaled; r.target_d = u->target_d;
     r.d_hidden = (__nv_bfloat16*)d_hidden; r.ld_d = ld_d; r.err = u->err;
     RUN(launched(launch_live_rows(r, st)));
 
@@ -305,26 +315,27 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
         if (v0 >= l.V) break;
         const int width = std::min(l.piece, l.V - v0), padded = (int)align_up((size_t)width, kUpTile);
         const unsigned char* w_piece = (const unsigned char*)lm_head + (size_t)v0 * l.H * 2;
-        RUN(map_k(&tm_w, w_piece, l.H, width, l.H));
-        RUN(map_mn(&tm_w_mn, w_piece, l.H, width, l.H));
+        RUN(map_k(&logits.a, w_piece, l.H, width, l.H));
+        RUN(map_mn(&dhidden.a, w_piece, l.H, width, l.H));
         UpParams p{};
-        p.m = n; p.n = padded; p.k = l.H; p.m_live = u->n_live; p.splits = 1; p.err = u->err;
-        p.e.target = u->target; p.e.lse = u->lse; p.e.weight = u->scaled; p.e.inv_temp = 1.f / temperature;
-        p.e.dlogits = u->dlogits; p.e.ld = l.piece; p.e.v0 = v0; p.e.vocab = l.V;
-        RUN(launched(launch_dlogits(tm_h, tm_w, p, u->sms, st)));
+        p.m = padded; p.n = lo ? lo : n; p.k = l.H; p.n_live = lo ? nullptr : u->n_live; p.splits = 1; p.err = u->err;
+        p.e.target = u->target; p.e.lse = u->lse; p.e.weight = u->scaled; p.e.target_d = u->target_d; p.e.n_live = u->n_live;
+        p.e.inv_temp = 1.f / temperature;
+        p.e.dlogits = u->dlogits; p.e.ld = l.piece; p.e.lo_rows = lo; p.e.v0 = v0; p.e.vocab = l.V;
+        RUN(launched(launch_dlogits(logits, p, u->sms, st)));
 
         UpParams q{};
-        q.m = n; q.n = l.H; q.k = padded; q.m_live = u->n_live; q.splits = splits; q.err = u->err;
+        q.m = l.H; q.n = lo ? 2 * lo : n; q.k = padded; q.n_live = lo ? nullptr : u->n_live; q.splits = splits; q.err = u->err;
         q.e.out = u->parts; q.e.ld = l.H; q.e.split_stride = stride; q.e.out_f32 = 1; q.e.accumulate = i > 0;
-        RUN(launched(launch_dhidden(tm_d, tm_w_mn, q, u->sms, st)));
+        RUN(launched(launch_dhidden(dhidden, q, u->sms, st)));
 
         UpParams s{};
-        s.m = width; s.n = l.H; s.k = n; s.k_live = u->n_live; s.splits = 1; s.err = u->err;
+        s.m = l.H; s.n = width; s.k = lo ? 2 * lo : n; s.k_live = lo ? nullptr : u->n_live; s.splits = 1; s.m_fastest = 1; s.err = u->err;
         s.e.out = (unsigned char*)d_lm_head + (size_t)v0 * l.H * out_bytes(d_type);
         s.e.ld = l.H; s.e.out_f32 = d_type == MARS_F32; s.e.accumulate = accumulate != 0;
-        RUN(launched(launch_dhead(tm_d_mn, tm_h_mn, s, u->sms, st)));
+        RUN(launched(launch_dhead(dhead, s, u->sms, st)));
     }
-    return launched(launch_dhidden_finish(u->parts, splits, stride, u->src, u->n_live, n, l.H, (__nv_bfloat16*)d_hidden, ld_d, st));
+    return launched(launch_dhidden_finish(u->parts, splits, stride, lo, u->src, u->n_live, n, l.H, (__nv_bfloat16*)d_hidden, ld_d, st));
 }
 
 mars_status_t mars_expert_matmul(mars_update_t* u, void* cuda_stream, int32_t E, int32_t rows, int32_t d_in, int32_t d_out,
@@ -339,14 +350,14 @@ mars_status_t mars_expert_matmul(mars_update_t* u, void* cuda_stream, int32_t E,
         overlap(y, oy, off, ((size_t)E + 1) * 4)) return MARS_ERR_INVALID_ARG;
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;
-    CUtensorMap tm_x, tm_w;
-    RUN(map_k(&tm_x, x, d_in, rows, ld_x));
-    RUN(map_stack(&tm_w, w, d_in, d_out, E, 128));
+    UpMaps maps{};
+    RUN(map_stack(&maps.a, w, d_in, d_out, E, 128));
+    RUN(map_rows(&maps, x, d_in, rows, ld_x));
     u->last_stream = (cudaStream_t)cuda_stream;
     UpParams p{};
-    p.n = d_out; p.k = d_in; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
+    p.m = d_out; p.k = d_in; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
     p.e.out = y; p.e.ld = ld_y; p.e.out_f32 = y_type == MARS_F32;
-    return launched(launch_expert_fwd(tm_x, tm_w, p, u->sms, u->last_stream));
+    return launched(launch_expert_fwd(maps, p, u->sms, u->last_stream));
 }
 
 mars_status_t mars_expert_matmul_dx(mars_update_t* u, void* cuda_stream, int32_t E, int32_t rows, int32_t d_in, int32_t d_out,
@@ -361,14 +372,14 @@ mars_status_t mars_expert_matmul_dx(mars_update_t* u, void* cuda_stream, int32_t
         overlap(dx, ox, off, ((size_t)E + 1) * 4)) return MARS_ERR_INVALID_ARG;
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;
-    CUtensorMap tm_dy, tm_w;
-    RUN(map_k(&tm_dy, dy, d_out, rows, ld_dy));
-    RUN(map_stack(&tm_w, w, d_in, d_out, E, 64));
+    UpMaps maps{};
+    RUN(map_stack(&maps.a, w, d_in, d_out, E, 64));
+    RUN(map_rows(&maps, dy, d_out, rows, ld_dy));
     u->last_stream = (cudaStream_t)cuda_stream;
     UpParams p{};
-    p.n = d_in; p.k = d_out; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
+    p.m = d_in; p.k = d_out; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
     p.e.out = dx; p.e.ld = ld_dx; p.e.out_f32 = dx_type == MARS_F32;
-    return launched(launch_expert_dx(tm_dy, tm_w, p, u->sms, u->last_stream));
+    return launched(launch_expert_dx(maps, p, u->sms, u->last_stream));
 }
 
 mars_status_t mars_expert_matmul_dw(mars_update_t* u, void* cuda_stream, int32_t E, int32_t rows, int32_t d_in, int32_t d_out,
@@ -388,13 +399,13 @@ mars_status_t mars_expert_matmul_dw(mars_update_t* u, void* cuda_stream, int32_t
         if (!accumulate) CUDA_TRY(cudaMemsetAsync(dw, 0, ow, st));
         return MARS_OK;
     }
-    CUtensorMap tm_dy, tm_x;
-    RUN(map_mn(&tm_dy, dy, d_out, rows, ld_dy));
-    RUN(map_mn(&tm_x, x, d_in, rows, ld_x));
+    UpMaps maps{};
+    RUN(map_mn(&maps.a, x, d_in, rows, ld_x));
+    RUN(map_mn(&maps.b[0], dy, d_out, rows, ld_dy));
     UpParams p{};
-    p.m = d_out; p.n = d_in; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
+    p.m = d_in; p.n = d_out; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
     p.e.out = dw; p.e.ld = d_in; p.e.out_f32 = dw_type == MARS_F32; p.e.accumulate = accumulate != 0;
-    return launched(launch_expert_dw(tm_dy, tm_x, p, u->sms, st));
+    return launched(launch_expert_dw(maps, p, u->sms, st));
 }
 
 // ------------------------------------------------------------------------------------ gradient lists
