@@ -15,7 +15,8 @@
 //   warp 0      TMA producer, 64 contraction indexes per stage, 128-byte swizzle, 6-stage mbarrier ring that
 //               runs on across tiles;
 //   warp 1      of the leading CTA: issues tcgen05.mma (M 256, K 16) into one of two TMEM accumulators;
-//   warps 2..9  epilogue of the previous tile (a thread owns one M index, half of the columns) meanwhile.
+//   warps 2..9  epilogue of the previous tile (a thread owns one M index, half of the columns) meanwhile;
+//   warp 10     dw_e: clears rows of ragged stages (below).
 // A K-major operand is a [rows][k] matrix, an MN-major one a [k][columns] matrix (boxes of 64 k x 64 columns),
 // so no transposed copy of anything is made.  Ragged groups: N rows of a tile behind the group's end are
 // computed and not stored; in dw_e, where the rows are the contraction, the stage that holds the end has the
@@ -31,7 +32,7 @@ namespace mars {
 namespace {
 
 constexpr int kTileM = 256, kTileN = 256, kStageK = 64;
-constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
+constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps + 32;
 constexpr uint32_t kSpin = 1u << 22;
 constexpr int kMnBox = 64 * kStageK * 2;                     // 8 KB: 64 contraction rows of 128 B
 constexpr int kABytes = 128 * kStageK * 2;                   // one CTA's half of a tile's A rows
@@ -153,20 +154,28 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
 }
+// 32 columns of this thread's TMEM lane: the request, and the wait after which the values may be used (they pass
+// through it, so that no use can be moved in front).
+__device__ __forceinline__ void tmem_request(uint32_t taddr, float (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                   "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+                   "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+                   "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                   "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                   "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+                   "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+                 :
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+    tmem_request(taddr, v);
+    tmem_wait(v);
 }
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -293,54 +302,93 @@ __device__ __forceinline__ void load_groups(const UpParams& p, int* off, int* fi
 // Two columns of a warp (32 M indexes each) as packed pairs: even lanes get (m, m + 1) of column j, odd lanes of
 // column j + 1, so that a store instruction writes 64 contiguous bytes for each of two output rows.
 __device__ __forceinline__ uint32_t pair_columns(float a, float b, bool odd) {
-    const float got = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
-    return odd ? pack_bf16(got, b) : pack_bf16(a, got);
+    const uint32_t mine = pack_bf16(a, b), other = __shfl_xor_sync(0xffffffffu, mine, 1);
+    return __byte_perm(mine, other, odd ? 0x3276 : 0x5410);
 }
 
-// Store the tile: bf16 (rounded once from the fp32 accumulator) or fp32, optionally on top of what is there.
-__device__ __forceinline__ void store_tile(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1, uint32_t taddr, bool zero) {
+// 32 columns of the tile, from column c on: bf16 (rounded once from the fp32 accumulator) or fp32, optionally on top
+// of what is there (added in fp32).
+__device__ __forceinline__ void store_chunk(const UpEpilogue& e, const Tile& t, int ch, int c, int left, float (&v)[32]) {
     const bool live = ch < t.m_valid, odd = ch & 1;
+    const bool whole = left >= 32 && (ch | 31) < t.m_valid;          // the same for the warp
+    if (e.out_f32) {
+        float* dst = reinterpret_cast<float*>(e.out) + t.out + (int64_t)c * e.ld + ch;
+        if (whole && !e.accumulate) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, dst += e.ld) *dst = v[j];
+            return;
+        }
+        if (e.accumulate) {
+            const float* old = dst;
+#pragma unroll
+            for (int j = 0; j < 32; ++j, old += e.ld)
+                if (live && j < left) v[j] += *old;
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j, dst += e.ld)
+            if (live && j < left) *dst = v[j];
+    } else {
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(e.out) + t.out + (int64_t)(c + odd) * e.ld + (ch - odd);
+        const int64_t step = 2 * e.ld;
+        if (e.accumulate) {
+            uint32_t old[16];
+            const __nv_bfloat16* q = dst;
+#pragma unroll
+            for (int j = 0; j < 16; ++j, q += step) old[j] = live && 2 * j + odd < left ? *reinterpret_cast<const uint32_t*>(q) : 0u;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float got = __shfl_xor_sync(0xffffffffu, odd ? bf16_lo(old[j]) : bf16_hi(old[j]), 1);
+                v[2 * j] += odd ? got : bf16_lo(old[j]);             // old[j]: this lane's column of the pair, both M indexes
+                v[2 * j + 1] += odd ? bf16_hi(old[j]) : got;
+            }
+        }
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2, dst += step) *reinterpret_cast<uint32_t*>(dst) = pair_columns(v[j], v[j + 1], odd);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 32; j += 2, dst += step) {
+            const uint32_t w = pair_columns(v[j], v[j + 1], odd);
+            if (live && j + odd < left) *reinterpret_cast<uint32_t*>(dst) = w;
+        }
+    }
+}
+
+// The tile's columns c0 .. c1, the next 32 requested from TMEM while the ones before are stored; `release` is called as
+// soon as the accumulator has been read.
+template <typename F>
+__device__ __forceinline__ void store_tile(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1, uint32_t taddr, F release) {
+    const int end = min(c1, t.n_valid);
+    float v[32], w[32];
+    if (c0 < end) {
+        tmem_request(taddr + c0, v);
+        tmem_wait(v);
+    }
+#pragma unroll 1
+    for (int c = c0; c < end; c += 64) {
+        const bool second = c + 32 < end, third = c + 64 < end;
+        if (second) tmem_request(taddr + c + 32, w);
+        else release();
+        store_chunk(e, t, ch, c, end - c, v);
+        if (!second) return;
+        tmem_wait(w);
+        if (third) tmem_request(taddr + c + 64, v);
+        else release();
+        store_chunk(e, t, ch, c + 32, end - c - 32, w);
+        if (!third) return;
+        tmem_wait(v);
+    }
+    release();          // no column of this warp exists
+}
+__device__ __forceinline__ void store_zeros(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1) {
     const int end = min(c1, t.n_valid);
 #pragma unroll 1
     for (int c = c0; c < end; c += 32) {
         float v[32];
-        if (zero) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = 0.f;
-        } else {
-            tmem_ld32(taddr + c, v);
-        }
-        const int left = end - c;
-        if (e.out_f32) {
-            float* dst = reinterpret_cast<float*>(e.out) + t.out + (int64_t)c * e.ld + ch;
-            if (e.accumulate) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (live && j < left) v[j] += dst[(int64_t)j * e.ld];
-            }
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (live && j < left) dst[(int64_t)j * e.ld] = v[j];
-        } else {
-            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(e.out) + t.out + (int64_t)(c + odd) * e.ld + (ch - odd);
-            uint32_t old[16];
-            if (e.accumulate) {
-#pragma unroll
-                for (int j = 0; j < 32; j += 2)
-                    if (live && j + odd < left) old[j / 2] = *reinterpret_cast<const uint32_t*>(dst + (int64_t)j * e.ld);
-            }
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-                uint32_t w;
-                if (e.accumulate) {          // added in fp32, rounded once
-                    const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
-                    w = live && j + odd < left ? pack_bf16((odd ? got : v[j]) + bf16_lo(old[j / 2]), (odd ? v[j + 1] : got) + bf16_hi(old[j / 2])) : 0u;
-                } else {
-                    w = pair_columns(v[j], v[j + 1], odd);
-                }
-                if (live && j + odd < left) *reinterpret_cast<uint32_t*>(dst + (int64_t)j * e.ld) = w;
-            }
-        }
+        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+        store_chunk(e, t, ch, c, end - c, v);
     }
 }
 
@@ -503,7 +551,7 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                 const uint32_t sa = ring + (uint32_t)s * kStageBytes, sb = sa + kABytes;
                 const int k = t.k0 + ks * kStageK;
                 const bool ragged = SCHED == kGroupK && (t.k_len - ks * kStageK) < kStageK && t.k_len % 16;
-                // a ragged stage is reported by warp 1 once it has cleared rows, any other by the copies to the leader
+                // a ragged stage is reported by the clearing warps, any other by the copies to the leader
                 const uint32_t bar = ragged ? in_cta(&tail[s], rank) : in_cta(&full[s], 0);
                 if (elected) {
                     if (ragged) {
@@ -545,10 +593,8 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                 for (uint32_t w = it > kStages ? it - kStages : 0; w < it; ++w) mb_wait(&full[w % kStages], (w / kStages) & 1);
         }
     } else if (warp == 1) {
-        // the leader's warp issues the MMAs; for kGroupK the other CTA's walks along to clear rows of its own half
-        if (SCHED == kGroupK || rank == 0) {
+        if (rank == 0) {
             const bool elected = elect_one();
-            uint32_t tails = 0;                               // parity of every stage's tail barrier
             int s = 0, local = 0;
             uint32_t phase = 0;
             bool ok = true;
@@ -558,53 +604,63 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                 const int nk = (t.k_len + kStageK - 1) / kStageK;
                 if (nk <= 0) continue;                        // nothing to contract: the epilogue writes zeros
                 const int buf = local & 1;
-                if (rank == 0) {
-                    ok = warp_wait<true>(&acc_empty[buf], ((local >> 1) & 1) ^ 1, dead);
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                }
+                ok = warp_wait<true>(&acc_empty[buf], ((local >> 1) & 1) ^ 1, dead);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t acc = tmem_d + (uint32_t)(buf * kTileN);
                 const uint32_t idesc = kIdesc<A_MN, B_MN> | ((uint32_t)(t.width >> 3) << 17);
                 for (int ks = 0; ok && ks < nk; ++ks) {
                     const int left = t.k_len - ks * kStageK;
                     const int steps = left >= kStageK ? 4 : (left + 15) / 16;
-                    if (SCHED == kGroupK && left < kStageK && left % 16) {
-                        ok = warp_wait(&tail[s], (tails >> s) & 1, dead);
-                        if (!ok) break;
-                        tails ^= 1u << s;
-                        unsigned char* st = smem + (size_t)s * kStageBytes;
-                        const int n_rows = steps * 16 - left;     // rows behind the group's end, up to the step's 16
-                        const int boxes = 2 + (t.width / 2 + 63) / 64;
-                        for (int i = lane; i < n_rows * boxes * 8; i += 32) {
-                            const int piece = i & 7, row = left + (i >> 3) % n_rows, box = (i >> 3) / n_rows;
-                            *reinterpret_cast<uint4*>(st + (size_t)box * kMnBox + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        asm volatile("fence.proxy.async;" ::: "memory");
-                        __syncwarp();
-                        if (elected) mb_arrive_at(in_cta(&full[s], 0));
-                        __syncwarp();
-                    }
-                    if (rank == 0) {
-                        ok = warp_wait<SCHED == kGroupK>(&full[s], phase, dead);
-                        if (!ok) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint64_t da = desc_a + (uint64_t)(s * (kStageBytes >> 4)), db = desc_b + (uint64_t)(s * (kStageBytes >> 4));
-                        if (elected) {
-                            if (steps == 4) {
+                    ok = warp_wait<SCHED == kGroupK>(&full[s], phase, dead);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t da = desc_a + (uint64_t)(s * (kStageBytes >> 4)), db = desc_b + (uint64_t)(s * (kStageBytes >> 4));
+                    if (elected) {
+                        if (steps == 4) {
 #pragma unroll
-                                for (int kk = 0; kk < 4; ++kk)
-                                    mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, kk == 0 ? ks != 0 : 1u);
-                            } else {
-                                for (int kk = 0; kk < steps; ++kk)
-                                    mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, (ks | kk) != 0);
-                            }
-                            commit(&empty[s]);
-                            if (ks == nk - 1) commit(&acc_full[buf]);
+                            for (int kk = 0; kk < 4; ++kk)
+                                mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, kk == 0 ? ks != 0 : 1u);
+                        } else {
+                            for (int kk = 0; kk < steps; ++kk)
+                                mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, (ks | kk) != 0);
                         }
-                        __syncwarp();
+                        commit(&empty[s]);
+                        if (ks == nk - 1) commit(&acc_full[buf]);
                     }
+                    __syncwarp();
                     if (++s == kStages) { s = 0; phase ^= 1; }
                 }
                 ++local;
+            }
+            if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
+        }
+    } else if (warp == 2 + kEpiWarps) {
+        // kGroupK, a warp of either CTA: the rows behind a group's end, up to the step's 16, are cleared in the stage
+        // that holds the end; the MMA warp finds the stage full once both CTAs have done so.
+        if (SCHED == kGroupK) {
+            const bool elected = elect_one();
+            uint32_t tails = 0;                               // parity of every stage's tail barrier
+            int s = 0;
+            bool ok = true;
+            for (int tile = worker; ok && tile < map.count; tile += workers) {
+                const Tile t = map.at(tile);
+                const int nk = (t.k_len + kStageK - 1) / kStageK;
+                if (nk <= 0) continue;
+                const int last = (s + nk - 1) % kStages, left = t.k_len - (nk - 1) * kStageK;
+                s = (s + nk) % kStages;
+                if (left % 16 == 0) continue;
+                ok = warp_wait(&tail[last], (tails >> last) & 1, dead);
+                if (!ok) break;
+                tails ^= 1u << last;
+                unsigned char* st = smem + (size_t)last * kStageBytes + (lane & 7) * 16;
+                const int boxes = 2 + (t.width / 2 + 63) / 64, end = (left + 15) & ~15;
+                for (int row = left + (lane >> 3); row < end; row += 4)
+                    for (int box = 0; box < boxes; ++box)
+                        *reinterpret_cast<uint4*>(st + (size_t)box * kMnBox + row * 128) = make_uint4(0, 0, 0, 0);
+                asm volatile("fence.proxy.async;" ::: "memory");
+                __syncwarp();
+                if (elected) mb_arrive_at(in_cta(&full[last], 0));
+                __syncwarp();
             }
             if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
         }
@@ -617,7 +673,7 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
             const Tile t = map.at(tile);
             const int mid = ((t.width / 2 + 31) & ~31), c0 = half ? mid : 0, c1 = half ? t.width : mid;
             if (t.k_len <= 0) {
-                if (EPI == kStore && !p.e.accumulate) store_tile(p.e, t, ch, c0, c1, 0, true);
+                if (EPI == kStore && !p.e.accumulate) store_zeros(p.e, t, ch, c0, c1);
                 continue;
             }
             const int buf = local & 1;
@@ -637,16 +693,21 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t taddr = tmem_d + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kTileN);
-            if (EPI == kStats)
+            const auto release = [&] {        // this warp has read its part of the accumulator
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mb_arrive_at(in_cta(&acc_empty[buf], 0));
+            };
+            if (EPI == kStats) {
                 stats_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float2*>(epi) + buf * 4 * kTileN, quarter, half, lane,
                            t.m_tile * 2 + rank, map.tiles_m * 2, p.n_live);
-            else if (EPI == kDlogits)
+                release();
+            } else if (EPI == kDlogits) {
                 dlogits_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float4*>(epi) + (warp - 2) * 32, lane, p.e.n_live);
-            else
-                store_tile(p.e, t, ch, c0, c1, taddr, false);
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mb_arrive_at(in_cta(&acc_empty[buf], 0));
+                release();
+            } else {
+                store_tile(p.e, t, ch, c0, c1, taddr, release);
+            }
             ++local;
         }
         if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
