@@ -12,9 +12,9 @@ extern thread_local int32_t g_last_cuda_error;
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-// bf16 tensor map with the 128-byte swizzle (mars_api.cu); box[0] is at most 64 elements.
+// bf16 (or fp32) tensor map with the 128-byte swizzle (mars_api.cu); box[0] is at most 128 bytes.
 mars_status_t make_tiled_map(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims,
-                             const cuuint64_t* strides_bytes, const cuuint32_t* box);
+                             const cuuint64_t* strides_bytes, const cuuint32_t* box, bool f32 = false);
 
 }  // namespace mars
 

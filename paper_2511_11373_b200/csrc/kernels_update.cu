@@ -1,10 +1,10 @@
 // Contractions of the policy update on the 5th-generation tensor cores (tcgen05 + TMEM), all of the form
-// C[n][m] = sum_k A(m, k) B(n, k) with the axis that is contiguous in the output on M (the TMEM lanes):
+// sum_k A(m, k) B(n, k), M being the TMEM lanes:
 //   log-prob of known tokens    logits: A = lm_head (M vocabulary), B = hidden rows; softmax statistics in the epilogue
 //   its gradient, per piece     d = g/T ([v = t] - softmax): the same contraction again, d stored as bf16
 //                               d_hidden += W_piece^T d: A = lm_head (M hidden, MN-major), B = d
-//                               d_lm_head_piece = d^T h: A = hidden rows (M hidden, MN-major), B = d (MN-major)
-//   expert products             y: A = w_e, B = x;   dx: A = w_e (MN-major), B = dy;   dw_e: A = x, B = dy (both MN-major)
+//                               d_lm_head_piece = d^T h: A = d (M vocabulary, MN-major), B = hidden rows (MN-major)
+//   expert products             y: A = w_e, B = x;   dx: A = w_e (MN-major), B = dy;   dw_e: A = dy, B = x (both MN-major)
 // One persistent kernel template serves all of them.  A pair of CTAs (cta_group::2) works on one tile of 256 x
 // up to 256: each CTA holds 128 rows of A and half of B's rows, its tensor core reads the other half from its
 // peer, so a 64-deep stage brings 32 KB into each SM where single-CTA 128 x 256 tiles bring 48 (those ran at the
@@ -31,6 +31,9 @@ namespace mars {
 
 namespace {
 
+enum Sched { kDense, kGroupRows, kGroupK };
+enum Epi { kStats, kDlogits, kStore, kStoreRows };      // kStore: out[n][m], kStoreRows: out[m][n]
+
 constexpr int kTileM = 256, kTileN = 256, kStageK = 64;
 constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps + 32;
 constexpr uint32_t kSpin = 1u << 22;
@@ -38,15 +41,16 @@ constexpr int kMnBox = 64 * kStageK * 2;                     // 8 KB: 64 contrac
 constexpr int kABytes = 128 * kStageK * 2;                   // one CTA's half of a tile's A rows
 constexpr int kBBytes = 128 * kStageK * 2;                   // room for one CTA's half of the widest tile's B rows
 constexpr int kStageBytes = kABytes + kBBytes;
-constexpr int kStages = 6;                                   // 192 KB of ring (3 stages: 10 % slower)
+// 192 KB of ring (3 stages: 10 % slower); 160 KB where a 4 KB stage for each epilogue warp stands beside it
+template <int EPI> constexpr int kStagesOf = EPI == kStoreRows ? 5 : 6;
 constexpr int kGroupWords = 2 * (kUpMaxExperts + 1);
-constexpr int kEpiBytes = 2 * 4 * kTileN * 8;                // statistics of two tiles, or the tokens' values of a chunk per warp
+// statistics of two tiles, or the tokens' values of a chunk per warp; output stages
+template <int EPI> constexpr int kEpiBytes = EPI == kStoreRows ? kEpiWarps * 4096 : 2 * 4 * kTileN * 8;
+template <int EPI>
 constexpr size_t smem_bytes(bool groups) {
-    return (size_t)kStages * kStageBytes + kEpiBytes + 1024 + (groups ? kGroupWords * 4 : 0);
+    return (size_t)kStagesOf<EPI> * kStageBytes + kEpiBytes<EPI> + 1024 + (groups ? kGroupWords * 4 : 0);
 }
 
-enum Sched { kDense, kGroupRows, kGroupK };
-enum Epi { kStats, kDlogits, kStore };
 
 __device__ __forceinline__ void mb_init(uint64_t* bar, int count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
@@ -194,11 +198,13 @@ struct Tile {
     int64_t out;              // element offset of the tile's corner in the output
 };
 
-__device__ __forceinline__ int tile_width(int n, int tiles) { return ((n + tiles - 1) / tiles + 31) & ~31; }
+// One width for all tiles of an extent: a multiple of 32 (the MMA's granularity), of 64 for out[m][n] (128-byte rows).
+template <int STEP>
+__device__ __forceinline__ int tile_width(int n, int tiles) { return ((n + tiles - 1) / tiles + STEP - 1) & ~(STEP - 1); }
 
 // The tiles of a call, numbered the same way in every role.  `off`, `first`: group bounds and the number of
 // tiles before each group, in shared memory.
-template <int SCHED>
+template <int SCHED, bool ROWS>
 struct TileMap {
     const UpParams& p;
     const int* off;
@@ -213,7 +219,7 @@ struct TileMap {
         }
         tiles_m = (p.m + kTileM - 1) / kTileM;
         tiles_n = (n + kTileN - 1) / kTileN;
-        width = tiles_n > 0 ? tile_width(n, tiles_n) : 32;
+        width = tiles_n > 0 ? tile_width<ROWS ? 64 : 32>(n, tiles_n) : 64;
         count = SCHED == kGroupRows ? first[p.experts] : tiles_m * tiles_n * (SCHED == kGroupK ? p.experts : p.splits);
     }
     __device__ __forceinline__ Tile at(int t) const {
@@ -228,15 +234,15 @@ struct TileMap {
             const int rows = off[lo + 1] - off[lo], per = (rows + kTileN - 1) / kTileN, u = t - first[lo];
             r.m_tile = u / per;                      // rows fastest: neighbours share the weights
             tn = u - r.m_tile * per;
-            r.width = tile_width(rows, per);
+            r.width = tile_width<32>(rows, per);
             r.k0 = 0; r.k_len = k; r.expert = lo;
             r.b_row = off[lo] + tn * r.width;
             r.n_valid = min(r.width, rows - tn * r.width);
-            r.out = (int64_t)r.b_row * p.e.ld;
+            r.out = 0;
         } else {
             const int per = tiles_m * tiles_n, group = t / per, u = t - group * per;
-            if (SCHED == kGroupK || p.m_fastest) { tn = u / tiles_m; r.m_tile = u - tn * tiles_m; }
-            else { r.m_tile = u / tiles_n; tn = u - r.m_tile * tiles_n; }
+            r.m_tile = u / tiles_n;                  // N fastest: neighbours share A
+            tn = u - r.m_tile * tiles_n;
             r.width = width;
             r.b_row = tn * width;
             r.n_valid = min(width, n - r.b_row);
@@ -244,19 +250,19 @@ struct TileMap {
                 r.expert = group;
                 r.k0 = off[group];
                 r.k_len = off[group + 1] - off[group];
-                r.out = ((int64_t)group * n + r.b_row) * p.e.ld;
+                r.out = (int64_t)group * p.e.split_stride;
             } else {
                 const int stages = (k + kStageK - 1) / kStageK;
                 const int s0 = (int)((int64_t)stages * group / p.splits), s1 = (int)((int64_t)stages * (group + 1) / p.splits);
                 r.expert = 0;
                 r.k0 = s0 * kStageK;
                 r.k_len = min(k, s1 * kStageK) - r.k0;
-                r.out = (int64_t)group * p.e.split_stride + (int64_t)r.b_row * p.e.ld;
+                r.out = (int64_t)group * p.e.split_stride;
             }
         }
         r.a_row = r.m_tile * kTileM;
         r.m_valid = p.m - r.a_row;
-        r.out += r.a_row;
+        r.out += ROWS ? (int64_t)r.a_row * p.e.ld + r.b_row : (int64_t)r.b_row * p.e.ld + r.a_row;
         return r;
     }
 };
@@ -355,9 +361,116 @@ __device__ __forceinline__ void store_chunk(const UpEpilogue& e, const Tile& t, 
     }
 }
 
+// The same for out[m][n]: a thread owns an output row and its columns lie side by side.
+__device__ __forceinline__ void store_rows_chunk(const UpEpilogue& e, const Tile& t, int row, int c, int left, float (&v)[32]) {
+    if (row >= t.m_valid) return;
+    const int64_t at = t.out + (int64_t)row * e.ld + c;
+    if (e.out_f32) {
+        float* dst = reinterpret_cast<float*>(e.out) + at;
+        if (e.accumulate) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+                if (j < left) {
+                    const float4 o = *reinterpret_cast<const float4*>(dst + j);
+                    v[j] += o.x; v[j + 1] += o.y; v[j + 2] += o.z; v[j + 3] += o.w;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 32; j += 8)
+            if (j < left) {                                     // extents are multiples of 8
+                *reinterpret_cast<float4*>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                *reinterpret_cast<float4*>(dst + j + 4) = make_float4(v[j + 4], v[j + 5], v[j + 6], v[j + 7]);
+            }
+    } else {
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(e.out) + at;
+        if (e.accumulate) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8)
+                if (j < left) {
+                    const uint4 o = *reinterpret_cast<const uint4*>(dst + j);
+                    const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) { v[j + 2 * q] += bf16_lo(ow[q]); v[j + 2 * q + 1] += bf16_hi(ow[q]); }
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 32; j += 8)
+            if (j < left)
+                *reinterpret_cast<uint4*>(dst + j) = make_uint4(pack_bf16(v[j], v[j + 1]), pack_bf16(v[j + 2], v[j + 3]),
+                                                                pack_bf16(v[j + 4], v[j + 5]), pack_bf16(v[j + 6], v[j + 7]));
+    }
+}
+
+// out[m][n] without adding, the way dw and d_lm_head leave the kernel: the contraction is short there and the output is
+// the work, so the load/store pipe must not be the limit (with pair stores and exchanges, or with 32-byte stores per
+// thread, dw of 128 x 1536 x 2048 took 250 - 290 us where HBM needs 123 us for the 805 MB).  A warp lays 32 rows of 128
+// bytes side by side in shared memory (128-byte swizzle, no bank conflicts) and a bulk tensor copy takes them out;
+// rows and columns behind the matrix's end are clipped by the copy.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"((uint64_t)tm), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+template <typename F>
+__device__ __forceinline__ void store_tile_bulk(const UpEpilogue& e, const CUtensorMap* tm, const Tile& t, int row0, int c0, int c1,
+                                                uint32_t taddr, unsigned char* stage, int lane, bool elected, F release) {
+    const int end = min(c1, t.n_valid);
+    const bool rows = row0 < t.m_valid;                              // the same for the warp
+    unsigned char* mine = stage + lane * 128;
+    const int turn = lane & 7;
+    const uint32_t src = smem_u32(stage);
+    const auto hand_over = [&](int x) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (elected) {
+            if (rows) tma_store_3d(tm, src, x, t.a_row + row0, t.expert);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    };
+    const auto reclaim = [&] {                                       // the copy before has read the stage
+        if (elected) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    };
+    float v[32], w[32];
+#pragma unroll 1
+    for (int c = c0; c < end; c += 64) {
+        tmem_request(taddr + c, v);
+        tmem_wait(v);
+        tmem_request(taddr + c + 32, w);
+        reclaim();
+        if (e.out_f32) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                *reinterpret_cast<float4*>(mine + ((q ^ turn) * 16)) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+            hand_over(t.b_row + c);
+            tmem_wait(w);
+            if (c + 64 >= end) release();
+            reclaim();
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                *reinterpret_cast<float4*>(mine + ((q ^ turn) * 16)) = make_float4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+            if (c + 32 < end) hand_over(t.b_row + c + 32);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<uint4*>(mine + ((q ^ turn) * 16)) =
+                    make_uint4(pack_bf16(v[8 * q], v[8 * q + 1]), pack_bf16(v[8 * q + 2], v[8 * q + 3]), pack_bf16(v[8 * q + 4], v[8 * q + 5]),
+                               pack_bf16(v[8 * q + 6], v[8 * q + 7]));
+            tmem_wait(w);
+            if (c + 64 >= end) release();
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<uint4*>(mine + (((q + 4) ^ turn) * 16)) =
+                    make_uint4(pack_bf16(w[8 * q], w[8 * q + 1]), pack_bf16(w[8 * q + 2], w[8 * q + 3]), pack_bf16(w[8 * q + 4], w[8 * q + 5]),
+                               pack_bf16(w[8 * q + 6], w[8 * q + 7]));
+            hand_over(t.b_row + c);
+        }
+    }
+    if (c0 >= end) release();
+}
+
 // The tile's columns c0 .. c1, the next 32 requested from TMEM while the ones before are stored; `release` is called as
 // soon as the accumulator has been read.
-template <typename F>
+template <bool ROWS, typename F>
 __device__ __forceinline__ void store_tile(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1, uint32_t taddr, F release) {
     const int end = min(c1, t.n_valid);
     float v[32], w[32];
@@ -370,17 +483,18 @@ __device__ __forceinline__ void store_tile(const UpEpilogue& e, const Tile& t, i
         const bool second = c + 32 < end, third = c + 64 < end;
         if (second) tmem_request(taddr + c + 32, w);
         else release();
-        store_chunk(e, t, ch, c, end - c, v);
+        if (ROWS) store_rows_chunk(e, t, ch, c, end - c, v); else store_chunk(e, t, ch, c, end - c, v);
         if (!second) return;
         tmem_wait(w);
         if (third) tmem_request(taddr + c + 64, v);
         else release();
-        store_chunk(e, t, ch, c + 32, end - c - 32, w);
+        if (ROWS) store_rows_chunk(e, t, ch, c + 32, end - c - 32, w); else store_chunk(e, t, ch, c + 32, end - c - 32, w);
         if (!third) return;
         tmem_wait(v);
     }
     release();          // no column of this warp exists
 }
+template <bool ROWS>
 __device__ __forceinline__ void store_zeros(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1) {
     const int end = min(c1, t.n_valid);
 #pragma unroll 1
@@ -388,7 +502,7 @@ __device__ __forceinline__ void store_zeros(const UpEpilogue& e, const Tile& t, 
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = 0.f;
-        store_chunk(e, t, ch, c, end - c, v);
+        if (ROWS) store_rows_chunk(e, t, ch, c, end - c, v); else store_chunk(e, t, ch, c, end - c, v);
     }
 }
 
@@ -498,8 +612,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpParams p) {
     extern __shared__ unsigned char up_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)up_raw + 1023) & ~(uintptr_t)1023);
+    constexpr int kStages = kStagesOf<EPI>;
     unsigned char* epi = smem + kStages * kStageBytes;
-    int* off = reinterpret_cast<int*>(epi + kEpiBytes);
+    int* off = reinterpret_cast<int*>(epi + kEpiBytes<EPI>);
     int* first = off + kUpMaxExperts + 1;
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], tail[kStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
@@ -528,7 +643,7 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_d = tmem_slot;
-    const TileMap<SCHED> map(p, off, first);
+    const TileMap<SCHED, EPI == kStoreRows> map(p, off, first);
     const uint32_t ring = smem_u32(smem);
 
     if (warp == 0) {
@@ -667,13 +782,15 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
     } else {
         // a warp may touch the TMEM lanes 32 (warp % 4) .. + 31; the first four warps take the left half of the columns
         const int quarter = warp & 3, half = (warp - 2) >> 2, ch = rank * 128 + quarter * 32 + lane;
+        const bool elected = elect_one();
         int local = 0;
         bool ok = true;
         for (int tile = worker; ok && tile < map.count; tile += workers) {
             const Tile t = map.at(tile);
-            const int mid = ((t.width / 2 + 31) & ~31), c0 = half ? mid : 0, c1 = half ? t.width : mid;
+            constexpr int kCols = EPI == kStoreRows ? 64 : 32;
+            const int mid = (t.width / 2 + kCols - 1) & ~(kCols - 1), c0 = half ? mid : 0, c1 = half ? t.width : mid;
             if (t.k_len <= 0) {
-                if (EPI == kStore && !p.e.accumulate) store_zeros(p.e, t, ch, c0, c1);
+                if ((EPI == kStore || EPI == kStoreRows) && !p.e.accumulate) store_zeros<EPI == kStoreRows>(p.e, t, ch, c0, c1);
                 continue;
             }
             const int buf = local & 1;
@@ -705,12 +822,16 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
             } else if (EPI == kDlogits) {
                 dlogits_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float4*>(epi) + (warp - 2) * 32, lane, p.e.n_live);
                 release();
+            } else if (EPI == kStoreRows && p.e.bulk) {
+                store_tile_bulk(p.e, &maps.out, t, ch - lane, c0, c1, taddr, epi + (warp - 2) * 4096, lane, elected, release);
             } else {
-                store_tile(p.e, t, ch, c0, c1, taddr, release);
+                store_tile<EPI == kStoreRows>(p.e, t, ch, c0, c1, taddr, release);
             }
             ++local;
         }
         if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
+        if (EPI == kStoreRows && elected) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // copies out have read their stages
+        __syncwarp();
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     // neither CTA of a pair leaves while the other may still signal its barriers or read its operands; after a wait
@@ -730,12 +851,12 @@ template <bool A_MN, bool B_MN, int SCHED, int EPI>
 cudaError_t launch(const UpMaps& m, const UpParams& p, int64_t tiles, int sms, cudaStream_t st) {
     const int64_t want = tiles < 1 ? 1 : tiles, pairs = sms / 2;
     return launch_chained(contract_kernel<A_MN, B_MN, SCHED, EPI>, dim3((unsigned)(want < pairs ? want : pairs) * 2), dim3(kThreads),
-                          smem_bytes(SCHED != kDense), st, m, p);
+                          smem_bytes<EPI>(SCHED != kDense), st, m, p);
 }
 template <bool A_MN, bool B_MN, int SCHED, int EPI>
 cudaError_t init_one() {
     return cudaFuncSetAttribute(contract_kernel<A_MN, B_MN, SCHED, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)smem_bytes(SCHED != kDense));
+                                (int)smem_bytes<EPI>(SCHED != kDense));
 }
 int64_t tiles_of(int64_t m, int64_t n) { return ((m + kTileM - 1) / kTileM) * ((n + kTileN - 1) / kTileN); }
 }  // namespace
@@ -744,10 +865,10 @@ cudaError_t init_update_kernels() {
     cudaError_t e = init_one<false, false, kDense, kStats>();
     if (e == cudaSuccess) e = init_one<false, false, kDense, kDlogits>();
     if (e == cudaSuccess) e = init_one<true, false, kDense, kStore>();
-    if (e == cudaSuccess) e = init_one<true, true, kDense, kStore>();
+    if (e == cudaSuccess) e = init_one<true, true, kDense, kStoreRows>();
     if (e == cudaSuccess) e = init_one<false, false, kGroupRows, kStore>();
     if (e == cudaSuccess) e = init_one<true, false, kGroupRows, kStore>();
-    if (e == cudaSuccess) e = init_one<true, true, kGroupK, kStore>();
+    if (e == cudaSuccess) e = init_one<true, true, kGroupK, kStoreRows>();
     return e;
 }
 
@@ -761,7 +882,7 @@ cudaError_t launch_dhidden(const UpMaps& m, const UpParams& p, int sms, cudaStre
     return launch<true, false, kDense, kStore>(m, p, tiles_of(p.m, p.n) * p.splits, sms, st);
 }
 cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<true, true, kDense, kStore>(m, p, tiles_of(p.m, p.n), sms, st);
+    return launch<true, true, kDense, kStoreRows>(m, p, tiles_of(p.m, p.n), sms, st);
 }
 cudaError_t launch_expert_fwd(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
     return launch<false, false, kGroupRows, kStore>(m, p, sms, sms, st);
@@ -770,7 +891,7 @@ cudaError_t launch_expert_dx(const UpMaps& m, const UpParams& p, int sms, cudaSt
     return launch<true, false, kGroupRows, kStore>(m, p, sms, sms, st);
 }
 cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
-    return launch<true, true, kGroupK, kStore>(m, p, tiles_of(p.m, p.n) * p.experts, sms, st);
+    return launch<true, true, kGroupK, kStoreRows>(m, p, tiles_of(p.m, p.n) * p.experts, sms, st);
 }
 
 // Parts of the d_hidden contraction (over the vocabulary piece, `stages` stages of 64): few rows give few output

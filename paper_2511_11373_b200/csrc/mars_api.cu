@@ -139,7 +139,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 mars_status_t mars::make_tiled_map(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims,
-                                   const cuuint64_t* strides_bytes, const cuuint32_t* box) {
+                                   const cuuint64_t* strides_bytes, const cuuint32_t* box, bool f32) {
     static std::atomic<void*> known{nullptr};      // looked up once per process
     void* fn = known.load(std::memory_order_relaxed);
     if (!fn) {
@@ -149,7 +149,7 @@ mars_status_t mars::make_tiled_map(CUtensorMap* tm, const void* base, int rank, 
         known.store(fn, std::memory_order_relaxed);
     }
     const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
-    CUresult r = ((EncodeTiledFn)fn)(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims,
+    CUresult r = ((EncodeTiledFn)fn)(tm, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims,
                                      strides_bytes, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);

@@ -15,17 +15,19 @@ constexpr int kUpLoRows = 128;      // calls of at most this many rows keep d as
 
 // Tensor maps of a contraction's operands (bf16, 128-byte swizzle).  K-major: boxes of 64 contraction indexes x 128
 // rows for A, x 16 << i rows for b[i]; MN-major: boxes of 64 contraction indexes x 64 columns (b[0] alone).
+// out: [matrices][rows][columns] of an out[m][n] contraction, boxes of 128 bytes x 32 rows.
 struct UpMaps {
-    CUtensorMap a, b[4];
+    CUtensorMap a, b[4], out;
 };
 
 // What the epilogue of a contraction does with its accumulator tile (M index = TMEM lane).
 struct UpEpilogue {
-    // store: out[n][m], fp32 or bf16, optionally added to what is there
+    // store: fp32 or bf16, optionally added to what is there
     void* out;
-    int64_t ld;               // elements between N rows of out (or of dlogits)
-    int64_t split_stride;     // elements between the outputs of two splits of the contraction
+    int64_t ld;               // elements between rows of out (or of dlogits)
+    int64_t split_stride;     // elements between the outputs of two splits of the contraction, or of two experts
     int out_f32, accumulate;
+    int bulk;                 // out[m][n]: leaves by bulk copies through UpMaps::out (no accumulation)
     // log-prob rows (compact, live rows only)
     const int32_t* target;    // vocabulary entry of every row
     const float* lse;         // log sum exp of every row (gradient)
@@ -39,13 +41,13 @@ struct UpEpilogue {
     int v0, vocab;            // first vocabulary entry of the piece, size of the vocabulary
 };
 
-// One contraction (or a family of them, one for each expert): C[n][m] = sum_k A(m, k) B(n, k).
+// One contraction (or a family of them, one for each expert): sum_k A(m, k) B(n, k) as out[n][m], or out[m][n] for dw and
+// d_lm_head.
 struct UpParams {
     int m, n, k;
     const int32_t* n_live;    // device counts that replace n / k where not null (live rows of a log-prob call)
     const int32_t* k_live;
     int splits;               // the contraction is cut into this many parts with outputs of their own
-    int m_fastest;            // order of the tiles: neighbours share B, or A
     const int32_t* expert_off;   // [experts + 1], device: groups of rows (expert products)
     int experts, rows;        // rows: extent of the row axis that the offsets refer to
     int32_t* err;
@@ -57,10 +59,10 @@ cudaError_t init_update_kernels();
 cudaError_t launch_logit_stats(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);    // a = lm_head, b = rows
 cudaError_t launch_dlogits(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);        // a = lm_head, b = rows
 cudaError_t launch_dhidden(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);        // a = lm_head (MN), b = dlogits
-cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);          // a = rows (MN), b = dlogits (MN)
+cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);          // a = dlogits (MN), b = rows (MN)
 cudaError_t launch_expert_fwd(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);     // a = w, b = x
 cudaError_t launch_expert_dx(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);      // a = w (MN), b = dy
-cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);      // a = x (MN), b = dy (MN)
+cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);      // a = dy (MN), b = x (MN)
 int dhidden_splits(int rows, int hidden, int stages, int sms);
 
 // Live rows of a log-prob call: those with a target (and, for the gradient, a non-zero weight).

@@ -186,6 +186,13 @@ mars_status_t check_experts(const mars_update* u, int32_t E, int32_t rows, int32
     return MARS_OK;
 }
 size_t out_bytes(int type) { return type == MARS_F32 ? 4 : 2; }
+// Output stack [matrices][rows][columns]: boxes of 128 bytes x 32 rows of one matrix.
+mars_status_t map_out(CUtensorMap* tm, void* p, uint64_t columns, uint64_t rows, uint64_t matrices, int type) {
+    const uint64_t eb = out_bytes(type);
+    const cuuint64_t dims[3] = {columns, rows, matrices}, strides[2] = {columns * eb, columns * rows * eb};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / eb), 32u, 1u};
+    return make_tiled_map(tm, p, 3, dims, strides, box, type == MARS_F32);
+}
 
 }  // namespace
 
@@ -294,8 +301,8 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
     UpMaps logits{}, dhidden{}, dhead{};
     RUN(map_rows(&logits, u->rows, l.H, l.rows, l.H));
     RUN(map_rows(&dhidden, u->dlogits, l.piece, l.rows, l.piece));
-    RUN(map_mn(&dhead.a, u->rows, l.H, l.rows, l.H));
-    RUN(map_mn(&dhead.b[0], u->dlogits, l.piece, l.rows, l.piece));
+    RUN(map_mn(&dhead.a, u->dlogits, l.piece, l.rows, l.piece));
+    RUN(map_mn(&dhead.b[0], u->rows, l.H, l.rows, l.H));
 
     LiveRows r{};
     r.hidden = (const __nv_bfloat16*)hidden; r.ld = ld; r.lm_head = (const __nv_bfloat16*)lm_head; r.targets = targets;
@@ -330,9 +337,11 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
         RUN(launched(launch_dhidden(dhidden, q, u->sms, st)));
 
         UpParams s{};
-        s.m = l.H; s.n = width; s.k = lo ? 2 * lo : n; s.k_live = lo ? nullptr : u->n_live; s.splits = 1; s.m_fastest = 1; s.err = u->err;
+        s.m = width; s.n = l.H; s.k = lo ? 2 * lo : n; s.k_live = lo ? nullptr : u->n_live; s.splits = 1; s.err = u->err;
         s.e.out = (unsigned char*)d_lm_head + (size_t)v0 * l.H * out_bytes(d_type);
         s.e.ld = l.H; s.e.out_f32 = d_type == MARS_F32; s.e.accumulate = accumulate != 0;
+        s.e.bulk = !accumulate;
+        if (s.e.bulk) RUN(map_out(&dhead.out, s.e.out, l.H, width, 1, d_type));
         RUN(launched(launch_dhead(dhead, s, u->sms, st)));
     }
     return launched(launch_dhidden_finish(u->parts, splits, stride, lo, u->src, u->n_live, n, l.H, (__nv_bfloat16*)d_hidden, ld_d, st));
@@ -400,11 +409,13 @@ mars_status_t mars_expert_matmul_dw(mars_update_t* u, void* cuda_stream, int32_t
         return MARS_OK;
     }
     UpMaps maps{};
-    RUN(map_mn(&maps.a, x, d_in, rows, ld_x));
-    RUN(map_mn(&maps.b[0], dy, d_out, rows, ld_dy));
+    RUN(map_mn(&maps.a, dy, d_out, rows, ld_dy));
+    RUN(map_mn(&maps.b[0], x, d_in, rows, ld_x));
     UpParams p{};
-    p.m = d_in; p.n = d_out; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
-    p.e.out = dw; p.e.ld = d_in; p.e.out_f32 = dw_type == MARS_F32; p.e.accumulate = accumulate != 0;
+    p.m = d_out; p.n = d_in; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
+    p.e.out = dw; p.e.ld = d_in; p.e.split_stride = (int64_t)d_in * d_out; p.e.out_f32 = dw_type == MARS_F32;
+    p.e.accumulate = accumulate != 0; p.e.bulk = !accumulate;
+    if (p.e.bulk) RUN(map_out(&maps.out, dw, d_in, d_out, E, dw_type));
     return launched(launch_expert_dw(maps, p, u->sms, st));
 }
 
