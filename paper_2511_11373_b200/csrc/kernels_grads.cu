@@ -1,8 +1,10 @@
 // The norm over all gradients of a list of tensors, and the list scaled down to a largest norm.
 //   norm = sqrt(sum_t sum_i t_i^2),   out_t = t min(1, max_norm / (norm + 1e-6))
 // Bound by HBM: the list is read once for the norm and, because no output may be written before the norm is
-// known, once more for the outputs.  The list is cut into chunks of kChunkBytes of a tensor's own memory; blocks
-// take chunks round robin, so one launch covers tensors of any number and size.  Squares are added in fp32 over
+// known, once more for the outputs.  The list is cut into chunks of kChunkBytes of a tensor's own memory; every
+// block takes a contiguous run of chunks (the tensor is searched once per run, then followed), so one launch covers
+// tensors of any number and size.  A thread has its eight 16-byte loads of a chunk in flight together.  The scaling
+// pass walks each run backwards: what the norm read last is still in L2.  Squares are added in fp32 over
 // at most a chunk's share of one thread and in fp64 beyond; a chunk whose fp32 sum overflowed, or is so small
 // that squares were lost below the smallest fp32 number, is summed again in fp64.  All sums run in a fixed
 // order: the same list gives the same bits on every call.
@@ -20,21 +22,40 @@ constexpr int kBlocksPerSm = 8;
 
 __host__ __device__ constexpr int elem_bytes(int type) { return type == 0 ? 4 : 2; }     // MARS_F32, MARS_BF16, MARS_F16
 
-__device__ __forceinline__ void unpack(uint4 v, int type, float (&f)[8]) {
+template <int T>
+__device__ __forceinline__ void unpack(uint4 v, float (&f)[8]) {         // fp32 fills the first four
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    if (type == 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
-    } else if (type == 2) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) {
+        if (T == 0) {
+            f[i] = __uint_as_float(w[i]);
+            f[i + 4] = 0.f;
+        } else if (T == 1) {
+            f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]);
+        } else {
             const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
             f[2 * i] = t.x; f[2 * i + 1] = t.y;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { f[i] = __uint_as_float(w[i]); f[i + 4] = 0.f; }
     }
+}
+template <int T>
+__device__ __forceinline__ uint4 scaled(uint4 v, float s) {
+    float f[8];
+    unpack<T>(v, f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] *= s;
+    if (T == 0) return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (T == 1) {
+            w[q] = pack_bf16(f[2 * q], f[2 * q + 1]);
+        } else {
+            const __half2 h = __floats2half2_rn(f[2 * q], f[2 * q + 1]);
+            w[q] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ float load_one(const unsigned char* p, int type) {
     if (type == 0) return *reinterpret_cast<const float*>(p);
@@ -64,8 +85,7 @@ __device__ __forceinline__ int find_tensor(const GradEntry* table, int n, int64_
     }
     return lo;
 }
-__device__ __forceinline__ Chunk chunk_at(const GradEntry* table, int n, int64_t chunk) {
-    const GradEntry g = table[find_tensor(table, n, chunk)];
+__device__ __forceinline__ Chunk chunk_at(const GradEntry& g, int64_t chunk) {
     Chunk c;
     c.type = g.type;
     c.src = reinterpret_cast<const unsigned char*>(g.src);
@@ -106,48 +126,67 @@ __device__ __forceinline__ double block_sum_double(double v, double* scratch) {
     return t;
 }
 
+constexpr int kPieces = kChunkBytes / 16 / kThreads;       // 16-byte pieces of a thread in a whole chunk
+
+// Sum of this thread's squares of a chunk.
+template <int T>
+__device__ __forceinline__ double chunk_squares(const Chunk& c) {
+    const int pieces = (int)((c.hi - c.lo) >> 4);
+    uint4 v[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int at = i * kThreads + threadIdx.x;
+        v[i] = at < pieces ? ldg_stream(c.lo + (size_t)at * 16) : make_uint4(0, 0, 0, 0);
+    }
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t seen = 0;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        float f[8];
+        unpack<T>(v[i], f);
+#pragma unroll
+        for (int j = 0; j < (T == 0 ? 4 : 8); ++j) part[j & 3] = fmaf(f[j], f[j], part[j & 3]);
+        seen |= v[i].x | v[i].y | v[i].z | v[i].w;
+    }
+    float sum = (part[0] + part[1]) + (part[2] + part[3]);
+    const int head = ragged_head(c), tail = ragged_tail(c);
+    float edge = 0.f;
+    if (threadIdx.x < head + tail) {
+        edge = load_one(c.src + ragged_offset(c, threadIdx.x, head, tail), T);
+        sum = fmaf(edge, edge, sum);
+        seen |= edge != 0.f;
+    }
+    // squares of one thread that left the range of fp32: again in fp64 (an infinity or a NaN comes out the same)
+    if (!(sum < 1e37f) || (sum < 1e-20f && (seen & (T == 0 ? 0x7fffffffu : 0x7fff7fffu)))) {
+        double d = (double)edge * (double)edge;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            float f[8];
+            unpack<T>(v[i], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d = fma((double)f[j], (double)f[j], d);
+        }
+        return d;
+    }
+    return sum;
+}
+
+// The run of chunks of a block.
+__device__ __forceinline__ int64_t run_begin(int64_t n_chunks, int64_t b) { return n_chunks * b / gridDim.x; }
+
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const GradEntry* table, int n, int64_t n_chunks, double* partials,
                                                              int32_t* ticket, float max_norm, float* norm_out, float* scale) {
     __shared__ double scratch[kThreads / 32];
     __shared__ int last;
     pdl_wait();
     double total = 0.;
-    for (int64_t chunk = blockIdx.x; chunk < n_chunks; chunk += gridDim.x) {
-        const Chunk c = chunk_at(table, n, chunk);
-        const int pieces = (int)((c.hi - c.lo) >> 4);
-        float sum = 0.f;
-        uint32_t seen = 0;
-        for (int i = threadIdx.x; i < pieces; i += kThreads) {
-            const uint4 v = ldg_stream(c.lo + (size_t)i * 16);
-            float f[8];
-            unpack(v, c.type, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(f[j], f[j], sum);
-            seen |= v.x | v.y | v.z | v.w;
-        }
-        const int head = ragged_head(c), tail = ragged_tail(c);
-        if (threadIdx.x < head + tail) {
-            const float f = load_one(c.src + ragged_offset(c, threadIdx.x, head, tail), c.type);
-            sum = fmaf(f, f, sum);
-            seen |= f != 0.f;
-        }
-        // squares of one thread that left the range of fp32: again in fp64 (an infinity or a NaN in the tensor
-        // comes out the same)
-        if (!(sum < 1e37f) || (sum < 1e-20f && (seen & (c.type == 0 ? 0x7fffffffu : 0x7fff7fffu)))) {
-            double d = 0.;
-            for (int i = threadIdx.x; i < pieces; i += kThreads) {
-                float f[8];
-                unpack(*reinterpret_cast<const uint4*>(c.lo + (size_t)i * 16), c.type, f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d = fma((double)f[j], (double)f[j], d);
-            }
-            if (threadIdx.x < head + tail) {
-                const double f = load_one(c.src + ragged_offset(c, threadIdx.x, head, tail), c.type);
-                d = fma(f, f, d);
-            }
-            total += d;
-        } else {
-            total += sum;
+    const int64_t begin = run_begin(n_chunks, blockIdx.x), end = run_begin(n_chunks, blockIdx.x + 1);
+    if (begin < end) {
+        int t = find_tensor(table, n, begin);
+        for (int64_t chunk = begin; chunk < end; ++chunk) {
+            while (t + 1 < n && table[t + 1].first_chunk <= chunk) ++t;
+            const Chunk c = chunk_at(table[t], chunk);
+            total += c.type == 0 ? chunk_squares<0>(c) : c.type == 1 ? chunk_squares<1>(c) : chunk_squares<2>(c);
         }
     }
     total = block_sum_double(total, scratch);
@@ -173,45 +212,54 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const GradEntry* ta
     }
 }
 
+template <int T>
+__device__ __forceinline__ void scale_chunk(const Chunk& c, float s) {
+    const int pieces = (int)((c.hi - c.lo) >> 4);
+    const int64_t first = c.lo - c.src;
+    constexpr int eb = elem_bytes(T);
+    uint4 v[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int at = i * kThreads + threadIdx.x;
+        if (at < pieces) v[i] = __ldcs(reinterpret_cast<const uint4*>(c.lo + (size_t)at * 16));
+    }
+    if ((((uintptr_t)c.dst ^ (uintptr_t)c.src) & 15) == 0) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int at = i * kThreads + threadIdx.x;
+            if (at < pieces) __stcs(reinterpret_cast<uint4*>(c.dst + first + (int64_t)at * 16), scaled<T>(v[i], s));
+        }
+    } else {                                  // grad and out lie differently in their 16 bytes
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int at = i * kThreads + threadIdx.x;
+            if (at >= pieces) continue;
+            float f[8];
+            unpack<T>(v[i], f);
+#pragma unroll
+            for (int j = 0; j < 16 / eb; ++j) store_one(c.dst + first + (int64_t)at * 16 + j * eb, T, f[j] * s);
+        }
+    }
+    const int head = ragged_head(c), tail = ragged_tail(c);
+    if (threadIdx.x < head + tail) {
+        const int64_t at = ragged_offset(c, threadIdx.x, head, tail);
+        store_one(c.dst + at, T, load_one(c.src + at, T) * s);
+    }
+}
+
 __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const GradEntry* table, int n, int64_t n_chunks, const float* scale) {
     pdl_wait();
     const float s = *scale;
-    for (int64_t chunk = blockIdx.x; chunk < n_chunks; chunk += gridDim.x) {
-        const Chunk c = chunk_at(table, n, n_chunks - 1 - chunk);       // from the end: what the norm read last is in L2
+    const int64_t begin = run_begin(n_chunks, blockIdx.x), end = run_begin(n_chunks, blockIdx.x + 1);
+    if (begin >= end) return;
+    int t = find_tensor(table, n, end - 1);
+    for (int64_t chunk = end - 1; chunk >= begin; --chunk) {
+        while (table[t].first_chunk > chunk || table[t].numel == 0) --t;
+        const Chunk c = chunk_at(table[t], chunk);
         if (s == 1.f && c.src == c.dst) continue;
-        const int pieces = (int)((c.hi - c.lo) >> 4), eb = elem_bytes(c.type);
-        const bool vec = (((uintptr_t)c.dst ^ (uintptr_t)c.src) & 15) == 0;
-        for (int i = threadIdx.x; i < pieces; i += kThreads) {
-            const int64_t at = (c.lo - c.src) + (int64_t)i * 16;
-            float f[8];
-            unpack(*reinterpret_cast<const uint4*>(c.src + at), c.type, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] *= s;
-            if (vec) {
-                uint4 o;
-                if (c.type == 0) {
-                    o = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-                } else if (c.type == 1) {
-                    o = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-                } else {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const __half2 h = __floats2half2_rn(f[2 * q], f[2 * q + 1]);
-                        w[q] = *reinterpret_cast<const uint32_t*>(&h);
-                    }
-                    o = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-                *reinterpret_cast<uint4*>(c.dst + at) = o;
-            } else {
-                for (int j = 0; j < 16 / eb; ++j) store_one(c.dst + at + j * eb, c.type, f[j]);
-            }
-        }
-        const int head = ragged_head(c), tail = ragged_tail(c);
-        if (threadIdx.x < head + tail) {
-            const int64_t at = ragged_offset(c, threadIdx.x, head, tail);
-            store_one(c.dst + at, c.type, load_one(c.src + at, c.type) * s);
-        }
+        if (c.type == 0) scale_chunk<0>(c, s);
+        else if (c.type == 1) scale_chunk<1>(c, s);
+        else scale_chunk<2>(c, s);
     }
 }
 }  // namespace
