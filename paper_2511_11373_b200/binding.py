@@ -443,14 +443,12 @@ MARS_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 def _want(t: torch.Tensor, name: str, dtypes, dev: torch.device, *shape, rows: bool = False):
     """Raises ValueError unless `t` has one of the dtypes and the shape, lies on the handle's device and is
     contiguous (rows: its rows are, with any row stride)."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or tuple(t.shape) != shape:
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.shape != shape:
         raise ValueError(f"{name}: expected {tuple(str(d) for d in dtypes)} {shape}, got "
                          f"{getattr(t, 'dtype', type(t))} {tuple(getattr(t, 'shape', ()))}")
     if t.device != dev:
         raise ValueError(f"{name}: on {t.device}, the handle on {dev}")
-    ok = t.is_contiguous() or (rows and t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1) and
-                               t.stride(0) >= t.shape[1])
-    if not ok:
+    if not t.is_contiguous() and not (rows and (shape[1] == 1 or t.stride(1) == 1) and t.stride(0) >= shape[1]):
         raise ValueError(f"{name}: strides {t.stride()} are not supported")
 
 
@@ -479,8 +477,8 @@ class Update:
     def poll_status(self) -> int:
         return lib().mars_update_poll_status(self.handle)
 
-    def _stream(self, stream) -> c_void_p:
-        return c_void_p((stream if stream is not None else torch.cuda.current_stream(self.device)).cuda_stream)
+    def _stream(self, stream) -> int:
+        return (stream if stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
 
     def close(self):
         if getattr(self, "handle", None):
@@ -504,8 +502,8 @@ def mars_logprob(update: Update, hidden: torch.Tensor, lm_head: torch.Tensor, ta
     _want(targets, "targets", (torch.int32,), dev, n)
     _want(out_logprobs, "out_logprobs", (torch.float32,), dev, n)
     _want(out_lse, "out_lse", (torch.float32,), dev, n)
-    return lib().mars_logprob(update.handle, update._stream(stream), n, _ptr(hidden), _ld(hidden), _ptr(lm_head),
-                              _ptr(targets), float(temperature), _ptr(out_logprobs), _ptr(out_lse))
+    return lib().mars_logprob(update.handle, update._stream(stream), n, hidden.data_ptr(), _ld(hidden), lm_head.data_ptr(),
+                              targets.data_ptr(), float(temperature), out_logprobs.data_ptr(), out_lse.data_ptr())
 
 
 def mars_logprob_grad(update: Update, hidden: torch.Tensor, lm_head: torch.Tensor, targets: torch.Tensor, temperature: float,
@@ -521,9 +519,9 @@ def mars_logprob_grad(update: Update, hidden: torch.Tensor, lm_head: torch.Tenso
     _want(d_logprobs, "d_logprobs", (torch.float32,), dev, n)
     _want(d_hidden, "d_hidden", (torch.bfloat16,), dev, n, update.hidden, rows=True)
     _want(d_lm_head, "d_lm_head", (torch.bfloat16, torch.float32), dev, update.vocab, update.hidden)
-    return lib().mars_logprob_grad(update.handle, update._stream(stream), n, _ptr(hidden), _ld(hidden), _ptr(lm_head),
-                                   _ptr(targets), float(temperature), _ptr(lse), _ptr(d_logprobs), _ptr(d_hidden),
-                                   _ld(d_hidden), _ptr(d_lm_head), MARS_TYPES[d_lm_head.dtype], int(bool(accumulate)))
+    return lib().mars_logprob_grad(update.handle, update._stream(stream), n, hidden.data_ptr(), _ld(hidden), lm_head.data_ptr(),
+                                   targets.data_ptr(), float(temperature), lse.data_ptr(), d_logprobs.data_ptr(), d_hidden.data_ptr(),
+                                   _ld(d_hidden), d_lm_head.data_ptr(), MARS_TYPES[d_lm_head.dtype], int(bool(accumulate)))
 
 
 def _expert_shapes(update: Update, w: torch.Tensor, expert_off: torch.Tensor, name: str, dtypes):
@@ -542,8 +540,8 @@ def mars_expert_matmul(update: Update, x: torch.Tensor, expert_off: torch.Tensor
     rows, out = x.shape[0], (torch.bfloat16, torch.float32)
     _want(x, "x", (torch.bfloat16,), update.device, rows, d_in, rows=True)
     _want(y, "y", out, update.device, rows, d_out, rows=True)
-    return lib().mars_expert_matmul(update.handle, update._stream(stream), E, rows, d_in, d_out, _ptr(x), _ld(x),
-                                    _ptr(expert_off), _ptr(w), _ptr(y), _ld(y), MARS_TYPES[y.dtype])
+    return lib().mars_expert_matmul(update.handle, update._stream(stream), E, rows, d_in, d_out, x.data_ptr(), _ld(x),
+                                    expert_off.data_ptr(), w.data_ptr(), y.data_ptr(), _ld(y), MARS_TYPES[y.dtype])
 
 
 def mars_expert_matmul_dx(update: Update, dy: torch.Tensor, expert_off: torch.Tensor, w: torch.Tensor, dx: torch.Tensor,
@@ -553,8 +551,8 @@ def mars_expert_matmul_dx(update: Update, dy: torch.Tensor, expert_off: torch.Te
     rows, out = dy.shape[0], (torch.bfloat16, torch.float32)
     _want(dy, "dy", (torch.bfloat16,), update.device, rows, d_out, rows=True)
     _want(dx, "dx", out, update.device, rows, d_in, rows=True)
-    return lib().mars_expert_matmul_dx(update.handle, update._stream(stream), E, rows, d_in, d_out, _ptr(dy), _ld(dy),
-                                       _ptr(expert_off), _ptr(w), _ptr(dx), _ld(dx), MARS_TYPES[dx.dtype])
+    return lib().mars_expert_matmul_dx(update.handle, update._stream(stream), E, rows, d_in, d_out, dy.data_ptr(), _ld(dy),
+                                       expert_off.data_ptr(), w.data_ptr(), dx.data_ptr(), _ld(dx), MARS_TYPES[dx.dtype])
 
 
 def mars_expert_matmul_dw(update: Update, dy: torch.Tensor, x: torch.Tensor, expert_off: torch.Tensor, dw: torch.Tensor,
@@ -564,8 +562,8 @@ def mars_expert_matmul_dw(update: Update, dy: torch.Tensor, x: torch.Tensor, exp
     rows = x.shape[0]
     _want(dy, "dy", (torch.bfloat16,), update.device, rows, d_out, rows=True)
     _want(x, "x", (torch.bfloat16,), update.device, rows, d_in, rows=True)
-    return lib().mars_expert_matmul_dw(update.handle, update._stream(stream), E, rows, d_in, d_out, _ptr(dy), _ld(dy),
-                                       _ptr(x), _ld(x), _ptr(expert_off), _ptr(dw), MARS_TYPES[dw.dtype],
+    return lib().mars_expert_matmul_dw(update.handle, update._stream(stream), E, rows, d_in, d_out, dy.data_ptr(), _ld(dy),
+                                       x.data_ptr(), _ld(x), expert_off.data_ptr(), dw.data_ptr(), MARS_TYPES[dw.dtype],
                                        int(bool(accumulate)))
 
 
@@ -614,10 +612,10 @@ class GradList:
 def mars_grads_norm(grads: GradList, out_norm: torch.Tensor, stream=None) -> int:
     """out_norm[0] = the 2-norm over all gradients of the list; returns the status code."""
     _want(out_norm, "out_norm", (torch.float32,), grads.device, 1)
-    return lib().mars_grads_norm(grads.handle, grads._stream(stream), _ptr(out_norm))
+    return lib().mars_grads_norm(grads.handle, grads._stream(stream), out_norm.data_ptr())
 
 
 def mars_grads_clip(grads: GradList, max_norm: float, out_norm: torch.Tensor, stream=None) -> int:
     """The norm, and every gradient scaled by min(1, max_norm / (norm + 1e-6)) into its out; returns the status code."""
     _want(out_norm, "out_norm", (torch.float32,), grads.device, 1)
-    return lib().mars_grads_clip(grads.handle, grads._stream(stream), float(max_norm), _ptr(out_norm))
+    return lib().mars_grads_clip(grads.handle, grads._stream(stream), float(max_norm), out_norm.data_ptr())

@@ -75,7 +75,7 @@ struct LiveRows {
     const float* lse_in;           // gradient: [n]
     int n, H, vocab;
     float inv_temp;
-    __nv_bfloat16* rows;           // [padded][H] compact copies, zeroed behind the last one up to a multiple of kUpTile
+    __nv_bfloat16* rows;           // [padded][H] compact copies, zeros behind the last one up to n rounded up to 16 (or lo_rows)
     int lo_rows;                   // not 0: a second copy this many rows further, both zeroed up to there
     int32_t *src, *target, *n_live;   // compact: original row, target
     float *target_logit, *lse, *scaled, *target_d;   // compact: logit of the target, lse, weight / T, d of the target's logit
