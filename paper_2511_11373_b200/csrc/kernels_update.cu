@@ -528,12 +528,19 @@ __device__ __forceinline__ void stats_tile(const UpEpilogue& e, const Tile& t, i
         float v[32];
         tmem_ld32(taddr + c, v);
         const int tok = t.b_row + c + lane;
-        const int tgt = tok < *n_live ? e.target[tok] : -1;
+        const int tgt = tok < *n_live ? e.target[tok] - (v_row - lane) : -1;           // its lane, if the warp holds the target
+        const uint32_t hits = __ballot_sync(0xffffffffu, (unsigned)tgt < 32u);
+        if (hits) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if ((hits >> j) & 1) {
+                    if (__shfl_sync(0xffffffffu, tgt, j) == lane) v[j] = -INFINITY;
+                }
+        }
         float mine = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-            const int tj = __shfl_sync(0xffffffffu, tgt, j);
-            if (!live || tj == v_row) v[j] = -INFINITY;
+            if (!live) v[j] = -INFINITY;
             const float m = redux_max(v[j]);
             if (lane == j) mine = m;
             v[j] = exp2_approx((v[j] - (m == -INFINITY ? 0.f : m)) * scale);       // nothing but -inf: all terms are 0
@@ -572,36 +579,65 @@ __device__ __forceinline__ void stats_tile(const UpEpilogue& e, const Tile& t, i
 // rows, which are streams of the lm_head anyway, what the rounding took off is stored as a second bf16 row.  The
 // target's own value w (1 - p) comes from its fp32 logit: no cancellation where p is close to 1.  Tokens and
 // entries behind the end are written as zeros: they are contraction indexes of those products.
-__device__ __forceinline__ void dlogits_tile(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1, uint32_t taddr, float4* tokens,
+// The factor is taken into the exponent, w p = sign exp2(z log2 e / T + log2 |w| - lse log2 e), so that a token's share
+// of the work on its 32 entries is one number out of shared memory (read four tokens at a time: the MMAs of the next
+// tile need that memory's bandwidth) and a sign out of a mask; a target is found by one ballot for 32 tokens.
+__device__ __forceinline__ void dlogits_tile(const UpEpilogue& e, const Tile& t, int ch, int c0, int c1, uint32_t taddr, float* tokens,
                                              int lane, const int* n_live) {
-    const int v_row = e.v0 + t.a_row + ch, end = min(c1, t.width);
+    const int v_row = e.v0 + t.a_row + ch, end = min(c1, t.width), n = *n_live;
     const bool live = v_row < e.vocab, odd = ch & 1;
     const float scale = e.inv_temp * 1.4426950408889634f;
 #pragma unroll 1
     for (int c = c0; c < end; c += 32) {
-        const int tok = t.b_row + c + lane;
-        float4 mine = make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
-        if (tok < *n_live) mine = make_float4(e.lse[tok] * -1.4426950408889634f, -e.weight[tok], __int_as_float(e.target[tok]), e.target_d[tok]);
-        __syncwarp();
-        tokens[lane] = mine;
         float v[32];
-        tmem_ld32(taddr + c, v);
+        tmem_request(taddr + c, v);
+        const int tok = t.b_row + c + lane;
+        const bool here = tok < n;
+        float k = -INFINITY, w = 0.f;
+        int tgt = -1;
+        if (here) {
+            w = e.weight[tok];
+            k = fmaf(e.lse[tok], -1.4426950408889634f, log2f(fabsf(w)));
+            tgt = e.target[tok] - (v_row - lane);                    // its lane, if the warp holds the target
+        }
+        __syncwarp();
+        tokens[lane] = k;
+        const uint32_t minus = __ballot_sync(0xffffffffu, w > 0.f), hits = __ballot_sync(0xffffffffu, (unsigned)tgt < 32u);
+        tmem_wait(v);
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float4 k = tokens[j];
-            const float d = k.y * exp2_approx(fmaf(v[j], scale, k.x));
-            v[j] = !live || k.y == 0.f ? 0.f : __float_as_int(k.z) == v_row ? k.w : d;      // live rows have a weight
+        for (int q = 0; q < 8; ++q) {
+            const float4 k4 = reinterpret_cast<const float4*>(tokens)[q];
+            const float ks[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = 4 * q + i;
+                v[j] = __uint_as_float(__float_as_uint(exp2_approx(fmaf(v[j], scale, ks[i]))) ^ ((minus << (31 - j)) & 0x80000000u));
+            }
+        }
+        if (hits) {
+            const float d = (unsigned)tgt < 32u ? e.target_d[tok] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if ((hits >> j) & 1) {
+                    const float dj = __shfl_sync(0xffffffffu, d, j);
+                    if (__shfl_sync(0xffffffffu, tgt, j) == lane) v[j] = dj;
+                }
+        }
+        const int left = n - (t.b_row + c);
+        if (left < 32 || v_row - lane + 32 > e.vocab) {              // tokens or entries behind the end
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = live && j < left ? v[j] : 0.f;
         }
         __nv_bfloat16* dst = e.dlogits + (int64_t)(t.b_row + c + odd) * e.ld + (t.a_row + ch - odd);
+        const int64_t step = 2 * e.ld, lo = (int64_t)e.lo_rows * e.ld;
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            const uint32_t w = pair_columns(v[j], v[j + 1], odd);
-            *reinterpret_cast<uint32_t*>(dst + (int64_t)j * e.ld) = w;
-            if (e.lo_rows) {
+        for (int j = 0; j < 32; j += 2, dst += step) {
+            const uint32_t u = pair_columns(v[j], v[j + 1], odd);
+            *reinterpret_cast<uint32_t*>(dst) = u;
+            if (lo) {
                 const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
-                *reinterpret_cast<uint32_t*>(dst + (int64_t)(j + e.lo_rows) * e.ld) =
-                    pack_bf16((odd ? got : v[j]) - bf16_lo(w), (odd ? v[j + 1] : got) - bf16_hi(w));
+                *reinterpret_cast<uint32_t*>(dst + lo) = pack_bf16((odd ? got : v[j]) - bf16_lo(u), (odd ? v[j + 1] : got) - bf16_hi(u));
             }
         }
     }
@@ -820,7 +856,7 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                            t.m_tile * 2 + rank, map.tiles_m * 2, p.n_live);
                 release();
             } else if (EPI == kDlogits) {
-                dlogits_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float4*>(epi) + (warp - 2) * 32, lane, p.e.n_live);
+                dlogits_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float*>(epi) + (warp - 2) * 32, lane, p.e.n_live);
                 release();
             } else if (EPI == kStoreRows && p.e.bulk) {
                 store_tile_bulk(p.e, &maps.out, t, ch - lane, c0, c1, taddr, epi + (warp - 2) * 4096, lane, elected, release);
