@@ -9,9 +9,9 @@
 // up to 256: each CTA holds 128 rows of A and half of B's rows, its tensor core reads the other half from its
 // peer, so a 64-deep stage brings 32 KB into each SM where single-CTA 128 x 256 tiles bring 48 (those ran at the
 // 11.5 TB/s that the L2 delivers: 758 us against 665 us for 131072 expert rows x 2048 -> 1536).
-// The N width of a tile is a multiple of 32 chosen from the rows there are (one width for all tiles of a group,
-// rows / ceil(rows / 256) rounded up): tokens sit on N, so ragged groups and short calls cost what they hold (a
-// group of 4 rows a 32-wide tile, 300 rows two of 160), and a call of few rows is a plain stream of the weights.
+// The N width of a tile is a multiple of 32 chosen from the rows there are (see cut): tokens sit on N, so ragged
+// groups and short calls cost what they hold (a group of 4 rows a 32-wide tile, 270 rows one of 128 and one of 160),
+// and a call of few rows is a plain stream of the weights.
 //   warp 0      TMA producer, 64 contraction indexes per stage, 128-byte swizzle, 6-stage mbarrier ring that
 //               runs on across tiles;
 //   warp 1      of the leading CTA: issues tcgen05.mma (M 256, K 16) into one of two TMEM accumulators;
@@ -198,9 +198,14 @@ struct Tile {
     int64_t out;              // element offset of the tile's corner in the output
 };
 
-// One width for all tiles of an extent: a multiple of 32 (the MMA's granularity), of 64 for out[m][n] (128-byte rows).
-template <int STEP>
-__device__ __forceinline__ int tile_width(int n, int tiles) { return ((n + tiles - 1) / tiles + STEP - 1) & ~(STEP - 1); }
+// Cuts an extent into `tiles` (= n / 256 rounded up) widths that differ by one unit at most: 32, the MMA's granularity, or
+// 64 for out[m][n] (128-byte rows).  300 rows make tiles of 160 and 160, 270 rows 128 and 160.
+template <int UNIT>
+__device__ __forceinline__ void cut(int n, int tiles, int i, int* start, int* width) {
+    const int units = (n + UNIT - 1) / UNIT, from = units * i / tiles;
+    *start = from * UNIT;
+    *width = (units * (i + 1) / tiles - from) * UNIT;
+}
 
 // The tiles of a call, numbered the same way in every role.  `off`, `first`: group bounds and the number of
 // tiles before each group, in shared memory.
@@ -209,7 +214,7 @@ struct TileMap {
     const UpParams& p;
     const int* off;
     const int* first;
-    int n, k, tiles_m, tiles_n, width, count;
+    int n, k, tiles_m, tiles_n, count;
 
     __device__ __forceinline__ TileMap(const UpParams& q, const int* o, const int* f) : p(q), off(o), first(f) {
         n = p.n; k = p.k;
@@ -219,7 +224,6 @@ struct TileMap {
         }
         tiles_m = (p.m + kTileM - 1) / kTileM;
         tiles_n = (n + kTileN - 1) / kTileN;
-        width = tiles_n > 0 ? tile_width<ROWS ? 64 : 32>(n, tiles_n) : 64;
         count = SCHED == kGroupRows ? first[p.experts] : tiles_m * tiles_n * (SCHED == kGroupK ? p.experts : p.splits);
     }
     __device__ __forceinline__ Tile at(int t) const {
@@ -234,18 +238,18 @@ struct TileMap {
             const int rows = off[lo + 1] - off[lo], per = (rows + kTileN - 1) / kTileN, u = t - first[lo];
             r.m_tile = u / per;                      // rows fastest: neighbours share the weights
             tn = u - r.m_tile * per;
-            r.width = tile_width<32>(rows, per);
+            int start;
+            cut<32>(rows, per, tn, &start, &r.width);
             r.k0 = 0; r.k_len = k; r.expert = lo;
-            r.b_row = off[lo] + tn * r.width;
-            r.n_valid = min(r.width, rows - tn * r.width);
+            r.b_row = off[lo] + start;
+            r.n_valid = min(r.width, rows - start);
             r.out = 0;
         } else {
             const int per = tiles_m * tiles_n, group = t / per, u = t - group * per;
             r.m_tile = u / tiles_n;                  // N fastest: neighbours share A
             tn = u - r.m_tile * tiles_n;
-            r.width = width;
-            r.b_row = tn * width;
-            r.n_valid = min(width, n - r.b_row);
+            cut<ROWS ? 64 : 32>(n, tiles_n, tn, &r.b_row, &r.width);
+            r.n_valid = min(r.width, n - r.b_row);
             if (SCHED == kGroupK) {
                 r.expert = group;
                 r.k0 = off[group];
