@@ -696,10 +696,8 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
             const Tile t = map.at(tile);
             const int nk = (t.k_len + kStageK - 1) / kStageK;
             const int half = t.width / 2, a_row = t.a_row + rank * 128, b_row = t.b_row + rank * half;
-            // B, K-major: one box of 16, 32, 64 or 128 rows holds the half; MN-major: one or two boxes of 64 columns
-            const int box = half <= 16 ? 0 : half <= 32 ? 1 : half <= 64 ? 2 : 3;
-            const uint32_t b_bytes = B_MN ? (uint32_t)((half + 63) / 64 * kMnBox) : (uint32_t)(16 << box) * 128u;
-            const CUtensorMap* tm_b = &maps.b[B_MN ? 0 : box];
+            // B, K-major: the half's rows in boxes of 128, or of 64, 32 and 16; MN-major: one or two boxes of 64 columns
+            const uint32_t b_bytes = B_MN ? (uint32_t)((half + 63) / 64 * kMnBox) : (uint32_t)half * 128u;
             for (int ks = 0; ks < nk; ++ks) {
                 ok = warp_wait(&empty[s], phase ^ 1, dead);
                 if (!ok) break;
@@ -726,10 +724,15 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                         else tma_2d(sa, &maps.a, k, a_row, bar);
                     }
                     if (B_MN) {
-                        tma_2d(sb, tm_b, b_row, k, bar);
-                        if (half > 64) tma_2d(sb + kMnBox, tm_b, b_row + 64, k, bar);
+                        tma_2d(sb, &maps.b[0], b_row, k, bar);
+                        if (half > 64) tma_2d(sb + kMnBox, &maps.b[0], b_row + 64, k, bar);
+                    } else if (half == 128) {
+                        tma_2d(sb, &maps.b[3], k, b_row, bar);
                     } else {
-                        tma_2d(sb, tm_b, k, b_row, bar);
+                        const int r32 = half & 64, r16 = half & 96;
+                        if (half & 64) tma_2d(sb, &maps.b[2], k, b_row, bar);
+                        if (half & 32) tma_2d(sb + r32 * 128, &maps.b[1], k, b_row + r32, bar);
+                        if (half & 16) tma_2d(sb + r16 * 128, &maps.b[0], k, b_row + r16, bar);
                     }
                 }
                 __syncwarp();
