@@ -12,8 +12,8 @@
 // The N width of a tile is a multiple of 32 chosen from the rows there are (see cut): tokens sit on N, so ragged
 // groups and short calls cost what they hold (a group of 4 rows a 32-wide tile, 270 rows one of 128 and one of 160),
 // and a call of few rows is a plain stream of the weights.
-//   warp 0      TMA producer, 64 contraction indexes per stage, 128-byte swizzle, 6-stage mbarrier ring that
-//               runs on across tiles;
+//   warp 0      TMA producer, 64 contraction indexes per stage, 128-byte swizzle, mbarrier ring of 5 to 12
+//               stages that runs on across tiles;
 //   warp 1      of the leading CTA: issues tcgen05.mma (M 256, K 16) into one of two TMEM accumulators;
 //   warps 2..9  epilogue of the previous tile (a thread owns one M index, half of the columns) meanwhile;
 //   warp 10     dw_e: clears rows of ragged stages (below).
@@ -23,6 +23,8 @@
 // rows behind it cleared in shared memory (they belong to the next expert and may hold anything, NaN included).
 // Every wait is bounded; one that gives up sets the status word, the CTA stops issuing, waits for its copies
 // in flight, frees its TMEM and returns.
+#include <algorithm>
+
 #include "common.cuh"
 #include "kernels.h"
 #include "update.h"
@@ -39,16 +41,18 @@ constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps + 32;
 constexpr uint32_t kSpin = 1u << 22;
 constexpr int kMnBox = 64 * kStageK * 2;                     // 8 KB: 64 contraction rows of 128 B
 constexpr int kABytes = 128 * kStageK * 2;                   // one CTA's half of a tile's A rows
-constexpr int kBBytes = 128 * kStageK * 2;                   // room for one CTA's half of the widest tile's B rows
-constexpr int kStageBytes = kABytes + kBBytes;
-// 192 KB of ring (3 stages: 10 % slower); 160 KB where a 4 KB stage for each epilogue warp stands beside it
-template <int EPI> constexpr int kStagesOf = EPI == kStoreRows ? 5 : 6;
+constexpr int kBBytes = 128 * kStageK * 2;                   // one CTA's half of the widest tile's B rows
+// 192 KB of ring, 160 KB where a 4 KB stage for each epilogue warp stands beside it: 6 or 5 stages of full width (3: 10 %
+// slower).  For log-prob rows a stage has as much room for B as the call's tiles take: 10 stages for a few rows (64 scored
+// rows 120 -> 117 us), 4 for pairs of full tiles.  Expert groups keep full stages (one token: 20.2 us, 20.8 with 10).
+template <int EPI> constexpr int kRingBytes = (EPI == kStoreRows ? 5 : 6) * 32768;
+constexpr int kMaxStages = 12;
 constexpr int kGroupWords = 2 * (kUpMaxExperts + 1);
 // statistics of two tiles, or the tokens' values of a chunk per warp; output stages
 template <int EPI> constexpr int kEpiBytes = EPI == kStoreRows ? kEpiWarps * 4096 : 2 * 4 * kTileN * 8;
 template <int EPI>
 constexpr size_t smem_bytes(bool groups) {
-    return (size_t)kStagesOf<EPI> * kStageBytes + kEpiBytes<EPI> + 1024 + (groups ? kGroupWords * 4 : 0);
+    return (size_t)kRingBytes<EPI> + kEpiBytes<EPI> + 1024 + (groups ? kGroupWords * 4 : 0);
 }
 
 
@@ -196,6 +200,8 @@ struct Tile {
     int expert;               // third coordinate of the expert stack
     int m_tile;
     int64_t out;              // element offset of the tile's corner in the output
+    int width2;               // not 0: a second tile beside it in N works on the same A (PAIRS)
+    int b_row2, n_valid2;
 };
 
 // Cuts an extent into `tiles` (= n / 256 rounded up) widths that differ by one unit at most: 32, the MMA's granularity, or
@@ -207,14 +213,29 @@ __device__ __forceinline__ void cut(int n, int tiles, int i, int* start, int* wi
     *width = (units * (i + 1) / tiles - from) * UNIT;
 }
 
-// The tiles of a call, numbered the same way in every role.  `off`, `first`: group bounds and the number of
-// tiles before each group, in shared memory.
-template <int SCHED, bool ROWS>
+// Two N tiles side by side as one unit of work (PAIRS, for d_hidden): a stage holds A once and both tiles' B, so that
+// 288 token rows, say, bring 34 KB per stage into an SM where two units bring 50 (one SM takes 75 - 85 GB/s from L2):
+// 271 rows x 151936 entries 192 us single, 134 us as pairs.  The price is that both accumulators are taken and the
+// epilogue does not hide behind the next unit, so it is for long contractions: for the logits (32 stages) pairs were
+// slower, 194 us against 177.
+__device__ __forceinline__ int n_units(int n, bool pairs) {
+    const int tiles = (n + kTileN - 1) / kTileN;
+    return pairs ? (tiles + 1) / 2 : tiles;
+}
+// Room for B in a stage, in units of 2 KB (half of 32 rows, 128 bytes each): the widest unit of an extent.
+__device__ __forceinline__ int b_room(int n, bool pairs) {
+    const int most = pairs ? 16 : 8;
+    return n <= most * 32 ? max(1, (n + 31) >> 5) : most;
+}
+
+// The units of work of a call, numbered the same way in every role.  `off`, `first`: group bounds and the number of
+// units before each group, in shared memory.
+template <int SCHED, bool ROWS, bool PAIRS>
 struct TileMap {
     const UpParams& p;
     const int* off;
     const int* first;
-    int n, k, tiles_m, tiles_n, count;
+    int n, k, tiles_m, units_n, count;
 
     __device__ __forceinline__ TileMap(const UpParams& q, const int* o, const int* f) : p(q), off(o), first(f) {
         n = p.n; k = p.k;
@@ -223,8 +244,29 @@ struct TileMap {
             if (p.k_live) k = *p.k_live;
         }
         tiles_m = (p.m + kTileM - 1) / kTileM;
-        tiles_n = (n + kTileN - 1) / kTileN;
-        count = SCHED == kGroupRows ? first[p.experts] : tiles_m * tiles_n * (SCHED == kGroupK ? p.experts : p.splits);
+        units_n = n_units(n, PAIRS);
+        count = SCHED == kGroupRows ? first[p.experts] : tiles_m * units_n * (SCHED == kGroupK ? p.experts : p.splits);
+    }
+    // N columns of unit tn of an extent of n that begins at row `base`.
+    __device__ __forceinline__ static void columns(Tile& r, int n, int tn, int base) {
+        const int tiles = (n + kTileN - 1) / kTileN, i = PAIRS ? 2 * tn : tn;
+        int start;
+        cut<ROWS ? 64 : 32>(n, tiles, i, &start, &r.width);
+        r.b_row = base + start;
+        r.n_valid = min(r.width, n - start);
+        r.width2 = 0;
+        if (PAIRS && i + 1 < tiles) {
+            cut<ROWS ? 64 : 32>(n, tiles, i + 1, &start, &r.width2);
+            r.b_row2 = base + start;
+            r.n_valid2 = min(r.width2, n - start);
+        }
+    }
+    // The second tile of a unit.
+    __device__ __forceinline__ Tile second(Tile r) const {
+        r.out += (int64_t)(r.b_row2 - r.b_row) * (ROWS ? 1 : p.e.ld);
+        r.b_row = r.b_row2; r.width = r.width2; r.n_valid = r.n_valid2;
+        r.width2 = 0;
+        return r;
     }
     __device__ __forceinline__ Tile at(int t) const {
         Tile r;
@@ -235,21 +277,18 @@ struct TileMap {
                 const int mid = (lo + hi + 1) >> 1;
                 if (first[mid] <= t) lo = mid; else hi = mid - 1;
             }
-            const int rows = off[lo + 1] - off[lo], per = (rows + kTileN - 1) / kTileN, u = t - first[lo];
+            const int rows = off[lo + 1] - off[lo];
+            const int per = n_units(rows, PAIRS), u = t - first[lo];
             r.m_tile = u / per;                      // rows fastest: neighbours share the weights
             tn = u - r.m_tile * per;
-            int start;
-            cut<32>(rows, per, tn, &start, &r.width);
             r.k0 = 0; r.k_len = k; r.expert = lo;
-            r.b_row = off[lo] + start;
-            r.n_valid = min(r.width, rows - start);
+            columns(r, rows, tn, off[lo]);
             r.out = 0;
         } else {
-            const int per = tiles_m * tiles_n, group = t / per, u = t - group * per;
-            r.m_tile = u / tiles_n;                  // N fastest: neighbours share A
-            tn = u - r.m_tile * tiles_n;
-            cut<ROWS ? 64 : 32>(n, tiles_n, tn, &r.b_row, &r.width);
-            r.n_valid = min(r.width, n - r.b_row);
+            const int per = tiles_m * units_n, group = t / per, u = t - group * per;
+            r.m_tile = u / units_n;                  // N fastest: neighbours share A
+            tn = u - r.m_tile * units_n;
+            columns(r, n, tn, 0);
             if (SCHED == kGroupK) {
                 r.expert = group;
                 r.k0 = off[group];
@@ -291,7 +330,7 @@ __device__ __forceinline__ void load_groups(const UpParams& p, int* off, int* fi
     for (int i = b; i < e; ++i) off[i] = max(off[i], before);
     __syncwarp();
     int sum = 0;
-    for (int i = b; i < min(e, E); ++i) sum += (off[i + 1] - off[i] + kTileN - 1) / kTileN * tiles_m;
+    for (int i = b; i < min(e, E); ++i) sum += n_units(off[i + 1] - off[i], false) * tiles_m;
     int pre = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -301,7 +340,7 @@ __device__ __forceinline__ void load_groups(const UpParams& p, int* off, int* fi
     pre -= sum;
     for (int i = b; i < e; ++i) {
         first[i] = pre;
-        if (i < E) pre += (off[i + 1] - off[i] + kTileN - 1) / kTileN * tiles_m;
+        if (i < E) pre += n_units(off[i + 1] - off[i], false) * tiles_m;
     }
     __syncwarp();
 }
@@ -647,16 +686,15 @@ __device__ __forceinline__ void dlogits_tile(const UpEpilogue& e, const Tile& t,
     }
 }
 
-template <bool A_MN, bool B_MN, int SCHED, int EPI>
+template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpParams p) {
     extern __shared__ unsigned char up_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)up_raw + 1023) & ~(uintptr_t)1023);
-    constexpr int kStages = kStagesOf<EPI>;
-    unsigned char* epi = smem + kStages * kStageBytes;
+    unsigned char* epi = smem + kRingBytes<EPI>;
     int* off = reinterpret_cast<int*>(epi + kEpiBytes<EPI>);
     int* first = off + kUpMaxExperts + 1;
-    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], tail[kStages], acc_full[2], acc_empty[2];
+    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], tail[kMaxStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int dead;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -665,9 +703,11 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
     // a stage of kGroupK is full after two arrivals: the leader's own two, or one of each CTA that cleared rows
     constexpr int kFullCount = SCHED == kGroupK ? 2 : 1;
 
-    if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) { mb_init(&full[i], kFullCount); mb_init(&empty[i], 1); mb_init(&tail[i], 1); }
-        for (int i = 0; i < 2; ++i) { mb_init(&acc_full[i], 1); mb_init(&acc_empty[i], 2 * kEpiWarps); }
+    if (tid < kMaxStages) {
+        mb_init(&full[tid], kFullCount);
+        mb_init(&empty[tid], 1);
+        mb_init(&tail[tid], 1);
+        if (tid < 2) { mb_init(&acc_full[tid], 1); mb_init(&acc_empty[tid], 2 * kEpiWarps); }
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -683,8 +723,11 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_d = tmem_slot;
-    const TileMap<SCHED, EPI == kStoreRows> map(p, off, first);
+    const TileMap<SCHED, EPI == kStoreRows, PAIRS> map(p, off, first);
     const uint32_t ring = smem_u32(smem);
+    constexpr bool kFullStages = B_MN || SCHED != kDense;
+    const uint32_t stage_bytes = kABytes + (kFullStages ? kBBytes : b_room(map.n, PAIRS) * 2048);
+    const int stages = kFullStages ? kRingBytes<EPI> / (kABytes + kBBytes) : min(kMaxStages, (int)(kRingBytes<EPI> / 2048u / (stage_bytes >> 11)));
 
     if (warp == 0) {
         const bool elected = elect_one();
@@ -696,12 +739,23 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
             const Tile t = map.at(tile);
             const int nk = (t.k_len + kStageK - 1) / kStageK;
             const int half = t.width / 2, a_row = t.a_row + rank * 128, b_row = t.b_row + rank * half;
+            const int half2 = PAIRS ? t.width2 / 2 : 0, b_row2 = t.b_row2 + rank * half2;
             // B, K-major: the half's rows in boxes of 128, or of 64, 32 and 16; MN-major: one or two boxes of 64 columns
-            const uint32_t b_bytes = B_MN ? (uint32_t)((half + 63) / 64 * kMnBox) : (uint32_t)half * 128u;
+            const uint32_t b_bytes = B_MN ? (uint32_t)((half + 63) / 64 * kMnBox) : (uint32_t)(half + half2) * 128u;
+            const auto load_rows = [&](uint32_t dst, int k, int row, int n, uint32_t bar) {
+                if (n == 128) {
+                    tma_2d(dst, &maps.b[3], k, row, bar);
+                    return;
+                }
+                const int r32 = n & 64, r16 = n & 96;
+                if (n & 64) tma_2d(dst, &maps.b[2], k, row, bar);
+                if (n & 32) tma_2d(dst + r32 * 128, &maps.b[1], k, row + r32, bar);
+                if (n & 16) tma_2d(dst + r16 * 128, &maps.b[0], k, row + r16, bar);
+            };
             for (int ks = 0; ks < nk; ++ks) {
                 ok = warp_wait(&empty[s], phase ^ 1, dead);
                 if (!ok) break;
-                const uint32_t sa = ring + (uint32_t)s * kStageBytes, sb = sa + kABytes;
+                const uint32_t sa = ring + (uint32_t)s * stage_bytes, sb = sa + kABytes;
                 const int k = t.k0 + ks * kStageK;
                 const bool ragged = SCHED == kGroupK && (t.k_len - ks * kStageK) < kStageK && t.k_len % 16;
                 // a ragged stage is reported by the clearing warps, any other by the copies to the leader
@@ -726,34 +780,31 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                     if (B_MN) {
                         tma_2d(sb, &maps.b[0], b_row, k, bar);
                         if (half > 64) tma_2d(sb + kMnBox, &maps.b[0], b_row + 64, k, bar);
-                    } else if (half == 128) {
-                        tma_2d(sb, &maps.b[3], k, b_row, bar);
                     } else {
-                        const int r32 = half & 64, r16 = half & 96;
-                        if (half & 64) tma_2d(sb, &maps.b[2], k, b_row, bar);
-                        if (half & 32) tma_2d(sb + r32 * 128, &maps.b[1], k, b_row + r32, bar);
-                        if (half & 16) tma_2d(sb + r16 * 128, &maps.b[0], k, b_row + r16, bar);
+                        load_rows(sb, k, b_row, half, bar);
+                        if (PAIRS && half2) load_rows(sb + half * 128, k, b_row2, half2, bar);
                     }
                 }
                 __syncwarp();
                 ++it;
-                if (++s == kStages) { s = 0; phase ^= 1; }
+                if (++s == stages) { s = 0; phase ^= 1; }
             }
         }
         // The last stages' release is waited for as well: it says that the copies into them and the MMAs on them are
         // done, and it is a signal from the leader's MMAs into this CTA's shared memory, which must not be given up
         // before (the epilogue's accumulator signal is another one and need not come later).  After a wait that
         // gave up the copies in flight are waited for instead.
-        for (uint32_t w = it > kStages ? it - kStages : 0; ok && w < it; ++w) ok = warp_wait(&empty[w % kStages], (w / kStages) & 1, dead);
+        const uint32_t st = (uint32_t)stages, from = it > st ? it - st : 0;
+        for (uint32_t w = from; ok && w < it; ++w) ok = warp_wait(&empty[w % st], (w / st) & 1, dead);
         if (!ok) {
             if (lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
             if (rank == 0)
-                for (uint32_t w = it > kStages ? it - kStages : 0; w < it; ++w) mb_wait(&full[w % kStages], (w / kStages) & 1);
+                for (uint32_t w = from; w < it; ++w) mb_wait(&full[w % st], (w / st) & 1);
         }
     } else if (warp == 1) {
         if (rank == 0) {
             const bool elected = elect_one();
-            int s = 0, local = 0;
+            int s = 0, local = 0;                             // stage; tiles so far (accumulators take turns)
             uint32_t phase = 0;
             bool ok = true;
             const uint64_t desc_a = smem_desc<A_MN>(ring), desc_b = smem_desc<B_MN>(ring + kABytes);
@@ -762,17 +813,20 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                 const int nk = (t.k_len + kStageK - 1) / kStageK;
                 if (nk <= 0) continue;                        // nothing to contract: the epilogue writes zeros
                 const int buf = local & 1;
+                const bool two = PAIRS && t.width2;
                 ok = warp_wait<true>(&acc_empty[buf], ((local >> 1) & 1) ^ 1, dead);
+                if (two && ok) ok = warp_wait<true>(&acc_empty[buf ^ 1], (((local + 1) >> 1) & 1) ^ 1, dead);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t acc = tmem_d + (uint32_t)(buf * kTileN);
+                const uint32_t acc = tmem_d + (uint32_t)(buf * kTileN), acc2 = tmem_d + (uint32_t)((buf ^ 1) * kTileN);
                 const uint32_t idesc = kIdesc<A_MN, B_MN> | ((uint32_t)(t.width >> 3) << 17);
+                const uint32_t idesc2 = kIdesc<A_MN, B_MN> | ((uint32_t)((PAIRS ? t.width2 : 0) >> 3) << 17);
                 for (int ks = 0; ok && ks < nk; ++ks) {
                     const int left = t.k_len - ks * kStageK;
                     const int steps = left >= kStageK ? 4 : (left + 15) / 16;
                     ok = warp_wait<SCHED == kGroupK>(&full[s], phase, dead);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t da = desc_a + (uint64_t)(s * (kStageBytes >> 4)), db = desc_b + (uint64_t)(s * (kStageBytes >> 4));
+                    const uint64_t da = desc_a + (uint64_t)(s * (stage_bytes >> 4)), db = desc_b + (uint64_t)(s * (stage_bytes >> 4));
                     if (elected) {
                         if (steps == 4) {
 #pragma unroll
@@ -782,13 +836,21 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                             for (int kk = 0; kk < steps; ++kk)
                                 mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, (ks | kk) != 0);
                         }
+                        if (two) {                            // half the first tile's rows x 128 bytes further, in units of 16
+                            const uint64_t db2 = db + (uint64_t)(t.width * 4);
+                            for (int kk = 0; kk < steps; ++kk)
+                                mma_f16(acc2, da + kDescStep<A_MN> * kk, db2 + kDescStep<B_MN> * kk, idesc2, (ks | kk) != 0);
+                        }
                         commit(&empty[s]);
-                        if (ks == nk - 1) commit(&acc_full[buf]);
+                        if (ks == nk - 1) {
+                            commit(&acc_full[buf]);
+                            if (two) commit(&acc_full[buf ^ 1]);
+                        }
                     }
                     __syncwarp();
-                    if (++s == kStages) { s = 0; phase ^= 1; }
+                    if (++s == stages) { s = 0; phase ^= 1; }
                 }
-                ++local;
+                local += two ? 2 : 1;
             }
             if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
         }
@@ -804,13 +866,13 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
                 const Tile t = map.at(tile);
                 const int nk = (t.k_len + kStageK - 1) / kStageK;
                 if (nk <= 0) continue;
-                const int last = (s + nk - 1) % kStages, left = t.k_len - (nk - 1) * kStageK;
-                s = (s + nk) % kStages;
+                const int last = (s + nk - 1) % stages, left = t.k_len - (nk - 1) * kStageK;
+                s = (s + nk) % stages;
                 if (left % 16 == 0) continue;
                 ok = warp_wait(&tail[last], (tails >> last) & 1, dead);
                 if (!ok) break;
                 tails ^= 1u << last;
-                unsigned char* st = smem + (size_t)last * kStageBytes + (lane & 7) * 16;
+                unsigned char* st = smem + (size_t)last * stage_bytes + (lane & 7) * 16;
                 const int boxes = 2 + (t.width / 2 + 63) / 64, end = (left + 15) & ~15;
                 for (int row = left + (lane >> 3); row < end; row += 4)
                     for (int box = 0; box < boxes; ++box)
@@ -828,8 +890,12 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
         const bool elected = elect_one();
         int local = 0;
         bool ok = true;
-        for (int tile = worker; ok && tile < map.count; tile += workers) {
-            const Tile t = map.at(tile);
+        for (int tile = worker, which = 0; ok && tile < map.count; tile += which ? 0 : workers) {
+            Tile t = map.at(tile);
+            if (PAIRS) {                  // the two tiles of a unit, one after the other
+                if (which) t = map.second(t);
+                which = !which && t.width2;
+            }
             constexpr int kCols = EPI == kStoreRows ? 64 : 32;
             const int mid = (t.width / 2 + kCols - 1) & ~(kCols - 1), c0 = half ? mid : 0, c1 = half ? t.width : mid;
             if (t.k_len <= 0) {
@@ -890,15 +956,15 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
     }
 }
 
-template <bool A_MN, bool B_MN, int SCHED, int EPI>
+template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS = false>
 cudaError_t launch(const UpMaps& m, const UpParams& p, int64_t tiles, int sms, cudaStream_t st) {
     const int64_t want = tiles < 1 ? 1 : tiles, pairs = sms / 2;
-    return launch_chained(contract_kernel<A_MN, B_MN, SCHED, EPI>, dim3((unsigned)(want < pairs ? want : pairs) * 2), dim3(kThreads),
+    return launch_chained(contract_kernel<A_MN, B_MN, SCHED, EPI, PAIRS>, dim3((unsigned)(want < pairs ? want : pairs) * 2), dim3(kThreads),
                           smem_bytes<EPI>(SCHED != kDense), st, m, p);
 }
-template <bool A_MN, bool B_MN, int SCHED, int EPI>
+template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS = false>
 cudaError_t init_one() {
-    return cudaFuncSetAttribute(contract_kernel<A_MN, B_MN, SCHED, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(contract_kernel<A_MN, B_MN, SCHED, EPI, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)smem_bytes<EPI>(SCHED != kDense));
 }
 int64_t tiles_of(int64_t m, int64_t n) { return ((m + kTileM - 1) / kTileM) * ((n + kTileN - 1) / kTileN); }
@@ -908,6 +974,7 @@ cudaError_t init_update_kernels() {
     cudaError_t e = init_one<false, false, kDense, kStats>();
     if (e == cudaSuccess) e = init_one<false, false, kDense, kDlogits>();
     if (e == cudaSuccess) e = init_one<true, false, kDense, kStore>();
+    if (e == cudaSuccess) e = init_one<true, false, kDense, kStore, true>();
     if (e == cudaSuccess) e = init_one<true, true, kDense, kStoreRows>();
     if (e == cudaSuccess) e = init_one<false, false, kGroupRows, kStore>();
     if (e == cudaSuccess) e = init_one<true, false, kGroupRows, kStore>();
@@ -922,6 +989,8 @@ cudaError_t launch_dlogits(const UpMaps& m, const UpParams& p, int sms, cudaStre
     return launch<false, false, kDense, kDlogits>(m, p, tiles_of(p.m, p.n), sms, st);
 }
 cudaError_t launch_dhidden(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    // two tiles of rows go as a pair; more of them fill the rounds better one by one (4096 rows: 771 us per piece as pairs, 575 single)
+    if (p.n <= 2 * kTileN) return launch<true, false, kDense, kStore, true>(m, p, tiles_of(p.m, 1) * p.splits, sms, st);
     return launch<true, false, kDense, kStore>(m, p, tiles_of(p.m, p.n) * p.splits, sms, st);
 }
 cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
@@ -937,15 +1006,18 @@ cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaSt
     return launch<true, true, kGroupK, kStoreRows>(m, p, tiles_of(p.m, p.n) * p.experts, sms, st);
 }
 
-// Parts of the d_hidden contraction (over the vocabulary piece, `stages` stages of 64): few rows give few output
-// tiles, and a piece is long, so it is cut until the tiles fill the pairs' rounds; at least 8 stages remain.
+// Parts of the d_hidden contraction (over the vocabulary piece, `stages` stages of 64): few rows give few units of
+// work, and a piece is long, so it is cut until the units fill the pairs' rounds; at least 8 stages remain.  A part more
+// costs the reading and writing of its fp32 sums, about 13 / stages of the contraction where that is bound by HBM.  Up to two tiles of rows the
+// number of units is known; beyond, the live rows may be fewer than `rows`, and half a round is lost on average.
 int dhidden_splits(int rows, int hidden, int stages, int sms) {
-    const int64_t tiles = tiles_of(hidden, rows), slots = sms / 2;
+    const bool known = rows <= 2 * kTileN;
+    const int64_t units = (hidden + kTileM - 1) / kTileM * (known ? 1 : (rows + kTileN - 1) / kTileN), slots = sms / 2;
     int best = 1;
     double best_fill = 0.;
     for (int s = 1; s <= 64 && (s == 1 || stages / s >= 8); ++s) {
-        const int64_t units = tiles * s, rounds = (units + slots - 1) / slots;
-        const double fill = (double)units / (double)(rounds * slots) - 0.01 * s;     // a part more costs its output's traffic
+        const double full = (double)(units * s) / (double)slots;
+        const double fill = (known ? full / (double)((units * s + slots - 1) / slots) : full / (full + 0.5)) - std::min(0.01, 13. / stages) * s;
         if (fill > best_fill) { best_fill = fill; best = s; }
     }
     return best;
