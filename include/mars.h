@@ -388,7 +388,7 @@ MARS_API const int32_t *mars_active_experts_device(const mars_model_t *model);
  *
  * mars_update_t holds the workspace of the first two groups: `hidden` x `vocab` is the lm_head, max_tokens
  * the largest number of rows of a log-prob call.  hidden = vocab = max_tokens = 0 makes a handle for the
- * expert products alone.  hidden: a multiple of 8, at least 8; vocab >= 1.  Workspace: 256-byte aligned device
+ * expert products alone.  hidden: a multiple of 8, at least 8; vocab >= 1; max_tokens <= 2^20.  Workspace: 256-byte aligned device
  * memory of the device that is current at creation (the handle's device; calls made while another device is
  * current switch to it and back), its content private between calls.  One call at a time per handle, on the
  * GPU as well: calls on several streams are to be ordered by the caller.  mars_update_poll_status works as

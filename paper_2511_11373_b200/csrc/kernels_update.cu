@@ -55,7 +55,6 @@ constexpr size_t smem_bytes(bool groups) {
     return (size_t)kRingBytes<EPI> + kEpiBytes<EPI> + 1024 + (groups ? kGroupWords * 4 : 0);
 }
 
-
 __device__ __forceinline__ void mb_init(uint64_t* bar, int count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
 }
@@ -445,10 +444,10 @@ __device__ __forceinline__ void store_rows_chunk(const UpEpilogue& e, const Tile
 }
 
 // out[m][n] without adding, the way dw and d_lm_head leave the kernel: the contraction is short there and the output is
-// the work, so the load/store pipe must not be the limit (with pair stores and exchanges, or with 32-byte stores per
-// thread, dw of 128 x 1536 x 2048 took 250 - 290 us where HBM needs 123 us for the 805 MB).  A warp lays 32 rows of 128
-// bytes side by side in shared memory (128-byte swizzle, no bank conflicts) and a bulk tensor copy takes them out;
-// rows and columns behind the matrix's end are clipped by the copy.
+// the work, so the load/store pipe must not be the limit (dw of 128 x 1536 x 2048 with few rows: 250 us with pair stores
+// and exchanges, 292 us with 32-byte stores per thread, 196 us this way, which is what writing 805 MB takes: a fill of
+// that size runs at 3.9 TB/s, 207 us).  A warp lays 32 rows of 128 bytes side by side in shared memory (128-byte swizzle,
+// no bank conflicts) and a bulk tensor copy takes them out; rows and columns behind the matrix's end are clipped by it.
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"((uint64_t)tm), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
@@ -912,6 +911,7 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
             }
             if (EPI == kStats) {          // the warps of a column half meet on a barrier: all of them go on, or none
                 uint32_t all_ok;
+                __syncwarp();
                 asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                              : "=r"(all_ok) : "r"((uint32_t)ok), "r"(1 + half) : "memory");
                 ok = all_ok != 0;

@@ -164,7 +164,7 @@ size_t carve_update(const Layout& l, unsigned char* base, mars_update* u) {
 bool update_shape_ok(int32_t hidden, int32_t vocab, int32_t max_tokens) {
     if (hidden == 0 && vocab == 0 && max_tokens == 0) return true;
     return hidden >= 8 && hidden % 8 == 0 && hidden <= (1 << 20) && vocab >= 1 && vocab <= (1 << 30) && max_tokens >= 1 &&
-           max_tokens <= (1 << 24);
+           max_tokens <= (1 << 20);
 }
 
 mars_status_t check_logprob(const mars_update* u, int32_t n, const void* hidden, int64_t ld, const void* lm_head,

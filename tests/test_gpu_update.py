@@ -313,6 +313,49 @@ def test_logprob_refusals():
     assert (d_h == 3).all() and (d_w == 3).all() and u.poll_status() == 0
 
 
+def test_lm_head_beyond_32_bit_offsets():
+    """2.5e9 entries: the target rows in the last and first parts of the matrix, against fp64 on the rows that count."""
+    n, H, V = 3, 8192, 300001
+    g = gen(31)
+    w = torch.empty(V, H, dtype=torch.bfloat16, device=DEV)
+    w.normal_(std=0.01, generator=g)
+    h = normal(g, n, H)
+    targets = torch.tensor([V - 1, 262145, 5], dtype=torch.int32, device=DEV)
+    d = torch.tensor([1.0, -0.5, 2.0], device=DEV)
+    u = binding.Update(H, V, n, device=DEV)
+    got = run_logprob(u, h, w, targets, 1.0, d)
+    z = torch.cat([h.double() @ w[a:a + 50000].double().t() for a in range(0, V, 50000)], dim=1)
+    lse = torch.logsumexp(z, dim=1)
+    at = targets.long()
+    logp = z[torch.arange(n), at] - lse
+    scale = max(float((h.double().abs() @ w[a:a + 50000].double().abs().t()).max()) for a in range(0, V, 50000))
+    tol = 2 * sum_error(H) * scale + 2.0 ** -22 * 32 + 2.0 ** -23 * math.sqrt(V)
+    assert (got["logp"].double() - logp).abs().max() <= tol
+    rows = torch.tensor([0, 5, 262143, 262144, 262145, V - 2, V - 1], device=DEV)
+    dz = -torch.exp(z[:, rows] - lse[:, None]) * d.double()[:, None]
+    for i in range(n):
+        dz[i] += torch.where(rows == at[i], d.double()[i], 0.0)
+    want = dz.t() @ h.double()
+    size = (dz.abs() + 2 * tol).t() @ h.double().abs()
+    assert ((got["d_w"][rows].double() - want).abs() <= size * (2 * U[torch.bfloat16] + 4 * tol)).all()
+
+
+def test_two_handles_on_two_streams_at_once():
+    cases = [logprob_case(400, 256, 3000, 1.0, 0.1, seed=s) for s in (41, 42)]
+    us = [binding.Update(256, 3000, 400, device=DEV) for _ in cases]
+    want = [run_logprob(u, *c[:3], 1.0, c[3]) for u, c in zip(us, cases)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        got = []
+        for u, c, s in zip(us, cases, streams):
+            with torch.cuda.stream(s):
+                got.append(run_logprob(u, *c[:3], 1.0, c[3]))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(a[k], b[k]) for k in a)
+
+
 # -------------------------------------------------------------------------------------- expert products
 
 def offsets(counts, start=0):
@@ -459,6 +502,32 @@ def test_many_experts_and_no_rows():
         assert (dw == 0).all()
         y2 = torch.full((rows, 40), 3.0, device=DEV)
         assert binding.mars_expert_matmul(u, x[:rows], none, w, y2) == 0 and (y2 == 3).all()
+
+
+def test_expert_stack_beyond_32_bit_offsets():
+    """2.7e9 weights: the last expert's rows, and a border between experts behind 2^31 elements."""
+    E, d = 40, 8192
+    counts = [0] * E
+    counts[0], counts[31], counts[32], counts[E - 1] = 2, 20, 5, 17
+    off, g = offsets(counts), gen(33)
+    n = sum(counts)
+    w = torch.empty(E, d, d, dtype=torch.bfloat16, device=DEV)
+    w.normal_(std=0.02, generator=g)
+    x, dy = normal(g, n, d), normal(g, n, d)
+    u = binding.Update(device=DEV)
+    y, dx = torch.empty_like(dy), torch.empty_like(x)
+    assert binding.mars_expert_matmul(u, x, off, w, y) == 0
+    assert binding.mars_expert_matmul_dx(u, dy, off, w, dx) == 0
+    dw = torch.full_like(w, 9.0)
+    assert binding.mars_expert_matmul_dw(u, dy, x, off, dw) == 0
+    o = off.tolist()
+    for e in (0, 31, 32, E - 1):
+        r = slice(o[e], o[e + 1])
+        we, xe, dye = w[e].double(), x[r].double(), dy[r].double()
+        check_rounded(y[r], xe @ we.t(), sum_error(d) * (xe.abs() @ we.abs().t()))
+        check_rounded(dx[r], dye @ we, sum_error(d) * (dye.abs() @ we.abs()))
+        check_rounded(dw[e], dye.t() @ xe, sum_error(20) * (dye.abs().t() @ xe.abs()))
+    assert (dw[1:31] == 0).all() and (dw[33:E - 1] == 0).all()
 
 
 def test_expert_gradients_against_differences():
@@ -640,6 +709,21 @@ def test_clip_is_the_same_every_time_and_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     check_clip(grads, outs, norm, 10.0)
+
+
+def test_a_tensor_beyond_32_bit_offsets():
+    n = 2 ** 32 + 12345
+    t = torch.full((n,), 0.5, dtype=torch.bfloat16, device=DEV)
+    t[-1], t[2 ** 31 + 7] = 300.0, -200.0
+    norm = torch.empty(1, device=DEV)
+    lst = binding.GradList([t[1:]])
+    assert binding.mars_grads_clip(lst, 100.0, norm) == 0
+    want = math.sqrt(0.25 * (n - 3) + 300.0 ** 2 + 200.0 ** 2)
+    assert abs(float(norm) - want) <= 66 * 2.0 ** -24 * want
+    s = 100.0 / want
+    for i, v in ((0, 0.5), (1, 0.5 * s), (2 ** 31 + 7, -200.0 * s), (2 ** 32, 0.5 * s), (n - 2, 0.5 * s), (n - 1, 300.0 * s)):
+        assert abs(float(t[i]) - v) <= abs(v) * (U[BF] + 1e-5), i
+    assert float(t[2 ** 32:].float().sum()) == pytest.approx(float(t[2].float()) * (12345 - 1) + float(t[-1]), rel=1e-5)
 
 
 def test_grad_list_refusals():
