@@ -442,14 +442,21 @@ MARS_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 def _want(t: torch.Tensor, name: str, dtypes, dev: torch.device, *shape, rows: bool = False):
     """Raises ValueError unless `t` has one of the dtypes and the shape, lies on the handle's device and is
-    contiguous (rows: its rows are, with any row stride)."""
+    contiguous (rows: its rows are, with any row stride).  Small calls are bound by the host: the checks are plain
+    comparisons, about 0.3 us a tensor."""
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.shape != shape:
         raise ValueError(f"{name}: expected {tuple(str(d) for d in dtypes)} {shape}, got "
                          f"{getattr(t, 'dtype', type(t))} {tuple(getattr(t, 'shape', ()))}")
-    if t.device != dev:
+    index = dev.index
+    if t.get_device() != (-1 if index is None else index):
         raise ValueError(f"{name}: on {t.device}, the handle on {dev}")
     if not t.is_contiguous() and not (rows and (shape[1] == 1 or t.stride(1) == 1) and t.stride(0) >= shape[1]):
         raise ValueError(f"{name}: strides {t.stride()} are not supported")
+
+
+# raw handle of the current stream; the public accessor builds a Stream object first (2 us)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _ld(t: torch.Tensor) -> int:
@@ -478,7 +485,7 @@ class Update:
         return lib().mars_update_poll_status(self.handle)
 
     def _stream(self, stream) -> int:
-        return (stream if stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
+        return stream.cuda_stream if stream is not None else _raw_stream(self.device.index)
 
     def close(self):
         if getattr(self, "handle", None):

@@ -66,9 +66,11 @@ mars_status_t map_k(CUtensorMap* tm, const void* p, uint64_t inner, uint64_t row
     const cuuint32_t box[2] = {64u, box_rows};
     return make_tiled_map(tm, p, 2, dims, strides, box);
 }
-// The rows of a K-major B operand in boxes of 16, 32, 64 and 128.
-mars_status_t map_rows(UpMaps* m, const void* p, uint64_t inner, uint64_t rows, uint64_t ld) {
-    for (int i = 0; i < 4; ++i) {
+// The rows of a K-major B operand in boxes of 16, 32, 64 and 128, as far as a call of `most` rows can use them: one tile
+// of up to 256 rows, of which each CTA loads half.
+mars_status_t map_rows(UpMaps* m, const void* p, uint64_t inner, uint64_t rows, uint64_t ld, int64_t most) {
+    const int64_t half = most > 256 ? 128 : (most + 31) / 32 * 16;
+    for (int i = 0; i < 4 && (16 << i) <= half; ++i) {
         const mars_status_t s = map_k(&m->b[i], p, inner, rows, ld, 16u << i);
         if (s != MARS_OK) return s;
     }
@@ -256,7 +258,7 @@ mars_status_t mars_logprob(mars_update_t* u, void* cuda_stream, int32_t n, const
     cudaStream_t st = (cudaStream_t)cuda_stream;
     UpMaps maps{};
     RUN(map_k(&maps.a, lm_head, l.H, l.V, l.H));
-    RUN(map_rows(&maps, u->rows, l.H, l.rows, l.H));
+    RUN(map_rows(&maps, u->rows, l.H, l.rows, l.H, n));
     u->last_stream = st;
 
     LiveRows r{};
@@ -299,8 +301,8 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
     // few rows: d as two bf16 rows each, the second ones behind the first; counts are then the padded ones
     const int lo = n <= kUpLoRows ? (int)align_up((size_t)n, 32) : 0;
     UpMaps logits{}, dhidden{}, dhead{};
-    RUN(map_rows(&logits, u->rows, l.H, l.rows, l.H));
-    RUN(map_rows(&dhidden, u->dlogits, l.piece, l.rows, l.piece));
+    RUN(map_rows(&logits, u->rows, l.H, l.rows, l.H, lo ? lo : n));
+    RUN(map_rows(&dhidden, u->dlogits, l.piece, l.rows, l.piece, lo ? 2 * lo : n));
     RUN(map_mn(&dhead.a, u->dlogits, l.piece, l.rows, l.piece));
     RUN(map_mn(&dhead.b[0], u->rows, l.H, l.rows, l.H));
 
@@ -361,7 +363,7 @@ mars_status_t mars_expert_matmul(mars_update_t* u, void* cuda_stream, int32_t E,
     if (!guard.ok) return MARS_ERR_CUDA;
     UpMaps maps{};
     RUN(map_stack(&maps.a, w, d_in, d_out, E, 128));
-    RUN(map_rows(&maps, x, d_in, rows, ld_x));
+    RUN(map_rows(&maps, x, d_in, rows, ld_x, rows));
     u->last_stream = (cudaStream_t)cuda_stream;
     UpParams p{};
     p.m = d_out; p.k = d_in; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
@@ -383,7 +385,7 @@ mars_status_t mars_expert_matmul_dx(mars_update_t* u, void* cuda_stream, int32_t
     if (!guard.ok) return MARS_ERR_CUDA;
     UpMaps maps{};
     RUN(map_stack(&maps.a, w, d_in, d_out, E, 64));
-    RUN(map_rows(&maps, dy, d_out, rows, ld_dy));
+    RUN(map_rows(&maps, dy, d_out, rows, ld_dy, rows));
     u->last_stream = (cudaStream_t)cuda_stream;
     UpParams p{};
     p.m = d_in; p.k = d_out; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
