@@ -212,11 +212,12 @@ __device__ __forceinline__ void cut(int n, int tiles, int i, int* start, int* wi
     *width = (units * (i + 1) / tiles - from) * UNIT;
 }
 
-// Two N tiles side by side as one unit of work (PAIRS, for d_hidden): a stage holds A once and both tiles' B, so that
+// Two N tiles side by side as one unit of work (PAIRS, for d_hidden of up to 512 rows): a stage holds A once and both tiles' B, so that
 // 288 token rows, say, bring 34 KB per stage into an SM where two units bring 50 (one SM takes 75 - 85 GB/s from L2):
 // 271 rows x 151936 entries 192 us single, 134 us as pairs.  The price is that both accumulators are taken and the
 // epilogue does not hide behind the next unit, so it is for long contractions: for the logits (32 stages) pairs were
-// slower, 194 us against 177.
+// slower, 194 us against 177, and more than two tiles fill the rounds better one by one (4096 rows: 771 us per piece as
+// pairs, 575 single).
 __device__ __forceinline__ int n_units(int n, bool pairs) {
     const int tiles = (n + kTileN - 1) / kTileN;
     return pairs ? (tiles + 1) / 2 : tiles;
@@ -685,9 +686,9 @@ __device__ __forceinline__ void dlogits_tile(const UpEpilogue& e, const Tile& t,
     }
 }
 
+// The work of one pair of CTAs, number `worker` of `workers` on this contraction.
 template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpParams p) {
+__device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, const int worker, const int workers) {
     extern __shared__ unsigned char up_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)up_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* epi = smem + kRingBytes<EPI>;
@@ -698,7 +699,6 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
     __shared__ volatile int dead;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int rank = (int)(blockIdx.x & 1);                    // place in the pair; rank 0 leads
-    const int worker = blockIdx.x / 2, workers = gridDim.x / 2;
     // a stage of kGroupK is full after two arrivals: the leader's own two, or one of each CTA that cleared rows
     constexpr int kFullCount = SCHED == kGroupK ? 2 : 1;
 
@@ -956,6 +956,24 @@ contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpP
     }
 }
 
+template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpParams p) {
+    contract<A_MN, B_MN, SCHED, EPI, PAIRS>(maps, p, blockIdx.x / 2, gridDim.x / 2);
+}
+
+// d_hidden and d_lm_head of a piece side by side, for small calls: the first pairs of CTAs work on the one, the others on
+// the other.  Both need nothing but d, and neither fills the SMs then (37 rows x 264 x 1013, both calls: 45.7 us with a
+// launch each, 39.3 us).  Where they do, each alone is bound by what one SM or HBM moves, and side by side takes as long
+// (64 rows x 2048 x 151936: 103 + 196 us, together 300; 500 rows 507 us, 611).
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+both_gradients_kernel(const __grid_constant__ UpMaps hidden_maps, const __grid_constant__ UpParams hidden,
+                      const __grid_constant__ UpMaps head_maps, const __grid_constant__ UpParams head, const int hidden_pairs) {
+    const int pair = blockIdx.x / 2;
+    if (pair < hidden_pairs) contract<true, false, kDense, kStore, true>(hidden_maps, hidden, pair, hidden_pairs);
+    else contract<true, true, kDense, kStoreRows, false>(head_maps, head, pair - hidden_pairs, gridDim.x / 2 - hidden_pairs);
+}
+
 template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS = false>
 cudaError_t launch(const UpMaps& m, const UpParams& p, int64_t tiles, int sms, cudaStream_t st) {
     const int64_t want = tiles < 1 ? 1 : tiles, pairs = sms / 2;
@@ -967,6 +985,7 @@ cudaError_t init_one() {
     return cudaFuncSetAttribute(contract_kernel<A_MN, B_MN, SCHED, EPI, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)smem_bytes<EPI>(SCHED != kDense));
 }
+constexpr size_t kBothBytes = std::max(smem_bytes<kStore>(false), smem_bytes<kStoreRows>(false));
 int64_t tiles_of(int64_t m, int64_t n) { return ((m + kTileM - 1) / kTileM) * ((n + kTileN - 1) / kTileN); }
 }  // namespace
 
@@ -975,6 +994,7 @@ cudaError_t init_update_kernels() {
     if (e == cudaSuccess) e = init_one<false, false, kDense, kDlogits>();
     if (e == cudaSuccess) e = init_one<true, false, kDense, kStore>();
     if (e == cudaSuccess) e = init_one<true, false, kDense, kStore, true>();
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(both_gradients_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBothBytes);
     if (e == cudaSuccess) e = init_one<true, true, kDense, kStoreRows>();
     if (e == cudaSuccess) e = init_one<false, false, kGroupRows, kStore>();
     if (e == cudaSuccess) e = init_one<true, false, kGroupRows, kStore>();
@@ -988,9 +1008,20 @@ cudaError_t launch_logit_stats(const UpMaps& m, const UpParams& p, int sms, cuda
 cudaError_t launch_dlogits(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
     return launch<false, false, kDense, kDlogits>(m, p, tiles_of(p.m, p.n), sms, st);
 }
+// Pairs of CTAs for d_hidden where d_lm_head leaves at least half of them: all that have no tile of it.  0: a launch each.
+int both_hidden_pairs(int rows, int width, int hidden, int slots) {
+    const int64_t tiles = tiles_of(width, hidden);
+    return rows <= kUpBothRows && 2 * tiles <= slots ? (int)(slots - tiles) : 0;
+}
+cudaError_t launch_both_gradients(const UpMaps& hidden_maps, const UpParams& hidden, const UpMaps& head_maps, const UpParams& head,
+                                  int hidden_pairs, int sms, cudaStream_t st) {
+    const int64_t units = (int64_t)(hidden.m + kTileM - 1) / kTileM * hidden.splits, tiles = tiles_of(head.m, head.n);
+    const int64_t first = std::min<int64_t>(units, hidden_pairs), second = std::min<int64_t>(tiles, sms / 2 - first);
+    return launch_chained(both_gradients_kernel, dim3((unsigned)(first + second) * 2), dim3(kThreads), kBothBytes, st, hidden_maps, hidden,
+                          head_maps, head, (int)first);
+}
 cudaError_t launch_dhidden(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
-    // two tiles of rows go as a pair; more of them fill the rounds better one by one (4096 rows: 771 us per piece as pairs, 575 single)
-    if (p.n <= 2 * kTileN) return launch<true, false, kDense, kStore, true>(m, p, tiles_of(p.m, 1) * p.splits, sms, st);
+    if (p.n <= kUpBothRows) return launch<true, false, kDense, kStore, true>(m, p, tiles_of(p.m, 1) * p.splits, sms, st);
     return launch<true, false, kDense, kStore>(m, p, tiles_of(p.m, p.n) * p.splits, sms, st);
 }
 cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
@@ -1010,9 +1041,9 @@ cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaSt
 // work, and a piece is long, so it is cut until the units fill the pairs' rounds; at least 8 stages remain.  A part more
 // costs the reading and writing of its fp32 sums, about 13 / stages of the contraction where that is bound by HBM.  Up to two tiles of rows the
 // number of units is known; beyond, the live rows may be fewer than `rows`, and half a round is lost on average.
-int dhidden_splits(int rows, int hidden, int stages, int sms) {
-    const bool known = rows <= 2 * kTileN;
-    const int64_t units = (hidden + kTileM - 1) / kTileM * (known ? 1 : (rows + kTileN - 1) / kTileN), slots = sms / 2;
+int dhidden_splits(int rows, int hidden, int stages, int slots) {
+    const bool known = rows <= kUpBothRows;
+    const int64_t units = (hidden + kTileM - 1) / kTileM * (known ? 1 : (rows + kTileN - 1) / kTileN);
     int best = 1;
     double best_fill = 0.;
     for (int s = 1; s <= 64 && (s == 1 || stages / s >= 8); ++s) {

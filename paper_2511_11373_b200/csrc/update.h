@@ -11,6 +11,7 @@ namespace mars {
 constexpr int kUpTile = 256;        // rows / columns by which workspace rows and vocabulary pieces are padded
 constexpr int kUpMaxExperts = 1024;
 
+constexpr int kUpBothRows = 512;    // two tiles of rows: d_hidden works on them as a pair
 constexpr int kUpLoRows = 128;      // calls of at most this many rows keep d as two bf16 rows (see dlogits_tile)
 
 // Tensor maps of a contraction's operands (bf16, 128-byte swizzle).  K-major: boxes of 64 contraction indexes x 128
@@ -63,7 +64,11 @@ cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream
 cudaError_t launch_expert_fwd(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);     // a = w, b = x
 cudaError_t launch_expert_dx(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);      // a = w (MN), b = dy
 cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st);      // a = dy (MN), b = x (MN)
-int dhidden_splits(int rows, int hidden, int stages, int sms);
+// d_hidden and d_lm_head of a piece in one launch, where both_hidden_pairs is not 0
+cudaError_t launch_both_gradients(const UpMaps& hidden_maps, const UpParams& hidden, const UpMaps& head_maps, const UpParams& head,
+                                  int hidden_pairs, int sms, cudaStream_t st);
+int both_hidden_pairs(int rows, int width, int hidden, int slots);
+int dhidden_splits(int rows, int hidden, int stages, int slots);
 
 // Live rows of a log-prob call: those with a target (and, for the gradient, a non-zero weight).
 struct LiveRows {

@@ -32,7 +32,7 @@ Layout make_update_layout(int H, int V, int n, int sms) {
     const int64_t tiles = (V + kUpTile - 1) / kUpTile, per = std::max<int64_t>(1, most / kUpTile);
     l.pieces = (int)((tiles + per - 1) / per);
     l.piece = (int)((tiles + l.pieces - 1) / l.pieces) * kUpTile;
-    l.splits = dhidden_splits(n, H, l.piece / 64, sms);
+    l.splits = dhidden_splits(n, H, l.piece / 64, sms / 2);
     return l;
 }
 
@@ -315,10 +315,11 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
     r.d_hidden = (__nv_bfloat16*)d_hidden; r.ld_d = ld_d; r.err = u->err;
     RUN(launched(launch_live_rows(r, st)));
 
-    // as many parts as the rows of this call leave room for
+    // as many parts of d_hidden as the rows of this call leave room for
     const int64_t rows_now = (int64_t)align_up((size_t)n, kUpTile), stride = rows_now * l.H;
-    const int splits = std::min((int)std::min<int64_t>(l.splits * l.rows / rows_now, 1 << 10),
-                                dhidden_splits(n, l.H, l.piece / 64, u->sms));
+    const int most_splits = (int)std::min<int64_t>(l.splits * l.rows / rows_now, 1 << 10), slots = u->sms / 2;
+    const int beside = l.pieces == 1 ? both_hidden_pairs(n, l.V, l.H, slots) : 0;
+    const int splits = std::min(most_splits, dhidden_splits(n, l.H, l.piece / 64, beside ? beside : slots));
     for (int i = 0; i < l.pieces; ++i) {
         const int v0 = i * l.piece;
         if (v0 >= l.V) break;
@@ -334,17 +335,21 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
         RUN(launched(launch_dlogits(logits, p, u->sms, st)));
 
         UpParams q{};
-        q.m = l.H; q.n = lo ? 2 * lo : n; q.k = padded; q.n_live = lo ? nullptr : u->n_live; q.splits = splits; q.err = u->err;
+        q.m = l.H; q.n = lo ? 2 * lo : n; q.k = padded; q.n_live = lo ? nullptr : u->n_live; q.err = u->err;
         q.e.out = u->parts; q.e.ld = l.H; q.e.split_stride = stride; q.e.out_f32 = 1; q.e.accumulate = i > 0;
-        RUN(launched(launch_dhidden(dhidden, q, u->sms, st)));
-
         UpParams s{};
         s.m = width; s.n = l.H; s.k = lo ? 2 * lo : n; s.k_live = lo ? nullptr : u->n_live; s.splits = 1; s.err = u->err;
         s.e.out = (unsigned char*)d_lm_head + (size_t)v0 * l.H * out_bytes(d_type);
         s.e.ld = l.H; s.e.out_f32 = d_type == MARS_F32; s.e.accumulate = accumulate != 0;
         s.e.bulk = !accumulate;
         if (s.e.bulk) RUN(map_out(&dhead.out, s.e.out, l.H, width, 1, d_type));
-        RUN(launched(launch_dhead(dhead, s, u->sms, st)));
+        q.splits = splits;
+        if (beside) {
+            RUN(launched(launch_both_gradients(dhidden, q, dhead, s, beside, u->sms, st)));
+        } else {
+            RUN(launched(launch_dhidden(dhidden, q, u->sms, st)));
+            RUN(launched(launch_dhead(dhead, s, u->sms, st)));
+        }
     }
     return launched(launch_dhidden_finish(u->parts, splits, stride, lo, u->src, u->n_live, n, l.H, (__nv_bfloat16*)d_hidden, ld_d, st));
 }
