@@ -247,6 +247,20 @@ struct TileMap {
         units_n = n_units(n, PAIRS);
         count = SCHED == kGroupRows ? first[p.experts] : tiles_m * units_n * (SCHED == kGroupK ? p.experts : p.splits);
     }
+    // Unit u of `per` N units x the M tiles: N fastest, so that neighbours share A, but in blocks of N whose B stays in
+    // L2 while the M tiles pass (one group of 131072 rows x 2048, 537 MB of rows,
+    // to 1536: 869 us without blocks, 690 us).
+    __device__ __forceinline__ void in_blocks(Tile& r, int u, int per, int& tn) const {
+        int first_n = 0, size = per;
+        if (per > p.n_block) {
+            const int b = u / (p.n_block * tiles_m);
+            first_n = b * p.n_block;
+            size = min(p.n_block, per - first_n);
+            u -= first_n * tiles_m;
+        }
+        r.m_tile = u / size;
+        tn = first_n + u - r.m_tile * size;
+    }
     // N columns of unit tn of an extent of n that begins at row `base`.
     __device__ __forceinline__ static void columns(Tile& r, int n, int tn, int base) {
         const int tiles = (n + kTileN - 1) / kTileN, i = PAIRS ? 2 * tn : tn;
@@ -278,16 +292,13 @@ struct TileMap {
                 if (first[mid] <= t) lo = mid; else hi = mid - 1;
             }
             const int rows = off[lo + 1] - off[lo];
-            const int per = n_units(rows, PAIRS), u = t - first[lo];
-            r.m_tile = u / per;                      // rows fastest: neighbours share the weights
-            tn = u - r.m_tile * per;
+            in_blocks(r, t - first[lo], n_units(rows, PAIRS), tn);
             r.k0 = 0; r.k_len = k; r.expert = lo;
             columns(r, rows, tn, off[lo]);
             r.out = 0;
         } else {
             const int per = tiles_m * units_n, group = t / per, u = t - group * per;
-            r.m_tile = u / units_n;                  // N fastest: neighbours share A
-            tn = u - r.m_tile * units_n;
+            in_blocks(r, u, units_n, tn);
             columns(r, n, tn, 0);
             if (SCHED == kGroupK) {
                 r.expert = group;

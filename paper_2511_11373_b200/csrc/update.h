@@ -48,12 +48,19 @@ struct UpParams {
     int m, n, k;
     const int32_t* n_live;    // device counts that replace n / k where not null (live rows of a log-prob call)
     const int32_t* k_live;
+    int n_block;              // N tiles whose B is kept in L2 while the M tiles pass (see update_n_block)
     int splits;               // the contraction is cut into this many parts with outputs of their own
     const int32_t* expert_off;   // [experts + 1], device: groups of rows (expert products)
     int experts, rows;        // rows: extent of the row axis that the offsets refer to
     int32_t* err;
     UpEpilogue e;
 };
+
+// 32 MB of B rows of k elements, in tiles of 256.
+inline int update_n_block(int64_t k) {
+    const int64_t tiles = ((int64_t)32 << 20) / (512 * k);
+    return (int)(tiles < 1 ? 1 : tiles > (1 << 20) ? 1 << 20 : tiles);
+}
 
 cudaError_t init_update_kernels();
 

@@ -268,7 +268,7 @@ mars_status_t mars_logprob(mars_update_t* u, void* cuda_stream, int32_t n, const
     r.logp_out = out_logprobs; r.lse_out = out_lse; r.err = u->err;
     RUN(launched(launch_live_rows(r, st)));
     UpParams p{};
-    p.m = l.V; p.n = n; p.k = l.H; p.n_live = u->n_live; p.splits = 1; p.err = u->err;
+    p.m = l.V; p.n = n; p.k = l.H; p.n_live = u->n_live; p.splits = 1; p.n_block = update_n_block(l.H); p.err = u->err;
     p.e.target = u->target; p.e.inv_temp = 1.f / temperature; p.e.stats = u->stats;
     RUN(launched(launch_logit_stats(maps, p, u->sms, st)));
     return launched(launch_logprob_finish(u->stats, (l.V + 255) / 256 * 2, u->target_logit, u->src, u->n_live, n, 1.f / temperature,
@@ -328,17 +328,17 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
         RUN(map_k(&logits.a, w_piece, l.H, width, l.H));
         RUN(map_mn(&dhidden.a, w_piece, l.H, width, l.H));
         UpParams p{};
-        p.m = padded; p.n = lo ? lo : n; p.k = l.H; p.n_live = lo ? nullptr : u->n_live; p.splits = 1; p.err = u->err;
+        p.m = padded; p.n = lo ? lo : n; p.k = l.H; p.n_live = lo ? nullptr : u->n_live; p.splits = 1; p.n_block = update_n_block(l.H); p.err = u->err;
         p.e.target = u->target; p.e.lse = u->lse; p.e.weight = u->scaled; p.e.target_d = u->target_d; p.e.n_live = u->n_live;
         p.e.inv_temp = 1.f / temperature;
         p.e.dlogits = u->dlogits; p.e.ld = l.piece; p.e.lo_rows = lo; p.e.v0 = v0; p.e.vocab = l.V;
         RUN(launched(launch_dlogits(logits, p, u->sms, st)));
 
         UpParams q{};
-        q.m = l.H; q.n = lo ? 2 * lo : n; q.k = padded; q.n_live = lo ? nullptr : u->n_live; q.err = u->err;
+        q.m = l.H; q.n = lo ? 2 * lo : n; q.k = padded; q.n_live = lo ? nullptr : u->n_live; q.n_block = 1 << 20; q.err = u->err;
         q.e.out = u->parts; q.e.ld = l.H; q.e.split_stride = stride; q.e.out_f32 = 1; q.e.accumulate = i > 0;
         UpParams s{};
-        s.m = width; s.n = l.H; s.k = lo ? 2 * lo : n; s.k_live = lo ? nullptr : u->n_live; s.splits = 1; s.err = u->err;
+        s.m = width; s.n = l.H; s.k = lo ? 2 * lo : n; s.k_live = lo ? nullptr : u->n_live; s.splits = 1; s.n_block = 1 << 20; s.err = u->err;
         s.e.out = (unsigned char*)d_lm_head + (size_t)v0 * l.H * out_bytes(d_type);
         s.e.ld = l.H; s.e.out_f32 = d_type == MARS_F32; s.e.accumulate = accumulate != 0;
         s.e.bulk = !accumulate;
@@ -371,7 +371,7 @@ mars_status_t mars_expert_matmul(mars_update_t* u, void* cuda_stream, int32_t E,
     RUN(map_rows(&maps, x, d_in, rows, ld_x, rows));
     u->last_stream = (cudaStream_t)cuda_stream;
     UpParams p{};
-    p.m = d_out; p.k = d_in; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
+    p.m = d_out; p.k = d_in; p.splits = 1; p.n_block = update_n_block(d_in); p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
     p.e.out = y; p.e.ld = ld_y; p.e.out_f32 = y_type == MARS_F32;
     return launched(launch_expert_fwd(maps, p, u->sms, u->last_stream));
 }
@@ -393,7 +393,7 @@ mars_status_t mars_expert_matmul_dx(mars_update_t* u, void* cuda_stream, int32_t
     RUN(map_rows(&maps, dy, d_out, rows, ld_dy, rows));
     u->last_stream = (cudaStream_t)cuda_stream;
     UpParams p{};
-    p.m = d_in; p.k = d_out; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
+    p.m = d_in; p.k = d_out; p.splits = 1; p.n_block = update_n_block(d_out); p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
     p.e.out = dx; p.e.ld = ld_dx; p.e.out_f32 = dx_type == MARS_F32;
     return launched(launch_expert_dx(maps, p, u->sms, u->last_stream));
 }
@@ -419,7 +419,7 @@ mars_status_t mars_expert_matmul_dw(mars_update_t* u, void* cuda_stream, int32_t
     RUN(map_mn(&maps.a, dy, d_out, rows, ld_dy));
     RUN(map_mn(&maps.b[0], x, d_in, rows, ld_x));
     UpParams p{};
-    p.m = d_out; p.n = d_in; p.splits = 1; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
+    p.m = d_out; p.n = d_in; p.splits = 1; p.n_block = 1 << 20; p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
     p.e.out = dw; p.e.ld = d_in; p.e.split_stride = (int64_t)d_in * d_out; p.e.out_f32 = dw_type == MARS_F32;
     p.e.accumulate = accumulate != 0; p.e.bulk = !accumulate;
     if (p.e.bulk) RUN(map_out(&maps.out, dw, d_in, d_out, E, dw_type));
