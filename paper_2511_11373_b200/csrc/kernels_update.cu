@@ -10,7 +10,7 @@
 // peer, so a 64-deep stage brings 32 KB into each SM where single-CTA 128 x 256 tiles bring 48 (those ran at the
 // 11.5 TB/s that the L2 delivers: 758 us against 665 us for 131072 expert rows x 2048 -> 1536).
 // The N width of a tile is a multiple of 32 chosen from the rows there are (see cut): tokens sit on N, so ragged
-// groups and short calls cost what they hold (a group of 4 rows a 32-wide tile, 270 rows one of 128 and one of 160),
+// groups and short calls cost what they hold (a group of 4 rows a 32-wide tile, 270 rows one of 160 and one of 128),
 // and a call of few rows is a plain stream of the weights.
 //   warp 0      TMA producer, 64 contraction indexes per stage, 128-byte swizzle, mbarrier ring of 5 to 12
 //               stages that runs on across tiles;
@@ -204,12 +204,12 @@ struct Tile {
 };
 
 // Cuts an extent into `tiles` (= n / 256 rounded up) widths that differ by one unit at most: 32, the MMA's granularity, or
-// 64 for out[m][n] (128-byte rows).  300 rows make tiles of 160 and 160, 270 rows 128 and 160.
+// 64 for out[m][n] (128-byte rows).  300 rows make tiles of 160 and 160, 270 rows 160 and 128.
 template <int UNIT>
 __device__ __forceinline__ void cut(int n, int tiles, int i, int* start, int* width) {
-    const int units = (n + UNIT - 1) / UNIT, from = units * i / tiles;
-    *start = from * UNIT;
-    *width = (units * (i + 1) / tiles - from) * UNIT;
+    const int units = (n + UNIT - 1) / UNIT, each = units / tiles, more = units - each * tiles;
+    *start = (each * i + min(i, more)) * UNIT;
+    *width = (each + (i < more ? 1 : 0)) * UNIT;
 }
 
 // Two N tiles side by side as one unit of work (PAIRS, for d_hidden of up to 512 rows): a stage holds A once and both tiles' B, so that

@@ -598,6 +598,18 @@ def test_expert_refusals():
     assert u.poll_status() == 0
 
 
+def test_more_rows_than_an_index_holds_are_refused():
+    """The C entry itself: nothing is launched, so the row count need not be backed by memory."""
+    u = binding.Update(device=DEV)
+    x, w = torch.zeros(6, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(2, 64, 64, dtype=torch.bfloat16, device=DEV)
+    y, off = torch.full_like(x, 3.0), offsets([3, 3])
+    call = binding.lib().mars_expert_matmul
+    for rows in (-1, (1 << 30) + 1, (1 << 31) - 1):
+        assert call(u.handle, u._stream(None), 2, rows, 64, 64, x.data_ptr(), 64, off.data_ptr(), w.data_ptr(), y.data_ptr(), 64, 1) == 1
+    torch.cuda.synchronize()
+    assert (y == 3).all()
+
+
 # -------------------------------------------------------------------------------------- gradient lists
 
 def grad_tensors(sizes, types, seed, aligned=True, std=1.0):
