@@ -476,6 +476,7 @@ class Update:
             self.workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
             self.device = self.workspace.device
             torch.cuda.current_stream().synchronize()      # the memory may still be in use by an earlier owner's kernels
+            self._home = _raw_stream(self.device.index)
             handle = c_void_p()
             _check(lib().mars_update_create(hidden, vocab, max_tokens, _ptr(self.workspace), nbytes, byref(handle)),
                    "mars_update_create")
@@ -485,7 +486,10 @@ class Update:
         return lib().mars_update_poll_status(self.handle)
 
     def _stream(self, stream) -> int:
-        return stream.cuda_stream if stream is not None else _raw_stream(self.device.index)
+        raw = stream.cuda_stream if stream is not None else _raw_stream(self.device.index)
+        if raw != self._home:       # the workspace must outlive the call there, even if the handle does not
+            self.workspace.record_stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+        return raw
 
     def close(self):
         if getattr(self, "handle", None):
@@ -598,6 +602,7 @@ class GradList:
             self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
             self.device = self.workspace.device
             torch.cuda.current_stream().synchronize()
+            self._home = _raw_stream(self.device.index)
             handle = c_void_p()
             _check(lib().mars_grads_create(table, len(grads), _ptr(self.workspace), nbytes, byref(handle)), "mars_grads_create")
         self.handle = handle

@@ -218,7 +218,9 @@ mars_status_t mars_update_create(int32_t hidden, int32_t vocab, int32_t max_toke
     if (!u) return MARS_ERR_INVALID_ARG;
     u->device = dev; u->sms = sms; u->l = l; u->last_stream = nullptr;
     carve_update(l, (unsigned char*)workspace, u);
-    const cudaError_t e = cudaMemset(u->err, 0, 512);
+    // cudaMemset returns before the memory is set, and a non-blocking stream does not wait for it
+    cudaError_t e = cudaMemset(u->err, 0, 512);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);
     if (e != cudaSuccess) { delete u; return launched(e); }
     *out = u;
     return MARS_OK;
@@ -237,7 +239,10 @@ mars_status_t mars_update_poll_status(mars_update_t* u) {
     CUDA_TRY(cudaStreamSynchronize(u->last_stream));
     int32_t word = 0;
     CUDA_TRY(cudaMemcpy(&word, u->err, 4, cudaMemcpyDeviceToHost));
-    if (word) CUDA_TRY(cudaMemset(u->err, 0, 4));
+    if (word) {
+        CUDA_TRY(cudaMemset(u->err, 0, 4));
+        CUDA_TRY(cudaStreamSynchronize(cudaStreamLegacy));       // else it could clear a later call's report
+    }
     if (word & kErrTimeout) return MARS_ERR_TIMEOUT;
     if (word & kErrBadToken) return MARS_ERR_BAD_TOKEN;
     return MARS_OK;
@@ -481,6 +486,7 @@ mars_status_t mars_grads_create(const mars_grad_t* tensors, int32_t n, void* wor
         unsigned char* base = (unsigned char*)workspace;
         CUDA_TRY(cudaMemcpy(base, table.data(), (size_t)n * sizeof(GradEntry), cudaMemcpyHostToDevice));
         CUDA_TRY(cudaMemset(base + ticket, 0, 256));
+        CUDA_TRY(cudaStreamSynchronize(cudaStreamLegacy));       // a non-blocking stream does not wait for the two
         mars_grads* g = new (std::nothrow) mars_grads();
         if (!g) return MARS_ERR_INVALID_ARG;
         g->device = dev; g->sms = sms; g->n = n; g->chunks = chunks;

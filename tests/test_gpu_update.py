@@ -753,6 +753,43 @@ def test_grad_list_refusals():
         binding.mars_grads_norm(lst, torch.empty(2, device=DEV))
 
 
+# ------------------------------------------------------------------------- handles and streams
+
+def test_a_new_handle_is_ready_for_any_stream():
+    """A side stream does not wait for the legacy stream, which is busy while the handles are made."""
+    h, w, targets, _ = logprob_case(8, 64, 100, 1.0, seed=5)
+    targets[3] = 100                                                    # beyond the vocabulary
+    lp, lse, norm = torch.empty(8, device=DEV), torch.empty(8, device=DEV), torch.empty(1, device=DEV)
+    t = torch.ones(64, device=DEV)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(400_000_000)                                      # about 0.2 s on the legacy stream
+    with torch.cuda.stream(side):
+        u, lst = binding.Update(64, 100, 8, device=DEV), binding.GradList([t])
+        assert binding.mars_logprob(u, h, w, targets, 1.0, lp, lse) == 0
+        assert binding.mars_grads_norm(lst, norm) == 0
+    side.synchronize()
+    assert u.poll_status() == 7 and u.poll_status() == 0
+    assert float(norm) == 8.0 and float(lp[3]) == 0.0
+
+
+def test_a_workspace_is_not_handed_on_while_a_side_stream_uses_it():
+    t, norm = torch.ones(64, device=DEV), torch.empty(1, device=DEV)
+    lst = binding.GradList([t])
+    at, nbytes = lst.workspace.data_ptr(), lst.workspace.numel()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)
+        assert binding.mars_grads_clip(lst, 1.0, norm) == 0
+    lst.close()
+    del lst
+    others = [torch.empty(nbytes, dtype=torch.uint8, device=DEV) for _ in range(4)]       # never written to
+    assert not side.query() and all(o.data_ptr() != at for o in others)
+    side.synchronize()
+    assert float(norm) == 8.0 and abs(float(t[0]) - 0.125) < 1e-6
+
+
 # ----------------------------------------------------------------------------------- as they are used
 
 def test_an_update_of_the_last_expert_layer_and_the_lm_head():
