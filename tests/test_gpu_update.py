@@ -313,6 +313,16 @@ def test_logprob_refusals():
     assert (d_h == 3).all() and (d_w == 3).all() and u.poll_status() == 0
 
 
+def test_a_temperature_without_a_reciprocal_is_refused():
+    h, w, targets, _ = logprob_case(8, 64, 100, 1.0, seed=1)
+    u = binding.Update(64, 100, 8, device=DEV)
+    lp, lse = torch.full((8,), 3.0, device=DEV), torch.empty(8, device=DEV)
+    assert binding.mars_logprob(u, h, w, targets, 2.0 ** -129, lp, lse) == 1           # 1 / T is an infinity in fp32
+    torch.cuda.synchronize()
+    assert (lp == 3).all()
+    assert binding.mars_logprob(u, h, w, targets, 2.0 ** -120, lp, lse) == 0           # and here it is not
+
+
 def test_lm_head_beyond_32_bit_offsets():
     """2.5e9 entries: the target rows in the last and first parts of the matrix, against fp64 on the rows that count."""
     n, H, V = 3, 8192, 300001
