@@ -99,6 +99,14 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const 
     const bool ok = !dead && mb_wait<CLUSTER>(bar, parity);
     return __all_sync(0xffffffffu, ok) != 0;
 }
+// The same for the epilogue's warps, whose wait is long: 256 polling lanes get in the way of the producer's and the MMA
+// warp's own polls (131072 expert rows: 729 us, 612 with one polling lane per warp), so lane 0 looks first.  What a warp
+// goes on by is still what each of its lanes has seen: all of them test the barrier once lane 0 has found it ready.
+__device__ __forceinline__ bool warp_wait_long(uint64_t* bar, uint32_t parity, int lane, const volatile int& dead) {
+    if (lane == 0 && !dead) mb_wait(bar, parity);
+    __syncwarp();
+    return warp_wait(bar, parity, dead);
+}
 // Address of the same shared-memory object in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t rank) {
     uint32_t r;
@@ -913,13 +921,7 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
                 continue;
             }
             const int buf = local & 1;
-            if (EPI == kStats) {
-                ok = warp_wait(&acc_full[buf], (local >> 1) & 1, dead);
-            } else {
-                if (lane == 0) ok = !dead && mb_wait(&acc_full[buf], (local >> 1) & 1);
-                __syncwarp();
-                ok = __all_sync(0xffffffffu, ok) != 0;
-            }
+            ok = EPI == kStats ? warp_wait(&acc_full[buf], (local >> 1) & 1, dead) : warp_wait_long(&acc_full[buf], (local >> 1) & 1, lane, dead);
             if (EPI == kStats) {          // the warps of a column half meet on a barrier: all of them go on, or none
                 uint32_t all_ok;
                 __syncwarp();

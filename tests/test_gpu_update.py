@@ -800,6 +800,30 @@ def test_a_workspace_is_not_handed_on_while_a_side_stream_uses_it():
     assert float(norm) == 8.0 and abs(float(t[0]) - 0.125) < 1e-6
 
 
+def test_every_contraction_again_and_again():
+    """Many ring rounds, tiles and launches of every kind of epilogue back to back: the same bits each time, no wait that
+    gives up."""
+    h, w, targets, d = logprob_case(640, 512, 5000, 1.0, 0.1, seed=51)
+    u, few = binding.Update(512, 5000, 640, device=DEV), slice(0, 90)
+    first, short = run_logprob(u, h, w, targets, 1.0, d), run_logprob(u, h[few], w, targets[few], 1.0, d[few])
+    off, g = offsets([300, 0, 77, 1, 512, 90]), gen(52)
+    x, dy, ew = normal(g, 980, 512), normal(g, 980, 768), normal(g, 6, 768, 512)
+
+    def products():
+        y, dx, dw = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(ew)
+        assert binding.mars_expert_matmul(u, x, off, ew, y) == 0
+        assert binding.mars_expert_matmul_dx(u, dy, off, ew, dx) == 0
+        assert binding.mars_expert_matmul_dw(u, dy, x, off, dw) == 0
+        return dict(y=y, dx=dx, dw=dw)
+
+    want = products()
+    for _ in range(60):
+        for a, b in ((first, run_logprob(u, h, w, targets, 1.0, d)), (want, products()),
+                     (short, run_logprob(u, h[few], w, targets[few], 1.0, d[few]))):
+            assert all(torch.equal(a[k], b[k]) for k in a)
+    assert u.poll_status() == 0
+
+
 # ----------------------------------------------------------------------------------- as they are used
 
 def test_an_update_of_the_last_expert_layer_and_the_lm_head():
