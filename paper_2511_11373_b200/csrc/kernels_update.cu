@@ -21,6 +21,7 @@
 // so no transposed copy of anything is made.  Ragged groups: N rows of a tile behind the group's end are
 // computed and not stored; in dw_e, where the rows are the contraction, the stage that holds the end has the
 // rows behind it cleared in shared memory (they belong to the next expert and may hold anything, NaN included).
+// Long contractions are cut into parts that are added in fp32 (kPartStages).
 // Every wait is bounded; one that gives up sets the status word, the CTA stops issuing, waits for its copies
 // in flight, frees its TMEM and returns.
 #include <algorithm>
@@ -47,6 +48,16 @@ constexpr int kBBytes = 128 * kStageK * 2;                   // one CTA's half o
 // rows 120 -> 117 us), 4 for pairs of full tiles.  Expert groups keep full stages (one token: 20.2 us, 20.8 with 10).
 template <int EPI> constexpr int kRingBytes = (EPI == kStoreRows ? 5 : 6) * 32768;
 constexpr int kMaxStages = 12;
+// The tensor cores' fp32 sums drop low bits, always towards zero, so their error grows with the number of steps: one group
+// of positive rows in dw, relative to fp64: 700 rows 1.2e-6, 32768 rows 1.8e-4, 2^20 rows 6.8e-3, more than a rounding to
+// bf16.  Kernels with PARTS therefore contract at most 64 stages (4096 indexes, 256 steps: 1.4e-5 in that example, at any
+// length) in one go; the epilogue adds these parts, rounding to nearest, in the other accumulator (add_part), which takes
+// about 1 us beside the 24 of a full part.  It also bounds how long an accumulator is waited for.  A call has it where its
+// contraction can be longer than a part: d_lm_head and dw of more than 4096 rows, y and dx of wider experts (in every call
+// it cost 131072 rows of y 10 %, 735 -> 815 us).  The logits contract the hidden size, and d_hidden, rounded to bf16, a part
+// of a vocabulary piece (151936 entries in one go: 2e-4): they do without.
+constexpr int kPartStages = 64;
+bool in_parts(int64_t k) { return k > kPartStages * kStageK; }
 constexpr int kGroupWords = 2 * (kUpMaxExperts + 1);
 // statistics of two tiles, or the tokens' values of a chunk per warp; output stages
 template <int EPI> constexpr int kEpiBytes = EPI == kStoreRows ? kEpiWarps * 4096 : 2 * 4 * kTileN * 8;
@@ -106,6 +117,14 @@ __device__ __forceinline__ bool warp_wait_long(uint64_t* bar, uint32_t parity, i
     if (lane == 0 && !dead) mb_wait(bar, parity);
     __syncwarp();
     return warp_wait(bar, parity, dead);
+}
+// A wait for the end of a contraction of nk stages: two seconds more for every 1024 of them (0.4 ms of work).
+__device__ __forceinline__ bool warp_wait_stages(uint64_t* bar, uint32_t parity, int nk, const volatile int& dead) {
+    for (int i = 0; i <= nk >> 10; ++i) {
+        if (warp_wait(bar, parity, dead)) return true;
+        if (__any_sync(0xffffffffu, dead)) return false;
+    }
+    return false;
 }
 // Address of the same shared-memory object in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t rank) {
@@ -191,6 +210,14 @@ __device__ __forceinline__ void tmem_wait(float (&v)[32]) {
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
     tmem_request(taddr, v);
     tmem_wait(v);
+}
+__device__ __forceinline__ void tmem_store(uint32_t taddr, const float (&v)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]),
+                   "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]),
+                   "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]),
+                   "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31])
+                 : "memory");
 }
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -568,6 +595,24 @@ __device__ __forceinline__ void store_zeros(const UpEpilogue& e, const Tile& t, 
     }
 }
 
+// A part of a long contraction (kPartStages) on top of the parts before it: columns c0 .. end of this warp, `sum` written and
+// read by the same threads only.
+__device__ __forceinline__ void add_part(uint32_t part, uint32_t sum, int c0, int end, bool first) {
+#pragma unroll 1
+    for (int c = c0; c < end; c += 32) {
+        float v[32];
+        tmem_ld32(part + c, v);
+        if (!first) {
+            float w[32];
+            tmem_ld32(sum + c, w);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += w[j];
+        }
+        tmem_store(sum + c, v);
+    }
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 __device__ __forceinline__ float redux_max(float v) {
     float r;
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
@@ -706,7 +751,7 @@ __device__ __forceinline__ void dlogits_tile(const UpEpilogue& e, const Tile& t,
 }
 
 // The work of one pair of CTAs, number `worker` of `workers` on this contraction.
-template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS>
+template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS, bool PARTS>
 __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, const int worker, const int workers) {
     extern __shared__ unsigned char up_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)up_raw + 1023) & ~(uintptr_t)1023);
@@ -822,22 +867,22 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
     } else if (warp == 1) {
         if (rank == 0) {
             const bool elected = elect_one();
-            int s = 0, local = 0;                             // stage; tiles so far (accumulators take turns)
-            uint32_t phase = 0;
+            int s = 0, buf = 0;                               // stage; accumulator (they take turns)
+            uint32_t phase = 0, uses = 0;                     // uses: parity of each accumulator's next use
             bool ok = true;
             const uint64_t desc_a = smem_desc<A_MN>(ring), desc_b = smem_desc<B_MN>(ring + kABytes);
             for (int tile = worker; ok && tile < map.count; tile += workers) {
                 const Tile t = map.at(tile);
                 const int nk = (t.k_len + kStageK - 1) / kStageK;
                 if (nk <= 0) continue;                        // nothing to contract: the epilogue writes zeros
-                const int buf = local & 1;
-                const bool two = PAIRS && t.width2;
-                ok = warp_wait<true>(&acc_empty[buf], ((local >> 1) & 1) ^ 1, dead);
-                if (two && ok) ok = warp_wait<true>(&acc_empty[buf ^ 1], (((local + 1) >> 1) & 1) ^ 1, dead);
+                const bool two = PAIRS && t.width2, parts = PARTS && nk > kPartStages, both = two || parts;
+                ok = warp_wait<true>(&acc_empty[buf], ((uses >> buf) & 1) ^ 1, dead);
+                if (both && ok) ok = warp_wait<true>(&acc_empty[buf ^ 1], ((uses >> (buf ^ 1)) & 1) ^ 1, dead);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t acc = tmem_d + (uint32_t)(buf * kTileN), acc2 = tmem_d + (uint32_t)((buf ^ 1) * kTileN);
                 const uint32_t idesc = kIdesc<A_MN, B_MN> | ((uint32_t)(t.width >> 3) << 17);
                 const uint32_t idesc2 = kIdesc<A_MN, B_MN> | ((uint32_t)((PAIRS ? t.width2 : 0) >> 3) << 17);
+                int from = 0, last = PARTS ? min(nk, kPartStages) - 1 : nk - 1;      // stages of the part
                 for (int ks = 0; ok && ks < nk; ++ks) {
                     const int left = t.k_len - ks * kStageK;
                     const int steps = left >= kStageK ? 4 : (left + 15) / 16;
@@ -849,26 +894,33 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
                         if (steps == 4) {
 #pragma unroll
                             for (int kk = 0; kk < 4; ++kk)
-                                mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, kk == 0 ? ks != 0 : 1u);
+                                mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, kk == 0 ? ks != from : 1u);
                         } else {
                             for (int kk = 0; kk < steps; ++kk)
-                                mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, (ks | kk) != 0);
+                                mma_f16(acc, da + kDescStep<A_MN> * kk, db + kDescStep<B_MN> * kk, idesc, ks != from || kk);
                         }
                         if (two) {                            // half the first tile's rows x 128 bytes further, in units of 16
                             const uint64_t db2 = db + (uint64_t)(t.width * 4);
                             for (int kk = 0; kk < steps; ++kk)
-                                mma_f16(acc2, da + kDescStep<A_MN> * kk, db2 + kDescStep<B_MN> * kk, idesc2, (ks | kk) != 0);
+                                mma_f16(acc2, da + kDescStep<A_MN> * kk, db2 + kDescStep<B_MN> * kk, idesc2, ks != from || kk);
                         }
                         commit(&empty[s]);
-                        if (ks == nk - 1) {
+                        if (ks == last) {
                             commit(&acc_full[buf]);
-                            if (two) commit(&acc_full[buf ^ 1]);
+                            if (both && ks == nk - 1) commit(&acc_full[buf ^ 1]);
                         }
                     }
                     __syncwarp();
+                    if (PARTS && ks == last && ks != nk - 1) {       // the next part, once this one has been taken
+                        from = ks + 1;
+                        last = min(nk, from + kPartStages) - 1;
+                        uses ^= 1u << buf;
+                        ok = warp_wait<true>(&acc_empty[buf], ((uses >> buf) & 1) ^ 1, dead);
+                    }
                     if (++s == stages) { s = 0; phase ^= 1; }
                 }
-                local += two ? 2 : 1;
+                uses ^= both ? 3u : 1u << buf;
+                if (!both) buf ^= 1;
             }
             if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
         }
@@ -887,7 +939,7 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
                 const int last = (s + nk - 1) % stages, left = t.k_len - (nk - 1) * kStageK;
                 s = (s + nk) % stages;
                 if (left % 16 == 0) continue;
-                ok = warp_wait(&tail[last], (tails >> last) & 1, dead);
+                ok = warp_wait_stages(&tail[last], (tails >> last) & 1, nk, dead);
                 if (!ok) break;
                 tails ^= 1u << last;
                 unsigned char* st = smem + (size_t)last * stage_bytes + (lane & 7) * 16;
@@ -906,8 +958,15 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
         // a warp may touch the TMEM lanes 32 (warp % 4) .. + 31; the first four warps take the left half of the columns
         const int quarter = warp & 3, half = (warp - 2) >> 2, ch = rank * 128 + quarter * 32 + lane;
         const bool elected = elect_one();
-        int local = 0;
+        int buf = 0;
+        uint32_t uses = 0;
         bool ok = true;
+        const uint32_t lanes = tmem_d + ((uint32_t)(quarter * 32) << 16);
+        const auto release_acc = [&](int b) {           // this warp has read its part of the accumulator
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mb_arrive_at(in_cta(&acc_empty[b], 0));
+        };
         for (int tile = worker, which = 0; ok && tile < map.count; tile += which ? 0 : workers) {
             Tile t = map.at(tile);
             if (PAIRS) {                  // the two tiles of a unit, one after the other
@@ -920,8 +979,21 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
                 if ((EPI == kStore || EPI == kStoreRows) && !p.e.accumulate) store_zeros<EPI == kStoreRows>(p.e, t, ch, c0, c1);
                 continue;
             }
-            const int buf = local & 1;
-            ok = EPI == kStats ? warp_wait(&acc_full[buf], (local >> 1) & 1, dead) : warp_wait_long(&acc_full[buf], (local >> 1) & 1, lane, dead);
+            const int nk = (t.k_len + kStageK - 1) / kStageK;
+            const bool parts = PARTS && nk > kPartStages;
+            if (parts) {
+                for (int ks = 0; ks < nk; ks += kPartStages) {
+                    ok = warp_wait_long(&acc_full[buf], (uses >> buf) & 1, lane, dead);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    add_part(lanes + (uint32_t)(buf * kTileN), lanes + (uint32_t)((buf ^ 1) * kTileN), c0, min(c1, t.n_valid), ks == 0);
+                    release_acc(buf);
+                    uses ^= 1u << buf;
+                }
+                if (!ok) break;
+            }
+            const int acc = parts ? buf ^ 1 : buf;       // what is stored
+            ok = EPI == kStats ? warp_wait(&acc_full[acc], (uses >> acc) & 1, dead) : warp_wait_long(&acc_full[acc], (uses >> acc) & 1, lane, dead);
             if (EPI == kStats) {          // the warps of a column half meet on a barrier: all of them go on, or none
                 uint32_t all_ok;
                 __syncwarp();
@@ -931,14 +1003,10 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
             }
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t taddr = tmem_d + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kTileN);
-            const auto release = [&] {        // this warp has read its part of the accumulator
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mb_arrive_at(in_cta(&acc_empty[buf], 0));
-            };
+            const uint32_t taddr = lanes + (uint32_t)(acc * kTileN);
+            const auto release = [&] { release_acc(acc); };
             if (EPI == kStats) {
-                stats_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float2*>(epi) + buf * 4 * kTileN, quarter, half, lane,
+                stats_tile(p.e, t, ch, c0, c1, taddr, reinterpret_cast<float2*>(epi) + acc * 4 * kTileN, quarter, half, lane,
                            t.m_tile * 2 + rank, map.tiles_m * 2, p.n_live);
                 release();
             } else if (EPI == kDlogits) {
@@ -949,7 +1017,8 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
             } else {
                 store_tile<EPI == kStoreRows>(p.e, t, ch, c0, c1, taddr, release);
             }
-            ++local;
+            uses ^= 1u << acc;
+            if (!parts) buf ^= 1;
         }
         if (!ok && lane == 0) { dead = 1; atomicOr(p.err, kErrTimeout); }
         if (EPI == kStoreRows && elected) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // copies out have read their stages
@@ -969,10 +1038,10 @@ __device__ __forceinline__ void contract(const UpMaps& maps, const UpParams& p, 
     }
 }
 
-template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS>
+template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS, bool PARTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 contract_kernel(const __grid_constant__ UpMaps maps, const __grid_constant__ UpParams p) {
-    contract<A_MN, B_MN, SCHED, EPI, PAIRS>(maps, p, blockIdx.x / 2, gridDim.x / 2);
+    contract<A_MN, B_MN, SCHED, EPI, PAIRS, PARTS>(maps, p, blockIdx.x / 2, gridDim.x / 2);
 }
 
 // d_hidden and d_lm_head of a piece side by side, for small calls: the first pairs of CTAs work on the one, the others on
@@ -983,19 +1052,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 both_gradients_kernel(const __grid_constant__ UpMaps hidden_maps, const __grid_constant__ UpParams hidden,
                       const __grid_constant__ UpMaps head_maps, const __grid_constant__ UpParams head, const int hidden_pairs) {
     const int pair = blockIdx.x / 2;
-    if (pair < hidden_pairs) contract<true, false, kDense, kStore, true>(hidden_maps, hidden, pair, hidden_pairs);
-    else contract<true, true, kDense, kStoreRows, false>(head_maps, head, pair - hidden_pairs, gridDim.x / 2 - hidden_pairs);
+    if (pair < hidden_pairs) contract<true, false, kDense, kStore, true, false>(hidden_maps, hidden, pair, hidden_pairs);
+    else contract<true, true, kDense, kStoreRows, false, false>(head_maps, head, pair - hidden_pairs, gridDim.x / 2 - hidden_pairs);
 }
 
-template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS = false>
+template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS = false, bool PARTS = false>
 cudaError_t launch(const UpMaps& m, const UpParams& p, int64_t tiles, int sms, cudaStream_t st) {
     const int64_t want = tiles < 1 ? 1 : tiles, pairs = sms / 2;
-    return launch_chained(contract_kernel<A_MN, B_MN, SCHED, EPI, PAIRS>, dim3((unsigned)(want < pairs ? want : pairs) * 2), dim3(kThreads),
+    return launch_chained(contract_kernel<A_MN, B_MN, SCHED, EPI, PAIRS, PARTS>, dim3((unsigned)(want < pairs ? want : pairs) * 2), dim3(kThreads),
                           smem_bytes<EPI>(SCHED != kDense), st, m, p);
 }
-template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS = false>
+template <bool A_MN, bool B_MN, int SCHED, int EPI, bool PAIRS = false, bool PARTS = false>
 cudaError_t init_one() {
-    return cudaFuncSetAttribute(contract_kernel<A_MN, B_MN, SCHED, EPI, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(contract_kernel<A_MN, B_MN, SCHED, EPI, PAIRS, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)smem_bytes<EPI>(SCHED != kDense));
 }
 constexpr size_t kBothBytes = std::max(smem_bytes<kStore>(false), smem_bytes<kStoreRows>(false));
@@ -1009,9 +1078,13 @@ cudaError_t init_update_kernels() {
     if (e == cudaSuccess) e = init_one<true, false, kDense, kStore, true>();
     if (e == cudaSuccess) e = cudaFuncSetAttribute(both_gradients_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBothBytes);
     if (e == cudaSuccess) e = init_one<true, true, kDense, kStoreRows>();
+    if (e == cudaSuccess) e = init_one<true, true, kDense, kStoreRows, false, true>();
     if (e == cudaSuccess) e = init_one<false, false, kGroupRows, kStore>();
+    if (e == cudaSuccess) e = init_one<false, false, kGroupRows, kStore, false, true>();
     if (e == cudaSuccess) e = init_one<true, false, kGroupRows, kStore>();
+    if (e == cudaSuccess) e = init_one<true, false, kGroupRows, kStore, false, true>();
     if (e == cudaSuccess) e = init_one<true, true, kGroupK, kStoreRows>();
+    if (e == cudaSuccess) e = init_one<true, true, kGroupK, kStoreRows, false, true>();
     return e;
 }
 
@@ -1038,15 +1111,19 @@ cudaError_t launch_dhidden(const UpMaps& m, const UpParams& p, int sms, cudaStre
     return launch<true, false, kDense, kStore>(m, p, tiles_of(p.m, p.n) * p.splits, sms, st);
 }
 cudaError_t launch_dhead(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    if (in_parts(p.k)) return launch<true, true, kDense, kStoreRows, false, true>(m, p, tiles_of(p.m, p.n), sms, st);
     return launch<true, true, kDense, kStoreRows>(m, p, tiles_of(p.m, p.n), sms, st);
 }
 cudaError_t launch_expert_fwd(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    if (in_parts(p.k)) return launch<false, false, kGroupRows, kStore, false, true>(m, p, sms, sms, st);
     return launch<false, false, kGroupRows, kStore>(m, p, sms, sms, st);
 }
 cudaError_t launch_expert_dx(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    if (in_parts(p.k)) return launch<true, false, kGroupRows, kStore, false, true>(m, p, sms, sms, st);
     return launch<true, false, kGroupRows, kStore>(m, p, sms, sms, st);
 }
 cudaError_t launch_expert_dw(const UpMaps& m, const UpParams& p, int sms, cudaStream_t st) {
+    if (in_parts(p.rows)) return launch<true, true, kGroupK, kStoreRows, false, true>(m, p, tiles_of(p.m, p.n) * p.experts, sms, st);
     return launch<true, true, kGroupK, kStoreRows>(m, p, tiles_of(p.m, p.n) * p.experts, sms, st);
 }
 

@@ -540,6 +540,83 @@ def test_expert_stack_beyond_32_bit_offsets():
     assert (dw[1:31] == 0).all() and (dw[33:E - 1] == 0).all()
 
 
+def in_parts(n):
+    """Relative to the sum of absolute products: at most 4096 indexes in one tensor-core sum, the parts added in fp32."""
+    return sum_error(min(n, 4096)) + -(-n // 4096) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_groups_do_not_lose_what_each_step_drops(dtype):
+    """Products of one sign, where the low bits that the tensor cores drop add up: the bound does not grow with the group."""
+    counts, d_in, d_out = [30000, 4096, 0, 4097, 8192, 12345, 63, 16384], 136, 328
+    off, g, u = offsets(counts), gen(61), binding.Update(device=DEV)
+    n, E = sum(counts), len(counts)
+    x, dy = normal(g, n, d_in).abs(), normal(g, n, d_out).abs()
+    base = torch.rand(E, d_out, d_in, generator=g, device=DEV).to(dtype)
+    dw, acc = torch.empty(E, d_out, d_in, dtype=dtype, device=DEV), base.clone()
+    assert binding.mars_expert_matmul_dw(u, dy, x, off, dw) == 0
+    assert binding.mars_expert_matmul_dw(u, dy, x, off, acc, accumulate=True) == 0
+    o = off.tolist()
+    for e in range(E):
+        want = dy[o[e]:o[e + 1]].double().t() @ x[o[e]:o[e + 1]].double()
+        tol = want * in_parts(counts[e])
+        check_rounded(dw[e], want, tol)
+        check_rounded(acc[e], want + base[e].double(), tol + 2.0 ** -23 * want)
+    assert u.poll_status() == 0
+
+
+def test_wide_experts_do_not_lose_what_each_step_drops():
+    counts, d = [5, 300, 0, 41], 20008
+    off, g, u = offsets(counts), gen(62), binding.Update(device=DEV)
+    n = sum(counts)
+    x, w = normal(g, n, d).abs(), normal(g, 4, 264, d).abs()
+    y = torch.empty(n, 264, device=DEV)
+    assert binding.mars_expert_matmul(u, x, off, w, y) == 0
+    wt = w.transpose(1, 2).contiguous()
+    dx = torch.empty(n, 264, device=DEV)
+    assert binding.mars_expert_matmul_dx(u, x, off, wt, dx) == 0          # the same sums, w the other way round
+    o = off.tolist()
+    for e in range(4):
+        r = slice(o[e], o[e + 1])
+        want = x[r].double() @ w[e].double().t()
+        for got in (y[r], dx[r]):
+            check_rounded(got, want, want * in_parts(d))
+
+
+def test_lm_head_gradient_of_many_rows_does_not_lose_what_each_step_drops():
+    """Two entries of equal logits: p is 1/2 and d exact in bf16, so that nothing but the sum over the rows can be off."""
+    n, H = 30011, 72
+    g = gen(63)
+    h = normal(g, n, H).abs()
+    w = normal(g, 1, H).expand(2, H).contiguous()
+    targets = torch.zeros(n, dtype=torch.int32, device=DEV)
+    targets[::1000] = -1
+    u = binding.Update(H, 2, n, device=DEV)
+    got = run_logprob(u, h, w, targets, 1.0, torch.ones(n, device=DEV), dtype=torch.float32)
+    half = 0.5 * torch.where((targets >= 0)[:, None], h.double(), 0.0).sum(0)
+    for row, want in ((0, half), (1, -half)):
+        check_rounded(got["d_w"][row], want, half * in_parts(n))
+
+
+def test_a_group_of_four_hundred_million_rows():
+    """Six million stages on one pair of CTAs: the work of seconds must not look like a wait that gave up."""
+    n, d = 400_000_000, 8
+    u, g = binding.Update(device=DEV), gen(64)
+    x, dy = (torch.empty(n, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    x.uniform_(0.5, 1.0, generator=g)
+    dy.uniform_(0.5, 1.0, generator=g)
+    dw = torch.empty(2, d, d, device=DEV)
+    off = torch.tensor([0, n - 5, n], dtype=torch.int32, device=DEV)
+    assert binding.mars_expert_matmul_dw(u, dy, x, off, dw) == 0
+    assert u.poll_status() == 0
+    want = torch.zeros(d, d, dtype=torch.float64, device=DEV)
+    for a in range(0, n - 5, 10_000_000):
+        b = min(a + 10_000_000, n - 5)
+        want += dy[a:b].double().t() @ x[a:b].double()
+    check_rounded(dw[0], want, want * in_parts(n))
+    check_rounded(dw[1], dy[n - 5:].double().t() @ x[n - 5:].double(), 5 * sum_error(5) * torch.ones(d, d, device=DEV))
+
+
 def test_expert_gradients_against_differences():
     """L = sum_r <c_r, w_e x_r> in fp64 along random directions of x and w."""
     counts, d_in, d_out = [9, 0, 40, 131], 72, 88
