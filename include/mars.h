@@ -418,6 +418,10 @@ MARS_API mars_status_t mars_update_poll_status(mars_update_t *update);
  * their hidden states hold.  accumulate_d_lm_head != 0 adds to what d_lm_head holds (micro-batches); the sum is
  * formed in fp32 and rounded once to the type of d_lm_head.  Precision: d loss / d logit is rounded to bf16
  * (relative 2^-8, independent per entry) before the two products, which accumulate in fp32.
+ * mars_logprob_grad_lp: the same, given the log-probs of mars_logprob too.  1 - p of a target is then -expm1(logp), to its
+ * full relative accuracy.  mars_logprob_grad (and logprobs = NULL) has it from lse, which is rounded to fp32: an absolute
+ * error of up to 2^-24 |lse| |d_logprobs| / temperature in d loss / d logit of the target, as much as the value itself
+ * where p is within some 1e-6 of 1.
  * n_tokens = 0 is allowed (d_lm_head is then zeroed, or left when it accumulates).  Row strides are in elements
  * and multiples of 8; matrices are 16-byte aligned, d_hidden [n_tokens][ld_d_hidden].  Outputs must not overlap inputs.
  * The same call on the same inputs gives the same bits. */
@@ -428,6 +432,11 @@ MARS_API mars_status_t mars_logprob_grad(mars_update_t *update, void *cuda_strea
                                          int64_t ld_hidden, const void *lm_head, const int32_t *targets, float temperature,
                                          const float *lse, const float *d_logprobs, void *d_hidden, int64_t ld_d_hidden,
                                          void *d_lm_head, int32_t d_lm_head_type, int32_t accumulate_d_lm_head);
+MARS_API mars_status_t mars_logprob_grad_lp(mars_update_t *update, void *cuda_stream, int32_t n_tokens, const void *hidden,
+                                            int64_t ld_hidden, const void *lm_head, const int32_t *targets, float temperature,
+                                            const float *logprobs, const float *lse, const float *d_logprobs, void *d_hidden,
+                                            int64_t ld_d_hidden, void *d_lm_head, int32_t d_lm_head_type,
+                                            int32_t accumulate_d_lm_head);
 
 /* Products of the mixture's experts: rows that are sorted by expert (the expert slots of a token permutation,
  * see expert_off in mars_debug_t), expert e owning rows expert_off[e] .. expert_off[e + 1] - 1:

@@ -123,6 +123,8 @@ SIGNATURES = {
                                c_void_p]),
     "mars_logprob_grad": (c_int32, [c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_void_p,
                                     c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_int32]),
+    "mars_logprob_grad_lp": (c_int32, [c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_void_p,
+                                       c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_int32]),
     "mars_expert_matmul": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p,
                                      c_void_p, c_void_p, c_int64, c_int32]),
     "mars_expert_matmul_dx": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p,
@@ -519,20 +521,24 @@ def mars_logprob(update: Update, hidden: torch.Tensor, lm_head: torch.Tensor, ta
 
 def mars_logprob_grad(update: Update, hidden: torch.Tensor, lm_head: torch.Tensor, targets: torch.Tensor, temperature: float,
                       lse: torch.Tensor, d_logprobs: torch.Tensor, d_hidden: torch.Tensor, d_lm_head: torch.Tensor,
-                      accumulate: bool = False, stream=None) -> int:
+                      accumulate: bool = False, stream=None, logprobs: torch.Tensor = None) -> int:
     """d_hidden (bf16) and d_lm_head (bf16 or fp32) of sum_i d_logprobs[i] logp_i, `lse` from mars_logprob; returns the
-    status code.  accumulate: add to d_lm_head."""
+    status code.  accumulate: add to d_lm_head.  logprobs: those of mars_logprob; with them the gradient of a token whose
+    probability is next to 1 keeps its relative accuracy (without: an absolute error of 2^-24 |lse| in its 1 - p)."""
     n, dev = hidden.shape[0], update.device
     _want(hidden, "hidden", (torch.bfloat16,), dev, n, update.hidden, rows=True)
     _want(lm_head, "lm_head", (torch.bfloat16,), dev, update.vocab, update.hidden)
     _want(targets, "targets", (torch.int32,), dev, n)
     _want(lse, "lse", (torch.float32,), dev, n)
     _want(d_logprobs, "d_logprobs", (torch.float32,), dev, n)
+    if logprobs is not None:
+        _want(logprobs, "logprobs", (torch.float32,), dev, n)
     _want(d_hidden, "d_hidden", (torch.bfloat16,), dev, n, update.hidden, rows=True)
     _want(d_lm_head, "d_lm_head", (torch.bfloat16, torch.float32), dev, update.vocab, update.hidden)
-    return lib().mars_logprob_grad(update.handle, update._stream(stream), n, hidden.data_ptr(), _ld(hidden), lm_head.data_ptr(),
-                                   targets.data_ptr(), float(temperature), lse.data_ptr(), d_logprobs.data_ptr(), d_hidden.data_ptr(),
-                                   _ld(d_hidden), d_lm_head.data_ptr(), MARS_TYPES[d_lm_head.dtype], int(bool(accumulate)))
+    return lib().mars_logprob_grad_lp(update.handle, update._stream(stream), n, hidden.data_ptr(), _ld(hidden), lm_head.data_ptr(),
+                                      targets.data_ptr(), float(temperature), None if logprobs is None else logprobs.data_ptr(),
+                                      lse.data_ptr(), d_logprobs.data_ptr(), d_hidden.data_ptr(), _ld(d_hidden), d_lm_head.data_ptr(),
+                                      MARS_TYPES[d_lm_head.dtype], int(bool(accumulate)))
 
 
 def _expert_shapes(update: Update, w: torch.Tensor, expert_off: torch.Tensor, name: str, dtypes):

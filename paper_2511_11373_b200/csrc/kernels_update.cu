@@ -684,7 +684,7 @@ __device__ __forceinline__ void stats_tile(const UpEpilogue& e, const Tile& t, i
 // Gradient of the logits: d = w ([v = t] - p), p = exp(z - lse), w = g / T, rounded to bf16 (relative 2^-8 at
 // most, independent from entry to entry) because it is an operand of two tensor-core products; for calls of few
 // rows, which are streams of the lm_head anyway, what the rounding took off is stored as a second bf16 row.  The
-// target's own value w (1 - p) comes from its fp32 logit: no cancellation where p is close to 1.  Tokens and
+// target's own value w (1 - p) is prepared per row (live_rows_kernel).  Tokens and
 // entries behind the end are written as zeros: they are contraction indexes of those products.
 // The factor is taken into the exponent, w p = sign exp2(z log2 e / T + log2 |w| - lse log2 e), so that a token's share
 // of the work on its 32 entries is one number out of shared memory (read four tokens at a time: the MMAs of the next
@@ -1150,7 +1150,9 @@ constexpr int kLiveWarps = 8, kLiveThreads = 32 * kLiveWarps, kLiveHeld = 8;
 
 // Copies the live rows side by side and takes each one's target logit as an fp32 dot product (the tensor cores'
 // sums drop low bits on the way, always towards zero; a target that leads its row carries that error into its own
-// log-prob in full).  A warp takes a row; its pieces and those of the target's lm_head row, 2048 elements at a time, are
+// log-prob in full).  The gradient's target entry is w (1 - p) = -w expm1(logp): from the caller's logp it keeps its relative
+// accuracy at any p; without one logp is z / T - lse, and the rounding of lse, 2^-24 of its size, is an absolute error of
+// 1 - p (at lse = 20 as large as a 1 - p of 1e-6 itself).  A warp takes a row; its pieces and those of the target's lm_head row, 2048 elements at a time, are
 // requested together and before anything else is waited for (the lm_head row is a DRAM access of its own: one
 // request after the other cost 19 us for 64 rows, now 6).  Meanwhile every block counts the live rows before its own
 // (targets and weights are a few bytes per row and sit in L2), so one launch does the whole compaction, in order.
@@ -1170,8 +1172,8 @@ __global__ void __launch_bounds__(kLiveThreads) live_rows_kernel(LiveRows a) {
 #pragma unroll
         for (int q = 0; q < kLiveHeld; ++q) {
             const int j = from + q * 32 + lane;
-            if (live && j < pieces) { x[q] = src[j]; w[q] = head[j]; }
-            else { x[q] = make_uint4(0, 0, 0, 0); w[q] = make_uint4(0, 0, 0, 0); }
+            x[q] = live && j < pieces ? src[j] : make_uint4(0, 0, 0, 0);
+            w[q] = live && j < pieces && !a.logp_in ? head[j] : make_uint4(0, 0, 0, 0);
         }
     };
     request(0);
@@ -1220,7 +1222,7 @@ __global__ void __launch_bounds__(kLiveThreads) live_rows_kernel(LiveRows a) {
                 const float s = weight * a.inv_temp, l = a.lse_in[i];
                 a.scaled[to] = s;
                 a.lse[to] = l;
-                a.target_d[to] = -s * expm1f(fmaf(dot, a.inv_temp, -l));
+                a.target_d[to] = -s * expm1f(a.logp_in ? a.logp_in[i] : fmaf(dot, a.inv_temp, -l));
             }
         }
     } else if (exists) {

@@ -85,6 +85,7 @@ struct LiveRows {
     const int32_t* targets;
     const float* weight;           // null: forward
     const float* lse_in;           // gradient: [n]
+    const float* logp_in;          // gradient: [n] or null (1 - p of the target then comes from its logit and lse_in)
     int n, H, vocab;
     float inv_temp;
     __nv_bfloat16* rows;           // [padded][H] compact copies, zeros behind the last one up to n rounded up to 16 (or lo_rows)

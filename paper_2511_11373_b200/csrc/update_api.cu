@@ -284,14 +284,22 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
                                 const void* lm_head, const int32_t* targets, float temperature, const float* lse,
                                 const float* d_logprobs, void* d_hidden, int64_t ld_d, void* d_lm_head, int32_t d_type,
                                 int32_t accumulate) {
+    return mars_logprob_grad_lp(u, cuda_stream, n, hidden, ld, lm_head, targets, temperature, nullptr, lse, d_logprobs, d_hidden, ld_d,
+                                d_lm_head, d_type, accumulate);
+}
+
+mars_status_t mars_logprob_grad_lp(mars_update_t* u, void* cuda_stream, int32_t n, const void* hidden, int64_t ld,
+                                   const void* lm_head, const int32_t* targets, float temperature, const float* logprobs,
+                                   const float* lse, const float* d_logprobs, void* d_hidden, int64_t ld_d, void* d_lm_head,
+                                   int32_t d_type, int32_t accumulate) {
     RUN(check_logprob(u, n, hidden, ld, lm_head, targets, temperature));
     if (!d_lm_head || !aligned16(d_lm_head) || (d_type != MARS_BF16 && d_type != MARS_F32)) return MARS_ERR_INVALID_ARG;
-    if (n > 0 && (!lse || !d_logprobs || !d_hidden || !aligned4(lse) || !aligned4(d_logprobs) ||
+    if (n > 0 && (!lse || !d_logprobs || !d_hidden || !aligned4(lse) || !aligned4(d_logprobs) || !aligned4(logprobs) ||
                    !aligned16(d_hidden) || ld_d < u->l.H || ld_d % 8)) return MARS_ERR_INVALID_ARG;
     const Layout& l = u->l;
     const size_t ow = (size_t)l.V * l.H * out_bytes(d_type), oh = span(n, ld_d, l.H, 2), nb = (size_t)n * 4;
     const struct { const void* p; size_t n; } ins[] = {{hidden, span(n, ld, l.H, 2)}, {lm_head, (size_t)l.V * l.H * 2},
-                                                       {targets, nb}, {lse, nb}, {d_logprobs, nb}};
+                                                       {targets, nb}, {lse, nb}, {d_logprobs, nb}, {logprobs, logprobs ? nb : 0}};
     for (const auto& i : ins)
         if (overlap(d_lm_head, ow, i.p, i.n) || overlap(d_hidden, oh, i.p, i.n)) return MARS_ERR_INVALID_ARG;
     if (overlap(d_lm_head, ow, d_hidden, oh)) return MARS_ERR_INVALID_ARG;
@@ -313,7 +321,7 @@ mars_status_t mars_logprob_grad(mars_update_t* u, void* cuda_stream, int32_t n, 
 
     LiveRows r{};
     r.hidden = (const __nv_bfloat16*)hidden; r.ld = ld; r.lm_head = (const __nv_bfloat16*)lm_head; r.targets = targets;
-    r.weight = d_logprobs; r.lse_in = lse;
+    r.weight = d_logprobs; r.lse_in = lse; r.logp_in = logprobs;
     r.n = n; r.H = l.H; r.vocab = l.V; r.inv_temp = 1.f / temperature;
     r.rows = u->rows; r.lo_rows = lo; r.src = u->src; r.target = u->target; r.n_live = u->n_live;
     r.target_logit = u->target_logit; r.lse = u->lse; r.scaled = u->scaled; r.target_d = u->target_d;

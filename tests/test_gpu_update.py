@@ -198,6 +198,69 @@ def test_confident_and_extreme_rows():
     check_logprob(run_logprob(u, h, w, t, 1.0, d), logprob_reference(h, w, t, 1.0, d))
 
 
+@pytest.mark.parametrize("n", [64, 200])
+@pytest.mark.parametrize("T", [1.0, 0.85, 0.6])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_confident_rows_keep_the_relative_accuracy_of_1_minus_p(n, T, dtype):
+    """1 - p of the targets from 1e-2 down to 1e-9, each row weighted by its 1 / (1 - p): with the log-probs at hand every
+    entry of d, the target's included, is right to the error of an exponent and its rounding."""
+    H, V = 64, 900
+    g = gen(71)
+    w = normal(g, V, H)
+    targets = torch.randperm(V, generator=g, device=DEV)[:n].to(torch.int32)
+    at, me = targets.long(), torch.arange(n, device=DEV)
+    rows = w[at].double()
+    h = (rows * (torch.linspace(12.0, 36.0, n, device=DEV)[:, None] * T / rows.square().sum(1, keepdim=True))).bfloat16()
+    hd, wd = h.double(), w.double()
+    z = hd @ wd.t() / T
+    e = torch.exp(z - z[me, at][:, None])
+    e[me, at] = 0
+    rest = e.sum(1)
+    one_p = rest / (1 + rest)
+    assert 1e-11 < float(one_p.min()) < 1e-7 and 5e-3 < float(one_p.max()) < 5e-2
+    weight = (1 / one_p).float()
+    u = binding.Update(H, V, n, device=DEV)
+    logp, lse = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    assert binding.mars_logprob(u, h, w, targets, T, logp, lse) == 0
+    d_h, d_w = torch.empty_like(h), torch.empty(V, H, dtype=dtype, device=DEV)
+    assert binding.mars_logprob_grad(u, h, w, targets, T, lse, weight, d_h, d_w, logprobs=logp) == 0
+    d = -e / (1 + rest)[:, None]
+    d[me, at] = one_p
+    d *= weight.double()[:, None] / T
+    # an entry is off by its exponent (two logits and lse) and by its rounding: one bf16 row, or two up to 128 rows
+    scale = (hd.abs() @ wd.abs().t()).max(dim=1).values / T
+    rel = 2 * (2 * sum_error(H) * scale + 2.0 ** -22 * (16 + z[me, at].abs()) + 2.0 ** -23 * math.sqrt(V))
+    assert float(rel.max()) < 1e-3
+    da = d.abs() * (rel + (2.0 ** -16 if n <= 128 else 1.01 * 2.0 ** -8))[:, None]
+    for got, want, tol in ((d_h, d @ wd, da @ wd.abs() + sum_error(V) * (d.abs() @ wd.abs())),
+                           (d_w, d.t() @ hd, da.t() @ hd.abs() + sum_error(n) * (d.abs().t() @ hd.abs()))):
+        check_rounded(got, want, tol)
+
+
+@pytest.mark.parametrize("T", [1.0, 0.85])
+def test_a_certain_token_has_no_gradient(T):
+    """Logits in the thousands, p = 1 in fp64: nothing is left, whatever the rounding of lse."""
+    g = gen(72)
+    w = normal(g, 300, 64)
+    targets = torch.arange(20, device=DEV, dtype=torch.int32)
+    h = (w[:20].float() * 40).bfloat16()
+    u = binding.Update(64, 300, 20, device=DEV)
+    logp, lse = torch.empty(20, device=DEV), torch.empty(20, device=DEV)
+    assert binding.mars_logprob(u, h, w, targets, T, logp, lse) == 0
+    assert (logp == 0).all()
+    d_h, d_w = torch.ones_like(h), torch.ones_like(w)
+    assert binding.mars_logprob_grad(u, h, w, targets, T, lse, torch.ones(20, device=DEV), d_h, d_w, logprobs=logp) == 0
+    assert (d_h == 0).all() and (d_w == 0).all()
+    bad = binding.lib().mars_logprob_grad_lp                    # the log-probs are an input like the others
+    args = [u.handle, None, 20, h.data_ptr(), 64, w.data_ptr(), targets.data_ptr(), T, logp.data_ptr() + 2, lse.data_ptr(), lse.data_ptr(),
+            d_h.data_ptr(), 64, d_w.data_ptr(), 1, 0]
+    assert bad(*args) == 1
+    args[8] = d_h.data_ptr()
+    assert bad(*args) == 1
+    with pytest.raises(ValueError):
+        binding.mars_logprob_grad(u, h, w, targets, T, lse, lse, d_h, d_w, logprobs=logp.double())
+
+
 def test_target_beyond_the_vocabulary_is_reported_and_left_out():
     h, w, targets, d = logprob_case(20, 64, 300, 1.0, seed=9)
     targets[4] = 300

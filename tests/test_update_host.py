@@ -119,3 +119,7 @@ def test_the_binding_refuses_tensors_of_another_kind():
                         ([torch.zeros(3, dtype=torch.float64)], None), ([torch.zeros(4, 4)[:, :2]], None), ([torch.zeros(3)], None)):
         with pytest.raises(ValueError):
             binding.GradList(grads, outs)
+
+
+def test_the_gradient_with_log_probs_refuses_a_null_handle(lib):
+    assert lib.mars_logprob_grad_lp(None, None, 1, None, 8, None, None, 1.0, None, None, None, None, 8, None, 1, 0) == 6
