@@ -197,7 +197,7 @@ def _run_own(s):
             got = dict(logp=s["logp"])
         else:
             st = st or binding.mars_logprob_grad(u, s["h"], s["w"], s["targets"], s["temperature"], s["lse"], s["d_logp"],
-                                                 s["d_h"], s["d_w"])
+                                                 s["d_h"], s["d_w"], logprobs=s["logp"])
             got = dict(logp=s["logp"], d_h=s["d_h"], d_w=s["d_w"])
     elif kind == "experts":
         st = binding.mars_expert_matmul(u, s["x"], s["off"], s["w"], s["y"])
