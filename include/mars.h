@@ -407,7 +407,8 @@ MARS_API mars_status_t mars_update_poll_status(mars_update_t *update);
  *   out_lse[i]      = log sum_v exp((lm_head hidden_i)_v / temperature)          (what the gradient needs)
  * in fp32, over the full vocabulary and without ever holding the logits; both are 0 where targets[i] < 0
  * (prompt and padding rows: their hidden states are not read and may hold anything).  A target >= vocab counts as
- * < 0 and is reported by mars_update_poll_status.  temperature: positive, itself and its reciprocal finite in fp32.
+ * < 0 and is reported by mars_update_poll_status.  temperature: positive; itself and
+ * log2(e) / temperature finite in fp32.
  *
  * mars_logprob_grad: with the same hidden, lm_head, targets and temperature, the lse of mars_logprob and
  * d_logprobs[i] = d loss / d logp_i (fp32; for Eq. 3 the clipped importance ratio times the advantage):

@@ -172,7 +172,9 @@ bool update_shape_ok(int32_t hidden, int32_t vocab, int32_t max_tokens) {
 mars_status_t check_logprob(const mars_update* u, int32_t n, const void* hidden, int64_t ld, const void* lm_head,
                             const int32_t* targets, float temperature) {
     if (!u) return MARS_ERR_BAD_HANDLE;
-    if (u->l.n < 1 || n < 0 || n > u->l.n || !(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return MARS_ERR_INVALID_ARG;
+    // the kernels scale logits by log2(e) / T: an infinite factor would make the largest logit's 0 x inf a NaN
+    if (u->l.n < 1 || n < 0 || n > u->l.n || !(temperature > 0.f) || !std::isfinite(temperature) ||
+        !std::isfinite(1.f / temperature * 1.4426950408889634f)) return MARS_ERR_INVALID_ARG;
     if (!lm_head || !aligned16(lm_head)) return MARS_ERR_INVALID_ARG;
     if (n > 0 && (!hidden || !targets || !aligned16(hidden) || !aligned4(targets) || ld < u->l.H || ld % 8))
         return MARS_ERR_INVALID_ARG;

@@ -386,6 +386,24 @@ def test_a_temperature_without_a_reciprocal_is_refused():
     assert binding.mars_logprob(u, h, w, targets, 2.0 ** -120, lp, lse) == 0           # and here it is not
 
 
+def test_the_smallest_temperatures():
+    """log2(e) / T, the factor that the kernels use, leaves fp32 before 1 / T does."""
+    h, w, targets, d = logprob_case(8, 64, 100, 1.0, seed=1)
+    h = (h.float() * 2.0 ** -40).bfloat16()                       # logits that stay finite when they are divided by T
+    u = binding.Update(64, 100, 8, device=DEV)
+    lp, lse = torch.full((8,), 3.0, device=DEV), torch.full((8,), 3.0, device=DEV)
+    d_h, d_w = torch.full_like(h, 3.0), torch.full_like(w, 3.0)
+    for T in (1.1 * 2.0 ** -128, 1.4 * 2.0 ** -128):
+        assert binding.mars_logprob(u, h, w, targets, T, lp, lse) == 1
+        assert binding.mars_logprob_grad(u, h, w, targets, T, lse, d, d_h, d_w) == 1
+    torch.cuda.synchronize()
+    assert all((t == 3).all() for t in (lp, lse, d_h, d_w))
+    for T in (1.5 * 2.0 ** -128, 2.0 ** -120):
+        got = run_logprob(u, h, w, targets, T)
+        assert torch.isfinite(got["logp"]).all()
+        check_logprob(got, logprob_reference(h, w, targets, T))
+
+
 def test_lm_head_beyond_32_bit_offsets():
     """2.5e9 entries: the target rows in the last and first parts of the matrix, against fp64 on the rows that count."""
     n, H, V = 3, 8192, 300001
