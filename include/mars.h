@@ -468,7 +468,8 @@ MARS_API mars_status_t mars_expert_matmul_dw(mars_update_t *update, void *cuda_s
  * alike; any element-aligned address (places in a flat buffer); numel 0 is allowed.  out = grad scales in place,
  * another out leaves the gradients as they are; an out that overlaps anything but its own grad in full is refused.
  *   mars_grads_norm   *out_norm = sqrt of the sum of all squares (device fp32), summed in fp32 / fp64
- *   mars_grads_clip   the same, and out_t = grad_t min(1, max_norm / (norm + 1e-6)), rounded once to its type.
+ *   mars_grads_clip   the same, and out_t = grad_t min(1, max_norm / (norm + 1e-6)): the factor in fp64,
+ *                     rounded to fp32 where that holds it in full precision; the product rounded to the type.
  * max_norm >= 0.  A NaN norm makes every out NaN; an infinite one makes finite values 0.  Where nothing has to be
  * scaled, tensors in place are not touched.  One call at a time per handle; same bits on every call. */
 typedef struct {

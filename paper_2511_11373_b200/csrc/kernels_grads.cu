@@ -7,7 +7,8 @@
 // pass walks each run backwards: what the norm read last is still in L2.  Squares are added in fp32 over
 // at most a chunk's share of one thread and in fp64 beyond; a chunk whose fp32 sum overflowed, or is so small
 // that squares were lost below the smallest fp32 number, is summed again in fp64.  All sums run in a fixed
-// order: the same list gives the same bits on every call.
+// order: the same list gives the same bits on every call.  The factor is kept in fp64 and rounded to fp32 for the products
+// (2^-24 beside the rounding of the result); one too small for fp32's full precision multiplies in fp64.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -175,7 +176,7 @@ __device__ __forceinline__ double chunk_squares(const Chunk& c) {
 __device__ __forceinline__ int64_t run_begin(int64_t n_chunks, int64_t b) { return n_chunks * b / gridDim.x; }
 
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const GradEntry* table, int n, int64_t n_chunks, double* partials,
-                                                             int32_t* ticket, float max_norm, float* norm_out, float* scale) {
+                                                             int32_t* ticket, float max_norm, float* norm_out, double* scale) {
     __shared__ double scratch[kThreads / 32];
     __shared__ int last;
     pdl_wait();
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const GradEntry* ta
         *norm_out = (float)norm;
         if (scale) {
             const double s = (double)max_norm / (norm + 1e-6);
-            *scale = s < 1. ? (float)s : (s >= 1. ? 1.f : __int_as_float(0x7fffffff));      // a NaN norm gives NaN
+            *scale = s >= 1. ? 1. : s;      // a NaN norm gives NaN
         }
     }
 }
@@ -247,9 +248,19 @@ __device__ __forceinline__ void scale_chunk(const Chunk& c, float s) {
     }
 }
 
-__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const GradEntry* table, int n, int64_t n_chunks, const float* scale) {
+// The same with a factor below the normal numbers of fp32 (finite gradients with a norm of 1e38 and more, or a tiny largest
+// norm): products in fp64, element by element.
+__device__ void scale_chunk_tiny(const Chunk& c, double s) {
+    const int eb = elem_bytes(c.type);
+    for (int64_t at = c.begin + (int64_t)threadIdx.x * eb; at < c.end; at += kThreads * eb)
+        store_one(c.dst + at, c.type, (float)((double)load_one(c.src + at, c.type) * s));
+}
+
+__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const GradEntry* table, int n, int64_t n_chunks, const double* scale) {
     pdl_wait();
-    const float s = *scale;
+    const double exact = *scale;
+    const float s = (float)exact;
+    const bool tiny = exact > 0. && exact < 1.17549435e-38;
     const int64_t begin = run_begin(n_chunks, blockIdx.x), end = run_begin(n_chunks, blockIdx.x + 1);
     if (begin >= end) return;
     int t = find_tensor(table, n, end - 1);
@@ -257,7 +268,8 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const GradEntry* t
         while (table[t].first_chunk > chunk || table[t].numel == 0) --t;
         const Chunk c = chunk_at(table[t], chunk);
         if (s == 1.f && c.src == c.dst) continue;
-        if (c.type == 0) scale_chunk<0>(c, s);
+        if (tiny) scale_chunk_tiny(c, exact);
+        else if (c.type == 0) scale_chunk<0>(c, s);
         else if (c.type == 1) scale_chunk<1>(c, s);
         else scale_chunk<2>(c, s);
     }
@@ -271,12 +283,12 @@ int64_t grad_chunks(const void* src, int64_t numel, int type) {
 int grad_blocks(int sms) { return sms * kBlocksPerSm; }
 
 cudaError_t launch_grad_norm(const GradEntry* table, int n_tensors, int64_t n_chunks, double* partials, int32_t* ticket,
-                             float max_norm, float* norm_out, float* scale, int blocks, cudaStream_t st) {
+                             float max_norm, float* norm_out, double* scale, int blocks, cudaStream_t st) {
     const int grid = (int)(n_chunks < 1 ? 1 : n_chunks < blocks ? n_chunks : blocks);
     return launch_chained(grad_norm_kernel, dim3(grid), dim3(kThreads), 0, st, table, n_tensors, n_chunks, partials, ticket,
                           max_norm, norm_out, scale);
 }
-cudaError_t launch_grad_scale(const GradEntry* table, int n_tensors, int64_t n_chunks, const float* scale, int blocks,
+cudaError_t launch_grad_scale(const GradEntry* table, int n_tensors, int64_t n_chunks, const double* scale, int blocks,
                               cudaStream_t st) {
     const int grid = (int)(n_chunks < 1 ? 1 : n_chunks < blocks ? n_chunks : blocks);
     return launch_chained(grad_scale_kernel, dim3(grid), dim3(kThreads), 0, st, table, n_tensors, n_chunks, scale);

@@ -112,8 +112,8 @@ struct GradEntry {
     int32_t type, pad;
 };
 cudaError_t launch_grad_norm(const GradEntry* table, int n_tensors, int64_t n_chunks, double* partials, int32_t* ticket,
-                             float max_norm, float* norm_out, float* scale, int blocks, cudaStream_t st);
-cudaError_t launch_grad_scale(const GradEntry* table, int n_tensors, int64_t n_chunks, const float* scale, int blocks,
+                             float max_norm, float* norm_out, double* scale, int blocks, cudaStream_t st);
+cudaError_t launch_grad_scale(const GradEntry* table, int n_tensors, int64_t n_chunks, const double* scale, int blocks,
                               cudaStream_t st);
 int64_t grad_chunks(const void* src, int64_t numel, int type);
 int grad_blocks(int sms);

@@ -129,7 +129,7 @@ struct mars_grads {
     GradEntry* table;
     double* partials;
     int32_t* ticket;
-    float* scale;
+    double* scale;
 };
 
 namespace {
@@ -501,7 +501,7 @@ mars_status_t mars_grads_create(const mars_grad_t* tensors, int32_t n, void* wor
         if (!g) return MARS_ERR_INVALID_ARG;
         g->device = dev; g->sms = sms; g->n = n; g->chunks = chunks;
         g->table = (GradEntry*)base; g->partials = (double*)(base + partials);
-        g->ticket = (int32_t*)(base + ticket); g->scale = (float*)(base + ticket + 64);
+        g->ticket = (int32_t*)(base + ticket); g->scale = (double*)(base + ticket + 64);
         *out = g;
         return MARS_OK;
     } catch (const std::bad_alloc&) {

@@ -853,6 +853,24 @@ def test_norms_whose_squares_leave_the_range_of_fp32(value):
     assert abs(float(norm) - want) <= 1e-5 * want
 
 
+@pytest.mark.parametrize("value,max_norm,count", [(3e38, 1.0, 100_003), (3e38, 1e-3, 777), (1e10, 1e-30, 100), (2e38, 1e-20, 50), (3.0, 1e-37, 9),
+                                                  (1e20, 3e-18, 300)])
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_factors_below_the_normal_numbers_of_fp32(value, max_norm, count, dtype, odd):
+    """max_norm / norm from 1e-37 down to 1e-60: results that fp32 holds are right all the same."""
+    t = (torch.rand(count + 1, generator=gen(3), device=DEV) * 0.5 + 0.5).mul_(value).to(dtype)[odd:count + odd]
+    o, norm = torch.full((count,), 7.0, dtype=dtype, device=DEV), torch.empty(1, device=DEV)
+    want_norm = math.sqrt(float((t.double() / value).square().sum())) * value
+    scale = max_norm / (want_norm + 1e-6)
+    assert binding.mars_grads_clip(binding.GradList([t], [o]), max_norm, norm) == 0
+    want = t.double() * scale
+    tol = want.abs() * (U[dtype] + 66 * 2.0 ** -24 + 2.0 ** -23) + (2.0 ** -150 if dtype == F32 else 2.0 ** -134 + 2.0 ** -150)
+    assert worst(o, want, tol) <= 1
+    assert binding.mars_grads_clip(binding.GradList([t]), max_norm, norm) == 0            # in place
+    assert torch.equal(t, o)
+
+
 def test_infinities_and_nan():
     norm = torch.empty(1, device=DEV)
     t = torch.ones(1000, device=DEV)
