@@ -391,8 +391,9 @@ MARS_API const int32_t *mars_active_experts_device(const mars_model_t *model);
  * expert products alone.  hidden: a multiple of 8, at least 8; vocab >= 1; max_tokens <= 2^20.  Workspace: 256-byte aligned device
  * memory of the device that is current at creation (the handle's device; calls made while another device is
  * current switch to it and back), its content private between calls.  One call at a time per handle, on the
- * GPU as well: calls on several streams are to be ordered by the caller.  mars_update_poll_status works as
- * mars_poll_status (MARS_OK, MARS_ERR_BAD_TOKEN, MARS_ERR_TIMEOUT). */
+ * GPU as well: calls on several streams are to be ordered by the caller.  mars_update_poll_status waits
+ * for all work on the handle's device (calls on any stream and replays of captured ones), reads the status word and clears it:
+ * MARS_OK, MARS_ERR_BAD_TOKEN or MARS_ERR_TIMEOUT.  Not while a stream is being captured. */
 typedef struct mars_update mars_update_t;
 enum { MARS_F32 = 0, MARS_BF16 = 1, MARS_F16 = 2 };
 MARS_API size_t mars_update_workspace_bytes(int32_t hidden, int32_t vocab, int32_t max_tokens);

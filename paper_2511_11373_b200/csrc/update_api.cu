@@ -120,7 +120,6 @@ struct mars_update {
     float2* stats;
     float *target_logit, *lse, *scaled, *target_d;
     int32_t *src, *target, *n_live;
-    cudaStream_t last_stream;
 };
 
 struct mars_grads {
@@ -218,7 +217,7 @@ mars_status_t mars_update_create(int32_t hidden, int32_t vocab, int32_t max_toke
     RUN(launched(init_update_kernels()));
     mars_update* u = new (std::nothrow) mars_update();
     if (!u) return MARS_ERR_INVALID_ARG;
-    u->device = dev; u->sms = sms; u->l = l; u->last_stream = nullptr;
+    u->device = dev; u->sms = sms; u->l = l;
     carve_update(l, (unsigned char*)workspace, u);
     // cudaMemset returns before the memory is set, and a non-blocking stream does not wait for it
     cudaError_t e = cudaMemset(u->err, 0, 512);
@@ -238,7 +237,8 @@ mars_status_t mars_update_poll_status(mars_update_t* u) {
     if (!u) return MARS_ERR_BAD_HANDLE;
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;
-    CUDA_TRY(cudaStreamSynchronize(u->last_stream));
+    // the streams of the calls are not all known here: a captured call runs on whatever stream its graph is replayed on
+    CUDA_TRY(cudaDeviceSynchronize());
     int32_t word = 0;
     CUDA_TRY(cudaMemcpy(&word, u->err, 4, cudaMemcpyDeviceToHost));
     if (word) {
@@ -266,7 +266,6 @@ mars_status_t mars_logprob(mars_update_t* u, void* cuda_stream, int32_t n, const
     UpMaps maps{};
     RUN(map_k(&maps.a, lm_head, l.H, l.V, l.H));
     RUN(map_rows(&maps, u->rows, l.H, l.rows, l.H, n));
-    u->last_stream = st;
 
     LiveRows r{};
     r.hidden = (const __nv_bfloat16*)hidden; r.ld = ld; r.lm_head = (const __nv_bfloat16*)lm_head; r.targets = targets;
@@ -308,7 +307,6 @@ mars_status_t mars_logprob_grad_lp(mars_update_t* u, void* cuda_stream, int32_t 
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    u->last_stream = st;
     if (n == 0) {
         if (!accumulate) CUDA_TRY(cudaMemsetAsync(d_lm_head, 0, ow, st));
         return MARS_OK;
@@ -384,11 +382,10 @@ mars_status_t mars_expert_matmul(mars_update_t* u, void* cuda_stream, int32_t E,
     UpMaps maps{};
     RUN(map_stack(&maps.a, w, d_in, d_out, E, 128));
     RUN(map_rows(&maps, x, d_in, rows, ld_x, rows));
-    u->last_stream = (cudaStream_t)cuda_stream;
     UpParams p{};
     p.m = d_out; p.k = d_in; p.splits = 1; p.n_block = update_n_block(d_in); p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
     p.e.out = y; p.e.ld = ld_y; p.e.out_f32 = y_type == MARS_F32;
-    return launched(launch_expert_fwd(maps, p, u->sms, u->last_stream));
+    return launched(launch_expert_fwd(maps, p, u->sms, (cudaStream_t)cuda_stream));
 }
 
 mars_status_t mars_expert_matmul_dx(mars_update_t* u, void* cuda_stream, int32_t E, int32_t rows, int32_t d_in, int32_t d_out,
@@ -406,11 +403,10 @@ mars_status_t mars_expert_matmul_dx(mars_update_t* u, void* cuda_stream, int32_t
     UpMaps maps{};
     RUN(map_stack(&maps.a, w, d_in, d_out, E, 64));
     RUN(map_rows(&maps, dy, d_out, rows, ld_dy, rows));
-    u->last_stream = (cudaStream_t)cuda_stream;
     UpParams p{};
     p.m = d_in; p.k = d_out; p.splits = 1; p.n_block = update_n_block(d_out); p.expert_off = off; p.experts = E; p.rows = rows; p.err = u->err;
     p.e.out = dx; p.e.ld = ld_dx; p.e.out_f32 = dx_type == MARS_F32;
-    return launched(launch_expert_dx(maps, p, u->sms, u->last_stream));
+    return launched(launch_expert_dx(maps, p, u->sms, (cudaStream_t)cuda_stream));
 }
 
 mars_status_t mars_expert_matmul_dw(mars_update_t* u, void* cuda_stream, int32_t E, int32_t rows, int32_t d_in, int32_t d_out,
@@ -425,7 +421,6 @@ mars_status_t mars_expert_matmul_dw(mars_update_t* u, void* cuda_stream, int32_t
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    u->last_stream = st;
     if (rows == 0) {
         if (!accumulate) CUDA_TRY(cudaMemsetAsync(dw, 0, ow, st));
         return MARS_OK;

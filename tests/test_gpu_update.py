@@ -959,6 +959,29 @@ def test_a_new_handle_is_ready_for_any_stream():
     assert float(norm) == 8.0 and float(lp[3]) == 0.0
 
 
+def test_the_status_of_a_replay_is_waited_for():
+    """The graph is replayed on another stream than it was captured on, behind other work, and polled at once."""
+    h, w, targets, _ = logprob_case(8, 64, 100, 1.0, seed=5)
+    targets[3] = 100
+    u, (lp, lse) = binding.Update(64, 100, 8, device=DEV), torch.empty(2, 8, device=DEV)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        assert binding.mars_logprob(u, h, w, targets, 1.0, lp, lse) == 0
+    assert u.poll_status() == 0                                         # captured, not run
+    for _ in range(2):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(200_000_000)
+            graph.replay()
+        assert u.poll_status() == 7 and u.poll_status() == 0
+    # the handle outlives the stream of its last call
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        assert binding.mars_logprob(u, h, w, targets, 1.0, lp, lse) == 0
+    del s
+    assert u.poll_status() == 7
+
+
 def test_a_workspace_is_not_handed_on_while_a_side_stream_uses_it():
     t, norm = torch.ones(64, device=DEV), torch.empty(1, device=DEV)
     lst = binding.GradList([t])
