@@ -449,8 +449,8 @@ MARS_API mars_status_t mars_logprob_grad_lp(mars_update_t *update, void *cuda_st
  * expert_off: DEVICE int32 [n_experts + 1], read on the device (no host copy, capturable).  Rows outside
  * [expert_off[0], expert_off[n_experts]) are not touched; their inputs may hold anything, and so may the rows
  * of other experts: nothing crosses a group's border.  Offsets are clamped to [0, n_rows] and a decreasing
- * offset counts as equal to the largest before it.  0 <= n_rows <= 2^30; 1 <= n_experts <= 1024; d_in, d_out and
- * row strides multiples of 8; matrices 16-byte aligned; outputs must not overlap inputs.  Same bits on every call. */
+ * offset counts as equal to the largest before it.  0 <= n_rows <= 2^30; 1 <= n_experts <= 1024; d_in and d_out
+ * multiples of 8 from 8 to 2^30, row strides multiples of 8; matrices 16-byte aligned; outputs must not overlap inputs.  Same bits on every call. */
 MARS_API mars_status_t mars_expert_matmul(mars_update_t *update, void *cuda_stream, int32_t n_experts, int32_t n_rows,
                                           int32_t d_in, int32_t d_out, const void *x, int64_t ld_x, const int32_t *expert_off,
                                           const void *w, void *y, int64_t ld_y, int32_t y_type);

@@ -183,7 +183,9 @@ mars_status_t check_logprob(const mars_update* u, int32_t n, const void* hidden,
 mars_status_t check_experts(const mars_update* u, int32_t E, int32_t rows, int32_t d_in, int32_t d_out, const void* rows_in,
                             int64_t ld_in, int64_t cols_in, const int32_t* off) {
     if (!u) return MARS_ERR_BAD_HANDLE;
-    if (E < 1 || E > kUpMaxExperts || rows < 0 || rows > (1 << 30) || d_in < 8 || d_out < 8 || d_in % 8 || d_out % 8) return MARS_ERR_INVALID_ARG;
+    // at most 2^30 of anything: extents are rounded up to tiles and stages in 32 bits
+    if (E < 1 || E > kUpMaxExperts || rows < 0 || rows > (1 << 30) || d_in < 8 || d_out < 8 || d_in > (1 << 30) || d_out > (1 << 30) ||
+        d_in % 8 || d_out % 8) return MARS_ERR_INVALID_ARG;
     if (!off || (uintptr_t)off % 4) return MARS_ERR_INVALID_ARG;
     if (rows > 0 && (!rows_in || !aligned16(rows_in) || ld_in < cols_in || ld_in % 8)) return MARS_ERR_INVALID_ARG;
     return MARS_OK;

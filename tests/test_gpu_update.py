@@ -778,6 +778,20 @@ def test_more_rows_than_an_index_holds_are_refused():
     assert (y == 3).all()
 
 
+def test_wider_experts_than_an_index_holds_are_refused():
+    """The C entries themselves: nothing is launched, so the sizes need not be backed by memory."""
+    u = binding.Update(device=DEV)
+    x, w, y, off = torch.zeros(64, device=DEV), torch.zeros(64, device=DEV), torch.full((64,), 3.0, device=DEV), offsets([1])
+    L, p = binding.lib(), [t.data_ptr() for t in (x, w, y)]
+    top = (1 << 31) - 8
+    for d_in, d_out in ((8, top), (top, 8), ((1 << 30) + 8, 8), (8, (1 << 30) + 8)):
+        assert L.mars_expert_matmul(u.handle, None, 1, 1, d_in, d_out, p[0], d_in, off.data_ptr(), p[1], p[2], d_out, 1) == 1
+        assert L.mars_expert_matmul_dx(u.handle, None, 1, 1, d_in, d_out, p[0], d_out, off.data_ptr(), p[1], p[2], d_in, 1) == 1
+        assert L.mars_expert_matmul_dw(u.handle, None, 1, 1, d_in, d_out, p[0], d_out, p[1], d_in, off.data_ptr(), p[2], 1, 0) == 1
+    torch.cuda.synchronize()
+    assert (y == 3).all()
+
+
 # -------------------------------------------------------------------------------------- gradient lists
 
 def grad_tensors(sizes, types, seed, aligned=True, std=1.0):
