@@ -425,7 +425,8 @@ MARS_API mars_status_t mars_update_poll_status(mars_update_t *update);
  * error of up to 2^-24 |lse| |d_logprobs| / temperature in d loss / d logit of the target, as much as the value itself
  * where p is within some 1e-6 of 1.
  * n_tokens = 0 is allowed (d_lm_head is then zeroed, or left when it accumulates).  Row strides are in elements
- * and multiples of 8; matrices are 16-byte aligned, d_hidden [n_tokens][ld_d_hidden].  Outputs must not overlap inputs.
+ * and multiples of 8; matrices are 16-byte aligned, d_hidden [n_tokens][ld_d_hidden].  Outputs must not overlap inputs
+ * (hidden and d_hidden may be column ranges of one buffer, side by side).
  * The same call on the same inputs gives the same bits. */
 MARS_API mars_status_t mars_logprob(mars_update_t *update, void *cuda_stream, int32_t n_tokens, const void *hidden,
                                     int64_t ld_hidden, const void *lm_head, const int32_t *targets, float temperature,
@@ -450,7 +451,8 @@ MARS_API mars_status_t mars_logprob_grad_lp(mars_update_t *update, void *cuda_st
  * [expert_off[0], expert_off[n_experts]) are not touched; their inputs may hold anything, and so may the rows
  * of other experts: nothing crosses a group's border.  Offsets are clamped to [0, n_rows] and a decreasing
  * offset counts as equal to the largest before it.  0 <= n_rows <= 2^30; 1 <= n_experts <= 1024; d_in and d_out
- * multiples of 8 from 8 to 2^30, row strides multiples of 8; matrices 16-byte aligned; outputs must not overlap inputs.  Same bits on every call. */
+ * multiples of 8 from 8 to 2^30, row strides multiples of 8; matrices 16-byte aligned; outputs must not overlap inputs
+ * (column ranges of one buffer, side by side, are fine).  Same bits on every call. */
 MARS_API mars_status_t mars_expert_matmul(mars_update_t *update, void *cuda_stream, int32_t n_experts, int32_t n_rows,
                                           int32_t d_in, int32_t d_out, const void *x, int64_t ld_x, const int32_t *expert_off,
                                           const void *w, void *y, int64_t ld_y, int32_t y_type);

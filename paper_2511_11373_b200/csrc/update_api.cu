@@ -57,6 +57,17 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 size_t span(int64_t rows, int64_t ld, int64_t cols, size_t elem) {
     return rows > 0 ? (size_t)((rows - 1) * ld + cols) * elem : 0;
 }
+// Two [rows][..] matrices with row strides (elements).  Column ranges of one buffer lie inside each other's span without
+// sharing a byte: with equal strides, b's columns must then fall between the end of a's and the end of the row.
+bool rows_overlap(const void* a, int64_t ld_a, int64_t cols_a, size_t elem_a, const void* b, int64_t ld_b, int64_t cols_b, size_t elem_b,
+                  int64_t rows) {
+    if (!overlap(a, span(rows, ld_a, cols_a, elem_a), b, span(rows, ld_b, cols_b, elem_b))) return false;
+    const size_t pitch = (size_t)ld_a * elem_a;
+    if (rows < 2 || pitch != (size_t)ld_b * elem_b) return true;
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    const size_t at = y >= x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;       // of b's columns in a's rows
+    return at < (size_t)cols_a * elem_a || at + (size_t)cols_b * elem_b > pitch;
+}
 bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 bool aligned4(const void* p) { return (uintptr_t)p % 4 == 0; }
 
@@ -301,10 +312,12 @@ mars_status_t mars_logprob_grad_lp(mars_update_t* u, void* cuda_stream, int32_t 
                    !aligned16(d_hidden) || ld_d < u->l.H || ld_d % 8)) return MARS_ERR_INVALID_ARG;
     const Layout& l = u->l;
     const size_t ow = (size_t)l.V * l.H * out_bytes(d_type), oh = span(n, ld_d, l.H, 2), nb = (size_t)n * 4;
-    const struct { const void* p; size_t n; } ins[] = {{hidden, span(n, ld, l.H, 2)}, {lm_head, (size_t)l.V * l.H * 2},
-                                                       {targets, nb}, {lse, nb}, {d_logprobs, nb}, {logprobs, logprobs ? nb : 0}};
+    const struct { const void* p; size_t n; } ins[] = {{lm_head, (size_t)l.V * l.H * 2}, {targets, nb}, {lse, nb}, {d_logprobs, nb},
+                                                       {logprobs, logprobs ? nb : 0}};
     for (const auto& i : ins)
         if (overlap(d_lm_head, ow, i.p, i.n) || overlap(d_hidden, oh, i.p, i.n)) return MARS_ERR_INVALID_ARG;
+    if (overlap(d_lm_head, ow, hidden, span(n, ld, l.H, 2)) || rows_overlap(d_hidden, ld_d, l.H, 2, hidden, ld, l.H, 2, n))
+        return MARS_ERR_INVALID_ARG;
     if (overlap(d_lm_head, ow, d_hidden, oh)) return MARS_ERR_INVALID_ARG;
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;
@@ -377,7 +390,7 @@ mars_status_t mars_expert_matmul(mars_update_t* u, void* cuda_stream, int32_t E,
     if (rows == 0) return MARS_OK;
     if (!y || !aligned16(y) || ld_y < d_out || ld_y % 8) return MARS_ERR_INVALID_ARG;
     const size_t oy = span(rows, ld_y, d_out, out_bytes(y_type));
-    if (overlap(y, oy, x, span(rows, ld_x, d_in, 2)) || overlap(y, oy, w, (size_t)E * d_in * d_out * 2) ||
+    if (rows_overlap(y, ld_y, d_out, out_bytes(y_type), x, ld_x, d_in, 2, rows) || overlap(y, oy, w, (size_t)E * d_in * d_out * 2) ||
         overlap(y, oy, off, ((size_t)E + 1) * 4)) return MARS_ERR_INVALID_ARG;
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;
@@ -398,7 +411,7 @@ mars_status_t mars_expert_matmul_dx(mars_update_t* u, void* cuda_stream, int32_t
     if (rows == 0) return MARS_OK;
     if (!dx || !aligned16(dx) || ld_dx < d_in || ld_dx % 8) return MARS_ERR_INVALID_ARG;
     const size_t ox = span(rows, ld_dx, d_in, out_bytes(dx_type));
-    if (overlap(dx, ox, dy, span(rows, ld_dy, d_out, 2)) || overlap(dx, ox, w, (size_t)E * d_in * d_out * 2) ||
+    if (rows_overlap(dx, ld_dx, d_in, out_bytes(dx_type), dy, ld_dy, d_out, 2, rows) || overlap(dx, ox, w, (size_t)E * d_in * d_out * 2) ||
         overlap(dx, ox, off, ((size_t)E + 1) * 4)) return MARS_ERR_INVALID_ARG;
     const DeviceGuard guard(u->device);
     if (!guard.ok) return MARS_ERR_CUDA;

@@ -778,6 +778,56 @@ def test_more_rows_than_an_index_holds_are_refused():
     assert (y == 3).all()
 
 
+def test_inputs_and_outputs_side_by_side_in_one_buffer():
+    """Column ranges of one [rows][...] buffer do not overlap; ranges that share a column, or reach into the next row, do."""
+    counts, d, o = [40, 0, 33], 64, 72
+    off, g, u, n = offsets(counts), gen(81), binding.Update(device=DEV), 73
+    w = normal(g, 3, o, d)
+    buf = normal(g, n + 1, 160)
+    x, dy = buf[:n, :d].clone(), normal(g, n, o)
+    y = torch.empty(n, o, dtype=torch.bfloat16, device=DEV)
+    dx = torch.empty_like(x)
+    assert binding.mars_expert_matmul(u, x, off, w, y) == 0 and binding.mars_expert_matmul_dx(u, dy, off, w, dx) == 0
+    rest = buf.clone()
+    assert binding.mars_expert_matmul(u, buf[:n, :d], off, w, buf[:n, d:d + o]) == 0
+    assert torch.equal(buf[:n, d:d + o], y)
+    rest[:n, d:d + o] = y
+    assert torch.equal(buf, rest)
+    buf[:n, :o] = dy                                                # the output in front or behind, and of four bytes
+    assert binding.mars_expert_matmul_dx(u, buf[:n, :o], off, w, buf[:n, 96:96 + d]) == 0
+    assert torch.equal(buf[:n, 96:96 + d], dx) and torch.equal(buf[:n, :o], dy)
+    buf[:n, 80:80 + o] = dy
+    assert binding.mars_expert_matmul_dx(u, buf[:n, 80:80 + o], off, w, buf[:n, 8:8 + d]) == 0
+    assert torch.equal(buf[:n, 8:8 + d], dx)
+    wide = torch.zeros(n, 256, device=DEV)                          # fp32 rows of 1024 bytes; x in the first 128 of them
+    half = wide.view(torch.bfloat16)
+    half[:, :d] = x
+    assert binding.mars_expert_matmul(u, half[:, :d], off, w, wide[:, 64:64 + o]) == 0
+    assert torch.equal(wide[:, 64:64 + o].bfloat16(), y) and torch.equal(half[:, :d], x)
+    before = buf.clone()
+    for a, b in ((0, 56), (56, 0), (8, 64)):                       # shared columns
+        assert binding.mars_expert_matmul(u, buf[:n, a:a + d], off, w, buf[:n, b:b + o]) == 1
+    late = buf.view(-1)[120:120 + n * 160].view(n, 160)             # begins in a row's columns 120 .. and ends in the next row's
+    assert binding.mars_expert_matmul(u, buf[:n, :d], off, w, late[:, :o]) == 1
+    assert binding.mars_expert_matmul(u, late[:, :d], off, w, buf[:n, :o]) == 1
+    narrow = buf.view(-1)[:n * 80].view(n, 80)                      # other row strides
+    assert binding.mars_expert_matmul(u, narrow[:, :d], off, w, buf[:n, d:d + o]) == 1
+    torch.cuda.synchronize()
+    assert torch.equal(buf, before)
+
+
+def test_hidden_and_its_gradient_side_by_side_in_one_buffer():
+    h, lm, targets, d = logprob_case(90, 64, 500, 1.0, 0.2, seed=82)
+    u = binding.Update(64, 500, 90, device=DEV)
+    want = run_logprob(u, h, lm, targets, 1.0, d)
+    buf = torch.full((90, 128), 5.0, dtype=torch.bfloat16, device=DEV)
+    buf[:, :64] = h
+    d_w = torch.empty_like(lm)
+    assert binding.mars_logprob_grad(u, buf[:, :64], lm, targets, 1.0, want["lse"], d, buf[:, 64:], d_w) == 0
+    assert torch.equal(buf[:, 64:], want["d_h"]) and torch.equal(buf[:, :64], h) and torch.equal(d_w, want["d_w"])
+    assert binding.mars_logprob_grad(u, buf[:, :64], lm, targets, 1.0, want["lse"], d, buf[:, 56:120], d_w) == 1
+
+
 def test_wider_experts_than_an_index_holds_are_refused():
     """The C entries themselves: nothing is launched, so the sizes need not be backed by memory."""
     u = binding.Update(device=DEV)
