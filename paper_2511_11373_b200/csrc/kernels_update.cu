@@ -12,7 +12,7 @@
 // The N width of a tile is a multiple of 32 chosen from the rows there are (see cut): tokens sit on N, so ragged
 // groups and short calls cost what they hold (a group of 4 rows a 32-wide tile, 270 rows one of 160 and one of 128),
 // and a call of few rows is a plain stream of the weights.
-//   warp 0      TMA producer, 64 contraction indexes per stage, 128-byte swizzle, mbarrier ring of 5 to 12
+//   warp 0      TMA producer, 64 contraction indexes per stage, 128-byte swizzle, mbarrier ring of 4 to 12
 //               stages that runs on across tiles;
 //   warp 1      of the leading CTA: issues tcgen05.mma (M 256, K 16) into one of two TMEM accumulators;
 //   warps 2..9  epilogue of the previous tile (a thread owns one M index, half of the columns) meanwhile;
@@ -401,8 +401,8 @@ __device__ __forceinline__ uint32_t pair_columns(float a, float b, bool odd) {
     return __byte_perm(mine, other, odd ? 0x3276 : 0x5410);
 }
 
-// 32 columns of the tile, from column c on: bf16 (rounded once from the fp32 accumulator) or fp32, optionally on top
-// of what is there (added in fp32).
+// 32 columns of the tile, from column c on: bf16 (rounded once from the fp32 accumulator) or fp32, the latter optionally
+// on top of what is there (the parts of d_hidden; nothing adds to bf16 here).
 __device__ __forceinline__ void store_chunk(const UpEpilogue& e, const Tile& t, int ch, int c, int left, float (&v)[32]) {
     const bool live = ch < t.m_valid, odd = ch & 1;
     const bool whole = left >= 32 && (ch | 31) < t.m_valid;          // the same for the warp
@@ -425,18 +425,6 @@ __device__ __forceinline__ void store_chunk(const UpEpilogue& e, const Tile& t, 
     } else {
         __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(e.out) + t.out + (int64_t)(c + odd) * e.ld + (ch - odd);
         const int64_t step = 2 * e.ld;
-        if (e.accumulate) {
-            uint32_t old[16];
-            const __nv_bfloat16* q = dst;
-#pragma unroll
-            for (int j = 0; j < 16; ++j, q += step) old[j] = live && 2 * j + odd < left ? *reinterpret_cast<const uint32_t*>(q) : 0u;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float got = __shfl_xor_sync(0xffffffffu, odd ? bf16_lo(old[j]) : bf16_hi(old[j]), 1);
-                v[2 * j] += odd ? got : bf16_lo(old[j]);             // old[j]: this lane's column of the pair, both M indexes
-                v[2 * j + 1] += odd ? bf16_hi(old[j]) : got;
-            }
-        }
         if (whole) {
 #pragma unroll
             for (int j = 0; j < 32; j += 2, dst += step) *reinterpret_cast<uint32_t*>(dst) = pair_columns(v[j], v[j + 1], odd);

@@ -12,8 +12,9 @@ using namespace mars;
 
 namespace {
 
-// The gradient of the logits is held for one vocabulary piece at a time: at most this many bytes of bf16.  Wide
-// pieces mean few passes over the fp32 sums of d_hidden (one read and write of rows x hidden per piece).
+// The gradient of the logits is held for one vocabulary piece at a time: this many bytes of bf16, or 2048 entries of every
+// row where that is more (above 131072 rows; 4 GB at 2^20).  Wide pieces mean few passes over the fp32 sums of d_hidden (one
+// read and write of rows x hidden per piece).
 constexpr size_t kPieceBytes = (size_t)512 << 20;
 constexpr int kMinPiece = 2048;
 
@@ -117,7 +118,8 @@ mars_status_t device_info(int* dev, int* sms) {
     return major == 10 ? MARS_OK : MARS_ERR_UNSUPPORTED;
 }
 
-// The sizes of a handle's workspace do not depend on the device: laid out for the largest split count.
+// The sizes of a handle's workspace do not depend on the device: laid out for the splits of d_hidden that 148 SMs and
+// max_tokens rows call for; a call takes as many as its own rows leave room for.
 constexpr int kPlanSms = 148;
 
 }  // namespace
