@@ -404,6 +404,41 @@ def test_the_smallest_temperatures():
         check_logprob(got, logprob_reference(h, w, targets, T))
 
 
+def gradient_error(n, V=4000, H=128):
+    """2-norm error of an fp32 d_lm_head relative to its size, rows of nearly uniform p (nothing but roundings of d)."""
+    g = gen(91)
+    w, h = normal(g, V, H, std=0.05), normal(g, n, H)
+    targets = torch.randint(V, (n,), generator=g, device=DEV, dtype=torch.int32)
+    d = torch.randn(n, generator=g, device=DEV)
+    u = binding.Update(H, V, n, device=DEV)
+    got = run_logprob(u, h, w, targets, 1.0, d, dtype=torch.float32)["d_w"].double()
+    z = h.double() @ w.double().t()
+    dz = -torch.softmax(z, dim=1)
+    dz[torch.arange(n), targets.long()] += 1
+    want = (dz * d.double()[:, None]).t() @ h.double()
+    other = torch.ones(V, dtype=torch.bool, device=DEV)
+    other[targets.long()] = False                                 # rows of p alone: entries of one size
+    return float((got[other] - want[other]).norm() / want[other].norm())
+
+
+def test_the_second_bf16_row_of_short_calls_counts():
+    """Up to 128 rows d is held in two bf16 rows, together within 2^-16 of an entry; beyond in one, within 2^-8 of it, which is
+    2^-8 / sqrt(7) in the 2-norm.  The logits' own errors (2e-6) are below both."""
+    assert gradient_error(128) < 2.0 ** -14
+    assert gradient_error(64) < 2.0 ** -14
+    assert 2.0 ** -11.5 < gradient_error(129) < 2.0 ** -9
+
+
+@pytest.mark.parametrize("n", [700, 1030])
+def test_log_probs_of_more_rows_than_a_block_of_tiles(n):
+    """At 16384 wide 1024 rows (four tiles) stay in L2 while the lm_head passes; at 65536 wide 256 do, one tile."""
+    for H, V in ((16384, 800), (65536, 300)):
+        h, w, targets, d = logprob_case(n, H, V, 1.0, 0.0, seed=n)
+        h, w = (h.float() / 16).bfloat16(), (w.float() / 4).bfloat16()
+        u = binding.Update(H, V, n, device=DEV)
+        check_logprob(run_logprob(u, h, w, targets, 0.85, d), logprob_reference(h, w, targets, 0.85, d))
+
+
 def test_lm_head_beyond_32_bit_offsets():
     """2.5e9 entries: the target rows in the last and first parts of the matrix, against fp64 on the rows that count."""
     n, H, V = 3, 8192, 300001
@@ -696,6 +731,26 @@ def test_a_group_of_four_hundred_million_rows():
         want += dy[a:b].double().t() @ x[a:b].double()
     check_rounded(dw[0], want, want * in_parts(n))
     check_rounded(dw[1], dy[n - 5:].double().t() @ x[n - 5:].double(), 5 * sum_error(5) * torch.ones(d, d, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_groups_of_more_rows_than_a_block_of_tiles(dtype):
+    """Groups whose rows exceed what is kept in L2 while the weights pass: at a width of 16384 that is 1024 rows, at 4104
+    3840, with the last block full, ragged, of one row."""
+    for counts, d, o in (([2500, 0, 1024, 1025, 300], 16384, 520), ([9000, 3840, 3841], 4104, 264)):
+        off, g, u = offsets(counts, 3), gen(92), binding.Update(device=DEV)
+        n, E = sum(counts) + 3, len(counts)
+        x, w = normal(g, n, d), normal(g, E, o, d, std=0.1)
+        y = torch.full((n, o), 5.0, dtype=dtype, device=DEV)
+        assert binding.mars_expert_matmul(u, x, off, w, y) == 0
+        wt = w.transpose(1, 2).contiguous()
+        dx = torch.full((n, o), 5.0, dtype=dtype, device=DEV)
+        assert binding.mars_expert_matmul_dx(u, x, off, wt, dx) == 0       # the same sums, w the other way round
+        v, tol = expert_reference("fwd", off, x, w, E)
+        for got in (y, dx):
+            check_rounded(got[3:], v[3:], tol[3:])
+            assert (got[:3] == 5).all()
+        assert u.poll_status() == 0
 
 
 def test_expert_gradients_against_differences():
