@@ -314,6 +314,16 @@ def test_several_vocabulary_pieces():
     assert (got["d_h"][~live] == 0).all()
 
 
+def test_the_largest_row_count():
+    n, H, V = 1 << 20, 16, 300
+    u = binding.Update(H, V, n, device=DEV)
+    h, w, targets, d = logprob_case(n, H, V, 1.0, 0.3, seed=3)
+    got = run_logprob(u, h, w, targets, 0.85, d, dtype=torch.float32)
+    assert u.poll_status() == 0
+    ref = logprob_reference(h, w, targets, 0.85, d)
+    check_logprob(got, ref)
+
+
 def test_full_vocabulary_rows():
     n, H, V = 70, 2048, 151936
     h, w, targets, d = logprob_case(n, H, V, 1.0, 0.1, seed=6)
