@@ -418,8 +418,10 @@ MARS_API mars_status_t mars_update_poll_status(mars_update_t *update);
  * The vocabulary is worked off in pieces; the probabilities of a piece are computed again from hidden and
  * lse.  Rows without a target and rows with d_logprobs = 0 take no part: their d_hidden is 0, whatever
  * their hidden states hold.  accumulate_d_lm_head != 0 adds to what d_lm_head holds (micro-batches); the sum is
- * formed in fp32 and rounded once to the type of d_lm_head.  Precision: d loss / d logit is rounded to bf16
- * (relative 2^-8, independent per entry) before the two products, which accumulate in fp32.
+ * formed in fp32 and rounded once to the type of d_lm_head.  Precision: the two products take d loss / d logit
+ * in bf16 and accumulate in fp32.  Calls of up to 128 rows hold it in two bf16 values (together within 2^-16 of an entry),
+ * larger ones in one (within 2^-8, independent per entry): a caller who wants the finer one splits the rows into calls of
+ * 128 that accumulate into an fp32 d_lm_head.  p = exp(z - lse) carries the rounding of lse, 2^-24 |lse| relative.
  * mars_logprob_grad_lp: the same, given the log-probs of mars_logprob too.  1 - p of a target is then -expm1(logp), to its
  * full relative accuracy.  mars_logprob_grad (and logprobs = NULL) has it from lse, which is rounded to fp32: an absolute
  * error of up to 2^-24 |lse| |d_logprobs| / temperature in d loss / d logit of the target, as much as the value itself
@@ -446,7 +448,8 @@ MARS_API mars_status_t mars_logprob_grad_lp(mars_update_t *update, void *cuda_st
  *   mars_expert_matmul      y_r  = w_e x_r           x [n_rows][ld_x], w [n_experts][d_out][d_in], y [n_rows][ld_y]
  *   mars_expert_matmul_dx   dx_r = w_e^T dy_r
  *   mars_expert_matmul_dw   dw_e = sum_r dy_r x_r^T  dw [n_experts][d_out][d_in], 0 for an expert without rows
- * x, w, dy are bf16, sums fp32; y, dx, dw are bf16 (rounded once) or fp32; accumulate != 0 adds to what dw holds.
+ * x, w, dy are bf16, sums fp32 (parts of at most 4096 products on the tensor cores, up to some 1.5e-5 low where all have one
+ * sign, added to nearest); y, dx, dw are bf16 (rounded once) or fp32; accumulate != 0 adds to what dw holds.
  * expert_off: DEVICE int32 [n_experts + 1], read on the device (no host copy, capturable).  Rows outside
  * [expert_off[0], expert_off[n_experts]) are not touched; their inputs may hold anything, and so may the rows
  * of other experts: nothing crosses a group's border.  Offsets are clamped to [0, n_rows] and a decreasing
@@ -473,8 +476,9 @@ MARS_API mars_status_t mars_expert_matmul_dw(mars_update_t *update, void *cuda_s
  *   mars_grads_norm   *out_norm = sqrt of the sum of all squares (device fp32), summed in fp32 / fp64
  *   mars_grads_clip   the same, and out_t = grad_t min(1, max_norm / (norm + 1e-6)): the factor in fp64,
  *                     rounded to fp32 where that holds it in full precision; the product rounded to the type.
- * max_norm >= 0.  A NaN norm makes every out NaN; an infinite one makes finite values 0.  Where nothing has to be
- * scaled, tensors in place are not touched.  One call at a time per handle; same bits on every call. */
+ * max_norm >= 0.  A NaN norm makes every out NaN; one that an infinite gradient makes infinite makes finite values 0.  A norm
+ * beyond fp32 is reported as infinite and scaled by all the same.  Where nothing has to be scaled, tensors in place are not
+ * touched.  out_norm lies in no tensor of the list.  One call at a time per handle; same bits on every call. */
 typedef struct {
     const void *grad;
     void *out;

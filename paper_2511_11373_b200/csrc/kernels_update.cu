@@ -8,7 +8,7 @@
 // One persistent kernel template serves all of them.  A pair of CTAs (cta_group::2) works on one tile of 256 x
 // up to 256: each CTA holds 128 rows of A and half of B's rows, its tensor core reads the other half from its
 // peer, so a 64-deep stage brings 32 KB into each SM where single-CTA 128 x 256 tiles bring 48 (those ran at the
-// 11.5 TB/s that the L2 delivers: 758 us against 665 us for 131072 expert rows x 2048 -> 1536).
+// 11.5 TB/s that the L2 delivers: 758 us against 665 us for 131072 expert rows x 2048 -> 1536, bursts on equal groups).
 // The N width of a tile is a multiple of 32 chosen from the rows there are (see cut): tokens sit on N, so ragged
 // groups and short calls cost what they hold (a group of 4 rows a 32-wide tile, 270 rows one of 160 and one of 128),
 // and a call of few rows is a plain stream of the weights.
