@@ -422,8 +422,8 @@ MARS_API mars_status_t mars_update_poll_status(mars_update_t *update);
  * in bf16 and accumulate in fp32.  Calls of up to 128 rows hold it in two bf16 values (together within 2^-16 of an entry),
  * larger ones in one (within 2^-8, independent per entry): a caller who wants the finer one splits the rows into calls of
  * 128 that accumulate into an fp32 d_lm_head.  p = exp(z - lse) carries the rounding of lse, 2^-24 |lse| relative.
- * mars_logprob_grad_lp: the same, given the log-probs of mars_logprob too.  1 - p of a target is then -expm1(logp), to its
- * full relative accuracy.  mars_logprob_grad (and logprobs = NULL) has it from lse, which is rounded to fp32: an absolute
+ * mars_logprob_grad_lp: the same, given the log-probs of mars_logprob too.  1 - p of a target is then -expm1(logp), with
+ * the relative accuracy of logp.  mars_logprob_grad (and logprobs = NULL) has it from lse, which is rounded to fp32: an absolute
  * error of up to 2^-24 |lse| |d_logprobs| / temperature in d loss / d logit of the target, as much as the value itself
  * where p is within some 1e-6 of 1.
  * n_tokens = 0 is allowed (d_lm_head is then zeroed, or left when it accumulates).  Row strides are in elements
