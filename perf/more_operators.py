@@ -312,7 +312,7 @@ def _run_own(s):
     else:
         st = binding.mars_policy_loss(u, s["lp"], s["old"], s["adv"], s["targets"], s["off"], s["stats"], s["d_lp"],
                                       ref_logprobs=s["ref"], clip_low=CLIP_LOW, clip_high=CLIP_HIGH, kl_coef=c["kl"],
-                                      reduce=c["reduce"], scale=s["scale"])
+                                      reduce=c["reduce"], scale=s["scale"], per_token=c["per_token"])
         got.update(stats=s["stats"], d_lp=s["d_lp"])
     if st:
         raise RuntimeError("status %d" % st)
