@@ -494,6 +494,130 @@ MARS_API mars_status_t mars_grads_free(mars_grads_t *grads);
 MARS_API mars_status_t mars_grads_norm(mars_grads_t *grads, void *cuda_stream, float *out_norm);
 MARS_API mars_status_t mars_grads_clip(mars_grads_t *grads, void *cuda_stream, float max_norm, float *out_norm);
 
+/* ---- operators of a training pass ----------------------------------------------------------------
+ * What the update of the policy still needs beside the calls above: the loss that turns log-probs into d_logprobs
+ * (Eq. 2), the mixture's router with its balance loss and gradient (its offsets are the expert_off of
+ * mars_expert_matmul), norms and the rotation of heads with their backward passes.  Like the calls above they work on plain
+ * device tensors, read every count on the device, wait for nothing and may be captured into a CUDA graph; the same call on
+ * the same inputs gives the same bits.  Types are MARS_F32, MARS_BF16 and MARS_F16; all arithmetic is fp32 or wider, rounded
+ * once.  Tensors are aligned to their elements; rows whose starts and lengths are multiples of 16 bytes are
+ * faster.  Row strides (ld) are in elements, at most 2^31.  Outputs must not overlap inputs or one another, with the
+ * exceptions named below, where an output takes the place of an input exactly (same address, same stride, same type);
+ * column ranges of one buffer, side by side with one stride, are no overlap.
+ *
+ * mars_train_t holds the workspace (256-byte aligned device memory of the current device) of norms of up to max_width, routers
+ * of up to max_experts and policy losses of up to max_seqs sequences; 0 leaves a group out, one at least is not 0.
+ * max_width <= 16384, max_experts <= 1024, max_seqs <= 2^20.  One call at a time per handle, on the GPU as well: calls on
+ * several streams are ordered by the caller, and two graphs that are replayed at the same time need a handle each.  (mars_norm
+ * and mars_router_grad use no workspace and may run beside anything.) */
+typedef struct mars_train mars_train_t;
+MARS_API size_t mars_train_workspace_bytes(int32_t max_width, int32_t max_experts, int32_t max_seqs);
+MARS_API mars_status_t mars_train_create(int32_t max_width, int32_t max_experts, int32_t max_seqs, void *workspace,
+                                         size_t workspace_bytes, mars_train_t **out);
+MARS_API mars_status_t mars_train_free(mars_train_t *train);
+
+/* Norms.  Row (t, h), h < heads, is the `width` elements at t * ld + h * width of a matrix: heads = 1 for rows of hidden
+ * states, the number of heads for the per-head norm of a projection.  weight and bias [width].
+ *   mars_norm       s = x (+ add, rounded to x's type and stored in sum if that is given)
+ *                   MARS_NORM_RMS:   y = s rstd weight,                   rstd = (mean(s^2) + eps)^-1/2
+ *                   MARS_NORM_LAYER: y = (s - mean) rstd weight (+ bias), rstd = (mean((s - mean)^2) + eps)^-1/2
+ *   mars_norm_grad  from dy, and x = the s of the forward call, with its mean and rstd:
+ *                   dx = d loss / d s (+ d_sum: the gradient that reaches the sum on its other way)
+ *                   dw = sum over all rows of dy (s - mean) rstd,  db = sum over all rows of dy
+ * x, sum, d_sum and dx have x_type; add, y and dy have y_type: the same, or x_type MARS_F32 (a residual stream) with any
+ * y_type; weight and bias w_type; dw and db dw_type (summed in fp32 and fp64, rounded once), added to what they hold if
+ * accumulate != 0.  add, sum (only with add), bias, mean, rstd, d_sum, dw and db may be NULL; mean, bias and db are for layer norms.
+ * n_rows >= 0 and n_rows * heads < 2^31; eps > 0.  The squares of a row must be within fp32.  sum or y may take the place of x or add,
+ * dx that of dy, x or d_sum. */
+enum { MARS_NORM_RMS = 0, MARS_NORM_LAYER = 1 };
+typedef struct {
+    int32_t kind, width, heads, x_type, y_type, w_type;
+    float eps;
+    int32_t reserved;
+} mars_norm_t;
+MARS_API mars_status_t mars_norm(mars_train_t *train, void *cuda_stream, const mars_norm_t *form, int32_t n_rows, const void *x,
+                                 int64_t ld_x, const void *add, int64_t ld_add, void *sum, int64_t ld_sum, const void *weight,
+                                 const void *bias, void *y, int64_t ld_y, float *mean, float *rstd);
+MARS_API mars_status_t mars_norm_grad(mars_train_t *train, void *cuda_stream, const mars_norm_t *form, int32_t n_rows, const void *dy,
+                                      int64_t ld_dy, const void *x, int64_t ld_x, const void *weight, const float *mean,
+                                      const float *rstd, const void *d_sum, int64_t ld_d_sum, void *dx, int64_t ld_dx, void *dw,
+                                      void *db, int32_t dw_type, int32_t accumulate);
+
+/* Rotation of heads by their positions.  Of every head the first `rotary` values (even, 2 .. 512) are turned in pairs, (i, i + rotary / 2)
+ * (MARS_ROPE_HALF, the layout of the model above) or (2i, 2i + 1) (MARS_ROPE_INTERLEAVED), by the angle position x frequency_i,
+ * and multiplied by `scale`; the others pass.  frequency_i = theta^(-2i / rotary), stretched for contexts longer than those of
+ * the training:
+ *   MARS_ROPE_LINEAR  divided by factor
+ *   MARS_ROPE_BASE    with theta factor^(rotary / (rotary - 2)) for theta (rotary > 2)
+ *   MARS_ROPE_PARTS   by how often a pair turns over trained_positions: from `fast` turns on unchanged, up to `slow` turns
+ *                     divided by factor, between them blended linearly in the number of turns (0 <= slow < fast)
+ * Angles are taken in fp64.  mars_rope_frequencies writes the rotary / 2 frequencies to HOST memory.  The handle keeps them
+ * in `workspace` (device memory, 256-byte aligned, mars_rope_bytes(form)); any number of calls may use it at once.
+ * mars_rope turns q [n_tokens][q_heads][head_dim] and, where k_heads > 0, k [n_tokens][k_heads][head_dim] (row strides ld, heads
+ * next to each other; q and k may be columns of one projection) by positions [n_tokens] (device, any int32); inverse != 0
+ * turns back, which is the gradient's way (the factor `scale` stays).  head_dim from rotary to 512.  Outputs may take the place
+ * of their inputs. */
+enum { MARS_ROPE_HALF = 0, MARS_ROPE_INTERLEAVED = 1 };
+enum { MARS_ROPE_PLAIN = 0, MARS_ROPE_LINEAR = 1, MARS_ROPE_BASE = 2, MARS_ROPE_PARTS = 3 };
+typedef struct {
+    int32_t rotary, layout, scaling, reserved;
+    double theta, factor, trained_positions, fast, slow, scale;
+} mars_rope_form_t;
+typedef struct mars_rope_table mars_rope_t;
+MARS_API mars_status_t mars_rope_frequencies(const mars_rope_form_t *form, double *out /*host*/);
+MARS_API size_t mars_rope_bytes(const mars_rope_form_t *form);
+MARS_API mars_status_t mars_rope_create(const mars_rope_form_t *form, void *workspace, size_t workspace_bytes, mars_rope_t **out);
+MARS_API mars_status_t mars_rope_free(mars_rope_t *rope);
+MARS_API mars_status_t mars_rope(mars_rope_t *rope, void *cuda_stream, int32_t n_tokens, const int32_t *positions, int32_t head_dim,
+                                 int32_t type, const void *q, int64_t ld_q, int32_t q_heads, void *out_q, int64_t ld_out_q,
+                                 const void *k, int64_t ld_k, int32_t k_heads, void *out_k, int64_t ld_out_k, int32_t inverse);
+
+/* The router of the mixture.  logits [n_rows][ld], n_experts of a row; live: NULL or one byte for each row, 0 = padding.
+ *   p = softmax(logits);  idx [n_rows][top_k]: the top_k largest, in that order, the lower expert first among equals;
+ *   weights [n_rows][top_k]: p of those, divided by their sum if renormalise != 0;  lse [n_rows]: log of the sum of exponentials
+ *   counts [n_experts]: rows that chose an expert;  offsets [n_experts + 1]: their exclusive sums (expert_off of a permutation by expert)
+ *   prob_sums [n_experts]: sum of p over the rows;  losses [2]: with N rows, f_e = counts_e / (N top_k),
+ *     [0] balance = n_experts sum_e f_e prob_sums_e / N (1 when even),  [1] z = sum of lse^2 / N
+ * lse, counts, offsets, prob_sums and losses may be NULL.  Rows that are not live, and rows without a logit above -inf, take no part:
+ * idx -1, weights and lse 0.  Logits of -inf have p = 0 and are chosen last.  A NaN in a live row makes its weights NaN and the sums
+ * with it; its choices are then any top_k different experts.  top_k <= 32.
+ * mars_router_grad: d_logits [n_rows][ld_d] (the type of the logits) of
+ *   sum of d_weights weights + balance_coef balance + z_coef z
+ * given idx, lse and counts of mars_router; the choice itself has no gradient (f_e is constant).  d_weights may be NULL.  counts may be
+ * those of several calls added up (micro-batches): N is then that of all of them.  Rows that took no part get 0; their logits and
+ * d_weights are not used.  An idx outside the experts is left out.  d_logits may take the place of logits. */
+MARS_API mars_status_t mars_router(mars_train_t *train, void *cuda_stream, int32_t n_rows, int32_t n_experts, int32_t top_k,
+                                   const void *logits, int64_t ld, int32_t type, const uint8_t *live, int32_t renormalise, int32_t *idx,
+                                   float *weights, float *lse, int32_t *counts, int32_t *offsets, float *prob_sums, float *losses);
+MARS_API mars_status_t mars_router_grad(mars_train_t *train, void *cuda_stream, int32_t n_rows, int32_t n_experts, int32_t top_k,
+                                        const void *logits, int64_t ld, int32_t type, const int32_t *idx, const float *lse,
+                                        const int32_t *counts, const float *d_weights, int32_t renormalise, float balance_coef,
+                                        float z_coef, void *d_logits, int64_t ld_d);
+
+/* The clipped policy loss with a KL term (Eq. 2) and its gradient.  Tokens of all sequences lie behind one another, sequence s at
+ * seq_off[s] .. seq_off[s + 1] - 1 (device int32 [n_seqs + 1], not decreasing); tokens outside of all sequences and tokens with
+ * targets < 0 (prompt, padding) take no part: their other inputs may hold anything, their gradient is 0.  With
+ * r = exp(logprobs - old_logprobs), A the token's or its sequence's advantage, x = ref_logprobs - logprobs, a token's term is
+ *   -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A) + kl_coef (exp(x) - x - 1)
+ *   stats[0] loss = scale times the mean of the terms over the tokens (MARS_MEAN_TOKENS), the mean over the sequences that have
+ *            tokens of the mean over their tokens (MARS_MEAN_SEQUENCES), or the sum of the terms (MARS_SUM; micro-batches put 1 / (tokens
+ *            of the whole batch) into scale)
+ *   stats[1] mean of exp(x) - x - 1 over the tokens (0 without ref),  [2] share of tokens whose ratio was cut,  [3] mean ratio,
+ *        [4] tokens that took part,  [5] sequences that have such tokens
+ *   d_logprobs[i] = d loss / d logprobs[i]  (the d_logprobs of mars_logprob_grad);  may be NULL
+ * At a border, where both products are equal, the gradient is that of r A.  Borders are decided in fp64.  logprobs and the others are
+ * fp32 [n_tokens], advantages [n_seqs] or [n_tokens]; ref_logprobs may be NULL where kl_coef = 0.  0 <= clip_low <= 1, clip_high >= 0.
+ * n_tokens <= 2^30, 1 <= n_seqs <= max_seqs.  d_logprobs may take the place of logprobs. */
+enum { MARS_MEAN_TOKENS = 0, MARS_MEAN_SEQUENCES = 1, MARS_SUM = 2 };
+typedef struct {
+    double clip_low, clip_high, kl_coef, scale;
+    int32_t reduce, advantages_per_token;
+} mars_policy_t;
+MARS_API mars_status_t mars_policy_loss(mars_train_t *train, void *cuda_stream, const mars_policy_t *form, int32_t n_tokens,
+                                        int32_t n_seqs, const int32_t *seq_off, const int32_t *targets, const float *logprobs,
+                                        const float *old_logprobs, const float *ref_logprobs, const float *advantages,
+                                        float *stats /*[6]*/, float *d_logprobs);
+
 MARS_API int32_t mars_last_cuda_error(void);
 MARS_API const char *mars_status_string(mars_status_t status);
 MARS_API const char *mars_version(void);

@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
 
@@ -67,6 +67,21 @@ class mars_step_info_t(ctypes.Structure):
 
 class mars_grad_t(ctypes.Structure):
     _fields_ = [("grad", c_void_p), ("out", c_void_p), ("numel", c_int64), ("type", c_int32), ("reserved", c_int32)]
+
+
+class mars_norm_t(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("kind", "width", "heads", "x_type", "y_type", "w_type")] + \
+               [("eps", c_float), ("reserved", c_int32)]
+
+
+class mars_rope_form_t(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("rotary", "layout", "scaling", "reserved")] + \
+               [(n, c_double) for n in ("theta", "factor", "trained_positions", "fast", "slow", "scale")]
+
+
+class mars_policy_t(ctypes.Structure):
+    _fields_ = [(n, c_double) for n in ("clip_low", "clip_high", "kl_coef", "scale")] + \
+               [("reduce", c_int32), ("advantages_per_token", c_int32)]
 
 
 # name -> (restype, argtypes); mirrors include/mars.h one to one
@@ -136,6 +151,25 @@ SIGNATURES = {
     "mars_grads_free": (c_int32, [c_void_p]),
     "mars_grads_norm": (c_int32, [c_void_p, c_void_p, c_void_p]),
     "mars_grads_clip": (c_int32, [c_void_p, c_void_p, c_float, c_void_p]),
+    "mars_train_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32]),
+    "mars_train_create": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_size_t, POINTER(c_void_p)]),
+    "mars_train_free": (c_int32, [c_void_p]),
+    "mars_norm": (c_int32, [c_void_p, c_void_p, POINTER(mars_norm_t), c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                            c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
+    "mars_norm_grad": (c_int32, [c_void_p, c_void_p, POINTER(mars_norm_t), c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                 c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_int32]),
+    "mars_rope_frequencies": (c_int32, [POINTER(mars_rope_form_t), POINTER(c_double)]),
+    "mars_rope_bytes": (c_size_t, [POINTER(mars_rope_form_t)]),
+    "mars_rope_create": (c_int32, [POINTER(mars_rope_form_t), c_void_p, c_size_t, POINTER(c_void_p)]),
+    "mars_rope_free": (c_int32, [c_void_p]),
+    "mars_rope": (c_int32, [c_void_p, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_void_p, c_int64, c_int32, c_void_p, c_int64,
+                            c_void_p, c_int64, c_int32, c_void_p, c_int64, c_int32]),
+    "mars_router": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_void_p,
+                              c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "mars_router_grad": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int64, c_int32, c_void_p, c_void_p,
+                                   c_void_p, c_void_p, c_int32, c_float, c_float, c_void_p, c_int64]),
+    "mars_policy_loss": (c_int32, [c_void_p, c_void_p, POINTER(mars_policy_t), c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_void_p, c_void_p, c_void_p]),
     "mars_last_cuda_error": (c_int32, []),
     "mars_status_string": (c_char_p, [c_int32]),
     "mars_version": (c_char_p, []),
@@ -637,3 +671,281 @@ def mars_grads_clip(grads: GradList, max_norm: float, out_norm: torch.Tensor, st
     """The norm, and every gradient scaled by min(1, max_norm / (norm + 1e-6)) into its out; returns the status code."""
     _want(out_norm, "out_norm", (torch.float32,), grads.device, 1)
     return lib().mars_grads_clip(grads.handle, grads._stream(stream), float(max_norm), out_norm.data_ptr())
+
+
+# ------------------------------------------------------------------------- operators of a training pass
+
+MARS_NORM_RMS, MARS_NORM_LAYER = 0, 1
+_ALL_TYPES = tuple(MARS_TYPES)
+_F32, _I32 = (torch.float32,), (torch.int32,)
+
+
+class Train:
+    """mars_train_create / mars_train_free: the workspace of norms of up to max_width, routers of up to max_experts and policy
+    losses of up to max_seqs sequences (0 leaves a group out)."""
+
+    def __init__(self, max_width: int = 0, max_experts: int = 0, max_seqs: int = 0, device="cuda"):
+        self.max_width, self.max_experts, self.max_seqs = max_width, max_experts, max_seqs
+        nbytes = lib().mars_train_workspace_bytes(max_width, max_experts, max_seqs)
+        if nbytes == 0:
+            raise MarsError(2, "mars_train_workspace_bytes")
+        with torch.cuda.device(torch.device(device)):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+            self.device = self.workspace.device
+            torch.cuda.current_stream().synchronize()      # the memory may still be in use by an earlier owner's kernels
+            self._home = _raw_stream(self.device.index)
+            handle = c_void_p()
+            _check(lib().mars_train_create(max_width, max_experts, max_seqs, _ptr(self.workspace), nbytes, byref(handle)),
+                   "mars_train_create")
+        self.handle = handle
+        self._forms = {}
+
+    _stream = Update._stream
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().mars_train_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _heads(t: torch.Tensor, name: str, dtypes, dev: torch.device, shape) -> int:
+    """The row stride of a [n, width] or [n, heads, width] tensor whose heads lie next to each other; ValueError otherwise."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.shape != shape:
+        raise ValueError(f"{name}: expected {tuple(str(d) for d in dtypes)} {tuple(shape)}, got "
+                         f"{getattr(t, 'dtype', type(t))} {tuple(getattr(t, 'shape', ()))}")
+    if t.get_device() != (-1 if dev.index is None else dev.index):
+        raise ValueError(f"{name}: on {t.device}, the handle on {dev}")
+    strides, width = t.stride(), shape[-1]
+    row = width if len(shape) == 2 else shape[1] * width
+    if (width > 1 and strides[-1] != 1) or (len(shape) == 3 and shape[1] > 1 and strides[1] != width):
+        raise ValueError(f"{name}: strides {strides} are not supported")
+    if shape[0] <= 1:
+        return row
+    if strides[0] < row:
+        raise ValueError(f"{name}: strides {strides} are not supported")
+    return strides[0]
+
+
+def _norm_form(train: Train, kind: int, x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor, eps: float) -> mars_norm_t:
+    key = (kind, x.shape[1:], x.dtype, y.dtype, weight.dtype, eps)
+    form = train._forms.get(key)
+    if form is None:
+        heads = x.shape[1] if x.dim() == 3 else 1
+        if len(train._forms) >= 256:
+            train._forms.clear()
+        form = train._forms[key] = mars_norm_t(kind, x.shape[-1], heads, MARS_TYPES[x.dtype], MARS_TYPES[y.dtype],
+                                               MARS_TYPES[weight.dtype], float(eps), 0)
+    return form
+
+
+def _norm_shapes(x):
+    if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
+        raise ValueError("x: expected [n, width] or [n, heads, width]")
+    return x.shape, x.shape[:-1], x.shape[-1]
+
+
+def mars_norm(train: Train, kind: int, x: torch.Tensor, weight: torch.Tensor, eps: float, y: torch.Tensor,
+              rstd: torch.Tensor = None, mean: torch.Tensor = None, bias: torch.Tensor = None, add: torch.Tensor = None,
+              out_sum: torch.Tensor = None, stream=None) -> int:
+    """y = norm(x + add) of every row of [n, width], or of every head of [n, heads, width] (any row stride); kind MARS_NORM_RMS
+    or MARS_NORM_LAYER.  rstd, mean: fp32, one for each row, for mars_norm_grad.  out_sum: x + add.  Returns the status code."""
+    shape, rows, width = _norm_shapes(x)
+    dev = train.device
+    ld_x = _heads(x, "x", _ALL_TYPES, dev, shape)
+    ld_y = _heads(y, "y", _ALL_TYPES, dev, shape)
+    _want(weight, "weight", _ALL_TYPES, dev, width)
+    ld_add = ld_sum = 0
+    if add is not None:
+        ld_add = _heads(add, "add", (y.dtype,), dev, shape)
+    if out_sum is not None:
+        ld_sum = _heads(out_sum, "out_sum", (x.dtype,), dev, shape)
+    if bias is not None:
+        _want(bias, "bias", (weight.dtype,), dev, width)
+    if rstd is not None:
+        _want(rstd, "rstd", _F32, dev, *rows)
+    if mean is not None:
+        _want(mean, "mean", _F32, dev, *rows)
+    form = _norm_form(train, kind, x, y, weight, eps)
+    return lib().mars_norm(train.handle, train._stream(stream), byref(form), shape[0], x.data_ptr(), ld_x, _opt(add), ld_add,
+                           _opt(out_sum), ld_sum, weight.data_ptr(), _opt(bias), y.data_ptr(), ld_y, _opt(mean), _opt(rstd))
+
+
+def mars_norm_grad(train: Train, kind: int, dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor,
+                   dx: torch.Tensor, dw: torch.Tensor = None, mean: torch.Tensor = None, db: torch.Tensor = None,
+                   d_sum: torch.Tensor = None, accumulate: bool = False, stream=None) -> int:
+    """dx (+ d_sum), dw and db of mars_norm; x: what was normalised (out_sum where there was an addition), rstd and mean those of
+    the forward call.  accumulate: add to dw and db.  Returns the status code."""
+    shape, rows, width = _norm_shapes(x)
+    dev = train.device
+    ld_x = _heads(x, "x", _ALL_TYPES, dev, shape)
+    ld_dy = _heads(dy, "dy", _ALL_TYPES, dev, shape)
+    ld_dx = _heads(dx, "dx", (x.dtype,), dev, shape)
+    _want(weight, "weight", _ALL_TYPES, dev, width)
+    _want(rstd, "rstd", _F32, dev, *rows)
+    ld_sum, dw_type = 0, 0
+    if mean is not None:
+        _want(mean, "mean", _F32, dev, *rows)
+    if d_sum is not None:
+        ld_sum = _heads(d_sum, "d_sum", (x.dtype,), dev, shape)
+    if dw is not None:
+        _want(dw, "dw", _ALL_TYPES, dev, width)
+        dw_type = MARS_TYPES[dw.dtype]
+    if db is not None:
+        _want(db, "db", _ALL_TYPES if dw is None else (dw.dtype,), dev, width)
+        dw_type = MARS_TYPES[db.dtype]
+    form = _norm_form(train, kind, x, dy, weight, 1.0)         # eps is in rstd
+    return lib().mars_norm_grad(train.handle, train._stream(stream), byref(form), shape[0], dy.data_ptr(), ld_dy, x.data_ptr(), ld_x,
+                                weight.data_ptr(), _opt(mean), rstd.data_ptr(), _opt(d_sum), ld_sum, dx.data_ptr(), ld_dx, _opt(dw),
+                                _opt(db), dw_type, int(bool(accumulate)))
+
+
+def _opt(t):
+    return None if t is None else t.data_ptr()
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+class Rope:
+    """mars_rope_create / mars_rope_free: the frequencies of a rotation of the first `rotary` values of a head.  layout: "half" or
+    "interleaved"; scaling: "none", "linear", "base" or "parts" (see mars_rope_form_t in mars.h)."""
+
+    def __init__(self, rotary: int, theta: float = 1e6, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+                 trained_positions: float = 0.0, fast: float = 32.0, slow: float = 1.0, scale: float = 1.0, device="cuda"):
+        if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+            raise ValueError(f"layout: one of {tuple(ROPE_LAYOUTS)}; scaling: one of {tuple(ROPE_SCALINGS)}")
+        self.form = mars_rope_form_t(rotary, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], 0, theta, factor, trained_positions, fast, slow,
+                                     scale)
+        nbytes = lib().mars_rope_bytes(byref(self.form))
+        if nbytes == 0:
+            raise MarsError(1, "mars_rope_bytes")
+        with torch.cuda.device(torch.device(device)):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+            self.device = self.workspace.device
+            torch.cuda.current_stream().synchronize()
+            self._home = _raw_stream(self.device.index)
+            handle = c_void_p()
+            _check(lib().mars_rope_create(byref(self.form), _ptr(self.workspace), nbytes, byref(handle)), "mars_rope_create")
+        self.handle = handle
+
+    _stream = Update._stream
+
+    def frequencies(self) -> torch.Tensor:
+        """Angle of every pair for one position (fp64, on the host)."""
+        return rope_frequencies(self.form)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().mars_rope_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def rope_frequencies(form: mars_rope_form_t) -> torch.Tensor:
+    out = (c_double * max(1, form.rotary // 2))()
+    _check(lib().mars_rope_frequencies(byref(form), out), "mars_rope_frequencies")
+    return torch.tensor(list(out), dtype=torch.float64)
+
+
+def mars_rope(rope: Rope, positions: torch.Tensor, q: torch.Tensor, out_q: torch.Tensor, k: torch.Tensor = None,
+              out_k: torch.Tensor = None, inverse: bool = False, stream=None) -> int:
+    """Turns the heads of q [n, heads, head_dim] (and k) by positions (int32 [n]); inverse: back, the gradient.  Outputs may be the
+    inputs themselves.  Returns the status code."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or (k is not None and (not isinstance(k, torch.Tensor) or k.dim() != 3)):
+        raise ValueError("q, k: expected [n, heads, head_dim]")
+    dev, (n, heads, dim) = rope.device, q.shape
+    _want(positions, "positions", _I32, dev, n)
+    ld_q = _heads(q, "q", _ALL_TYPES, dev, q.shape)
+    ld_oq = _heads(out_q, "out_q", (q.dtype,), dev, q.shape)
+    k_heads = ld_k = ld_ok = 0
+    if k is not None:
+        k_heads = k.shape[1]
+        if k.shape[0] != n or k.shape[2] != dim:
+            raise ValueError(f"k: expected {(n, k_heads, dim)}, got {tuple(k.shape)}")
+        ld_k = _heads(k, "k", (q.dtype,), dev, k.shape)
+        ld_ok = _heads(out_k, "out_k", (q.dtype,), dev, k.shape)
+    return lib().mars_rope(rope.handle, rope._stream(stream), n, positions.data_ptr(), dim, MARS_TYPES[q.dtype], q.data_ptr(), ld_q, heads,
+                           out_q.data_ptr(), ld_oq, _opt(k), ld_k, k_heads, _opt(out_k) if k is not None else None, ld_ok,
+                           int(bool(inverse)))
+
+
+def mars_router(train: Train, logits: torch.Tensor, out_idx: torch.Tensor, out_weights: torch.Tensor, out_lse: torch.Tensor = None,
+                out_counts: torch.Tensor = None, out_offsets: torch.Tensor = None, out_prob_sums: torch.Tensor = None,
+                out_losses: torch.Tensor = None, live: torch.Tensor = None, renormalise: bool = True, stream=None) -> int:
+    """The top_k experts of every row of logits [n, experts] (any row stride) with their weights, [n, top_k] both; lse [n], counts
+    [experts], offsets [experts + 1], prob_sums [experts], losses [2] = balance and z.  live: bool [n].  Returns the status code."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not isinstance(out_idx, torch.Tensor) or out_idx.dim() != 2:
+        raise ValueError("logits: expected [n, experts]; out_idx: expected [n, top_k]")
+    dev, (n, experts), k = train.device, logits.shape, out_idx.shape[1]
+    _want(logits, "logits", _ALL_TYPES, dev, n, experts, rows=True)
+    _want(out_idx, "out_idx", _I32, dev, n, k)
+    _want(out_weights, "out_weights", _F32, dev, n, k)
+    for t, name, dtypes, size in ((out_lse, "out_lse", _F32, n), (out_counts, "out_counts", _I32, experts),
+                                  (out_offsets, "out_offsets", _I32, experts + 1), (out_prob_sums, "out_prob_sums", _F32, experts),
+                                  (out_losses, "out_losses", _F32, 2), (live, "live", (torch.bool, torch.uint8), n)):
+        if t is not None:
+            _want(t, name, dtypes, dev, size)
+    return lib().mars_router(train.handle, train._stream(stream), n, experts, k, logits.data_ptr(), _ld(logits), MARS_TYPES[logits.dtype],
+                             _opt(live), int(bool(renormalise)), out_idx.data_ptr(), out_weights.data_ptr(), _opt(out_lse),
+                             _opt(out_counts), _opt(out_offsets), _opt(out_prob_sums), _opt(out_losses))
+
+
+def mars_router_grad(train: Train, logits: torch.Tensor, idx: torch.Tensor, lse: torch.Tensor, counts: torch.Tensor,
+                     d_logits: torch.Tensor, d_weights: torch.Tensor = None, balance_coef: float = 0.0, z_coef: float = 0.0,
+                     renormalise: bool = True, stream=None) -> int:
+    """d_logits of d_weights and of balance_coef balance + z_coef z, with idx, lse and counts of mars_router; returns the status
+    code.  d_logits may be logits itself."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not isinstance(idx, torch.Tensor) or idx.dim() != 2:
+        raise ValueError("logits: expected [n, experts]; idx: expected [n, top_k]")
+    dev, (n, experts), k = train.device, logits.shape, idx.shape[1]
+    _want(logits, "logits", _ALL_TYPES, dev, n, experts, rows=True)
+    _want(idx, "idx", _I32, dev, n, k)
+    _want(lse, "lse", _F32, dev, n)
+    _want(counts, "counts", _I32, dev, experts)
+    _want(d_logits, "d_logits", (logits.dtype,), dev, n, experts, rows=True)
+    if d_weights is not None:
+        _want(d_weights, "d_weights", _F32, dev, n, k)
+    return lib().mars_router_grad(train.handle, train._stream(stream), n, experts, k, logits.data_ptr(), _ld(logits),
+                                  MARS_TYPES[logits.dtype], idx.data_ptr(), lse.data_ptr(), counts.data_ptr(), _opt(d_weights),
+                                  int(bool(renormalise)), float(balance_coef), float(z_coef), d_logits.data_ptr(), _ld(d_logits))
+
+
+POLICY_REDUCE = {"tokens": 0, "sequences": 1, "sum": 2}
+
+
+def mars_policy_loss(train: Train, logprobs: torch.Tensor, old_logprobs: torch.Tensor, advantages: torch.Tensor,
+                     targets: torch.Tensor, seq_off: torch.Tensor, out_stats: torch.Tensor, out_d_logprobs: torch.Tensor = None,
+                     ref_logprobs: torch.Tensor = None, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                     reduce: str = "tokens", scale: float = 1.0, per_token: bool = False, stream=None) -> int:
+    """The clipped policy loss over the tokens of the sequences seq_off (int32 [n_seqs + 1]) that have a target (>= 0) and its
+    gradient to logprobs (fp32 [n]).  advantages: fp32, one for each sequence, or for each token (per_token).  out_stats: fp32 [6], loss, KL, share of cut ratios, mean ratio, tokens, sequences.  reduce:
+    "tokens", "sequences" or "sum".  Returns the status code."""
+    if reduce not in POLICY_REDUCE:
+        raise ValueError(f"reduce: one of {tuple(POLICY_REDUCE)}")
+    dev, n, seqs = train.device, logprobs.shape[0], seq_off.shape[0] - 1
+    _want(logprobs, "logprobs", _F32, dev, n)
+    _want(old_logprobs, "old_logprobs", _F32, dev, n)
+    _want(advantages, "advantages", _F32, dev, n if per_token else seqs)
+    _want(targets, "targets", _I32, dev, n)
+    _want(seq_off, "seq_off", _I32, dev, seqs + 1)
+    _want(out_stats, "out_stats", _F32, dev, 6)
+    if out_d_logprobs is not None:
+        _want(out_d_logprobs, "out_d_logprobs", _F32, dev, n)
+    if ref_logprobs is not None:
+        _want(ref_logprobs, "ref_logprobs", _F32, dev, n)
+    form = mars_policy_t(clip_low, clip_high, kl_coef, scale, POLICY_REDUCE[reduce], int(per_token))
+    return lib().mars_policy_loss(train.handle, train._stream(stream), byref(form), n, seqs, seq_off.data_ptr(), targets.data_ptr(),
+                                  logprobs.data_ptr(), old_logprobs.data_ptr(), _opt(ref_logprobs), advantages.data_ptr(),
+                                  out_stats.data_ptr(), _opt(out_d_logprobs))

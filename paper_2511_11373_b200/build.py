@@ -17,6 +17,7 @@ OBJ_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libmars.so")
 SOURCES = ["kernels_dense.cu", "kernels_attn.cu", "kernels_moe.cu", "kernels_sample.cu", "kernels_umma.cu", "kernels_fattn.cu", "kernels_kv.cu",
            "kernels_update.cu", "kernels_grads.cu", "update_api.cu",
+           "kernels_norm.cu", "kernels_rope.cu", "kernels_router.cu", "kernels_policy.cu", "train_api.cu",
            "mars_api.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-I", os.path.join(ROOT, "include")]

@@ -1,0 +1,525 @@
+// Norms of rows and their gradients.
+//   s = x (+ add, rounded to x's type);  RMS: u = s, layer: u = s - mean(s);  r = 1 / sqrt(mean(u^2) + eps)
+//   y = u r w (+ b);   n = u r, g = dy w:
+//   dx = r (g - n mean(g n) - [layer] mean(g)) (+ d_sum),   dw = sum over rows of dy n,   db = sum of dy
+// Bound by HBM: every matrix is read or written once.  A row stays in the registers of a group of threads (a part of a warp, a warp,
+// or several that meet at a named barrier of their own, so that groups of a block do not wait for one another), in 16-byte
+// pieces.  Rows that allow no such pieces go value by value and are read again where the other form keeps them.  The variance is taken from the centred
+// values, in a second sum over the registers: sum of squares minus square of the sum would lose a mean that is large
+// beside the spread.
+// The gradient runs on a grid that fits the SMs at once: a thread keeps the sums of dw and db of its columns in fp32
+// registers over all rows of its group and asks for the next row before it reduces the present one; groups of a block meet in
+// shared memory, blocks in a second kernel that adds their sums in fp64 in a fixed order: the same call gives the same bits.
+#include <type_traits>
+
+#include "train.h"
+#include "train_types.cuh"
+
+namespace mars {
+
+namespace {
+
+constexpr int kChunk = 8;
+constexpr int kLoopSmem = 2 * kNormMaxWidth * 4;      // the sums of the widest row
+// Rows that the gradient keeps in registers, 16 values of a thread: 512 threads, or 256 with twice the registers for fp32.
+constexpr int grad_row_threads(bool x_is_fp32) { return x_is_fp32 ? 256 : 512; }
+
+// Threads of a row and chunks of eight neighbouring values of a thread (`most` at the most).
+struct NormPlan { int group, nv, block; };
+NormPlan norm_plan(int width, int most) {
+    const int chunks = (width + kChunk - 1) / kChunk;
+    NormPlan p;
+    if (chunks <= 32) {
+        p.nv = 1;
+        p.group = 1;
+        while (p.group < chunks) p.group *= 2;
+    } else {
+        p.nv = chunks < 256 || most < 4 ? 2 : 4;
+        p.group = (chunks + 32 * p.nv - 1) / (32 * p.nv) * 32;
+    }
+    p.block = p.group >= 256 ? p.group : 256 / p.group * p.group;
+    return p;
+}
+// The same for rows that are read again instead of kept.
+NormPlan loop_plan(int width) {
+    NormPlan p;
+    p.nv = 0;
+    p.group = 32;
+    while (p.group < 256 && p.group * 8 < width) p.group *= 2;
+    p.block = 256;
+    return p;
+}
+
+// Chunk j of a thread, zeros behind the row.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_chunk(const T* row, int j, int lane, int group, int width) {
+    const int c = (j * group + lane) * kChunk;
+    Raw8<T> r;
+    if (c < width) {
+        r = load8(row + c);
+    } else {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.v[i] = make_uint4(0, 0, 0, 0);
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* row, int j, int lane, int group, int width, const Raw8<T>& r) {
+    const int c = (j * group + lane) * kChunk;
+    if (c < width) store8(row + c, r);
+}
+__device__ __forceinline__ void load_weight(const void* w, int type, int j, int lane, int group, int width, float (&o)[8]) {
+    const int c = (j * group + lane) * kChunk;
+    if (c >= width) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = 0.f;
+    } else if (type == 0) unpack8<float>(load8(static_cast<const float*>(w) + c), o);
+    else if (type == 1) unpack8<__nv_bfloat16>(load8(static_cast<const __nv_bfloat16*>(w) + c), o);
+    else unpack8<__half>(load8(static_cast<const __half*>(w) + c), o);
+}
+
+// Sums over the threads of a group.  Groups of more than a warp use one half of `scratch` after the other: who writes a half
+// again has passed the barrier that all readers of it reached after reading.
+template <int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], int group, int index, float* scratch, int& half) {
+    if (group <= 32) {
+        for (int o = group >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+    const int warps = group >> 5, warp = threadIdx.x >> 5, first = index * warps;
+    float* s = scratch + half * 16 * N;
+    half ^= 1;
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[warp * N + i] = v[i];
+    }
+    asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(group) : "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    for (int w = 0; w < warps; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += s[(first + w) * N + i];
+}
+
+__device__ __forceinline__ int64_t row_offset(int row, int heads, int width, int64_t ld) {
+    if (heads == 1) return (int64_t)row * ld;
+    const int t = row / heads;
+    return (int64_t)t * ld + (int64_t)(row - t * heads) * width;
+}
+
+// Rows in registers.
+template <typename XT, typename YT, int NV>
+__global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, const int group) {
+    __shared__ float scratch[2 * 16];
+    const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
+    int half = 0;
+    const float inv = 1.f / (float)a.width;
+    for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += (int64_t)gridDim.x * groups) {
+        const bool on = base + index < a.rows;                // the trip count is the same for all threads of a block
+        const int row = on ? (int)(base + index) : 0;
+        const int W = on ? a.width : 0;
+        const XT* x = static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x);
+        Raw8<XT> fx[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) fx[j] = load_chunk(x, j, lane, group, W);
+        float v[NV][8];
+        if (a.has_add) {
+            const YT* add = static_cast<const YT*>(a.add) + row_offset(row, a.heads, a.width, a.ld_add);
+            Raw8<YT> fa[NV];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) fa[j] = load_chunk(add, j, lane, group, W);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float b[8];
+                unpack8<XT>(fx[j], v[j]);
+                unpack8<YT>(fa[j], b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] += b[i];
+                fx[j] = pack8<XT>(v[j]);                      // the norm is that of the stored sum
+                if (a.sum) store_chunk(static_cast<XT*>(a.sum) + row_offset(row, a.heads, a.width, a.ld_sum), j, lane, group, W, fx[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) unpack8<XT>(fx[j], v[j]);
+        float mean = 0.f;
+        if (a.layer) {
+            float s[1] = {0.f};
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[0] += v[j][i];
+            group_sum(s, group, index, scratch, half);
+            mean = s[0] * inv;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const bool in = (j * group + lane) * kChunk < a.width;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] = in ? v[j][i] - mean : 0.f;
+            }
+        }
+        float q[1] = {0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[0] = fmaf(v[j][i], v[j][i], q[0]);
+        group_sum(q, group, index, scratch, half);
+        const float rstd = 1.f / sqrtf(q[0] * inv + a.eps);
+        YT* y = static_cast<YT*>(a.y) + row_offset(row, a.heads, a.width, a.ld_y);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float w[8];
+            load_weight(a.weight, a.w_type, j, lane, group, W, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * rstd * w[i];
+            if (a.has_bias) {
+                load_weight(a.bias, a.w_type, j, lane, group, W, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] += w[i];
+            }
+            store_chunk(y, j, lane, group, W, pack8<YT>(v[j]));
+        }
+        if (on && lane == 0) {
+            if (a.rstd) a.rstd[row] = rstd;
+            if (a.mean && a.layer) a.mean[row] = mean;
+        }
+    }
+}
+
+// Any width and alignment, value by value: a row is read again (from L1 or L2) for every sum and for the result.
+template <typename XT, typename YT>
+__global__ void __launch_bounds__(256, 2) norm_loop_kernel(const NormArgs a, const int group) {
+    __shared__ float scratch[2 * 16];
+    const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
+    int half = 0;
+    const float inv = 1.f / (float)a.width;
+    for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += (int64_t)gridDim.x * groups) {
+        const bool on = base + index < a.rows;
+        const int row = on ? (int)(base + index) : 0;
+        const int W = on ? a.width : 0;
+        const XT* x = static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x);
+        const YT* add = static_cast<const YT*>(a.add) + row_offset(row, a.heads, a.width, a.ld_add);
+        bool adds = a.has_add;
+        if (a.sum) {                                          // a thread reads later what it stores here itself
+            XT* sum = static_cast<XT*>(a.sum) + row_offset(row, a.heads, a.width, a.ld_sum);
+#pragma unroll 4
+            for (int c = lane; c < W; c += group) sum[c] = from_float<XT>(to_float(x[c]) + to_float(add[c]));
+            x = sum;
+            adds = false;
+        }
+        auto value = [&](int c) { return adds ? to_float(from_float<XT>(to_float(x[c]) + to_float(add[c]))) : to_float(x[c]); };
+        float mean = 0.f;
+        if (a.layer) {
+            float s[1] = {0.f};
+#pragma unroll 4
+            for (int c = lane; c < W; c += group) s[0] += value(c);
+            group_sum(s, group, index, scratch, half);
+            mean = s[0] * inv;
+        }
+        float q[1] = {0.f};
+#pragma unroll 4
+        for (int c = lane; c < W; c += group) {
+            const float u = value(c) - mean;
+            q[0] = fmaf(u, u, q[0]);
+        }
+        group_sum(q, group, index, scratch, half);
+        const float rstd = 1.f / sqrtf(q[0] * inv + a.eps);
+        YT* y = static_cast<YT*>(a.y) + row_offset(row, a.heads, a.width, a.ld_y);
+#pragma unroll 4
+        for (int c = lane; c < W; c += group) {
+            float o = (value(c) - mean) * rstd * load_any(a.weight, a.w_type, c);
+            if (a.has_bias) o += load_any(a.bias, a.w_type, c);
+            y[c] = from_float<YT>(o);
+        }
+        if (on && lane == 0) {
+            if (a.rstd) a.rstd[row] = rstd;
+            if (a.mean && a.layer) a.mean[row] = mean;
+        }
+    }
+}
+
+// Rows in registers, with the sums of the weight's gradient.
+template <typename XT, typename YT, int NV, bool LAYER>
+__global__ void __launch_bounds__(NV == 1 ? 256 : grad_row_threads(sizeof(XT) == 4), NV == 1 ? 2 : 1) norm_grad_rows_kernel(const NormGradArgs a, const int group) {
+    __shared__ float scratch[2 * 16 * 2];
+    extern __shared__ float sums[];                           // [groups][width]
+    const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
+    int half = 0;
+    const float inv = 1.f / (float)a.width;
+    float acc_w[NV][8], acc_b[LAYER ? NV : 1][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            acc_w[j][i] = 0.f;
+            if (LAYER) acc_b[j][i] = 0.f;
+        }
+    const XT* px = static_cast<const XT*>(a.x);
+    const YT* pdy = static_cast<const YT*>(a.dy);
+    Raw8<XT> x[NV];
+    Raw8<YT> dy[NV];
+    float rstd = 0.f, mean = 0.f;
+    auto fetch = [&](int64_t r) {
+        const bool on = r < a.rows;
+        const int row = on ? (int)r : 0, W = on ? a.width : 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) x[j] = load_chunk(px + row_offset(row, a.heads, a.width, a.ld_x), j, lane, group, W);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) dy[j] = load_chunk(pdy + row_offset(row, a.heads, a.width, a.ld_dy), j, lane, group, W);
+        rstd = on ? a.rstd[row] : 0.f;
+        if (LAYER) mean = on ? a.mean[row] : 0.f;
+    };
+    const int64_t stride = (int64_t)gridDim.x * groups;
+    int64_t base = (int64_t)blockIdx.x * groups;
+    if (base < a.rows) fetch(base + index);
+    for (; base < a.rows; base += stride) {
+        const bool on = base + index < a.rows;
+        const int row = on ? (int)(base + index) : 0, W = on ? a.width : 0;
+        float n[NV][8], g[NV][8];
+        float c[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float w[8];
+            load_weight(a.weight, a.w_type, j, lane, group, W, w);
+            unpack8<XT>(x[j], n[j]);
+            unpack8<YT>(dy[j], g[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[j][i] = (LAYER ? n[j][i] - mean : n[j][i]) * rstd;
+                acc_w[j][i] = fmaf(g[j][i], n[j][i], acc_w[j][i]);
+                if (LAYER) acc_b[j][i] += g[j][i];
+                g[j][i] *= w[i];
+                c[0] = fmaf(g[j][i], n[j][i], c[0]);
+                if (LAYER) c[1] += g[j][i];
+            }
+        }
+        const float r = rstd;
+        Raw8<XT> ds[NV];
+        if (a.has_d_sum) {
+            const XT* p = static_cast<const XT*>(a.d_sum) + row_offset(row, a.heads, a.width, a.ld_d_sum);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) ds[j] = load_chunk(p, j, lane, group, W);
+        }
+        fetch(base + stride + index);                         // the next row is on its way while this one is reduced
+        group_sum(c, group, index, scratch, half);
+        const float c0 = c[0] * inv, c1 = LAYER ? c[1] * inv : 0.f;
+        XT* dx = static_cast<XT*>(a.dx) + row_offset(row, a.heads, a.width, a.ld_dx);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[j][i] = fmaf(-n[j][i], c0, LAYER ? g[j][i] - c1 : g[j][i]) * r;
+            if (a.has_d_sum) {
+                float s[8];
+                unpack8<XT>(ds[j], s);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[j][i] += s[i];
+            }
+            store_chunk(dx, j, lane, group, W, pack8<XT>(g[j]));
+        }
+    }
+#pragma unroll
+    for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
+        float* out = which ? a.part_b : a.part_w;
+        if (!out) continue;
+        out += (int64_t)blockIdx.x * a.width;
+        float* own = groups == 1 ? out : sums + index * a.width;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = (j * group + lane) * kChunk + i;
+                if (c < a.width) own[c] = which ? acc_b[LAYER ? j : 0][i] : acc_w[j][i];
+            }
+        if (groups == 1) continue;
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.width; c += blockDim.x) {
+            float t = 0.f;
+            for (int k = 0; k < groups; ++k) t += sums[k * a.width + c];
+            out[c] = t;
+        }
+    }
+}
+
+// Any width and alignment, value by value: a row is read twice, the sums of its columns lie in shared memory, where every column of a
+// group belongs to one thread.
+template <typename XT, typename YT, bool LAYER>
+__global__ void __launch_bounds__(256, 2) norm_grad_loop_kernel(const NormGradArgs a, const int group) {
+    __shared__ float scratch[2 * 16 * 2];
+    extern __shared__ float sums[];                           // [groups][width], the same again for db
+    const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
+    int half = 0;
+    const float inv = 1.f / (float)a.width;
+    float* sw = sums + index * a.width;
+    float* sb = sums + (groups + index) * a.width;
+    for (int c = lane; c < a.width; c += group) {
+        sw[c] = 0.f;
+        if (LAYER) sb[c] = 0.f;
+    }
+    for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += (int64_t)gridDim.x * groups) {
+        const bool on = base + index < a.rows;
+        const int row = on ? (int)(base + index) : 0, W = on ? a.width : 0;
+        const XT* x = static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x);
+        const YT* dy = static_cast<const YT*>(a.dy) + row_offset(row, a.heads, a.width, a.ld_dy);
+        const XT* ds = static_cast<const XT*>(a.d_sum) + row_offset(row, a.heads, a.width, a.ld_d_sum);
+        const float r = on ? a.rstd[row] : 0.f, mean = LAYER && on ? a.mean[row] : 0.f;
+        float s[2] = {0.f, 0.f};
+#pragma unroll 4
+        for (int c = lane; c < W; c += group) {
+            const float n = (to_float(x[c]) - mean) * r, d = to_float(dy[c]), g = d * load_any(a.weight, a.w_type, c);
+            sw[c] = fmaf(d, n, sw[c]);
+            s[0] = fmaf(g, n, s[0]);
+            if (LAYER) {
+                sb[c] += d;
+                s[1] += g;
+            }
+        }
+        group_sum(s, group, index, scratch, half);
+        const float c0 = s[0] * inv, c1 = LAYER ? s[1] * inv : 0.f;
+        XT* dx = static_cast<XT*>(a.dx) + row_offset(row, a.heads, a.width, a.ld_dx);
+#pragma unroll 4
+        for (int c = lane; c < W; c += group) {
+            const float n = (to_float(x[c]) - mean) * r, g = to_float(dy[c]) * load_any(a.weight, a.w_type, c);
+            float d = fmaf(-n, c0, LAYER ? g - c1 : g) * r;
+            if (a.has_d_sum) d += to_float(ds[c]);
+            dx[c] = from_float<XT>(d);
+        }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.width; c += blockDim.x) {
+        float t = 0.f, u = 0.f;
+        for (int k = 0; k < groups; ++k) {
+            t += sums[k * a.width + c];
+            if (LAYER) u += sums[(groups + k) * a.width + c];
+        }
+        if (a.part_w) a.part_w[(int64_t)blockIdx.x * a.width + c] = t;
+        if (LAYER && a.part_b) a.part_b[(int64_t)blockIdx.x * a.width + c] = u;
+    }
+}
+
+__device__ __forceinline__ void store_any(void* p, int type, int64_t i, float v) {
+    if (type == 0) static_cast<float*>(p)[i] = v;
+    else if (type == 1) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+    else static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+// dw (block row 0) and db (row 1): the blocks' sums of 32 columns, 32 runs of blocks side by side.
+__global__ void __launch_bounds__(1024) norm_columns_kernel(const float* part_w, const float* part_b, int blocks, int width, void* dw,
+                                                            void* db, int type, int accumulate) {
+    __shared__ double s[32][33];
+    const float* part = blockIdx.y ? part_b : part_w;
+    void* out = blockIdx.y ? db : dw;
+    const int c = blockIdx.x * 32 + threadIdx.x;
+    double t = 0.;
+    if (out && c < width) {
+#pragma unroll 8
+        for (int b = threadIdx.y; b < blocks; b += 32) t += part[(int64_t)b * width + c];
+    }
+    s[threadIdx.y][threadIdx.x] = t;
+    __syncthreads();
+    if (threadIdx.y == 0 && out && c < width) {
+        t = 0.;
+        for (int i = 0; i < 32; ++i) t += s[i][threadIdx.x];
+        if (accumulate) t += (double)load_any(out, type, c);
+        store_any(out, type, c, (float)t);
+    }
+}
+
+int64_t row_blocks(int64_t rows, const NormPlan& p) { return (rows + p.block / p.group - 1) / (p.block / p.group); }
+
+template <typename XT, typename YT>
+cudaError_t norm_typed(const NormArgs& a, bool vector, int sms, cudaStream_t st) {
+    const NormPlan p = vector ? norm_plan(a.width, 4) : loop_plan(a.width);
+    const int64_t blocks = row_blocks(a.rows, p), most = (int64_t)sms * 64;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    if (!vector) return launch_plain(norm_loop_kernel<XT, YT>, grid, dim3(p.block), 0, st, a, p.group);
+    if (p.nv == 1) return launch_plain(norm_rows_kernel<XT, YT, 1>, grid, dim3(p.block), 0, st, a, p.group);
+    if (p.nv == 2) return launch_plain(norm_rows_kernel<XT, YT, 2>, grid, dim3(p.block), 0, st, a, p.group);
+    return launch_plain(norm_rows_kernel<XT, YT, 4>, grid, dim3(p.block), 0, st, a, p.group);
+}
+
+struct GradPlan {
+    NormPlan p;
+    bool rows;              // rows in registers
+    int blocks, smem;
+};
+GradPlan grad_plan(int64_t rows, int width, bool layer, bool x_is_fp32, bool vector, int sms) {
+    GradPlan g;
+    g.rows = vector && width <= 16 * grad_row_threads(x_is_fp32);
+    g.p = g.rows ? norm_plan(width, 2) : loop_plan(width);
+    const int groups = g.p.block / g.p.group;
+    g.smem = g.rows ? (groups > 1 ? groups * width * 4 : 0) : groups * width * 4 * (layer ? 2 : 1);
+    // as many blocks as run at once: registers of 512 threads; shared memory of one, two or more
+    const int most = sms * (g.rows ? 512 / g.p.block : g.smem > 100 * 1024 ? 1 : width > 2048 ? 2 : 4);
+    const int64_t need = row_blocks(rows, g.p);
+    g.blocks = (int)(need < 1 ? 1 : need < most ? need : most);
+    return g;
+}
+template <typename XT, typename YT, bool LAYER>
+cudaError_t norm_grad_typed(const NormGradArgs& a, const GradPlan& g, cudaStream_t st) {
+    const dim3 grid(g.blocks), block(g.p.block);
+    if (!g.rows) return launch_plain(norm_grad_loop_kernel<XT, YT, LAYER>, grid, block, g.smem, st, a, g.p.group);
+    if (g.p.nv == 1) return launch_plain(norm_grad_rows_kernel<XT, YT, 1, LAYER>, grid, block, g.smem, st, a, g.p.group);
+    return launch_plain(norm_grad_rows_kernel<XT, YT, 2, LAYER>, grid, block, g.smem, st, a, g.p.group);
+}
+
+// x and y of one type, or x fp32 (a residual stream) and y of 16 bits.
+template <typename F>
+cudaError_t for_types(int x_type, int y_type, F f) {
+    if (x_type == 1) return f((__nv_bfloat16*)nullptr, (__nv_bfloat16*)nullptr);
+    if (x_type == 2) return f((__half*)nullptr, (__half*)nullptr);
+    if (y_type == 1) return f((float*)nullptr, (__nv_bfloat16*)nullptr);
+    if (y_type == 2) return f((float*)nullptr, (__half*)nullptr);
+    return f((float*)nullptr, (float*)nullptr);
+}
+
+}  // namespace
+
+// Sums of dw or db: blocks x width (grad_plan: at most four blocks on an SM up to a width of 2048, two beyond).
+size_t norm_grad_part_bytes(int max_width) {
+    const size_t narrow = 4 * (size_t)(max_width < 2048 ? max_width : 2048), wide = 2 * (size_t)max_width;
+    return (size_t)kTrainSms * (narrow > wide ? narrow : wide) * 4;
+}
+
+cudaError_t init_norm_kernels() {
+    for (int t = 0; t < 5; ++t) {
+        const cudaError_t e = for_types(t < 3 ? 0 : t - 2, t < 3 ? t : t - 2, [&](auto* x, auto* y) {
+            using XT = std::remove_pointer_t<decltype(x)>;
+            using YT = std::remove_pointer_t<decltype(y)>;
+            const cudaError_t r = init_all(0, norm_rows_kernel<XT, YT, 1>, norm_rows_kernel<XT, YT, 2>, norm_rows_kernel<XT, YT, 4>,
+                                           norm_loop_kernel<XT, YT>, norm_grad_rows_kernel<XT, YT, 1, false>,
+                                           norm_grad_rows_kernel<XT, YT, 1, true>, norm_grad_rows_kernel<XT, YT, 2, false>,
+                                           norm_grad_rows_kernel<XT, YT, 2, true>);
+            return r != cudaSuccess ? r : init_all(kLoopSmem, norm_grad_loop_kernel<XT, YT, false>, norm_grad_loop_kernel<XT, YT, true>);
+        });
+        if (e != cudaSuccess) return e;
+    }
+    return init_all(0, norm_columns_kernel);
+}
+
+cudaError_t launch_norm(const NormArgs& a, int x_type, int y_type, bool vector, int sms, cudaStream_t st) {
+    return for_types(x_type, y_type, [&](auto* x, auto* y) {
+        using XT = std::remove_pointer_t<decltype(x)>;
+        using YT = std::remove_pointer_t<decltype(y)>;
+        return norm_typed<XT, YT>(a, vector, sms, st);
+    });
+}
+cudaError_t launch_norm_grad(const NormGradArgs& a, int x_type, int y_type, bool vector, int sms, void* dw, void* db, int dw_type,
+                             int accumulate, cudaStream_t st) {
+    const GradPlan g = grad_plan(a.rows, a.width, a.layer, x_type == 0, vector, sms);
+    if (a.rows > 0) {
+        const cudaError_t e = for_types(x_type, y_type, [&](auto* x, auto* y) {
+            using XT = std::remove_pointer_t<decltype(x)>;
+            using YT = std::remove_pointer_t<decltype(y)>;
+            return a.layer ? norm_grad_typed<XT, YT, true>(a, g, st) : norm_grad_typed<XT, YT, false>(a, g, st);
+        });
+        if (e != cudaSuccess) return e;
+    }
+    if (!dw && !db) return cudaSuccess;
+    return launch_plain(norm_columns_kernel, dim3((unsigned)((a.width + 31) / 32), db ? 2u : 1u), dim3(32, 32), 0, st,
+                        (const float*)a.part_w, (const float*)a.part_b, a.rows > 0 ? g.blocks : 0, a.width, dw, db, dw_type, accumulate);
+}
+
+}  // namespace mars

@@ -1,0 +1,380 @@
+// The mixture's router in training: softmax over the experts, the k largest (the lower index on ties), their weights, and what
+// the balance and z losses need; and the gradient of the logits.
+//   p = softmax(z), lse = log sum exp z;   weights p_i, or p_i / sum of the selected p
+//   balance = E sum_e f_e P_e,  f_e = counts_e / (N k),  P_e = sum_t p_te / N;   z loss = sum_t lse_t^2 / N;   N live rows
+//   d z_j = p_j (g_j - sum_e p_e g_e) + 2 c_z lse / N p_j + (weights), g_e = c_b E f_e / N
+//   weights' part: renormalised, over the selected: w_i (dw_i - sum w dw);  else  p_j ([j selected] dw_j - sum p dw)
+// A warp has a row: its lanes hold the logits in registers, in neighbouring fours where alignment allows.  Logits are compared
+// as integers that order like them; a lane keeps the best of its own, a round takes the largest of the lanes and, among
+// equals, the lowest expert.  Sums over rows stay in fp32 registers for the rows of a warp, go through shared memory
+// in the order of the warps, and the last block to finish adds the blocks' sums in fp64: the same call gives the same bits.
+#include "train.h"
+#include "train_types.cuh"
+
+namespace mars {
+
+namespace {
+
+template <int NG> constexpr int kWarpsOf = NG == 8 ? 8 : 16;     // more registers for 32 logits of a lane
+
+// Place of element i of group j of a lane among the experts.
+template <bool V>
+__device__ __forceinline__ int expert_of(int j, int i, int lane) { return V ? (j * 32 + lane) * 4 + i : (j * 4 + i) * 32 + lane; }
+
+template <typename T, bool V>
+__device__ __forceinline__ void load4(const T* row, int j, int lane, int experts, float (&o)[4], float fill) {
+    if (V) {
+        const int c = (j * 32 + lane) * 4;
+        if (c >= experts) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fill;
+        } else if (sizeof(T) == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(row + c);
+            o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(row + c);
+            if constexpr (sizeof(T) == 2) {
+                unpack2(v.x, o[0], o[1], T());
+                unpack2(v.y, o[2], o[3], T());
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = expert_of<false>(j, i, lane);
+            o[i] = c < experts ? to_float(row[c]) : fill;
+        }
+    }
+}
+template <typename T, bool V>
+__device__ __forceinline__ void store4(T* row, int j, int lane, int experts, const float (&v)[4]) {
+    if (V) {
+        const int c = (j * 32 + lane) * 4;
+        if (c >= experts) return;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint2*>(row + c) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = expert_of<false>(j, i, lane);
+            if (c < experts) row[c] = from_float<T>(v[i]);
+        }
+    }
+}
+
+// Unsigned integers that order like the floats; -0 counts as 0, a NaN as the largest.  0 is below the key of -inf.
+__device__ __forceinline__ uint32_t order_key(float v) {
+    if (v != v) return 0xffffffffu;
+    const uint32_t b = __float_as_uint(v + 0.f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
+constexpr uint32_t kKeyNegInf = 0x007fffffu;
+
+template <typename T, int NG, bool V>
+__global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_kernel(const RouterArgs a) {
+    constexpr int kWarps = kWarpsOf<NG>, kThreads = kWarps * 32;
+    __shared__ float sums[kRouterMaxExperts];
+    __shared__ int counts[kRouterMaxExperts];
+    __shared__ double reduce[kWarps];
+    __shared__ int last;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts, k = a.top_k;
+    for (int e = threadIdx.x; e < E; e += kThreads) { sums[e] = 0.f; counts[e] = 0; }
+    __syncthreads();
+    float acc[NG][4];
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+    double z = 0.;
+    for (int64_t row = (int64_t)blockIdx.x * kWarps + warp; row < a.rows; row += (int64_t)gridDim.x * kWarps) {
+        bool on = !a.has_live || a.live[row];
+        float v[NG][4];
+        uint32_t key[NG][4], best = 0;
+        int at = 0;
+        if (on) {
+#pragma unroll
+            for (int j = 0; j < NG; ++j) load4<T, V>(static_cast<const T*>(a.logits) + row * a.ld, j, lane, E, v[j], 0.f);
+#pragma unroll
+            for (int j = 0; j < NG; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    key[j][i] = expert_of<V>(j, i, lane) < E ? order_key(v[j][i]) : 0u;
+                    if (key[j][i] > best) { best = key[j][i]; at = expert_of<V>(j, i, lane); }
+                }
+        }
+        const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+        on = on && top > kKeyNegInf;                          // a row without a logit above -inf takes no part
+        if (!on) {
+            if (lane < k) { a.idx[row * k + lane] = -1; a.weights[row * k + lane] = 0.f; }
+            if (a.lse && lane == 0) a.lse[row] = 0.f;
+            continue;
+        }
+        const float m = key_value(top);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < NG; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[j][i] = expert_of<V>(j, i, lane) < E ? expf(v[j][i] - m) : 0.f;
+                sum += v[j][i];
+            }
+        sum = warp_sum(sum);
+        const float inv = 1.f / sum;
+#pragma unroll
+        for (int j = 0; j < NG; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(v[j][i], inv, acc[j][i]);
+        uint32_t mine = 0;                                    // lane i: key and expert of place i
+        int chosen = 0;
+        for (int i = 0; i < k; ++i) {
+            const uint32_t most = i == 0 ? top : __reduce_max_sync(0xffffffffu, best);
+            const int e = (int)__reduce_min_sync(0xffffffffu, best == most ? (uint32_t)at : 0xffffffffu);
+            if (lane == i) { mine = most; chosen = e; }
+            if (best == most && at == e) {
+                best = 0;
+#pragma unroll
+                for (int j = 0; j < NG; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (expert_of<V>(j, q, lane) == e) key[j][q] = 0;
+                        if (key[j][q] > best) { best = key[j][q]; at = expert_of<V>(j, q, lane); }
+                    }
+            }
+        }
+        const float w = lane < k ? expf(key_value(mine) - m) : 0.f;
+        const float total = a.renormalise ? warp_sum(w) : sum;
+        if (lane < k) {
+            a.idx[row * k + lane] = chosen;
+            a.weights[row * k + lane] = w / total;
+            atomicAdd(&counts[chosen], 1);
+        }
+        const float lse = m + logf(sum);
+        if (lane == 0) {
+            if (a.lse) a.lse[row] = lse;
+            z += (double)lse * (double)lse;
+        }
+    }
+    for (int w = 0; w < kWarps; ++w) {
+        if (w == warp)
+#pragma unroll
+            for (int j = 0; j < NG; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (expert_of<V>(j, i, lane) < E) sums[expert_of<V>(j, i, lane)] += acc[j][i];
+        __syncthreads();
+    }
+    if (lane == 0) reduce[warp] = z;
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += kThreads) {
+        a.parts[(int64_t)blockIdx.x * E + e] = sums[e];
+        if (counts[e]) atomicAdd(&a.work_counts[e], counts[e]);
+    }
+    if (threadIdx.x == 0) {
+        z = 0.;
+        for (int w = 0; w < kWarps; ++w) z += reduce[w];
+        a.z_parts[blockIdx.x] = z;
+    }
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    // counts, offsets, sums and losses
+    __shared__ double total_z;
+    __shared__ int64_t total_count;
+    for (int e = threadIdx.x; e < E; e += kThreads) counts[e] = __ldcg(a.work_counts + e);
+    z = 0.;
+    for (int b = threadIdx.x; b < (int)gridDim.x; b += kThreads) z += __ldcg(a.z_parts + b);
+    z = warp_sum_double(z);
+    __syncthreads();
+    if (lane == 0) reduce[warp] = z;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        z = 0.;
+        for (int w = 0; w < kWarps; ++w) z += reduce[w];
+        total_z = z;
+        int run = 0;
+        for (int e = 0; e < E; ++e) {
+            if (a.offsets) a.offsets[e] = run;
+            run += counts[e];
+        }
+        if (a.offsets) a.offsets[E] = run;
+        total_count = run;
+        *a.ticket = 0;
+    }
+    __syncthreads();
+    double balance = 0.;
+    for (int e = threadIdx.x; e < E; e += kThreads) {
+        double s = 0.;
+#pragma unroll 16
+        for (int b = 0; b < (int)gridDim.x; ++b) s += __ldcg(a.parts + (int64_t)b * E + e);
+        if (a.prob_sums) a.prob_sums[e] = (float)s;
+        if (a.counts) a.counts[e] = counts[e];
+        a.work_counts[e] = 0;
+        balance += s * counts[e];
+    }
+    balance = warp_sum_double(balance);
+    __syncthreads();
+    if (lane == 0) reduce[warp] = balance;
+    __syncthreads();
+    if (threadIdx.x == 0 && a.losses) {
+        balance = 0.;
+        for (int w = 0; w < kWarps; ++w) balance += reduce[w];
+        const double n = (double)total_count / k;
+        a.losses[0] = n > 0. ? (float)(E * balance / (n * n * k)) : 0.f;
+        a.losses[1] = n > 0. ? (float)(total_z / n) : 0.f;
+    }
+}
+
+template <typename T, int NG, bool V>
+__global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_grad_kernel(const RouterGradArgs a) {
+    constexpr int kWarps = kWarpsOf<NG>, kThreads = kWarps * 32;
+    extern __shared__ float smem[];                           // [warps][experts]: the weights' part of a row
+    __shared__ double reduce[kWarps];
+    __shared__ double total;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts, k = a.top_k;
+    float* mine = smem + warp * E;
+    double c = 0.;
+    for (int e = threadIdx.x; e < E; e += kThreads) c += a.counts[e];
+    c = warp_sum_double(c);
+    if (lane == 0) reduce[warp] = c;
+    for (int e = lane; e < E; e += 32) mine[e] = 0.f;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        c = 0.;
+        for (int w = 0; w < kWarps; ++w) c += reduce[w];
+        total = c;
+    }
+    __syncthreads();
+    const double n = total > 0. ? total / k : 1.;             // live rows
+    float g[NG][4];
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = expert_of<V>(j, i, lane);
+            g[j][i] = e < E && total > 0. ? (float)((double)a.balance * E / n * a.counts[e] / total) : 0.f;
+        }
+    const float zc = (float)(2. * (double)a.z / n);
+    for (int64_t row = (int64_t)blockIdx.x * kWarps + warp; row < a.rows; row += (int64_t)gridDim.x * kWarps) {
+        T* out = static_cast<T*>(a.d_logits) + row * a.ld_d;
+        const T* in = static_cast<const T*>(a.logits) + row * a.ld;
+        const int32_t first = a.idx[row * k];
+        float v[NG][4];
+        if (first < 0) {                                      // took no part: its logits may be anything
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+                store4<T, V>(out, j, lane, E, zero);
+            }
+            continue;
+        }
+        const float lse = a.lse[row];
+#pragma unroll
+        for (int j = 0; j < NG; ++j) load4<T, V>(in, j, lane, E, v[j], -INFINITY);
+        const int e = lane < k ? a.idx[row * k + lane] : -1;
+        const bool sel = (unsigned)e < (unsigned)E;
+        float dot = 0.f;                                      // sum of p g, plus that of the selected where weights are p
+#pragma unroll
+        for (int j = 0; j < NG; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[j][i] = expert_of<V>(j, i, lane) < E ? expf(v[j][i] - lse) : 0.f;
+                dot = fmaf(v[j][i], g[j][i], dot);
+            }
+        if (a.has_d_weights) {
+            float w = sel ? expf(to_float(in[e]) - lse) : 0.f;
+            const float dw = lane < k ? a.d_weights[row * k + lane] : 0.f;
+            float push;
+            if (a.renormalise) {
+                w /= warp_sum(w);
+                push = w * (dw - warp_sum(sel ? w * dw : 0.f));
+            } else {
+                push = w * dw;
+                if (sel) dot += push;
+            }
+            if (sel) atomicAdd(mine + e, push);
+            __syncwarp();
+        }
+        dot = warp_sum(dot);
+        const float shift = zc * lse - dot;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+            float d[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int q = expert_of<V>(j, i, lane);
+                d[i] = v[j][i] * (g[j][i] + shift);
+                if (a.has_d_weights && q < E) {
+                    d[i] += mine[q];
+                    mine[q] = 0.f;
+                }
+            }
+            store4<T, V>(out, j, lane, E, d);
+        }
+        __syncwarp();
+    }
+}
+
+int router_blocks(int rows, int warps, int sms) {
+    const int most = router_max_blocks(sms), need = (int)(((int64_t)rows + warps - 1) / warps);
+    return need < 1 ? 1 : need < most ? need : most;
+}
+
+template <typename T, int NG, bool V>
+cudaError_t router_launch(const RouterArgs& a, int sms, cudaStream_t st) {
+    constexpr int W = kWarpsOf<NG>;
+    return launch_plain(router_kernel<T, NG, V>, dim3(router_blocks(a.rows, W, sms)), dim3(W * 32), 0, st, a);
+}
+template <typename T, bool V>
+cudaError_t router_typed(const RouterArgs& a, int sms, cudaStream_t st) {
+    if (a.experts <= 128) return router_launch<T, 1, V>(a, sms, st);
+    if (a.experts <= 256) return router_launch<T, 2, V>(a, sms, st);
+    if (a.experts <= 512) return router_launch<T, 4, V>(a, sms, st);
+    return router_launch<T, 8, V>(a, sms, st);
+}
+template <typename T, int NG, bool V>
+cudaError_t router_grad_launch(const RouterGradArgs& a, int sms, cudaStream_t st) {
+    constexpr int W = kWarpsOf<NG>;
+    return launch_plain(router_grad_kernel<T, NG, V>, dim3(router_blocks(a.rows, W, sms)), dim3(W * 32), (size_t)W * a.experts * 4, st, a);
+}
+template <typename T, bool V>
+cudaError_t router_grad_typed(const RouterGradArgs& a, int sms, cudaStream_t st) {
+    if (a.experts <= 128) return router_grad_launch<T, 1, V>(a, sms, st);
+    if (a.experts <= 256) return router_grad_launch<T, 2, V>(a, sms, st);
+    if (a.experts <= 512) return router_grad_launch<T, 4, V>(a, sms, st);
+    return router_grad_launch<T, 8, V>(a, sms, st);
+}
+
+template <typename T, bool V>
+cudaError_t router_init() {
+    return init_all(0, router_kernel<T, 1, V>, router_kernel<T, 2, V>, router_kernel<T, 4, V>, router_kernel<T, 8, V>, router_grad_kernel<T, 1, V>,
+                    router_grad_kernel<T, 2, V>, router_grad_kernel<T, 4, V>, router_grad_kernel<T, 8, V>);
+}
+
+}  // namespace
+
+cudaError_t init_router_kernels() {
+    const cudaError_t all[6] = {router_init<float, false>(), router_init<float, true>(), router_init<__nv_bfloat16, false>(),
+                                router_init<__nv_bfloat16, true>(), router_init<__half, false>(), router_init<__half, true>()};
+    for (cudaError_t e : all)
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
+
+int router_max_blocks(int sms) { return (sms < kTrainSms ? sms : kTrainSms) * 2; }
+
+cudaError_t launch_router(const RouterArgs& a, int type, bool vector, int sms, cudaStream_t st) {
+    if (type == 0) return vector ? router_typed<float, true>(a, sms, st) : router_typed<float, false>(a, sms, st);
+    if (type == 1) return vector ? router_typed<__nv_bfloat16, true>(a, sms, st) : router_typed<__nv_bfloat16, false>(a, sms, st);
+    return vector ? router_typed<__half, true>(a, sms, st) : router_typed<__half, false>(a, sms, st);
+}
+cudaError_t launch_router_grad(const RouterGradArgs& a, int type, bool vector, int sms, cudaStream_t st) {
+    if (type == 0) return vector ? router_grad_typed<float, true>(a, sms, st) : router_grad_typed<float, false>(a, sms, st);
+    if (type == 1) return vector ? router_grad_typed<__nv_bfloat16, true>(a, sms, st) : router_grad_typed<__nv_bfloat16, false>(a, sms, st);
+    return vector ? router_grad_typed<__half, true>(a, sms, st) : router_grad_typed<__half, false>(a, sms, st);
+}
+
+}  // namespace mars

@@ -37,41 +37,6 @@ Layout make_update_layout(int H, int V, int n, int sms) {
     return l;
 }
 
-struct DeviceGuard {           // calls run on the handle's device, whatever is current
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        int cur = -1;
-        ok = cudaGetDevice(&cur) == cudaSuccess;
-        if (ok && cur != dev) {
-            ok = cudaSetDevice(dev) == cudaSuccess;
-            if (ok) prev = cur;
-        }
-    }
-    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
-};
-
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return na && nb && x < y + nb && y < x + na;
-}
-size_t span(int64_t rows, int64_t ld, int64_t cols, size_t elem) {
-    return rows > 0 ? (size_t)((rows - 1) * ld + cols) * elem : 0;
-}
-// Two [rows][..] matrices with row strides (elements).  Column ranges of one buffer lie inside each other's span without
-// sharing a byte: with equal strides, b's columns must then fall between the end of a's and the end of the row.
-bool rows_overlap(const void* a, int64_t ld_a, int64_t cols_a, size_t elem_a, const void* b, int64_t ld_b, int64_t cols_b, size_t elem_b,
-                  int64_t rows) {
-    if (!overlap(a, span(rows, ld_a, cols_a, elem_a), b, span(rows, ld_b, cols_b, elem_b))) return false;
-    const size_t pitch = (size_t)ld_a * elem_a;
-    if (rows < 2 || pitch != (size_t)ld_b * elem_b) return true;
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    const size_t at = y >= x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;       // of b's columns in a's rows
-    return at < (size_t)cols_a * elem_a || at + (size_t)cols_b * elem_b > pitch;
-}
-bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
-bool aligned4(const void* p) { return (uintptr_t)p % 4 == 0; }
-
 // K-major operand: `rows` rows of `inner` contraction indexes; boxes of 64 x box_rows.
 mars_status_t map_k(CUtensorMap* tm, const void* p, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_rows = 128) {
     const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
@@ -97,25 +62,6 @@ mars_status_t map_stack(CUtensorMap* tm, const void* p, uint64_t inner, uint64_t
     const cuuint64_t dims[3] = {inner, rows, experts}, strides[2] = {inner * 2, inner * rows * 2};
     const cuuint32_t box[3] = {64u, box_rows, 1u};
     return make_tiled_map(tm, p, 3, dims, strides, box);
-}
-
-mars_status_t launched(cudaError_t e) {
-    if (e == cudaSuccess) return MARS_OK;
-    g_last_cuda_error = (int32_t)e;
-    return MARS_ERR_CUDA;
-}
-#define RUN(expr)                                              \
-    do {                                                       \
-        const mars_status_t _s = (expr);                       \
-        if (_s != MARS_OK) return _s;                          \
-    } while (0)
-
-mars_status_t device_info(int* dev, int* sms) {
-    int major = 0;
-    CUDA_TRY(cudaGetDevice(dev));
-    CUDA_TRY(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *dev));
-    CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev));
-    return major == 10 ? MARS_OK : MARS_ERR_UNSUPPORTED;
 }
 
 // The sizes of a handle's workspace do not depend on the device: laid out for the splits of d_hidden that 148 SMs and
