@@ -46,17 +46,40 @@ __device__ __forceinline__ void load4(const T* row, int j, int lane, int experts
         }
     }
 }
-template <typename T, bool V>
-__device__ __forceinline__ void store4(T* row, int j, int lane, int experts, const float (&v)[4]) {
-    if (V) {
-        const int c = (j * 32 + lane) * 4;
+// The same for groups of L lanes.
+template <typename T, int L, bool V>
+__device__ __forceinline__ void group_load4(const T* row, int j, int l, int experts, float (&o)[4]) {
+    if constexpr (V) {
+        const int c = (j * L + l) * 4;
+        if (c >= experts) {
+            o[0] = o[1] = o[2] = o[3] = 0.f;
+        } else if constexpr (sizeof(T) == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(row + c);
+            o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(row + c);
+            unpack2(v.x, o[0], o[1], T());
+            unpack2(v.y, o[2], o[3], T());
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = (j * 4 + i) * L + l;
+            o[i] = c < experts ? to_float(row[c]) : 0.f;
+        }
+    }
+}
+template <typename T, int L, bool V>
+__device__ __forceinline__ void group_store4(T* row, int j, int l, int experts, const float (&v)[4]) {
+    if constexpr (V) {
+        const int c = (j * L + l) * 4;
         if (c >= experts) return;
         if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
         else *reinterpret_cast<uint2*>(row + c) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int c = expert_of<false>(j, i, lane);
+            const int c = (j * 4 + i) * L + l;
             if (c < experts) row[c] = from_float<T>(v[i]);
         }
     }
@@ -70,6 +93,7 @@ __device__ __forceinline__ uint32_t order_key(float v) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
 constexpr uint32_t kKeyNegInf = 0x007fffffu;
+constexpr float kLog2e = 1.44269504f;
 
 template <typename T, int NG, bool V>
 __global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_kernel(const RouterArgs a) {
@@ -228,91 +252,115 @@ __global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_ker
     }
 }
 
-template <typename T, int NG, bool V>
-__global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_grad_kernel(const RouterGradArgs a) {
-    constexpr int kWarps = kWarpsOf<NG>, kThreads = kWarps * 32;
-    extern __shared__ float smem[];                           // [warps][experts]: the weights' part of a row
+// Gradient: L lanes have a row (so that a warp reduces several rows in one go), NG fours of experts each.
+template <typename T, int L, int NG, bool V>
+__global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const RouterGradArgs a) {
+    constexpr int kWarps = 8, kThreads = 256, R = 32 / L;     // rows of a warp
+    extern __shared__ float smem[];                           // [rows of the block][pitch]: the weights' part of a row
     __shared__ double reduce[kWarps];
-    __shared__ double total;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts, k = a.top_k;
-    float* mine = smem + warp * E;
-    double c = 0.;
-    for (int e = threadIdx.x; e < E; e += kThreads) c += a.counts[e];
-    c = warp_sum_double(c);
-    if (lane == 0) reduce[warp] = c;
-    for (int e = lane; e < E; e += 32) mine[e] = 0.f;
+    const int sub = lane / L, l = lane % L, pitch = (E + 3) / 4 * 4 + 4;
+    float* mine = smem + (warp * R + sub) * pitch;
+    double total = 0.;
+    for (int e = threadIdx.x; e < E; e += kThreads) total += a.counts[e];
+    total = warp_sum_double(total);
+    if (lane == 0) reduce[warp] = total;
+    for (int i = threadIdx.x; i < kWarps * R * pitch; i += kThreads) smem[i] = 0.f;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        c = 0.;
-        for (int w = 0; w < kWarps; ++w) c += reduce[w];
-        total = c;
-    }
-    __syncthreads();
+    total = 0.;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) total += reduce[w];
     const double n = total > 0. ? total / k : 1.;             // live rows
+    const float unit = total > 0. ? (float)((double)a.balance * E / n / total) : 0.f, zc = (float)(2. * (double)a.z / n);
+    auto expert = [&](int j, int i) { return V ? (j * L + l) * 4 + i : (j * 4 + i) * L + l; };
     float g[NG][4];
 #pragma unroll
     for (int j = 0; j < NG; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = expert_of<V>(j, i, lane);
-            g[j][i] = e < E && total > 0. ? (float)((double)a.balance * E / n * a.counts[e] / total) : 0.f;
-        }
-    const float zc = (float)(2. * (double)a.z / n);
-    for (int64_t row = (int64_t)blockIdx.x * kWarps + warp; row < a.rows; row += (int64_t)gridDim.x * kWarps) {
-        T* out = static_cast<T*>(a.d_logits) + row * a.ld_d;
+        for (int i = 0; i < 4; ++i) g[j][i] = expert(j, i) < E ? unit * a.counts[expert(j, i)] : 0.f;
+    const int64_t stride = (int64_t)gridDim.x * kWarps * R;
+    // the next row's logits, lse and choices (the first L of them) are on their way while this row is worked on
+    float next[NG][4], next_lse = 0.f, next_dw = 0.f;
+    int next_idx = -1, next_first = -1;
+    auto fetch = [&](int64_t row) {
+        const bool in_range = row < a.rows;
+        const int64_t r = in_range ? row : 0;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) group_load4<T, L, V>(static_cast<const T*>(a.logits) + r * a.ld, j, l, in_range ? E : 0, next[j]);
+        next_lse = in_range ? a.lse[r] : 0.f;
+        next_first = in_range ? a.idx[r * k] : -1;
+        next_idx = in_range && l < k ? a.idx[r * k + l] : -1;
+        next_dw = in_range && l < k && a.has_d_weights ? a.d_weights[r * k + l] : 0.f;
+    };
+    int64_t base = ((int64_t)blockIdx.x * kWarps + warp) * R;
+    if (base < a.rows) fetch(base + sub);
+    for (; base < a.rows; base += stride) {
+        const bool in_range = base + sub < a.rows, on = next_first >= 0;      // a row that took no part may hold anything
+        const int64_t row = in_range ? base + sub : 0;
         const T* in = static_cast<const T*>(a.logits) + row * a.ld;
-        const int32_t first = a.idx[row * k];
+        T* out = static_cast<T*>(a.d_logits) + row * a.ld_d;
+        const int W = on ? E : 0, first_idx = next_idx;
+        const float lse = next_lse, first_dw = next_dw;
         float v[NG][4];
-        if (first < 0) {                                      // took no part: its logits may be anything
-#pragma unroll
-            for (int j = 0; j < NG; ++j) {
-                const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-                store4<T, V>(out, j, lane, E, zero);
-            }
-            continue;
-        }
-        const float lse = a.lse[row];
-#pragma unroll
-        for (int j = 0; j < NG; ++j) load4<T, V>(in, j, lane, E, v[j], -INFINITY);
-        const int e = lane < k ? a.idx[row * k + lane] : -1;
-        const bool sel = (unsigned)e < (unsigned)E;
         float dot = 0.f;                                      // sum of p g, plus that of the selected where weights are p
 #pragma unroll
         for (int j = 0; j < NG; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                v[j][i] = expert_of<V>(j, i, lane) < E ? expf(v[j][i] - lse) : 0.f;
+                v[j][i] = expert(j, i) < W ? ex2((next[j][i] - lse) * kLog2e) : 0.f;
                 dot = fmaf(v[j][i], g[j][i], dot);
             }
+        float w_first = 0.f;                                  // p of this lane's first choice
+        if (a.has_d_weights && on && (unsigned)first_idx < (unsigned)E) w_first = ex2((to_float(in[first_idx]) - lse) * kLog2e);
+        fetch(base + stride + sub);
         if (a.has_d_weights) {
-            float w = sel ? expf(to_float(in[e]) - lse) : 0.f;
-            const float dw = lane < k ? a.d_weights[row * k + lane] : 0.f;
-            float push;
-            if (a.renormalise) {
-                w /= warp_sum(w);
-                push = w * (dw - warp_sum(sel ? w * dw : 0.f));
-            } else {
-                push = w * dw;
-                if (sel) dot += push;
+            float w_sum = w_first, wdw = w_first != 0.f ? w_first * first_dw : 0.f;
+            for (int i = l + L; i < k; i += L) {
+                const int e = on ? a.idx[row * k + i] : -1;
+                if ((unsigned)e < (unsigned)E) {
+                    const float w = ex2((to_float(in[e]) - lse) * kLog2e);
+                    w_sum += w;
+                    wdw = fmaf(w, a.d_weights[row * k + i], wdw);
+                }
             }
-            if (sel) atomicAdd(mine + e, push);
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1) {
+                w_sum += __shfl_xor_sync(0xffffffffu, w_sum, o);
+                wdw += __shfl_xor_sync(0xffffffffu, wdw, o);
+            }
+            const float inv = a.renormalise ? 1.f / w_sum : 1.f, mean = a.renormalise ? wdw * inv : 0.f;
+            if (on && (unsigned)first_idx < (unsigned)E) atomicAdd(mine + first_idx, w_first * inv * (first_dw - mean));
+            for (int i = l + L; i < k; i += L) {
+                const int e = on ? a.idx[row * k + i] : -1;
+                if ((unsigned)e < (unsigned)E)
+                    atomicAdd(mine + e, ex2((to_float(in[e]) - lse) * kLog2e) * inv * (a.d_weights[row * k + i] - mean));
+            }
+            if (!a.renormalise) dot += wdw / L;
             __syncwarp();
         }
-        dot = warp_sum(dot);
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
         const float shift = zc * lse - dot;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            float d[4];
+            float d[4], m[4] = {0.f, 0.f, 0.f, 0.f};
+            if (a.has_d_weights) {
+                if (V) {
+                    if (expert(j, 0) < E) {
+                        const float4 q = *reinterpret_cast<const float4*>(mine + expert(j, 0));
+                        m[0] = q.x; m[1] = q.y; m[2] = q.z; m[3] = q.w;
+                        *reinterpret_cast<float4*>(mine + expert(j, 0)) = make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int q = expert_of<V>(j, i, lane);
-                d[i] = v[j][i] * (g[j][i] + shift);
-                if (a.has_d_weights && q < E) {
-                    d[i] += mine[q];
-                    mine[q] = 0.f;
+                    for (int i = 0; i < 4; ++i)
+                        if (expert(j, i) < E) { m[i] = mine[expert(j, i)]; mine[expert(j, i)] = 0.f; }
                 }
             }
-            store4<T, V>(out, j, lane, E, d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = fmaf(v[j][i], g[j][i] + shift, m[i]);
+            if (!on) d[0] = d[1] = d[2] = d[3] = 0.f;
+            if (in_range) group_store4<T, L, V>(out, j, l, E, d);
         }
         __syncwarp();
     }
@@ -335,23 +383,28 @@ cudaError_t router_typed(const RouterArgs& a, int sms, cudaStream_t st) {
     if (a.experts <= 512) return router_launch<T, 4, V>(a, sms, st);
     return router_launch<T, 8, V>(a, sms, st);
 }
-template <typename T, int NG, bool V>
+template <typename T, int L, int NG, bool V>
 cudaError_t router_grad_launch(const RouterGradArgs& a, int sms, cudaStream_t st) {
-    constexpr int W = kWarpsOf<NG>;
-    return launch_plain(router_grad_kernel<T, NG, V>, dim3(router_blocks(a.rows, W, sms)), dim3(W * 32), (size_t)W * a.experts * 4, st, a);
+    constexpr int R = 32 / L;
+    const int64_t need = ((int64_t)a.rows + 8 * R - 1) / (8 * R), most = (int64_t)sms * (NG <= 4 ? 2 : 1);
+    const size_t smem = (size_t)8 * R * ((a.experts + 3) / 4 * 4 + 4) * 4;
+    return launch_plain(router_grad_kernel<T, L, NG, V>, dim3((unsigned)(need < most ? need : most)), dim3(256), smem, st, a);
 }
+// Sixteen experts for a lane where a row has as many; a row for a whole warp beyond 256.
 template <typename T, bool V>
 cudaError_t router_grad_typed(const RouterGradArgs& a, int sms, cudaStream_t st) {
-    if (a.experts <= 128) return router_grad_launch<T, 1, V>(a, sms, st);
-    if (a.experts <= 256) return router_grad_launch<T, 2, V>(a, sms, st);
-    if (a.experts <= 512) return router_grad_launch<T, 4, V>(a, sms, st);
-    return router_grad_launch<T, 8, V>(a, sms, st);
+    if (a.experts <= 32) return router_grad_launch<T, 4, 2, V>(a, sms, st);
+    if (a.experts <= 128) return router_grad_launch<T, 8, 4, V>(a, sms, st);
+    if (a.experts <= 256) return router_grad_launch<T, 16, 4, V>(a, sms, st);
+    if (a.experts <= 512) return router_grad_launch<T, 32, 4, V>(a, sms, st);
+    return router_grad_launch<T, 32, 8, V>(a, sms, st);
 }
 
 template <typename T, bool V>
 cudaError_t router_init() {
-    return init_all(0, router_kernel<T, 1, V>, router_kernel<T, 2, V>, router_kernel<T, 4, V>, router_kernel<T, 8, V>, router_grad_kernel<T, 1, V>,
-                    router_grad_kernel<T, 2, V>, router_grad_kernel<T, 4, V>, router_grad_kernel<T, 8, V>);
+    return init_all(0, router_kernel<T, 1, V>, router_kernel<T, 2, V>, router_kernel<T, 4, V>, router_kernel<T, 8, V>, router_grad_kernel<T, 4, 2, V>,
+                    router_grad_kernel<T, 8, 4, V>, router_grad_kernel<T, 16, 4, V>, router_grad_kernel<T, 32, 4, V>,
+                    router_grad_kernel<T, 32, 8, V>);
 }
 
 }  // namespace

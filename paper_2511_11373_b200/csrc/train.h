@@ -112,7 +112,7 @@ int router_max_blocks(int sms);
 // ------------------------------------------------------------------------------------------- policy loss
 struct PolicyArgs {
     int tokens, seqs, reduce, per_token;     // reduce: MARS_MEAN_TOKENS, MARS_MEAN_SEQUENCES, MARS_SUM
-    int has_ref;
+    int has_ref, vector;                     // vector: every array of a value for each token starts on a 16-byte boundary
     const float *lp, *old_lp, *ref, *adv;
     const int32_t *targets, *seq_off;
     double log_low, log_high;                // borders of log r
@@ -120,9 +120,9 @@ struct PolicyArgs {
     double scale;
     float *stats, *d_lp;                     // d_lp: may be null
     int32_t* seq_live;                       // [seqs] live tokens, zero between calls
-    int32_t* totals;                         // [0] live tokens, [1] sequences with one
+    int32_t* totals;                         // [0] live tokens, [1] sequences with one, zero between calls
     double* parts;                           // [blocks][4]
-    int32_t* ticket;                         // [2], zero between calls
+    int32_t* ticket;                         // zero between calls
 };
 cudaError_t launch_policy_loss(const PolicyArgs& a, int sms, cudaStream_t st);
 int policy_max_blocks(int sms);

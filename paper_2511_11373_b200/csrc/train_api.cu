@@ -34,7 +34,8 @@ size_t router_scratch(int e) {
     const size_t blocks = (size_t)router_max_blocks(kTrainSms);
     return e ? align_up(blocks * e * 4, 256) + blocks * 8 : 0;
 }
-size_t policy_scratch(int s) { return s ? (size_t)policy_max_blocks(kTrainSms) * 4 * 8 : 0; }
+size_t policy_parts() { return align_up((size_t)policy_max_blocks(kTrainSms) * 4 * 8, 256); }
+size_t policy_scratch(int s) { return s ? policy_parts() : 0; }
 
 size_t carve_train(int w, int e, int s, unsigned char* base, mars_train* t) {
     size_t at = 0;
@@ -381,7 +382,10 @@ mars_status_t mars_policy_loss(mars_train_t* t, void* cuda_stream, const mars_po
     a.has_ref = ref_logprobs != nullptr; a.ref = ref_logprobs ? ref_logprobs : logprobs; a.adv = advantages; a.targets = targets; a.seq_off = seq_off;
     a.log_low = f->clip_low < 1. ? std::log1p(-f->clip_low) : -HUGE_VAL; a.log_high = std::log1p(f->clip_high);
     a.low = (float)(1. - f->clip_low); a.high = (float)(1. + f->clip_high); a.kl = (float)f->kl_coef; a.scale = f->scale;
-    a.stats = stats; a.d_lp = d_logprobs; a.seq_live = t->seq_live; a.totals = t->totals; a.parts = (double*)t->scratch; a.ticket = t->tickets + 1;
+    a.stats = stats; a.d_lp = d_logprobs; a.seq_live = t->seq_live; a.totals = t->totals; a.parts = (double*)t->scratch;
+    a.ticket = t->tickets + 1;
+    a.vector = aligned16(targets) && aligned16(logprobs) && aligned16(old_logprobs) && aligned16(ref_logprobs) && aligned16(d_logprobs) &&
+               (!per_token || aligned16(advantages));
     return launched(launch_policy_loss(a, t->sms, (cudaStream_t)cuda_stream));
 }
 

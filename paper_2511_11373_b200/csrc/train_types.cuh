@@ -74,6 +74,12 @@ __device__ __forceinline__ float load_any(const void* p, int type, int64_t i) {
     return __half2float(static_cast<const __half*>(p)[i]);
 }
 
+// 2^x, results below the normal numbers are 0.
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ double warp_sum_double(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
