@@ -95,13 +95,108 @@ __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(
 constexpr uint32_t kKeyNegInf = 0x007fffffu;
 constexpr float kLog2e = 1.44269504f;
 
+// The end of a block: its sums and counts for all, and by the last block the call's totals.  sums, counts: [experts] in shared memory,
+// complete; z: the sum of lse^2 of lane 0 of each warp.
+template <int WARPS>
+__device__ __forceinline__ void router_finish(const RouterArgs& a, float* sums, int* counts, double z) {
+    __shared__ double reduce[WARPS], part[WARPS * 32];
+    __shared__ int last, total_count, scan[WARPS];
+    constexpr int THREADS = WARPS * 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts;
+    if (lane == 0) reduce[warp] = z;
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += THREADS) {
+        a.parts[(int64_t)blockIdx.x * E + e] = sums[e];
+        if (counts[e]) atomicAdd(&a.work_counts[e], counts[e]);
+    }
+    if (threadIdx.x == 0) {
+        z = 0.;
+        for (int w = 0; w < WARPS; ++w) z += reduce[w];
+        a.z_parts[blockIdx.x] = z;
+    }
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    const int blocks = gridDim.x;
+    z = 0.;
+    for (int b = threadIdx.x; b < blocks; b += THREADS) z += __ldcg(a.z_parts + b);
+    z = warp_sum_double(z);
+    // counts and their exclusive sums: every thread has a run of neighbouring experts
+    const int each = (E + THREADS - 1) / THREADS;
+    int run = 0;
+    for (int i = 0; i < each; ++i) {
+        const int e = threadIdx.x * each + i;
+        if (e < E) run += counts[e] = __ldcg(a.work_counts + e);
+    }
+    int before = run;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += v;
+    }
+    __syncthreads();
+    if (lane == 0) reduce[warp] = z;
+    if (lane == 31) scan[warp] = before;
+    __syncthreads();
+    int base = 0;
+    for (int w = 0; w < warp; ++w) base += scan[w];
+    int at = base + before - run;
+    for (int i = 0; i < each; ++i) {
+        const int e = threadIdx.x * each + i;
+        if (e >= E) break;
+        if (a.offsets) a.offsets[e] = at;
+        at += counts[e];
+        if (a.counts) a.counts[e] = counts[e];
+        a.work_counts[e] = 0;
+    }
+    if (threadIdx.x == THREADS - 1) {
+        total_count = base + before;
+        if (a.offsets) a.offsets[E] = total_count;
+        *a.ticket = 0;
+    }
+    __syncthreads();
+    // blocks' sums: as many threads for a column as there are for all columns at once, each with a run of blocks
+    double balance = 0.;
+    const int slices = max(1, THREADS / E), here = min(E, THREADS);
+    for (int c0 = 0; c0 < E; c0 += THREADS) {
+        const int s = threadIdx.x / here, c = c0 + threadIdx.x - s * here;
+        double v = 0.;
+        if (s < slices && c < E) {
+#pragma unroll 16
+            for (int b = blocks * s / slices; b < blocks * (s + 1) / slices; ++b) v += __ldcg(a.parts + (int64_t)b * E + c);
+        }
+        part[threadIdx.x] = v;
+        __syncthreads();
+        if (s == 0 && c < E) {
+            for (int i = 1; i < slices; ++i) v += part[i * here + threadIdx.x];
+            if (a.prob_sums) a.prob_sums[c] = (float)v;
+            balance += v * counts[c];
+        }
+        __syncthreads();
+    }
+    z = 0.;
+    for (int w = 0; w < WARPS; ++w) z += reduce[w];
+    balance = warp_sum_double(balance);
+    __syncthreads();
+    if (lane == 0) reduce[warp] = balance;
+    __syncthreads();
+    if (threadIdx.x == 0 && a.losses) {
+        balance = 0.;
+        for (int w = 0; w < WARPS; ++w) balance += reduce[w];
+        const double n = (double)total_count / a.top_k;
+        a.losses[0] = n > 0. ? (float)(E * balance / (n * n * a.top_k)) : 0.f;
+        a.losses[1] = n > 0. ? (float)(z / n) : 0.f;
+    }
+}
+
 template <typename T, int NG, bool V>
 __global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_kernel(const RouterArgs a) {
     constexpr int kWarps = kWarpsOf<NG>, kThreads = kWarps * 32;
     __shared__ float sums[kRouterMaxExperts];
     __shared__ int counts[kRouterMaxExperts];
-    __shared__ double reduce[kWarps];
-    __shared__ int last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts, k = a.top_k;
     for (int e = threadIdx.x; e < E; e += kThreads) { sums[e] = 0.f; counts[e] = 0; }
     __syncthreads();
@@ -188,68 +283,271 @@ __global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_ker
                     if (expert_of<V>(j, i, lane) < E) sums[expert_of<V>(j, i, lane)] += acc[j][i];
         __syncthreads();
     }
-    if (lane == 0) reduce[warp] = z;
-    __syncthreads();
-    for (int e = threadIdx.x; e < E; e += kThreads) {
-        a.parts[(int64_t)blockIdx.x * E + e] = sums[e];
-        if (counts[e]) atomicAdd(&a.work_counts[e], counts[e]);
+    router_finish<kWarps>(a, sums, counts, z);
+}
+
+// Many rows: a thread has a row.  A warp brings 32 rows into shared memory (fp32, rows apart by an odd number of 16 bytes, so that eight
+// threads read their 16 bytes from different banks) and goes over them thread by thread.  The k <= 8 largest of a row lie in the eight
+// fours with the largest maxima; both choices, of fours and of logits, are made on 32-bit keys (leading bits that order like the value,
+// last bits that prefer the lower index), eight at a time: sorted (Batcher's odd-even merge, 19 exchanges) and merged into the eight
+// largest so far (the larger ones of the two ends, then a bitonic merge of 12 exchanges).  What bounds it is the integer pipe (half a
+// minimum or maximum a clock and scheduler): 8 of them a logit, where rounds over a warp took 40.  The keys hold bf16 and fp16 in full;
+// for fp32 a row whose last choice and largest loser agree in the leading bits, or whose choices are out of order, is checked against the
+// values, and chosen again by the warp where that shows a difference.  The same pass over the row takes the exponentials, which go back
+// to shared memory; the lanes then add the columns up.
+constexpr int kManyExperts = 256, kManyK = 8, kManyRows = 8192;
+// Warps of the one block that an SM's shared memory holds: few blocks leave few sums for the last one to add.
+template <bool WIDE> constexpr int kManyWarps = WIDE ? 6 : 12;
+__host__ __device__ constexpr int many_pitch(int experts) { return (experts + 31) / 32 * 32 + 4; }
+
+__device__ __forceinline__ void exchange(uint32_t& a, uint32_t& b) {       // the larger one first
+    const uint32_t m = max(a, b);
+    b = min(a, b);
+    a = m;
+}
+__device__ __forceinline__ void sort8(uint32_t (&k)[8]) {
+    exchange(k[0], k[1]); exchange(k[2], k[3]); exchange(k[4], k[5]); exchange(k[6], k[7]);
+    exchange(k[0], k[2]); exchange(k[1], k[3]); exchange(k[4], k[6]); exchange(k[5], k[7]);
+    exchange(k[1], k[2]); exchange(k[5], k[6]);
+    exchange(k[0], k[4]); exchange(k[1], k[5]); exchange(k[2], k[6]); exchange(k[3], k[7]);
+    exchange(k[2], k[4]); exchange(k[3], k[5]);
+    exchange(k[1], k[2]); exchange(k[3], k[4]); exchange(k[5], k[6]);
+}
+
+// Sorts eight keys into the eight largest so far; lost: the largest that is not among them.
+__device__ __forceinline__ void take8(uint32_t (&best)[8], uint32_t (&key)[8], uint32_t& lost) {
+    sort8(key);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lost = max(lost, min(best[i], key[7 - i]));
+        best[i] = max(best[i], key[7 - i]);
     }
-    if (threadIdx.x == 0) {
-        z = 0.;
-        for (int w = 0; w < kWarps; ++w) z += reduce[w];
-        a.z_parts[blockIdx.x] = z;
-    }
-    __threadfence();
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((i & d) == 0) exchange(best[i], best[i + d]);
+}
+// The leading bits of a float as an integer that orders like it (-0 as 0).
+template <uint32_t LOW>
+__device__ __forceinline__ uint32_t leading(float v) {
+    const uint32_t b = __float_as_uint(v + 0.f);
+    return (b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) & ~LOW;
+}
+
+template <typename T, bool V, bool WIDE>
+__global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(const RouterArgs a) {
+    constexpr int kWarps = kManyWarps<WIDE>, kThreads = kWarps * 32, kColumns = WIDE ? 2 : 1;     // columns: fours of a lane
+    extern __shared__ float tiles[];                          // [warps][32][pitch]
+    __shared__ float sums[kManyExperts], scale[kWarps][32];
+    __shared__ int counts[kManyExperts];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts, k = a.top_k, pitch = many_pitch(E), padded = pitch - 4, fours = (E + 3) / 4;
+    float* tile = tiles + warp * 32 * pitch;
+    float* mine = tile + lane * pitch;
+    for (int e = threadIdx.x; e < E; e += kThreads) { sums[e] = 0.f; counts[e] = 0; }
     __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    // counts, offsets, sums and losses
-    __shared__ double total_z;
-    __shared__ int64_t total_count;
-    for (int e = threadIdx.x; e < E; e += kThreads) counts[e] = __ldcg(a.work_counts + e);
-    z = 0.;
-    for (int b = threadIdx.x; b < (int)gridDim.x; b += kThreads) z += __ldcg(a.z_parts + b);
-    z = warp_sum_double(z);
-    __syncthreads();
-    if (lane == 0) reduce[warp] = z;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        z = 0.;
-        for (int w = 0; w < kWarps; ++w) z += reduce[w];
-        total_z = z;
-        int run = 0;
-        for (int e = 0; e < E; ++e) {
-            if (a.offsets) a.offsets[e] = run;
-            run += counts[e];
+    float acc[kColumns][4];
+#pragma unroll
+    for (int j = 0; j < kColumns; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+    double z2 = 0.;
+    const bool packed = k % 4 == 0 && (((uintptr_t)a.idx | (uintptr_t)a.weights) & 15) == 0;
+    const int64_t stride = (int64_t)gridDim.x * kWarps * 32;
+    for (int64_t base = ((int64_t)blockIdx.x * kWarps + warp) * 32; base < a.rows; base += stride) {
+        const int rows = (int)min((int64_t)32, a.rows - base);
+        // the tile
+        const T* in = static_cast<const T*>(a.logits) + base * a.ld;
+        if (V && sizeof(T) == 4) {
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r)
+                for (int c = lane * 4; c < E; c += 128) cp_async16(tile + r * pitch + c, in + r * a.ld + c);
+            cp_async_commit();
+        } else if (V) {
+            for (int r0 = 0; r0 < rows; r0 += 8)              // four values of 16 bits a load, eight rows' loads in flight
+                for (int f = lane; f < fours; f += 32) {
+                    float v[8][4];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        if (r0 + r < rows) group_load4<T, 1, true>(in + (r0 + r) * a.ld + f * 4, 0, 0, 4, v[r]);
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        if (r0 + r < rows) *reinterpret_cast<float4*>(tile + (r0 + r) * pitch + f * 4) = make_float4(v[r][0], v[r][1], v[r][2], v[r][3]);
+                }
+        } else {
+            for (int r0 = 0; r0 < rows; r0 += 8)
+                for (int c = lane; c < E; c += 32) {
+                    float v[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) v[r] = r0 + r < rows ? to_float(in[(r0 + r) * a.ld + c]) : 0.f;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        if (r0 + r < rows) tile[(r0 + r) * pitch + c] = v[r];
+                }
         }
-        if (a.offsets) a.offsets[E] = run;
-        total_count = run;
-        *a.ticket = 0;
+        for (int c = E; c < padded; ++c) mine[c] = -INFINITY;
+        const int64_t row = base + lane;
+        bool on = lane < rows && (!a.has_live || a.live[row]);
+        if (V && sizeof(T) == 4) cp_async_wait<0>();
+        __syncwarp();
+        // the eight fours with the largest maxima, and the eight largest of them
+        uint32_t groups[8] = {0, 0, 0, 0, 0, 0, 0, 0}, best[8] = {0, 0, 0, 0, 0, 0, 0, 0}, lost_group = 0, lost = 0;
+        for (int c = 0; c < padded / 32; ++c) {
+            uint32_t key[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 v = *reinterpret_cast<const float4*>(mine + c * 32 + i * 4);
+                key[i] = leading<63>(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))) | (uint32_t)(63 - c * 8 - i);
+            }
+            take8(groups, key, lost_group);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            uint32_t key[8];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int g = min(63 - (int)(groups[i + q] & 63u), padded / 4 - 1);
+                const float4 v = *reinterpret_cast<const float4*>(mine + g * 4);
+                const uint32_t code = 255 - g * 4;            // 255 - expert
+                key[q * 4] = leading<255>(v.x) | code;
+                key[q * 4 + 1] = leading<255>(v.y) | (code - 1);
+                key[q * 4 + 2] = leading<255>(v.z) | (code - 2);
+                key[q * 4 + 3] = leading<255>(v.w) | (code - 3);
+            }
+            take8(best, key, lost);
+        }
+        int idx[8];
+        float val[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            idx[i] = min(255 - (int)(best[i] & 255u), E - 1);
+            val[i] = mine[idx[i]];
+        }
+        float m = val[0], sum = 0.f;
+        if (sizeof(T) == 4) {
+            float least = val[0];
+            uint32_t last = best[0], next = best[1];          // of the chosen, and the one behind it
+            bool sorted = true;
+#pragma unroll
+            for (int i = 1; i < 8; ++i)
+                if (i < k) {
+                    sorted = sorted && (val[i - 1] > val[i] || (val[i - 1] == val[i] && idx[i - 1] < idx[i]));
+                    least = val[i];
+                    last = best[i];
+                    next = i < 7 ? best[i < 7 ? i + 1 : 7] : 0u;
+                }
+            const bool close = !sorted || (last >> 8) == (max(next, lost) >> 8) || (groups[7] >> 6) == (lost_group >> 6);
+            int larger = 0, above = 0;                        // logits, and chosen ones, that are larger than the least chosen
+            if (__any_sync(0xffffffffu, on && close)) {
+                for (int c = 0; c < fours; ++c) {
+                    const float4 v = *reinterpret_cast<const float4*>(mine + c * 4);
+                    larger += (v.x > least) + (v.y > least) + (v.z > least) + (v.w > least);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) above += i < k && val[i] > least;
+            }
+            // rows whose choice is not that of the values: the warp chooses again, one row after the other
+            unsigned again = __ballot_sync(0xffffffffu, on && (!sorted || larger != above) && !(m != m));
+            while (again) {
+                const int r = __ffs(again) - 1;
+                again &= again - 1;
+                const float* other = tile + r * pitch;
+                uint32_t key[kManyExperts / 32];
+#pragma unroll
+                for (int j = 0; j < kManyExperts / 32; ++j) key[j] = j * 32 + lane < E ? order_key(other[j * 32 + lane]) : 0u;
+                for (int i = 0; i < k; ++i) {
+                    uint32_t top = 0;
+                    int at = 0;
+#pragma unroll
+                    for (int j = 0; j < kManyExperts / 32; ++j)
+                        if (key[j] > top) { top = key[j]; at = j * 32 + lane; }
+                    const uint32_t most = __reduce_max_sync(0xffffffffu, top);
+                    const int e = (int)__reduce_min_sync(0xffffffffu, top == most ? (uint32_t)at : 0xffffffffu);
+#pragma unroll
+                    for (int j = 0; j < kManyExperts / 32; ++j)
+                        if (j * 32 + lane == e) key[j] = 0;
+                    if (lane == r) {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (q == i) { idx[q] = e; val[q] = mine[e]; }
+                    }
+                }
+            }
+            m = val[0];
+        }
+        on = on && !(m == -INFINITY);                         // a row without a logit above -inf takes no part
+#pragma unroll 2
+        for (int c = 0; c < fours; ++c) {
+            float4 v = *reinterpret_cast<const float4*>(mine + c * 4);
+            v.x = ex2((v.x - m) * kLog2e);                    // (of rows that take no part: left out below)
+            v.y = ex2((v.y - m) * kLog2e);
+            v.z = ex2((v.z - m) * kLog2e);
+            v.w = ex2((v.w - m) * kLog2e);
+            sum += (v.x + v.y) + (v.z + v.w);
+            *reinterpret_cast<float4*>(mine + c * 4) = v;
+        }
+        float w[8], total = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w[i] = i < k && on ? ex2((val[i] - m) * kLog2e) : 0.f;
+            total += w[i];
+        }
+        // (a NaN in the row makes its sum NaN, and the weights)
+        const float inv = !on ? 0.f : sum != sum ? sum : 1.f / (a.renormalise ? total : sum), lse = on ? m + logf(sum) : 0.f;
+        scale[warp][lane] = on ? 1.f / sum : 0.f;
+        if (lane < rows) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] *= inv;
+                idx[i] = on ? idx[i] : -1;
+                if (i < k && on) atomicAdd(&counts[idx[i]], 1);
+            }
+            if (packed) {
+#pragma unroll
+                for (int i = 0; i < 8; i += 4)
+                    if (i < k) {
+                        *reinterpret_cast<int4*>(a.idx + row * k + i) = make_int4(idx[i], idx[i + 1], idx[i + 2], idx[i + 3]);
+                        *reinterpret_cast<float4*>(a.weights + row * k + i) = make_float4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < k) { a.idx[row * k + i] = idx[i]; a.weights[row * k + i] = w[i]; }
+            }
+            if (a.lse) a.lse[row] = lse;
+            z2 += (double)lse * (double)lse;
+        }
+        __syncwarp();
+        // columns, of the rows that take part
+        const unsigned part = __ballot_sync(0xffffffffu, on);
+#pragma unroll
+        for (int j = 0; j < kColumns; ++j) {
+            const int c = j * 128 + lane * 4;
+            if (c < fours * 4) {
+#pragma unroll 8
+                for (int r = 0; r < 32; ++r) {
+                    if (!(part >> r & 1)) continue;
+                    const float4 v = *reinterpret_cast<const float4*>(tile + r * pitch + c);
+                    const float s = scale[warp][r];
+                    acc[j][0] = fmaf(v.x, s, acc[j][0]);
+                    acc[j][1] = fmaf(v.y, s, acc[j][1]);
+                    acc[j][2] = fmaf(v.z, s, acc[j][2]);
+                    acc[j][3] = fmaf(v.w, s, acc[j][3]);
+                }
+            }
+        }
+        __syncwarp();
     }
-    __syncthreads();
-    double balance = 0.;
-    for (int e = threadIdx.x; e < E; e += kThreads) {
-        double s = 0.;
-#pragma unroll 16
-        for (int b = 0; b < (int)gridDim.x; ++b) s += __ldcg(a.parts + (int64_t)b * E + e);
-        if (a.prob_sums) a.prob_sums[e] = (float)s;
-        if (a.counts) a.counts[e] = counts[e];
-        a.work_counts[e] = 0;
-        balance += s * counts[e];
+    for (int w = 0; w < kWarps; ++w) {
+        if (w == warp)
+#pragma unroll
+            for (int j = 0; j < kColumns; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (j * 128 + lane * 4 + i < E) sums[j * 128 + lane * 4 + i] += acc[j][i];
+        __syncthreads();
     }
-    balance = warp_sum_double(balance);
-    __syncthreads();
-    if (lane == 0) reduce[warp] = balance;
-    __syncthreads();
-    if (threadIdx.x == 0 && a.losses) {
-        balance = 0.;
-        for (int w = 0; w < kWarps; ++w) balance += reduce[w];
-        const double n = (double)total_count / k;
-        a.losses[0] = n > 0. ? (float)(E * balance / (n * n * k)) : 0.f;
-        a.losses[1] = n > 0. ? (float)(total_z / n) : 0.f;
-    }
+    router_finish<kWarps>(a, sums, counts, warp_sum_double(z2));
 }
 
 // Gradient: L lanes have a row (so that a warp reduces several rows in one go), NG fours of experts each.
@@ -367,7 +665,7 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const
 }
 
 int router_blocks(int rows, int warps, int sms) {
-    const int most = router_max_blocks(sms), need = (int)(((int64_t)rows + warps - 1) / warps);
+    const int most = sms * 2, need = (int)(((int64_t)rows + warps - 1) / warps);
     return need < 1 ? 1 : need < most ? need : most;
 }
 
@@ -378,6 +676,12 @@ cudaError_t router_launch(const RouterArgs& a, int sms, cudaStream_t st) {
 }
 template <typename T, bool V>
 cudaError_t router_typed(const RouterArgs& a, int sms, cudaStream_t st) {
+    if (a.experts <= kManyExperts && a.top_k <= kManyK && a.rows >= kManyRows) {
+        const int warps = a.experts <= 128 ? kManyWarps<false> : kManyWarps<true>;
+        const int64_t need = ((int64_t)a.rows + warps * 32 - 1) / (warps * 32);
+        return launch_plain(a.experts <= 128 ? router_many_kernel<T, V, false> : router_many_kernel<T, V, true>,
+                            dim3((unsigned)(need < sms ? need : sms)), dim3(warps * 32), (size_t)warps * 32 * many_pitch(a.experts) * 4, st, a);
+    }
     if (a.experts <= 128) return router_launch<T, 1, V>(a, sms, st);
     if (a.experts <= 256) return router_launch<T, 2, V>(a, sms, st);
     if (a.experts <= 512) return router_launch<T, 4, V>(a, sms, st);
@@ -402,6 +706,9 @@ cudaError_t router_grad_typed(const RouterGradArgs& a, int sms, cudaStream_t st)
 
 template <typename T, bool V>
 cudaError_t router_init() {
+    cudaError_t e = init_all(kManyWarps<false> * 32 * many_pitch(128) * 4, router_many_kernel<T, V, false>);
+    if (e == cudaSuccess) e = init_all(kManyWarps<true> * 32 * many_pitch(kManyExperts) * 4, router_many_kernel<T, V, true>);
+    if (e != cudaSuccess) return e;
     return init_all(0, router_kernel<T, 1, V>, router_kernel<T, 2, V>, router_kernel<T, 4, V>, router_kernel<T, 8, V>, router_grad_kernel<T, 4, 2, V>,
                     router_grad_kernel<T, 8, 4, V>, router_grad_kernel<T, 16, 4, V>, router_grad_kernel<T, 32, 4, V>,
                     router_grad_kernel<T, 32, 8, V>);

@@ -519,6 +519,49 @@ def router_grad_reference(z, k, got, dw, renormalise, cb, cz):
     return want, scale * (128 + 4 * far) * V + 1e-45
 
 
+@pytest.mark.parametrize("E,k", [(2, 2), (8, 8), (9, 1), (60, 4), (61, 5), (64, 6), (128, 8), (129, 3), (250, 8), (256, 7), (256, 10), (300, 8)])
+@pytest.mark.parametrize("t", [F, B, H])
+def test_router_of_many_rows(E, k, t):
+    n = 8192 + 77
+    train = binding.Train(max_experts=E, device=DEV)
+    for renormalise, masked, pad in ((True, False, 0), (False, True, 4 if E % 4 == 0 else 1)):
+        z = router_logits(n, E, t, seed=E, pad=pad)
+        z[5, :] = -math.inf
+        z[6, 1:] = -math.inf
+        z[7, :] = 0.5
+        z[8, : E // 2] = torch.finfo(t).min
+        live = torch.rand(n, generator=gen(2), device=DEV) < 0.6 if masked else None
+        if live is not None:
+            live[5:9] = True
+            z[~live] = math.nan
+        got = run_router(train, z, k, live, renormalise)
+        check_router(z, k, got, live, renormalise)
+        again = run_router(train, z, k, live, renormalise)
+        assert all(torch.equal(got[n_], again[n_]) for n_ in got if n_ != "losses")
+
+
+def test_logits_that_differ_in_their_last_bits():
+    """fp32 logits whose leading bits agree: the order is that of the values, not of the leading bits."""
+    n, E, k = 9000, 128, 8
+    train = binding.Train(max_experts=E, device=DEV)
+    g = gen(9)
+    steps = torch.randint(0, 200, (n, E), generator=g, device=DEV)
+    z = (torch.tensor(2.5, device=DEV).view(torch.int32) + steps.int()).view(F)      # 2.5 and the 199 numbers after it, ties among them
+    z[::3] = -z[::3]
+    z[1::7] = router_logits(len(z[1::7]), E, F)
+    z[2::5, 100:] = z[2::5, :28]                                 # pairs of equal logits
+    got = run_router(train, z, k)
+    check_router(z, k, got)
+    z[17, 3], z[18, 100], z[19, 5], z[20, :], z[21, 2:] = math.nan, math.inf, -math.nan, math.nan, -math.nan
+    bad = run_router(train, z, k)
+    keep = torch.ones(n, dtype=torch.bool, device=DEV)
+    keep[17:22] = False
+    assert torch.equal(bad["idx"][keep], got["idx"][keep]) and torch.equal(bad["w"][keep], got["w"][keep])
+    for row in bad["idx"][17:22].tolist():
+        assert len(set(row)) == k and min(row) >= 0 and max(row) < E
+    assert bad["w"][17:22].isnan().any(1).all()
+
+
 def test_equal_logits_go_to_the_lower_expert():
     for E in (8, 128, 130, 600):
         train = binding.Train(max_experts=E, device=DEV)
