@@ -21,12 +21,11 @@ namespace {
 
 constexpr int kChunk = 8;
 constexpr int kLoopSmem = 2 * kNormMaxWidth * 4;      // the sums of the widest row
-// Rows that the gradient keeps in registers, 16 values of a thread: 512 threads, or 256 with twice the registers for fp32.
-constexpr int grad_row_threads(bool x_is_fp32) { return x_is_fp32 ? 256 : 512; }
+constexpr int kRowWidth = 8192;          // widest row that is kept in registers: 256 threads x 32 values
 
-// Threads of a row and chunks of eight neighbouring values of a thread (`most` at the most).
+// Threads of a row and chunks of eight neighbouring values of a thread; blocks of at most 256 threads.
 struct NormPlan { int group, nv, block; };
-NormPlan norm_plan(int width, int most) {
+NormPlan norm_plan(int width) {
     const int chunks = (width + kChunk - 1) / kChunk;
     NormPlan p;
     if (chunks <= 32) {
@@ -34,12 +33,17 @@ NormPlan norm_plan(int width, int most) {
         p.group = 1;
         while (p.group < chunks) p.group *= 2;
     } else {
-        p.nv = chunks < 256 || most < 4 ? 2 : 4;
+        p.nv = chunks <= 512 ? 2 : 4;
         p.group = (chunks + 32 * p.nv - 1) / (32 * p.nv) * 32;
     }
-    p.block = p.group >= 256 ? p.group : 256 / p.group * p.group;
+    p.block = 256 / p.group * p.group;
     return p;
 }
+// Blocks on an SM for which registers are planned, forward and backward; rows of a group that are worked on together.
+__host__ __device__ constexpr int forward_blocks(int nv, bool x_is_fp32) { return nv == 4 ? 1 : nv == 2 ? (x_is_fp32 ? 2 : 3) : x_is_fp32 ? 3 : 4; }
+__host__ __device__ constexpr int grad_blocks_sm(int nv, bool x_is_fp32, bool layer) { return nv == 4 ? 1 : nv == 1 && !x_is_fp32 && !layer ? 3 : 2; }
+__host__ __device__ constexpr int rows_together(int nv) { return nv == 1 ? 2 : 1; }
+
 // The same for rows that are read again instead of kept.
 NormPlan loop_plan(int width) {
     NormPlan p;
@@ -111,40 +115,52 @@ __device__ __forceinline__ int64_t row_offset(int row, int heads, int width, int
     return (int64_t)t * ld + (int64_t)(row - t * heads) * width;
 }
 
-// Rows in registers.
+// Rows in registers.  A block stays for many rows: the weight's values stay too, and the next rows are on their way while the present
+// ones are reduced.
 template <typename XT, typename YT, int NV>
-__global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, const int group) {
+__global__ void __launch_bounds__(256, forward_blocks(NV, sizeof(XT) == 4)) norm_rows_kernel(const NormArgs a, const int group) {
     __shared__ float scratch[2 * 16];
     const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
     int half = 0;
     const float inv = 1.f / (float)a.width;
-    for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += (int64_t)gridDim.x * groups) {
-        const bool on = base + index < a.rows;                // the trip count is the same for all threads of a block
+    float weight[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load_weight(a.weight, a.w_type, j, lane, group, a.width, weight[j]);
+    Raw8<XT> x[NV];
+    Raw8<YT> add[NV];
+    auto fetch = [&](int64_t r) {
+        const bool on = r < a.rows;
+        const int row = on ? (int)r : 0, W = on ? a.width : 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) x[j] = load_chunk(static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x), j, lane, group, W);
+        if (a.has_add) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                add[j] = load_chunk(static_cast<const YT*>(a.add) + row_offset(row, a.heads, a.width, a.ld_add), j, lane, group, W);
+        }
+    };
+    const int64_t stride = (int64_t)gridDim.x * groups;
+    int64_t base = (int64_t)blockIdx.x * groups;
+    if (base < a.rows) fetch(base + index);
+    for (; base < a.rows; base += stride) {                   // the trip count is the same for all threads of a block
+        const bool on = base + index < a.rows;
         const int row = on ? (int)(base + index) : 0;
         const int W = on ? a.width : 0;
-        const XT* x = static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x);
-        Raw8<XT> fx[NV];
-#pragma unroll
-        for (int j = 0; j < NV; ++j) fx[j] = load_chunk(x, j, lane, group, W);
         float v[NV][8];
-        if (a.has_add) {
-            const YT* add = static_cast<const YT*>(a.add) + row_offset(row, a.heads, a.width, a.ld_add);
-            Raw8<YT> fa[NV];
 #pragma unroll
-            for (int j = 0; j < NV; ++j) fa[j] = load_chunk(add, j, lane, group, W);
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
+        for (int j = 0; j < NV; ++j) {
+            unpack8<XT>(x[j], v[j]);
+            if (a.has_add) {
                 float b[8];
-                unpack8<XT>(fx[j], v[j]);
-                unpack8<YT>(fa[j], b);
+                unpack8<YT>(add[j], b);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[j][i] += b[i];
-                fx[j] = pack8<XT>(v[j]);                      // the norm is that of the stored sum
-                if (a.sum) store_chunk(static_cast<XT*>(a.sum) + row_offset(row, a.heads, a.width, a.ld_sum), j, lane, group, W, fx[j]);
+                const Raw8<XT> s = pack8<XT>(v[j]);           // the norm is that of the stored sum
+                unpack8<XT>(s, v[j]);
+                if (a.sum) store_chunk(static_cast<XT*>(a.sum) + row_offset(row, a.heads, a.width, a.ld_sum), j, lane, group, W, s);
             }
         }
-#pragma unroll
-        for (int j = 0; j < NV; ++j) unpack8<XT>(fx[j], v[j]);
+        fetch(base + stride + index);
         float mean = 0.f;
         if (a.layer) {
             float s[1] = {0.f};
@@ -171,14 +187,13 @@ __global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, const 
         YT* y = static_cast<YT*>(a.y) + row_offset(row, a.heads, a.width, a.ld_y);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            float w[8];
-            load_weight(a.weight, a.w_type, j, lane, group, W, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * rstd * w[i];
+            for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * rstd * weight[j][i];
             if (a.has_bias) {
-                load_weight(a.bias, a.w_type, j, lane, group, W, w);
+                float b[8];
+                load_weight(a.bias, a.w_type, j, lane, group, W, b);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[j][i] += w[i];
+                for (int i = 0; i < 8; ++i) v[j][i] += b[i];
             }
             store_chunk(y, j, lane, group, W, pack8<YT>(v[j]));
         }
@@ -243,8 +258,9 @@ __global__ void __launch_bounds__(256, 2) norm_loop_kernel(const NormArgs a, con
 
 // Rows in registers, with the sums of the weight's gradient.
 template <typename XT, typename YT, int NV, bool LAYER>
-__global__ void __launch_bounds__(NV == 1 ? 256 : grad_row_threads(sizeof(XT) == 4), NV == 1 ? 2 : 1) norm_grad_rows_kernel(const NormGradArgs a, const int group) {
-    __shared__ float scratch[2 * 16 * 2];
+__global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER)) norm_grad_rows_kernel(const NormGradArgs a, const int group) {
+    constexpr int R = rows_together(NV), N = LAYER ? 2 * R : R;
+    __shared__ float scratch[2 * 16 * N];
     extern __shared__ float sums[];                           // [groups][width]
     const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
     int half = 0;
@@ -259,65 +275,81 @@ __global__ void __launch_bounds__(NV == 1 ? 256 : grad_row_threads(sizeof(XT) ==
         }
     const XT* px = static_cast<const XT*>(a.x);
     const YT* pdy = static_cast<const YT*>(a.dy);
-    Raw8<XT> x[NV];
-    Raw8<YT> dy[NV];
-    float rstd = 0.f, mean = 0.f;
-    auto fetch = [&](int64_t r) {
-        const bool on = r < a.rows;
-        const int row = on ? (int)r : 0, W = on ? a.width : 0;
+    Raw8<XT> x[R][NV];
+    Raw8<YT> dy[R][NV];
+    float rstd[R], mean[R];
+    auto fetch = [&](int64_t first) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) x[j] = load_chunk(px + row_offset(row, a.heads, a.width, a.ld_x), j, lane, group, W);
+        for (int k = 0; k < R; ++k) {
+            const int64_t r = first + (int64_t)k * groups;
+            const bool on = r < a.rows;
+            const int row = on ? (int)r : 0, W = on ? a.width : 0;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) dy[j] = load_chunk(pdy + row_offset(row, a.heads, a.width, a.ld_dy), j, lane, group, W);
-        rstd = on ? a.rstd[row] : 0.f;
-        if (LAYER) mean = on ? a.mean[row] : 0.f;
+            for (int j = 0; j < NV; ++j) x[k][j] = load_chunk(px + row_offset(row, a.heads, a.width, a.ld_x), j, lane, group, W);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) dy[k][j] = load_chunk(pdy + row_offset(row, a.heads, a.width, a.ld_dy), j, lane, group, W);
+            rstd[k] = on ? a.rstd[row] : 0.f;
+            mean[k] = LAYER && on ? a.mean[row] : 0.f;
+        }
     };
-    const int64_t stride = (int64_t)gridDim.x * groups;
-    int64_t base = (int64_t)blockIdx.x * groups;
+    const int64_t stride = (int64_t)gridDim.x * groups * R;
+    int64_t base = (int64_t)blockIdx.x * groups * R;
     if (base < a.rows) fetch(base + index);
     for (; base < a.rows; base += stride) {
-        const bool on = base + index < a.rows;
-        const int row = on ? (int)(base + index) : 0, W = on ? a.width : 0;
-        float n[NV][8], g[NV][8];
-        float c[2] = {0.f, 0.f};
+        float n[R][NV][8], g[R][NV][8], c[N], r[R];
+#pragma unroll
+        for (int i = 0; i < N; ++i) c[i] = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float w[8];
-            load_weight(a.weight, a.w_type, j, lane, group, W, w);
-            unpack8<XT>(x[j], n[j]);
-            unpack8<YT>(dy[j], g[j]);
+            load_weight(a.weight, a.w_type, j, lane, group, a.width, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                n[j][i] = (LAYER ? n[j][i] - mean : n[j][i]) * rstd;
-                acc_w[j][i] = fmaf(g[j][i], n[j][i], acc_w[j][i]);
-                if (LAYER) acc_b[j][i] += g[j][i];
-                g[j][i] *= w[i];
-                c[0] = fmaf(g[j][i], n[j][i], c[0]);
-                if (LAYER) c[1] += g[j][i];
+            for (int k = 0; k < R; ++k) {
+                unpack8<XT>(x[k][j], n[k][j]);
+                unpack8<YT>(dy[k][j], g[k][j]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    n[k][j][i] = (LAYER ? n[k][j][i] - mean[k] : n[k][j][i]) * rstd[k];
+                    acc_w[j][i] = fmaf(g[k][j][i], n[k][j][i], acc_w[j][i]);
+                    if (LAYER) acc_b[j][i] += g[k][j][i];
+                    g[k][j][i] *= w[i];
+                    c[k] = fmaf(g[k][j][i], n[k][j][i], c[k]);
+                    if (LAYER) c[R + k] += g[k][j][i];
+                }
             }
         }
-        const float r = rstd;
-        Raw8<XT> ds[NV];
-        if (a.has_d_sum) {
-            const XT* p = static_cast<const XT*>(a.d_sum) + row_offset(row, a.heads, a.width, a.ld_d_sum);
+        Raw8<XT> ds[R][NV];
 #pragma unroll
-            for (int j = 0; j < NV; ++j) ds[j] = load_chunk(p, j, lane, group, W);
-        }
-        fetch(base + stride + index);                         // the next row is on its way while this one is reduced
-        group_sum(c, group, index, scratch, half);
-        const float c0 = c[0] * inv, c1 = LAYER ? c[1] * inv : 0.f;
-        XT* dx = static_cast<XT*>(a.dx) + row_offset(row, a.heads, a.width, a.ld_dx);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) g[j][i] = fmaf(-n[j][i], c0, LAYER ? g[j][i] - c1 : g[j][i]) * r;
+        for (int k = 0; k < R; ++k) {
+            r[k] = rstd[k];
+            const bool on = base + index + (int64_t)k * groups < a.rows;
+            const int row = on ? (int)(base + index + (int64_t)k * groups) : 0;
             if (a.has_d_sum) {
-                float s[8];
-                unpack8<XT>(ds[j], s);
+                const XT* p = static_cast<const XT*>(a.d_sum) + row_offset(row, a.heads, a.width, a.ld_d_sum);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[j][i] += s[i];
+                for (int j = 0; j < NV; ++j) ds[k][j] = load_chunk(p, j, lane, group, on ? a.width : 0);
             }
-            store_chunk(dx, j, lane, group, W, pack8<XT>(g[j]));
+        }
+        fetch(base + stride + index);                         // the next rows are on their way while these are reduced
+        group_sum(c, group, index, scratch, half);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const bool on = base + index + (int64_t)k * groups < a.rows;
+            const int row = on ? (int)(base + index + (int64_t)k * groups) : 0;
+            const float c0 = c[k] * inv, c1 = LAYER ? c[LAYER ? R + k : 0] * inv : 0.f;
+            XT* dx = static_cast<XT*>(a.dx) + row_offset(row, a.heads, a.width, a.ld_dx);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[k][j][i] = fmaf(-n[k][j][i], c0, LAYER ? g[k][j][i] - c1 : g[k][j][i]) * r[k];
+                if (a.has_d_sum) {
+                    float s[8];
+                    unpack8<XT>(ds[k][j], s);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) g[k][j][i] += s[i];
+                }
+                store_chunk(dx, j, lane, group, on ? a.width : 0, pack8<XT>(g[k][j]));
+            }
         }
     }
 #pragma unroll
@@ -431,10 +463,11 @@ int64_t row_blocks(int64_t rows, const NormPlan& p) { return (rows + p.block / p
 
 template <typename XT, typename YT>
 cudaError_t norm_typed(const NormArgs& a, bool vector, int sms, cudaStream_t st) {
-    const NormPlan p = vector ? norm_plan(a.width, 4) : loop_plan(a.width);
-    const int64_t blocks = row_blocks(a.rows, p), most = (int64_t)sms * 64;
+    const bool rows = vector && a.width <= kRowWidth;
+    const NormPlan p = rows ? norm_plan(a.width) : loop_plan(a.width);
+    const int64_t blocks = row_blocks(a.rows, p), most = (int64_t)sms * (rows ? forward_blocks(p.nv, sizeof(XT) == 4) : 64);
     const dim3 grid((unsigned)(blocks < most ? blocks : most));
-    if (!vector) return launch_plain(norm_loop_kernel<XT, YT>, grid, dim3(p.block), 0, st, a, p.group);
+    if (!rows) return launch_plain(norm_loop_kernel<XT, YT>, grid, dim3(p.block), 0, st, a, p.group);
     if (p.nv == 1) return launch_plain(norm_rows_kernel<XT, YT, 1>, grid, dim3(p.block), 0, st, a, p.group);
     if (p.nv == 2) return launch_plain(norm_rows_kernel<XT, YT, 2>, grid, dim3(p.block), 0, st, a, p.group);
     return launch_plain(norm_rows_kernel<XT, YT, 4>, grid, dim3(p.block), 0, st, a, p.group);
@@ -447,13 +480,14 @@ struct GradPlan {
 };
 GradPlan grad_plan(int64_t rows, int width, bool layer, bool x_is_fp32, bool vector, int sms) {
     GradPlan g;
-    g.rows = vector && width <= 16 * grad_row_threads(x_is_fp32);
-    g.p = g.rows ? norm_plan(width, 2) : loop_plan(width);
+    g.rows = vector && width <= kRowWidth;
+    g.p = g.rows ? norm_plan(width) : loop_plan(width);
     const int groups = g.p.block / g.p.group;
     g.smem = g.rows ? (groups > 1 ? groups * width * 4 : 0) : groups * width * 4 * (layer ? 2 : 1);
-    // as many blocks as run at once: registers of 512 threads; shared memory of one, two or more
-    const int most = sms * (g.rows ? 512 / g.p.block : g.smem > 100 * 1024 ? 1 : width > 2048 ? 2 : 4);
-    const int64_t need = row_blocks(rows, g.p);
+    // as many blocks as run at once: by registers; by shared memory one, two or more
+    const int most = sms * (g.rows ? grad_blocks_sm(g.p.nv, x_is_fp32, layer) : g.smem > 100 * 1024 ? 1 : width > 2048 ? 2 : 4);
+    const int together = g.rows ? rows_together(g.p.nv) : 1;
+    const int64_t need = (row_blocks(rows, g.p) + together - 1) / together;
     g.blocks = (int)(need < 1 ? 1 : need < most ? need : most);
     return g;
 }
@@ -462,7 +496,8 @@ cudaError_t norm_grad_typed(const NormGradArgs& a, const GradPlan& g, cudaStream
     const dim3 grid(g.blocks), block(g.p.block);
     if (!g.rows) return launch_plain(norm_grad_loop_kernel<XT, YT, LAYER>, grid, block, g.smem, st, a, g.p.group);
     if (g.p.nv == 1) return launch_plain(norm_grad_rows_kernel<XT, YT, 1, LAYER>, grid, block, g.smem, st, a, g.p.group);
-    return launch_plain(norm_grad_rows_kernel<XT, YT, 2, LAYER>, grid, block, g.smem, st, a, g.p.group);
+    if (g.p.nv == 2) return launch_plain(norm_grad_rows_kernel<XT, YT, 2, LAYER>, grid, block, g.smem, st, a, g.p.group);
+    return launch_plain(norm_grad_rows_kernel<XT, YT, 4, LAYER>, grid, block, g.smem, st, a, g.p.group);
 }
 
 // x and y of one type, or x fp32 (a residual stream) and y of 16 bits.
@@ -477,10 +512,15 @@ cudaError_t for_types(int x_type, int y_type, F f) {
 
 }  // namespace
 
-// Sums of dw or db: blocks x width (grad_plan: at most four blocks on an SM up to a width of 2048, two beyond).
+// Sums of dw or db: blocks x width (grad_plan: at most four blocks on an SM up to a width of 2048, three up to 4096, two beyond).
 size_t norm_grad_part_bytes(int max_width) {
-    const size_t narrow = 4 * (size_t)(max_width < 2048 ? max_width : 2048), wide = 2 * (size_t)max_width;
-    return (size_t)kTrainSms * (narrow > wide ? narrow : wide) * 4;
+    size_t most = 0;
+    const int limit[3] = {2048, 4096, kNormMaxWidth};
+    for (int i = 0; i < 3; ++i) {
+        const size_t n = (size_t)(4 - i) * (size_t)(max_width < limit[i] ? max_width : limit[i]);
+        if (n > most) most = n;
+    }
+    return (size_t)kTrainSms * most * 4;
 }
 
 cudaError_t init_norm_kernels() {
@@ -491,7 +531,8 @@ cudaError_t init_norm_kernels() {
             const cudaError_t r = init_all(0, norm_rows_kernel<XT, YT, 1>, norm_rows_kernel<XT, YT, 2>, norm_rows_kernel<XT, YT, 4>,
                                            norm_loop_kernel<XT, YT>, norm_grad_rows_kernel<XT, YT, 1, false>,
                                            norm_grad_rows_kernel<XT, YT, 1, true>, norm_grad_rows_kernel<XT, YT, 2, false>,
-                                           norm_grad_rows_kernel<XT, YT, 2, true>);
+                                           norm_grad_rows_kernel<XT, YT, 2, true>, norm_grad_rows_kernel<XT, YT, 4, false>,
+                                           norm_grad_rows_kernel<XT, YT, 4, true>);
             return r != cudaSuccess ? r : init_all(kLoopSmem, norm_grad_loop_kernel<XT, YT, false>, norm_grad_loop_kernel<XT, YT, true>);
         });
         if (e != cudaSuccess) return e;
