@@ -87,9 +87,11 @@ __device__ __forceinline__ void load_weight(const void* w, int type, int j, int 
 template <int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], int group, int index, float* scratch, int& half) {
     if (group <= 32) {
-        for (int o = group >> 1; o > 0; o >>= 1)
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        for (int o = 16; o > 0; o >>= 1)
+            if (o < group)
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
         return;
     }
 #pragma unroll
@@ -109,10 +111,11 @@ __device__ __forceinline__ void group_sum(float (&v)[N], int group, int index, f
         for (int i = 0; i < N; ++i) v[i] += s[(first + w) * N + i];
 }
 
+// Offset of row (t, h); ld and heads * width fit 32 bits.
 __device__ __forceinline__ int64_t row_offset(int row, int heads, int width, int64_t ld) {
-    if (heads == 1) return (int64_t)row * ld;
-    const int t = row / heads;
-    return (int64_t)t * ld + (int64_t)(row - t * heads) * width;
+    if (heads == 1) return (int64_t)((uint64_t)(uint32_t)row * (uint32_t)ld);
+    const int t = (heads & (heads - 1)) == 0 ? row >> (31 - __clz(heads)) : row / heads;
+    return (int64_t)((uint64_t)(uint32_t)t * (uint32_t)ld) + (row - t * heads) * width;
 }
 
 // Rows in registers.  A block stays for many rows: the weight's values stay too, and the next rows are on their way while the present
@@ -257,52 +260,79 @@ __global__ void __launch_bounds__(256, 2) norm_loop_kernel(const NormArgs a, con
 }
 
 // Rows in registers, with the sums of the weight's gradient.
-template <typename XT, typename YT, int NV, bool LAYER>
+// FULL: the chunks of a group's threads are the row's, none lies behind it.
+template <typename XT, typename YT, int NV, bool LAYER, bool FULL>
 __global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER)) norm_grad_rows_kernel(const NormGradArgs a, const int group) {
     constexpr int R = rows_together(NV), N = LAYER ? 2 * R : R;
     __shared__ float scratch[2 * 16 * N];
-    extern __shared__ float sums[];                           // [groups][width]
+    extern __shared__ float sums[];                           // the weight, in the end the sums [groups][width]
     const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
     int half = 0;
     const float inv = 1.f / (float)a.width;
+    for (int c = threadIdx.x; c < a.width; c += blockDim.x) sums[c] = load_any(a.weight, a.w_type, c);
+    __syncthreads();
     float acc_w[NV][8], acc_b[LAYER ? NV : 1][8];
+    bool in[NV];                                              // chunks of this thread inside the row; the others are zeros throughout
+    Raw8<XT> x[R][NV], ds[R][NV];
+    Raw8<YT> dy[R][NV];
+    const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+        in[j] = FULL || (j * group + lane) * kChunk < a.width;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             acc_w[j][i] = 0.f;
             if (LAYER) acc_b[j][i] = 0.f;
         }
-    const XT* px = static_cast<const XT*>(a.x);
-    const YT* pdy = static_cast<const YT*>(a.dy);
-    Raw8<XT> x[R][NV];
-    Raw8<YT> dy[R][NV];
+        if (!FULL) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                x[k][j] = ds[k][j] = pack8<XT>(zeros);
+                dy[k][j] = pack8<YT>(zeros);
+            }
+        }
+    }
+    const XT* px = static_cast<const XT*>(a.x) + lane * kChunk;
+    const YT* pdy = static_cast<const YT*>(a.dy) + lane * kChunk;
+    const XT* pds = static_cast<const XT*>(a.d_sum) + lane * kChunk;
+    XT* pdx = static_cast<XT*>(a.dx) + lane * kChunk;
+    const int step = group * kChunk;                          // from a chunk of a thread to its next
     float rstd[R], mean[R];
-    auto fetch = [&](int64_t first) {
+    auto fetch = [&](int64_t first) {                         // rows behind the last one: the last one again, left out where it is used
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const int64_t r = first + (int64_t)k * groups;
-            const bool on = r < a.rows;
-            const int row = on ? (int)r : 0, W = on ? a.width : 0;
+            const int row = (int)min(first + (int64_t)k * groups, (int64_t)a.rows - 1);
+            const XT* p = px + row_offset(row, a.heads, a.width, a.ld_x);
+            const YT* q = pdy + row_offset(row, a.heads, a.width, a.ld_dy);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) x[k][j] = load_chunk(px + row_offset(row, a.heads, a.width, a.ld_x), j, lane, group, W);
+            for (int j = 0; j < NV; ++j)
+                if (in[j]) x[k][j] = load8(p + j * step);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) dy[k][j] = load_chunk(pdy + row_offset(row, a.heads, a.width, a.ld_dy), j, lane, group, W);
-            rstd[k] = on ? a.rstd[row] : 0.f;
-            mean[k] = LAYER && on ? a.mean[row] : 0.f;
+            for (int j = 0; j < NV; ++j)
+                if (in[j]) dy[k][j] = load8(q + j * step);
+            rstd[k] = a.rstd[row];
+            mean[k] = LAYER ? a.mean[row] : 0.f;
         }
     };
     const int64_t stride = (int64_t)gridDim.x * groups * R;
     int64_t base = (int64_t)blockIdx.x * groups * R;
-    if (base < a.rows) fetch(base + index);
-    for (; base < a.rows; base += stride) {
+    // one round of the block; whole: all of its rows exist
+    auto round = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
         float n[R][NV][8], g[R][NV][8], c[N], r[R];
+        bool on[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) on[k] = WHOLE || base + index + (int64_t)k * groups < a.rows;
 #pragma unroll
         for (int i = 0; i < N; ++i) c[i] = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            float w[8];
-            load_weight(a.weight, a.w_type, j, lane, group, a.width, w);
+            float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (in[j]) {
+                const float4 lo = *reinterpret_cast<const float4*>(sums + lane * kChunk + j * step);
+                const float4 hi = *reinterpret_cast<const float4*>(sums + lane * kChunk + j * step + 4);
+                w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w; w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+            }
 #pragma unroll
             for (int k = 0; k < R; ++k) {
                 unpack8<XT>(x[k][j], n[k][j]);
@@ -310,6 +340,7 @@ __global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     n[k][j][i] = (LAYER ? n[k][j][i] - mean[k] : n[k][j][i]) * rstd[k];
+                    if (!WHOLE && !on[k]) n[k][j][i] = g[k][j][i] = 0.f;
                     acc_w[j][i] = fmaf(g[k][j][i], n[k][j][i], acc_w[j][i]);
                     if (LAYER) acc_b[j][i] += g[k][j][i];
                     g[k][j][i] *= w[i];
@@ -318,40 +349,42 @@ __global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER
                 }
             }
         }
-        Raw8<XT> ds[R][NV];
+        int64_t at[R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             r[k] = rstd[k];
-            const bool on = base + index + (int64_t)k * groups < a.rows;
-            const int row = on ? (int)(base + index + (int64_t)k * groups) : 0;
+            const int row = (int)min(base + index + (int64_t)k * groups, (int64_t)a.rows - 1);
+            at[k] = row_offset(row, a.heads, a.width, a.ld_dx);
             if (a.has_d_sum) {
-                const XT* p = static_cast<const XT*>(a.d_sum) + row_offset(row, a.heads, a.width, a.ld_d_sum);
+                const XT* p = pds + row_offset(row, a.heads, a.width, a.ld_d_sum);
 #pragma unroll
-                for (int j = 0; j < NV; ++j) ds[k][j] = load_chunk(p, j, lane, group, on ? a.width : 0);
+                for (int j = 0; j < NV; ++j)
+                    if (in[j]) ds[k][j] = load8(p + j * step);
             }
         }
         fetch(base + stride + index);                         // the next rows are on their way while these are reduced
         group_sum(c, group, index, scratch, half);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const bool on = base + index + (int64_t)k * groups < a.rows;
-            const int row = on ? (int)(base + index + (int64_t)k * groups) : 0;
-            const float c0 = c[k] * inv, c1 = LAYER ? c[LAYER ? R + k : 0] * inv : 0.f;
-            XT* dx = static_cast<XT*>(a.dx) + row_offset(row, a.heads, a.width, a.ld_dx);
+            const float c0 = -c[k] * inv * r[k], c1 = LAYER ? c[LAYER ? R + k : 0] * inv : 0.f;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[k][j][i] = fmaf(-n[k][j][i], c0, LAYER ? g[k][j][i] - c1 : g[k][j][i]) * r[k];
+                for (int i = 0; i < 8; ++i) g[k][j][i] = fmaf(LAYER ? g[k][j][i] - c1 : g[k][j][i], r[k], n[k][j][i] * c0);
                 if (a.has_d_sum) {
                     float s[8];
                     unpack8<XT>(ds[k][j], s);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) g[k][j][i] += s[i];
                 }
-                store_chunk(dx, j, lane, group, on ? a.width : 0, pack8<XT>(g[k][j]));
+                if (in[j] && on[k]) store8(pdx + at[k] + j * step, pack8<XT>(g[k][j]));
             }
         }
-    }
+    };
+    if (base < a.rows) fetch(base + index);
+    for (; base + groups * R <= a.rows; base += stride) round(std::true_type());
+    if (base < a.rows) round(std::false_type());
+    __syncthreads();                                          // the weight is not needed any more
 #pragma unroll
     for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
         float* out = which ? a.part_b : a.part_w;
@@ -483,7 +516,7 @@ GradPlan grad_plan(int64_t rows, int width, bool layer, bool x_is_fp32, bool vec
     g.rows = vector && width <= kRowWidth;
     g.p = g.rows ? norm_plan(width) : loop_plan(width);
     const int groups = g.p.block / g.p.group;
-    g.smem = g.rows ? (groups > 1 ? groups * width * 4 : 0) : groups * width * 4 * (layer ? 2 : 1);
+    g.smem = g.rows ? groups * width * 4 : groups * width * 4 * (layer ? 2 : 1);
     // as many blocks as run at once: by registers; by shared memory one, two or more
     const int most = sms * (g.rows ? grad_blocks_sm(g.p.nv, x_is_fp32, layer) : g.smem > 100 * 1024 ? 1 : width > 2048 ? 2 : 4);
     const int together = g.rows ? rows_together(g.p.nv) : 1;
@@ -495,9 +528,21 @@ template <typename XT, typename YT, bool LAYER>
 cudaError_t norm_grad_typed(const NormGradArgs& a, const GradPlan& g, cudaStream_t st) {
     const dim3 grid(g.blocks), block(g.p.block);
     if (!g.rows) return launch_plain(norm_grad_loop_kernel<XT, YT, LAYER>, grid, block, g.smem, st, a, g.p.group);
-    if (g.p.nv == 1) return launch_plain(norm_grad_rows_kernel<XT, YT, 1, LAYER>, grid, block, g.smem, st, a, g.p.group);
-    if (g.p.nv == 2) return launch_plain(norm_grad_rows_kernel<XT, YT, 2, LAYER>, grid, block, g.smem, st, a, g.p.group);
-    return launch_plain(norm_grad_rows_kernel<XT, YT, 4, LAYER>, grid, block, g.smem, st, a, g.p.group);
+    if (g.p.group * g.p.nv * kChunk == a.width) {
+        if (g.p.nv == 1) return launch_plain(norm_grad_rows_kernel<XT, YT, 1, LAYER, true>, grid, block, g.smem, st, a, g.p.group);
+        if (g.p.nv == 2) return launch_plain(norm_grad_rows_kernel<XT, YT, 2, LAYER, true>, grid, block, g.smem, st, a, g.p.group);
+        return launch_plain(norm_grad_rows_kernel<XT, YT, 4, LAYER, true>, grid, block, g.smem, st, a, g.p.group);
+    }
+    if (g.p.nv == 1) return launch_plain(norm_grad_rows_kernel<XT, YT, 1, LAYER, false>, grid, block, g.smem, st, a, g.p.group);
+    if (g.p.nv == 2) return launch_plain(norm_grad_rows_kernel<XT, YT, 2, LAYER, false>, grid, block, g.smem, st, a, g.p.group);
+    return launch_plain(norm_grad_rows_kernel<XT, YT, 4, LAYER, false>, grid, block, g.smem, st, a, g.p.group);
+}
+
+template <typename XT, typename YT, bool LAYER>
+cudaError_t init_grad_rows() {
+    return init_all(0, norm_grad_rows_kernel<XT, YT, 1, LAYER, false>, norm_grad_rows_kernel<XT, YT, 2, LAYER, false>,
+                    norm_grad_rows_kernel<XT, YT, 4, LAYER, false>, norm_grad_rows_kernel<XT, YT, 1, LAYER, true>,
+                    norm_grad_rows_kernel<XT, YT, 2, LAYER, true>, norm_grad_rows_kernel<XT, YT, 4, LAYER, true>);
 }
 
 // x and y of one type, or x fp32 (a residual stream) and y of 16 bits.
@@ -528,11 +573,9 @@ cudaError_t init_norm_kernels() {
         const cudaError_t e = for_types(t < 3 ? 0 : t - 2, t < 3 ? t : t - 2, [&](auto* x, auto* y) {
             using XT = std::remove_pointer_t<decltype(x)>;
             using YT = std::remove_pointer_t<decltype(y)>;
-            const cudaError_t r = init_all(0, norm_rows_kernel<XT, YT, 1>, norm_rows_kernel<XT, YT, 2>, norm_rows_kernel<XT, YT, 4>,
-                                           norm_loop_kernel<XT, YT>, norm_grad_rows_kernel<XT, YT, 1, false>,
-                                           norm_grad_rows_kernel<XT, YT, 1, true>, norm_grad_rows_kernel<XT, YT, 2, false>,
-                                           norm_grad_rows_kernel<XT, YT, 2, true>, norm_grad_rows_kernel<XT, YT, 4, false>,
-                                           norm_grad_rows_kernel<XT, YT, 4, true>);
+            cudaError_t r = init_all(0, norm_rows_kernel<XT, YT, 1>, norm_rows_kernel<XT, YT, 2>, norm_rows_kernel<XT, YT, 4>, norm_loop_kernel<XT, YT>);
+            if (r == cudaSuccess) r = init_grad_rows<XT, YT, false>();
+            if (r == cudaSuccess) r = init_grad_rows<XT, YT, true>();
             return r != cudaSuccess ? r : init_all(kLoopSmem, norm_grad_loop_kernel<XT, YT, false>, norm_grad_loop_kernel<XT, YT, true>);
         });
         if (e != cudaSuccess) return e;
