@@ -676,8 +676,6 @@ def mars_grads_clip(grads: GradList, max_norm: float, out_norm: torch.Tensor, st
 # ------------------------------------------------------------------------- operators of a training pass
 
 MARS_NORM_RMS, MARS_NORM_LAYER = 0, 1
-_ALL_TYPES = tuple(MARS_TYPES)
-_F32, _I32 = (torch.float32,), (torch.int32,)
 
 
 class Train:
@@ -698,9 +696,13 @@ class Train:
             _check(lib().mars_train_create(max_width, max_experts, max_seqs, _ptr(self.workspace), nbytes, byref(handle)),
                    "mars_train_create")
         self.handle = handle
-        self._forms = {}
+        self._forms, self._index = {}, self.device.index
 
-    _stream = Update._stream
+    def _stream(self, stream) -> int:
+        raw = stream.cuda_stream if stream is not None else _raw_stream(self._index)
+        if raw != self._home:       # the workspace must outlive the call there, even if the handle does not
+            self.workspace.record_stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+        return raw
 
     def close(self):
         if getattr(self, "handle", None):
@@ -714,40 +716,55 @@ class Train:
             pass
 
 
-def _heads(t: torch.Tensor, name: str, dtypes, dev: torch.device, shape) -> int:
-    """The row stride of a [n, width] or [n, heads, width] tensor whose heads lie next to each other; ValueError otherwise."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.shape != shape:
-        raise ValueError(f"{name}: expected {tuple(str(d) for d in dtypes)} {tuple(shape)}, got "
+# Small calls are bound by the host: these checks look at the common case in a few plain comparisons and leave the message to _want.
+
+def _vector(t, name, dtype, train, n):
+    """Address of a contiguous one-dimensional tensor of n values of the handle's device; ValueError otherwise."""
+    if t.__class__ is not torch.Tensor or t.dtype is not dtype or t.numel() != n or t.dim() != 1 or t.get_device() != train._index or \
+            not t.is_contiguous():
+        _want(t, name, (dtype,), train.device, n)
+    return t.data_ptr()
+
+
+def _like(t, name, dtype, train, shape):
+    """The same for any shape."""
+    if t.__class__ is not torch.Tensor or t.dtype is not dtype or t.shape != shape or t.get_device() != train._index or not t.is_contiguous():
+        _want(t, name, (dtype,), train.device, *shape)
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, name: str, dtype, train, shape, row: int) -> int:
+    """The row stride of a [n, width] or [n, heads, width] tensor (row = heads * width) whose heads lie next to each other; ValueError
+    otherwise.  dtype None: fp32, bf16 or fp16."""
+    if not isinstance(t, torch.Tensor) or (t.dtype is not dtype if dtype is not None else t.dtype not in MARS_TYPES) or t.shape != shape:
+        raise ValueError(f"{name}: expected {dtype or tuple(MARS_TYPES)} {tuple(shape)}, got "
                          f"{getattr(t, 'dtype', type(t))} {tuple(getattr(t, 'shape', ()))}")
-    if t.get_device() != (-1 if dev.index is None else dev.index):
-        raise ValueError(f"{name}: on {t.device}, the handle on {dev}")
-    strides, width = t.stride(), shape[-1]
-    row = width if len(shape) == 2 else shape[1] * width
-    if (width > 1 and strides[-1] != 1) or (len(shape) == 3 and shape[1] > 1 and strides[1] != width):
-        raise ValueError(f"{name}: strides {strides} are not supported")
-    if shape[0] <= 1:
+    if t.get_device() != train._index:
+        raise ValueError(f"{name}: on {t.device}, the handle on {train.device}")
+    if t.is_contiguous():
         return row
-    if strides[0] < row:
+    strides, width = t.stride(), shape[-1]
+    if (width > 1 and strides[-1] != 1) or (len(shape) == 3 and shape[1] > 1 and strides[1] != width) or (shape[0] > 1 and strides[0] < row):
         raise ValueError(f"{name}: strides {strides} are not supported")
-    return strides[0]
+    return strides[0] if shape[0] > 1 else row
 
 
-def _norm_form(train: Train, kind: int, x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor, eps: float) -> mars_norm_t:
-    key = (kind, x.shape[1:], x.dtype, y.dtype, weight.dtype, eps)
+def _norm_form(train: Train, kind: int, x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor, eps: float, heads: int, width: int):
+    key = (kind, width, heads, x.dtype, y.dtype, weight.dtype, eps)
     form = train._forms.get(key)
     if form is None:
-        heads = x.shape[1] if x.dim() == 3 else 1
         if len(train._forms) >= 256:
             train._forms.clear()
-        form = train._forms[key] = mars_norm_t(kind, x.shape[-1], heads, MARS_TYPES[x.dtype], MARS_TYPES[y.dtype],
-                                               MARS_TYPES[weight.dtype], float(eps), 0)
-    return form
+        form = mars_norm_t(kind, width, heads, MARS_TYPES[x.dtype], MARS_TYPES[y.dtype], MARS_TYPES[weight.dtype], float(eps), 0)
+        form = train._forms[key] = (byref(form), form)
+    return form[0]
 
 
-def _norm_shapes(x):
+def _norm_shape(x):
     if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
         raise ValueError("x: expected [n, width] or [n, heads, width]")
-    return x.shape, x.shape[:-1], x.shape[-1]
+    shape = x.shape
+    return (shape, shape[0], 1, shape[1]) if len(shape) == 2 else (shape, shape[0], shape[1], shape[2])
 
 
 def mars_norm(train: Train, kind: int, x: torch.Tensor, weight: torch.Tensor, eps: float, y: torch.Tensor,
@@ -755,25 +772,27 @@ def mars_norm(train: Train, kind: int, x: torch.Tensor, weight: torch.Tensor, ep
               out_sum: torch.Tensor = None, stream=None) -> int:
     """y = norm(x + add) of every row of [n, width], or of every head of [n, heads, width] (any row stride); kind MARS_NORM_RMS
     or MARS_NORM_LAYER.  rstd, mean: fp32, one for each row, for mars_norm_grad.  out_sum: x + add.  Returns the status code."""
-    shape, rows, width = _norm_shapes(x)
-    dev = train.device
-    ld_x = _heads(x, "x", _ALL_TYPES, dev, shape)
-    ld_y = _heads(y, "y", _ALL_TYPES, dev, shape)
-    _want(weight, "weight", _ALL_TYPES, dev, width)
+    shape, n, heads, width = _norm_shape(x)
+    row = heads * width
+    ld_x = _heads(x, "x", None, train, shape, row)
+    ld_y = _heads(y, "y", None, train, shape, row)
+    if not isinstance(weight, torch.Tensor) or weight.dtype not in MARS_TYPES:
+        raise ValueError(f"weight: expected {tuple(MARS_TYPES)}")
+    p_weight = _vector(weight, "weight", weight.dtype, train, width)
     ld_add = ld_sum = 0
+    p_add = p_sum = p_bias = p_rstd = p_mean = None
     if add is not None:
-        ld_add = _heads(add, "add", (y.dtype,), dev, shape)
+        ld_add, p_add = _heads(add, "add", y.dtype, train, shape, row), add.data_ptr()
     if out_sum is not None:
-        ld_sum = _heads(out_sum, "out_sum", (x.dtype,), dev, shape)
+        ld_sum, p_sum = _heads(out_sum, "out_sum", x.dtype, train, shape, row), out_sum.data_ptr()
     if bias is not None:
-        _want(bias, "bias", (weight.dtype,), dev, width)
+        p_bias = _vector(bias, "bias", weight.dtype, train, width)
     if rstd is not None:
-        _want(rstd, "rstd", _F32, dev, *rows)
+        p_rstd = _like(rstd, "rstd", torch.float32, train, (n,) if len(shape) == 2 else (n, heads))
     if mean is not None:
-        _want(mean, "mean", _F32, dev, *rows)
-    form = _norm_form(train, kind, x, y, weight, eps)
-    return lib().mars_norm(train.handle, train._stream(stream), byref(form), shape[0], x.data_ptr(), ld_x, _opt(add), ld_add,
-                           _opt(out_sum), ld_sum, weight.data_ptr(), _opt(bias), y.data_ptr(), ld_y, _opt(mean), _opt(rstd))
+        p_mean = _like(mean, "mean", torch.float32, train, (n,) if len(shape) == 2 else (n, heads))
+    return lib().mars_norm(train.handle, train._stream(stream), _norm_form(train, kind, x, y, weight, eps, heads, width), n, x.data_ptr(), ld_x,
+                           p_add, ld_add, p_sum, ld_sum, p_weight, p_bias, y.data_ptr(), ld_y, p_mean, p_rstd)
 
 
 def mars_norm_grad(train: Train, kind: int, dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor,
@@ -781,32 +800,36 @@ def mars_norm_grad(train: Train, kind: int, dy: torch.Tensor, x: torch.Tensor, w
                    d_sum: torch.Tensor = None, accumulate: bool = False, stream=None) -> int:
     """dx (+ d_sum), dw and db of mars_norm; x: what was normalised (out_sum where there was an addition), rstd and mean those of
     the forward call.  accumulate: add to dw and db.  Returns the status code."""
-    shape, rows, width = _norm_shapes(x)
-    dev = train.device
-    ld_x = _heads(x, "x", _ALL_TYPES, dev, shape)
-    ld_dy = _heads(dy, "dy", _ALL_TYPES, dev, shape)
-    ld_dx = _heads(dx, "dx", (x.dtype,), dev, shape)
-    _want(weight, "weight", _ALL_TYPES, dev, width)
-    _want(rstd, "rstd", _F32, dev, *rows)
+    shape, n, heads, width = _norm_shape(x)
+    row = heads * width
+    ld_x = _heads(x, "x", None, train, shape, row)
+    ld_dy = _heads(dy, "dy", None, train, shape, row)
+    ld_dx = _heads(dx, "dx", x.dtype, train, shape, row)
+    if not isinstance(weight, torch.Tensor) or weight.dtype not in MARS_TYPES:
+        raise ValueError(f"weight: expected {tuple(MARS_TYPES)}")
+    p_weight = _vector(weight, "weight", weight.dtype, train, width)
+    rows = (n,) if len(shape) == 2 else (n, heads)
+    p_rstd = _like(rstd, "rstd", torch.float32, train, rows)
     ld_sum, dw_type = 0, 0
+    p_mean = p_d_sum = p_dw = p_db = None
     if mean is not None:
-        _want(mean, "mean", _F32, dev, *rows)
+        p_mean = _like(mean, "mean", torch.float32, train, rows)
     if d_sum is not None:
-        ld_sum = _heads(d_sum, "d_sum", (x.dtype,), dev, shape)
-    if dw is not None:
-        _want(dw, "dw", _ALL_TYPES, dev, width)
-        dw_type = MARS_TYPES[dw.dtype]
-    if db is not None:
-        _want(db, "db", _ALL_TYPES if dw is None else (dw.dtype,), dev, width)
-        dw_type = MARS_TYPES[db.dtype]
-    form = _norm_form(train, kind, x, dy, weight, 1.0)         # eps is in rstd
-    return lib().mars_norm_grad(train.handle, train._stream(stream), byref(form), shape[0], dy.data_ptr(), ld_dy, x.data_ptr(), ld_x,
-                                weight.data_ptr(), _opt(mean), rstd.data_ptr(), _opt(d_sum), ld_sum, dx.data_ptr(), ld_dx, _opt(dw),
-                                _opt(db), dw_type, int(bool(accumulate)))
-
-
-def _opt(t):
-    return None if t is None else t.data_ptr()
+        ld_sum, p_d_sum = _heads(d_sum, "d_sum", x.dtype, train, shape, row), d_sum.data_ptr()
+    for t, name in ((dw, "dw"), (db, "db")):
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or t.dtype not in MARS_TYPES or (name == "db" and dw is not None and t.dtype is not dw.dtype):
+            raise ValueError(f"{name}: expected {tuple(MARS_TYPES) if dw is None or t is dw else dw.dtype}")
+        dw_type = MARS_TYPES[t.dtype]
+        if name == "dw":
+            p_dw = _vector(t, name, t.dtype, train, width)
+        else:
+            p_db = _vector(t, name, t.dtype, train, width)
+    # eps is in rstd
+    return lib().mars_norm_grad(train.handle, train._stream(stream), _norm_form(train, kind, x, dy, weight, 1.0, heads, width), n, dy.data_ptr(),
+                                ld_dy, x.data_ptr(), ld_x, p_weight, p_mean, p_rstd, p_d_sum, ld_sum, dx.data_ptr(), ld_dx, p_dw, p_db,
+                                dw_type, int(bool(accumulate)))
 
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
@@ -833,9 +856,9 @@ class Rope:
             self._home = _raw_stream(self.device.index)
             handle = c_void_p()
             _check(lib().mars_rope_create(byref(self.form), _ptr(self.workspace), nbytes, byref(handle)), "mars_rope_create")
-        self.handle = handle
+        self.handle, self._index = handle, self.device.index
 
-    _stream = Update._stream
+    _stream = Train._stream
 
     def frequencies(self) -> torch.Tensor:
         """Angle of every pair for one position (fp64, on the host)."""
@@ -865,20 +888,29 @@ def mars_rope(rope: Rope, positions: torch.Tensor, q: torch.Tensor, out_q: torch
     inputs themselves.  Returns the status code."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or (k is not None and (not isinstance(k, torch.Tensor) or k.dim() != 3)):
         raise ValueError("q, k: expected [n, heads, head_dim]")
-    dev, (n, heads, dim) = rope.device, q.shape
-    _want(positions, "positions", _I32, dev, n)
-    ld_q = _heads(q, "q", _ALL_TYPES, dev, q.shape)
-    ld_oq = _heads(out_q, "out_q", (q.dtype,), dev, q.shape)
+    shape = q.shape
+    n, heads, dim = shape
+    p_positions = _vector(positions, "positions", torch.int32, rope, n)
+    ld_q = _heads(q, "q", None, rope, shape, heads * dim)
+    ld_oq = _heads(out_q, "out_q", q.dtype, rope, shape, heads * dim)
     k_heads = ld_k = ld_ok = 0
+    p_k = p_ok = None
     if k is not None:
         k_heads = k.shape[1]
         if k.shape[0] != n or k.shape[2] != dim:
             raise ValueError(f"k: expected {(n, k_heads, dim)}, got {tuple(k.shape)}")
-        ld_k = _heads(k, "k", (q.dtype,), dev, k.shape)
-        ld_ok = _heads(out_k, "out_k", (q.dtype,), dev, k.shape)
-    return lib().mars_rope(rope.handle, rope._stream(stream), n, positions.data_ptr(), dim, MARS_TYPES[q.dtype], q.data_ptr(), ld_q, heads,
-                           out_q.data_ptr(), ld_oq, _opt(k), ld_k, k_heads, _opt(out_k) if k is not None else None, ld_ok,
-                           int(bool(inverse)))
+        ld_k, p_k = _heads(k, "k", q.dtype, rope, k.shape, k_heads * dim), k.data_ptr()
+        ld_ok = _heads(out_k, "out_k", q.dtype, rope, k.shape, k_heads * dim)
+        p_ok = out_k.data_ptr()
+    return lib().mars_rope(rope.handle, rope._stream(stream), n, p_positions, dim, MARS_TYPES[q.dtype], q.data_ptr(), ld_q, heads,
+                           out_q.data_ptr(), ld_oq, p_k, ld_k, k_heads, p_ok, ld_ok, 1 if inverse else 0)
+
+
+def _logits(t, name, dtype, train, n, experts):
+    if t.dtype is not dtype or t.shape != (n, experts) or t.get_device() != train._index or not t.is_contiguous():
+        _want(t, name, (dtype,), train.device, n, experts, rows=True)
+        return _ld(t)
+    return max(experts, 1)
 
 
 def mars_router(train: Train, logits: torch.Tensor, out_idx: torch.Tensor, out_weights: torch.Tensor, out_lse: torch.Tensor = None,
@@ -888,18 +920,25 @@ def mars_router(train: Train, logits: torch.Tensor, out_idx: torch.Tensor, out_w
     [experts], offsets [experts + 1], prob_sums [experts], losses [2] = balance and z.  live: bool [n].  Returns the status code."""
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not isinstance(out_idx, torch.Tensor) or out_idx.dim() != 2:
         raise ValueError("logits: expected [n, experts]; out_idx: expected [n, top_k]")
-    dev, (n, experts), k = train.device, logits.shape, out_idx.shape[1]
-    _want(logits, "logits", _ALL_TYPES, dev, n, experts, rows=True)
-    _want(out_idx, "out_idx", _I32, dev, n, k)
-    _want(out_weights, "out_weights", _F32, dev, n, k)
-    for t, name, dtypes, size in ((out_lse, "out_lse", _F32, n), (out_counts, "out_counts", _I32, experts),
-                                  (out_offsets, "out_offsets", _I32, experts + 1), (out_prob_sums, "out_prob_sums", _F32, experts),
-                                  (out_losses, "out_losses", _F32, 2), (live, "live", (torch.bool, torch.uint8), n)):
-        if t is not None:
-            _want(t, name, dtypes, dev, size)
-    return lib().mars_router(train.handle, train._stream(stream), n, experts, k, logits.data_ptr(), _ld(logits), MARS_TYPES[logits.dtype],
-                             _opt(live), int(bool(renormalise)), out_idx.data_ptr(), out_weights.data_ptr(), _opt(out_lse),
-                             _opt(out_counts), _opt(out_offsets), _opt(out_prob_sums), _opt(out_losses))
+    if logits.dtype not in MARS_TYPES:
+        raise ValueError(f"logits: expected {tuple(MARS_TYPES)}")
+    (n, experts), k = logits.shape, out_idx.shape[1]
+    ld = _logits(logits, "logits", logits.dtype, train, n, experts)
+    p_idx = _like(out_idx, "out_idx", torch.int32, train, (n, k))
+    p_weights = _like(out_weights, "out_weights", torch.float32, train, (n, k))
+    p_live = None
+    if live is not None:
+        if not isinstance(live, torch.Tensor) or live.dtype not in (torch.bool, torch.uint8):
+            raise ValueError("live: expected bool")
+        p_live = _vector(live, "live", live.dtype, train, n)
+    f32, i32 = torch.float32, torch.int32
+    return lib().mars_router(train.handle, train._stream(stream), n, experts, k, logits.data_ptr(), ld, MARS_TYPES[logits.dtype],
+                             p_live, 1 if renormalise else 0, p_idx, p_weights,
+                             None if out_lse is None else _vector(out_lse, "out_lse", f32, train, n),
+                             None if out_counts is None else _vector(out_counts, "out_counts", i32, train, experts),
+                             None if out_offsets is None else _vector(out_offsets, "out_offsets", i32, train, experts + 1),
+                             None if out_prob_sums is None else _vector(out_prob_sums, "out_prob_sums", f32, train, experts),
+                             None if out_losses is None else _vector(out_losses, "out_losses", f32, train, 2))
 
 
 def mars_router_grad(train: Train, logits: torch.Tensor, idx: torch.Tensor, lse: torch.Tensor, counts: torch.Tensor,
@@ -909,17 +948,18 @@ def mars_router_grad(train: Train, logits: torch.Tensor, idx: torch.Tensor, lse:
     code.  d_logits may be logits itself."""
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not isinstance(idx, torch.Tensor) or idx.dim() != 2:
         raise ValueError("logits: expected [n, experts]; idx: expected [n, top_k]")
-    dev, (n, experts), k = train.device, logits.shape, idx.shape[1]
-    _want(logits, "logits", _ALL_TYPES, dev, n, experts, rows=True)
-    _want(idx, "idx", _I32, dev, n, k)
-    _want(lse, "lse", _F32, dev, n)
-    _want(counts, "counts", _I32, dev, experts)
-    _want(d_logits, "d_logits", (logits.dtype,), dev, n, experts, rows=True)
-    if d_weights is not None:
-        _want(d_weights, "d_weights", _F32, dev, n, k)
-    return lib().mars_router_grad(train.handle, train._stream(stream), n, experts, k, logits.data_ptr(), _ld(logits),
-                                  MARS_TYPES[logits.dtype], idx.data_ptr(), lse.data_ptr(), counts.data_ptr(), _opt(d_weights),
-                                  int(bool(renormalise)), float(balance_coef), float(z_coef), d_logits.data_ptr(), _ld(d_logits))
+    if logits.dtype not in MARS_TYPES:
+        raise ValueError(f"logits: expected {tuple(MARS_TYPES)}")
+    (n, experts), k = logits.shape, idx.shape[1]
+    ld = _logits(logits, "logits", logits.dtype, train, n, experts)
+    if not isinstance(d_logits, torch.Tensor):
+        raise ValueError("d_logits: expected a tensor")
+    ld_d = _logits(d_logits, "d_logits", logits.dtype, train, n, experts)
+    return lib().mars_router_grad(train.handle, train._stream(stream), n, experts, k, logits.data_ptr(), ld, MARS_TYPES[logits.dtype],
+                                  _like(idx, "idx", torch.int32, train, (n, k)), _vector(lse, "lse", torch.float32, train, n),
+                                  _vector(counts, "counts", torch.int32, train, experts),
+                                  None if d_weights is None else _like(d_weights, "d_weights", torch.float32, train, (n, k)),
+                                  1 if renormalise else 0, float(balance_coef), float(z_coef), d_logits.data_ptr(), ld_d)
 
 
 POLICY_REDUCE = {"tokens": 0, "sequences": 1, "sum": 2}
@@ -934,18 +974,18 @@ def mars_policy_loss(train: Train, logprobs: torch.Tensor, old_logprobs: torch.T
     "tokens", "sequences" or "sum".  Returns the status code."""
     if reduce not in POLICY_REDUCE:
         raise ValueError(f"reduce: one of {tuple(POLICY_REDUCE)}")
-    dev, n, seqs = train.device, logprobs.shape[0], seq_off.shape[0] - 1
-    _want(logprobs, "logprobs", _F32, dev, n)
-    _want(old_logprobs, "old_logprobs", _F32, dev, n)
-    _want(advantages, "advantages", _F32, dev, n if per_token else seqs)
-    _want(targets, "targets", _I32, dev, n)
-    _want(seq_off, "seq_off", _I32, dev, seqs + 1)
-    _want(out_stats, "out_stats", _F32, dev, 6)
-    if out_d_logprobs is not None:
-        _want(out_d_logprobs, "out_d_logprobs", _F32, dev, n)
-    if ref_logprobs is not None:
-        _want(ref_logprobs, "ref_logprobs", _F32, dev, n)
-    form = mars_policy_t(clip_low, clip_high, kl_coef, scale, POLICY_REDUCE[reduce], int(per_token))
-    return lib().mars_policy_loss(train.handle, train._stream(stream), byref(form), n, seqs, seq_off.data_ptr(), targets.data_ptr(),
-                                  logprobs.data_ptr(), old_logprobs.data_ptr(), _opt(ref_logprobs), advantages.data_ptr(),
-                                  out_stats.data_ptr(), _opt(out_d_logprobs))
+    n, seqs, f32, i32 = logprobs.shape[0], seq_off.shape[0] - 1, torch.float32, torch.int32
+    key = (clip_low, clip_high, kl_coef, scale, reduce, per_token)
+    form = train._forms.get(key)
+    if form is None:
+        if len(train._forms) >= 256:
+            train._forms.clear()
+        form = mars_policy_t(clip_low, clip_high, kl_coef, scale, POLICY_REDUCE[reduce], int(bool(per_token)))
+        form = train._forms[key] = (byref(form), form)
+    return lib().mars_policy_loss(train.handle, train._stream(stream), form[0], n, seqs, _vector(seq_off, "seq_off", i32, train, seqs + 1),
+                                  _vector(targets, "targets", i32, train, n), _vector(logprobs, "logprobs", f32, train, n),
+                                  _vector(old_logprobs, "old_logprobs", f32, train, n),
+                                  None if ref_logprobs is None else _vector(ref_logprobs, "ref_logprobs", f32, train, n),
+                                  _vector(advantages, "advantages", f32, train, n if per_token else seqs),
+                                  _vector(out_stats, "out_stats", f32, train, 6),
+                                  None if out_d_logprobs is None else _vector(out_d_logprobs, "out_d_logprobs", f32, train, n))

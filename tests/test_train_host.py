@@ -199,7 +199,7 @@ def test_frequencies(lib, rotary, scaling):
 
 
 class Fake:                                               # stands for a handle: the checks come before the library
-    handle, device, max_width, max_experts, max_seqs, _forms = None, torch.device("cpu"), 64, 64, 64, {}
+    handle, device, max_width, max_experts, max_seqs, _forms, _index = None, torch.device("cpu"), 64, 64, 64, {}, -1
 
     def _stream(self, stream):
         return 0
