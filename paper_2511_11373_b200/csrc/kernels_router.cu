@@ -69,6 +69,35 @@ __device__ __forceinline__ void group_load4(const T* row, int j, int l, int expe
         }
     }
 }
+// Four values as they lie in memory.
+template <typename T> struct Four { uint2 v; };
+template <> struct Four<float> { float4 v; };
+__device__ __forceinline__ void unpack_four(const Four<float>& f, float (&o)[4]) { o[0] = f.v.x; o[1] = f.v.y; o[2] = f.v.z; o[3] = f.v.w; }
+template <typename T>
+__device__ __forceinline__ void unpack_four(const Four<T>& f, float (&o)[4]) {
+    unpack2(f.v.x, o[0], o[1], T());
+    unpack2(f.v.y, o[2], o[3], T());
+}
+template <typename T, int L, bool V>
+__device__ __forceinline__ Four<T> load_four(const T* row, int j, int l, int experts) {
+    Four<T> f;
+    if constexpr (V) {
+        const int c = (j * L + l) * 4;
+        if (c < experts) {
+            f.v = *reinterpret_cast<const decltype(f.v)*>(row + c);
+        } else if constexpr (sizeof(T) == 4) {
+            f.v = make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+            f.v = make_uint2(0u, 0u);
+        }
+    } else {
+        float o[4];
+        group_load4<T, L, false>(row, j, l, experts, o);
+        if constexpr (sizeof(T) == 4) f.v = make_float4(o[0], o[1], o[2], o[3]);
+        else f.v = make_uint2(pack2(o[0], o[1], T()), pack2(o[2], o[3], T()));
+    }
+    return f;
+}
 template <typename T, int L, bool V>
 __device__ __forceinline__ void group_store4(T* row, int j, int l, int experts, const float (&v)[4]) {
     if constexpr (V) {
@@ -577,40 +606,53 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const
 #pragma unroll
         for (int i = 0; i < 4; ++i) g[j][i] = expert(j, i) < E ? unit * a.counts[expert(j, i)] : 0.f;
     const int64_t stride = (int64_t)gridDim.x * kWarps * R;
-    // the next row's logits, lse and choices (the first L of them) are on their way while this row is worked on
-    float next[NG][4], next_lse = 0.f, next_dw = 0.f;
-    int next_idx = -1, next_first = -1;
-    auto fetch = [&](int64_t row) {
+    // the logits, lse and choices (the first L of them) of the next rows are on their way while this row is worked on: of two of 16 bits,
+    // of one of fp32 (registers)
+    constexpr int D = sizeof(T) == 2 && NG <= 4 ? 2 : 1;
+    Four<T> ahead[D][NG];
+    float ahead_lse[D], ahead_dw[D];
+    int ahead_idx[D], ahead_first[D];
+    auto fetch = [&](int64_t row, Four<T> (&z)[NG], float& lse, float& dw, int& idx, int& first) {
         const bool in_range = row < a.rows;
         const int64_t r = in_range ? row : 0;
 #pragma unroll
-        for (int j = 0; j < NG; ++j) group_load4<T, L, V>(static_cast<const T*>(a.logits) + r * a.ld, j, l, in_range ? E : 0, next[j]);
-        next_lse = in_range ? a.lse[r] : 0.f;
-        next_first = in_range ? a.idx[r * k] : -1;
-        next_idx = in_range && l < k ? a.idx[r * k + l] : -1;
-        next_dw = in_range && l < k && a.has_d_weights ? a.d_weights[r * k + l] : 0.f;
+        for (int j = 0; j < NG; ++j) z[j] = load_four<T, L, V>(static_cast<const T*>(a.logits) + r * a.ld, j, l, in_range ? E : 0);
+        lse = in_range ? a.lse[r] : 0.f;
+        first = in_range ? a.idx[r * k] : -1;
+        idx = in_range && l < k ? a.idx[r * k + l] : -1;
+        dw = in_range && l < k && a.has_d_weights ? a.d_weights[r * k + l] : 0.f;
     };
     int64_t base = ((int64_t)blockIdx.x * kWarps + warp) * R;
-    if (base < a.rows) fetch(base + sub);
+    if (base < a.rows) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) fetch(base + d * stride + sub, ahead[d], ahead_lse[d], ahead_dw[d], ahead_idx[d], ahead_first[d]);
+    }
     for (; base < a.rows; base += stride) {
-        const bool in_range = base + sub < a.rows, on = next_first >= 0;      // a row that took no part may hold anything
+        const bool in_range = base + sub < a.rows, on = ahead_first[0] >= 0;      // a row that took no part may hold anything
         const int64_t row = in_range ? base + sub : 0;
         const T* in = static_cast<const T*>(a.logits) + row * a.ld;
         T* out = static_cast<T*>(a.d_logits) + row * a.ld_d;
-        const int W = on ? E : 0, first_idx = next_idx;
-        const float lse = next_lse, first_dw = next_dw;
+        const int W = on ? E : 0, first_idx = ahead_idx[0];
+        const float lse = ahead_lse[0], first_dw = ahead_dw[0];
         float v[NG][4];
         float dot = 0.f;                                      // sum of p g, plus that of the selected where weights are p
 #pragma unroll
-        for (int j = 0; j < NG; ++j)
+        for (int j = 0; j < NG; ++j) {
+            unpack_four(ahead[0][j], v[j]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                v[j][i] = expert(j, i) < W ? ex2((next[j][i] - lse) * kLog2e) : 0.f;
+                v[j][i] = expert(j, i) < W ? ex2((v[j][i] - lse) * kLog2e) : 0.f;
                 dot = fmaf(v[j][i], g[j][i], dot);
             }
+        }
         float w_first = 0.f;                                  // p of this lane's first choice
         if (a.has_d_weights && on && (unsigned)first_idx < (unsigned)E) w_first = ex2((to_float(in[first_idx]) - lse) * kLog2e);
-        fetch(base + stride + sub);
+        if (D == 2) {
+#pragma unroll
+            for (int j = 0; j < NG; ++j) ahead[0][j] = ahead[D - 1][j];
+            ahead_lse[0] = ahead_lse[D - 1]; ahead_dw[0] = ahead_dw[D - 1]; ahead_idx[0] = ahead_idx[D - 1]; ahead_first[0] = ahead_first[D - 1];
+        }
+        fetch(base + D * stride + sub, ahead[D - 1], ahead_lse[D - 1], ahead_dw[D - 1], ahead_idx[D - 1], ahead_first[D - 1]);
         if (a.has_d_weights) {
             float w_sum = w_first, wdw = w_first != 0.f ? w_first * first_dw : 0.f;
             for (int i = l + L; i < k; i += L) {
