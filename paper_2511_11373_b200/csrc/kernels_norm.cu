@@ -324,6 +324,8 @@ __global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER
 #pragma unroll
         for (int k = 0; k < R; ++k) on[k] = WHOLE || base + index + (int64_t)k * groups < a.rows;
 #pragma unroll
+        for (int k = 0; k < R; ++k) r[k] = rstd[k];
+#pragma unroll
         for (int i = 0; i < N; ++i) c[i] = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -352,7 +354,6 @@ __global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER
         int64_t at[R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            r[k] = rstd[k];
             const int row = (int)min(base + index + (int64_t)k * groups, (int64_t)a.rows - 1);
             at[k] = row_offset(row, a.heads, a.width, a.ld_dx);
             if (a.has_d_sum) {

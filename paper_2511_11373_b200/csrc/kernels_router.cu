@@ -315,19 +315,20 @@ __global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_ker
     router_finish<kWarps>(a, sums, counts, z);
 }
 
-// Many rows: a thread has a row.  A warp brings 32 rows into shared memory (fp32, rows apart by an odd number of 16 bytes, so that eight
+// Many rows: two threads have a row, each half of its columns.  A warp brings 16 rows into shared memory (fp32, rows apart by an odd number of 16 bytes, so that eight
 // threads read their 16 bytes from different banks) and goes over them thread by thread.  The k <= 8 largest of a row lie in the eight
 // fours with the largest maxima; both choices, of fours and of logits, are made on 32-bit keys (leading bits that order like the value,
 // last bits that prefer the lower index), eight at a time: sorted (Batcher's odd-even merge, 19 exchanges) and merged into the eight
-// largest so far (the larger ones of the two ends, then a bitonic merge of 12 exchanges).  What bounds it is the integer pipe (half a
+// largest so far (the larger ones of the two ends, then a bitonic merge of 12 exchanges), and so are the two halves.  What bounds it is the integer pipe (half a
 // minimum or maximum a clock and scheduler): 8 of them a logit, where rounds over a warp took 40.  The keys hold bf16 and fp16 in full;
 // for fp32 a row whose last choice and largest loser agree in the leading bits, or whose choices are out of order, is checked against the
 // values, and chosen again by the warp where that shows a difference.  The same pass over the row takes the exponentials, which go back
 // to shared memory; the lanes then add the columns up.
 constexpr int kManyExperts = 256, kManyK = 8, kManyRows = 8192;
 // Warps of the one block that an SM's shared memory holds: few blocks leave few sums for the last one to add.
-template <bool WIDE> constexpr int kManyWarps = WIDE ? 6 : 12;
-__host__ __device__ constexpr int many_pitch(int experts) { return (experts + 31) / 32 * 32 + 4; }
+template <bool WIDE> constexpr int kManyWarps = WIDE ? 12 : 24;
+constexpr int kTileRows = 16;
+__host__ __device__ constexpr int many_pitch(int experts) { return (experts + 63) / 64 * 64 + 4; }
 
 __device__ __forceinline__ void exchange(uint32_t& a, uint32_t& b) {       // the larger one first
     const uint32_t m = max(a, b);
@@ -343,9 +344,8 @@ __device__ __forceinline__ void sort8(uint32_t (&k)[8]) {
     exchange(k[1], k[2]); exchange(k[3], k[4]); exchange(k[5], k[6]);
 }
 
-// Sorts eight keys into the eight largest so far; lost: the largest that is not among them.
-__device__ __forceinline__ void take8(uint32_t (&best)[8], uint32_t (&key)[8], uint32_t& lost) {
-    sort8(key);
+// Merges eight sorted keys into the eight largest so far; lost: the largest that is not among them.
+__device__ __forceinline__ void merge8(uint32_t (&best)[8], const uint32_t (&key)[8], uint32_t& lost) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         lost = max(lost, min(best[i], key[7 - i]));
@@ -357,6 +357,10 @@ __device__ __forceinline__ void take8(uint32_t (&best)[8], uint32_t (&key)[8], u
         for (int i = 0; i < 8; ++i)
             if ((i & d) == 0) exchange(best[i], best[i + d]);
 }
+__device__ __forceinline__ void take8(uint32_t (&best)[8], uint32_t (&key)[8], uint32_t& lost) {
+    sort8(key);
+    merge8(best, key, lost);
+}
 // The leading bits of a float as an integer that orders like it (-0 as 0).
 template <uint32_t LOW>
 __device__ __forceinline__ uint32_t leading(float v) {
@@ -367,12 +371,13 @@ __device__ __forceinline__ uint32_t leading(float v) {
 template <typename T, bool V, bool WIDE>
 __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(const RouterArgs a) {
     constexpr int kWarps = kManyWarps<WIDE>, kThreads = kWarps * 32, kColumns = WIDE ? 2 : 1;     // columns: fours of a lane
-    extern __shared__ float tiles[];                          // [warps][32][pitch]
-    __shared__ float sums[kManyExperts], scale[kWarps][32];
+    extern __shared__ float tiles[];                          // [warps][16][pitch]
+    __shared__ float sums[kManyExperts], scale[kWarps][kTileRows];
     __shared__ int counts[kManyExperts];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts, k = a.top_k, pitch = many_pitch(E), padded = pitch - 4, fours = (E + 3) / 4;
-    float* tile = tiles + warp * 32 * pitch;
-    float* mine = tile + lane * pitch;
+    const int r = lane & 15, h = lane >> 4, half = padded / 2;           // row of the tile and half of it
+    float* tile = tiles + warp * kTileRows * pitch;
+    float* mine = tile + r * pitch;
     for (int e = threadIdx.x; e < E; e += kThreads) { sums[e] = 0.f; counts[e] = 0; }
     __syncthreads();
     float acc[kColumns][4];
@@ -382,53 +387,68 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
         for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
     double z2 = 0.;
     const bool packed = k % 4 == 0 && (((uintptr_t)a.idx | (uintptr_t)a.weights) & 15) == 0;
-    const int64_t stride = (int64_t)gridDim.x * kWarps * 32;
-    for (int64_t base = ((int64_t)blockIdx.x * kWarps + warp) * 32; base < a.rows; base += stride) {
-        const int rows = (int)min((int64_t)32, a.rows - base);
+    const int64_t stride = (int64_t)gridDim.x * kWarps * kTileRows;
+    for (int64_t base = ((int64_t)warp * gridDim.x + blockIdx.x) * kTileRows; base < a.rows; base += stride) {     // few tiles: one for each SM first
+        const int rows = (int)min((int64_t)kTileRows, a.rows - base);
         // the tile
         const T* in = static_cast<const T*>(a.logits) + base * a.ld;
         if (V && sizeof(T) == 4) {
-#pragma unroll 4
-            for (int r = 0; r < rows; ++r)
-                for (int c = lane * 4; c < E; c += 128) cp_async16(tile + r * pitch + c, in + r * a.ld + c);
+#pragma unroll
+            for (int j = 0; j < kColumns; ++j) {
+                const int c = j * 128 + lane * 4;
+                if (c < E) {
+                    const T* from = in + c;
+                    float* to = tile + c;
+                    const int64_t ld = a.ld;
+#pragma unroll 8
+                    for (int q = 0; q < rows; ++q, from += ld, to += pitch) cp_async16(to, from);
+                }
+            }
             cp_async_commit();
         } else if (V) {
             for (int r0 = 0; r0 < rows; r0 += 8)              // four values of 16 bits a load, eight rows' loads in flight
                 for (int f = lane; f < fours; f += 32) {
                     float v[8][4];
 #pragma unroll
-                    for (int r = 0; r < 8; ++r)
-                        if (r0 + r < rows) group_load4<T, 1, true>(in + (r0 + r) * a.ld + f * 4, 0, 0, 4, v[r]);
+                    for (int q = 0; q < 8; ++q)
+                        if (r0 + q < rows) group_load4<T, 1, true>(in + (r0 + q) * a.ld + f * 4, 0, 0, 4, v[q]);
 #pragma unroll
-                    for (int r = 0; r < 8; ++r)
-                        if (r0 + r < rows) *reinterpret_cast<float4*>(tile + (r0 + r) * pitch + f * 4) = make_float4(v[r][0], v[r][1], v[r][2], v[r][3]);
+                    for (int q = 0; q < 8; ++q)
+                        if (r0 + q < rows) *reinterpret_cast<float4*>(tile + (r0 + q) * pitch + f * 4) = make_float4(v[q][0], v[q][1], v[q][2], v[q][3]);
                 }
         } else {
             for (int r0 = 0; r0 < rows; r0 += 8)
                 for (int c = lane; c < E; c += 32) {
                     float v[8];
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) v[r] = r0 + r < rows ? to_float(in[(r0 + r) * a.ld + c]) : 0.f;
+                    for (int q = 0; q < 8; ++q) v[q] = r0 + q < rows ? to_float(in[(r0 + q) * a.ld + c]) : 0.f;
 #pragma unroll
-                    for (int r = 0; r < 8; ++r)
-                        if (r0 + r < rows) tile[(r0 + r) * pitch + c] = v[r];
+                    for (int q = 0; q < 8; ++q)
+                        if (r0 + q < rows) tile[(r0 + q) * pitch + c] = v[q];
                 }
         }
-        for (int c = E; c < padded; ++c) mine[c] = -INFINITY;
-        const int64_t row = base + lane;
-        bool on = lane < rows && (!a.has_live || a.live[row]);
+        if (h) for (int c = E; c < padded; ++c) mine[c] = -INFINITY;
+        const int64_t row = base + r;
+        bool on = r < rows && (!a.has_live || a.live[row]);
         if (V && sizeof(T) == 4) cp_async_wait<0>();
         __syncwarp();
-        // the eight fours with the largest maxima, and the eight largest of them
+        // of this half the eight fours with the largest maxima, and the eight largest of them
         uint32_t groups[8] = {0, 0, 0, 0, 0, 0, 0, 0}, best[8] = {0, 0, 0, 0, 0, 0, 0, 0}, lost_group = 0, lost = 0;
-        for (int c = 0; c < padded / 32; ++c) {
-            uint32_t key[8];
+        const int first = h * half / 4;                       // its first four
+        if (half > 32) {
+            for (int c = 0; c < half / 32; ++c) {
+                uint32_t key[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 v = *reinterpret_cast<const float4*>(mine + c * 32 + i * 4);
-                key[i] = leading<63>(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))) | (uint32_t)(63 - c * 8 - i);
+                for (int i = 0; i < 8; ++i) {
+                    const int g = first + c * 8 + i;
+                    const float4 v = *reinterpret_cast<const float4*>(mine + g * 4);
+                    key[i] = leading<63>(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))) | (uint32_t)(63 - g);
+                }
+                take8(groups, key, lost_group);
             }
-            take8(groups, key, lost_group);
+        } else {                                              // eight fours in all
+#pragma unroll
+            for (int i = 0; i < 8; ++i) groups[i] = 0xffffffc0u | (uint32_t)(63 - first - i);
         }
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
@@ -444,6 +464,13 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
                 key[q * 4 + 3] = leading<255>(v.w) | (code - 3);
             }
             take8(best, key, lost);
+        }
+        {                                                     // with the other half
+            uint32_t key[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) key[i] = __shfl_xor_sync(0xffffffffu, best[i], 16);
+            merge8(best, key, lost);
+            lost = max(lost, __shfl_xor_sync(0xffffffffu, lost, 16));
         }
         int idx[8];
         float val[8];
@@ -465,22 +492,23 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
                     last = best[i];
                     next = i < 7 ? best[i < 7 ? i + 1 : 7] : 0u;
                 }
-            const bool close = !sorted || (last >> 8) == (max(next, lost) >> 8) || (groups[7] >> 6) == (lost_group >> 6);
+            bool close = !sorted || (last >> 8) == (max(next, lost) >> 8) || (groups[7] >> 6) == (lost_group >> 6);
             int larger = 0, above = 0;                        // logits, and chosen ones, that are larger than the least chosen
             if (__any_sync(0xffffffffu, on && close)) {
-                for (int c = 0; c < fours; ++c) {
+                for (int c = first; c < min(fours, first + half / 4); ++c) {
                     const float4 v = *reinterpret_cast<const float4*>(mine + c * 4);
                     larger += (v.x > least) + (v.y > least) + (v.z > least) + (v.w > least);
                 }
+                larger += __shfl_xor_sync(0xffffffffu, larger, 16);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) above += i < k && val[i] > least;
             }
             // rows whose choice is not that of the values: the warp chooses again, one row after the other
-            unsigned again = __ballot_sync(0xffffffffu, on && (!sorted || larger != above) && !(m != m));
+            unsigned again = __ballot_sync(0xffffffffu, on && (!sorted || larger != above) && !(m != m)) & 0xffffu;
             while (again) {
-                const int r = __ffs(again) - 1;
+                const int bad = __ffs(again) - 1;
                 again &= again - 1;
-                const float* other = tile + r * pitch;
+                const float* other = tile + bad * pitch;
                 uint32_t key[kManyExperts / 32];
 #pragma unroll
                 for (int j = 0; j < kManyExperts / 32; ++j) key[j] = j * 32 + lane < E ? order_key(other[j * 32 + lane]) : 0u;
@@ -495,7 +523,7 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
 #pragma unroll
                     for (int j = 0; j < kManyExperts / 32; ++j)
                         if (j * 32 + lane == e) key[j] = 0;
-                    if (lane == r) {
+                    if (r == bad) {
 #pragma unroll
                         for (int q = 0; q < 8; ++q)
                             if (q == i) { idx[q] = e; val[q] = mine[e]; }
@@ -505,16 +533,23 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
             m = val[0];
         }
         on = on && !(m == -INFINITY);                         // a row without a logit above -inf takes no part
-#pragma unroll 2
-        for (int c = 0; c < fours; ++c) {
-            float4 v = *reinterpret_cast<const float4*>(mine + c * 4);
-            v.x = ex2((v.x - m) * kLog2e);                    // (of rows that take no part: left out below)
-            v.y = ex2((v.y - m) * kLog2e);
-            v.z = ex2((v.z - m) * kLog2e);
-            v.w = ex2((v.w - m) * kLog2e);
-            sum += (v.x + v.y) + (v.z + v.w);
-            *reinterpret_cast<float4*>(mine + c * 4) = v;
+        __syncwarp();                                         // a half's exponentials take the place of what the other may still look at
+        const int end = min(fours, first + half / 4);
+        if (on) {
+#pragma unroll 4
+            for (int c = first; c < end; ++c) {
+                float4 v = *reinterpret_cast<const float4*>(mine + c * 4);
+                v.x = ex2((v.x - m) * kLog2e);
+                v.y = ex2((v.y - m) * kLog2e);
+                v.z = ex2((v.z - m) * kLog2e);
+                v.w = ex2((v.w - m) * kLog2e);
+                sum += (v.x + v.y) + (v.z + v.w);
+                *reinterpret_cast<float4*>(mine + c * 4) = v;
+            }
+        } else {
+            for (int c = first; c < end; ++c) *reinterpret_cast<float4*>(mine + c * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
         }
+        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
         float w[8], total = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -523,41 +558,49 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
         }
         // (a NaN in the row makes its sum NaN, and the weights)
         const float inv = !on ? 0.f : sum != sum ? sum : 1.f / (a.renormalise ? total : sum), lse = on ? m + logf(sum) : 0.f;
-        scale[warp][lane] = on ? 1.f / sum : 0.f;
-        if (lane < rows) {
+        if (h == 0) scale[warp][r] = on ? 1.f / sum : 0.f;
+        if (r < rows) {
+            if (h == 0) {                                     // the choices by one thread of a row, the weights by the other
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] *= inv;
-                idx[i] = on ? idx[i] : -1;
-                if (i < k && on) atomicAdd(&counts[idx[i]], 1);
-            }
-            if (packed) {
+                for (int i = 0; i < 8; ++i) {
+                    idx[i] = on ? idx[i] : -1;
+                    if (i < k && on) atomicAdd(&counts[idx[i]], 1);
+                }
+                if (packed) {
 #pragma unroll
-                for (int i = 0; i < 8; i += 4)
-                    if (i < k) {
-                        *reinterpret_cast<int4*>(a.idx + row * k + i) = make_int4(idx[i], idx[i + 1], idx[i + 2], idx[i + 3]);
-                        *reinterpret_cast<float4*>(a.weights + row * k + i) = make_float4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-                    }
+                    for (int i = 0; i < 8; i += 4)
+                        if (i < k) *reinterpret_cast<int4*>(a.idx + row * k + i) = make_int4(idx[i], idx[i + 1], idx[i + 2], idx[i + 3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i < k) a.idx[row * k + i] = idx[i];
+                }
+                if (a.lse) a.lse[row] = lse;
+                z2 += (double)lse * (double)lse;
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < k) { a.idx[row * k + i] = idx[i]; a.weights[row * k + i] = w[i]; }
+                for (int i = 0; i < 8; ++i) w[i] *= inv;
+                if (packed) {
+#pragma unroll
+                    for (int i = 0; i < 8; i += 4)
+                        if (i < k) *reinterpret_cast<float4*>(a.weights + row * k + i) = make_float4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i < k) a.weights[row * k + i] = w[i];
+                }
             }
-            if (a.lse) a.lse[row] = lse;
-            z2 += (double)lse * (double)lse;
         }
         __syncwarp();
-        // columns, of the rows that take part
-        const unsigned part = __ballot_sync(0xffffffffu, on);
+        // columns (rows that take no part are zeros)
 #pragma unroll
         for (int j = 0; j < kColumns; ++j) {
             const int c = j * 128 + lane * 4;
             if (c < fours * 4) {
 #pragma unroll 8
-                for (int r = 0; r < 32; ++r) {
-                    if (!(part >> r & 1)) continue;
-                    const float4 v = *reinterpret_cast<const float4*>(tile + r * pitch + c);
-                    const float s = scale[warp][r];
+                for (int q = 0; q < kTileRows; ++q) {
+                    const float4 v = *reinterpret_cast<const float4*>(tile + q * pitch + c);
+                    const float s = scale[warp][q];
                     acc[j][0] = fmaf(v.x, s, acc[j][0]);
                     acc[j][1] = fmaf(v.y, s, acc[j][1]);
                     acc[j][2] = fmaf(v.z, s, acc[j][2]);
@@ -720,9 +763,9 @@ template <typename T, bool V>
 cudaError_t router_typed(const RouterArgs& a, int sms, cudaStream_t st) {
     if (a.experts <= kManyExperts && a.top_k <= kManyK && a.rows >= kManyRows) {
         const int warps = a.experts <= 128 ? kManyWarps<false> : kManyWarps<true>;
-        const int64_t need = ((int64_t)a.rows + warps * 32 - 1) / (warps * 32);
+        const int64_t need = ((int64_t)a.rows + kTileRows - 1) / kTileRows;
         return launch_plain(a.experts <= 128 ? router_many_kernel<T, V, false> : router_many_kernel<T, V, true>,
-                            dim3((unsigned)(need < sms ? need : sms)), dim3(warps * 32), (size_t)warps * 32 * many_pitch(a.experts) * 4, st, a);
+                            dim3((unsigned)(need < sms ? need : sms)), dim3(warps * 32), (size_t)warps * kTileRows * many_pitch(a.experts) * 4, st, a);
     }
     if (a.experts <= 128) return router_launch<T, 1, V>(a, sms, st);
     if (a.experts <= 256) return router_launch<T, 2, V>(a, sms, st);
@@ -748,8 +791,8 @@ cudaError_t router_grad_typed(const RouterGradArgs& a, int sms, cudaStream_t st)
 
 template <typename T, bool V>
 cudaError_t router_init() {
-    cudaError_t e = init_all(kManyWarps<false> * 32 * many_pitch(128) * 4, router_many_kernel<T, V, false>);
-    if (e == cudaSuccess) e = init_all(kManyWarps<true> * 32 * many_pitch(kManyExperts) * 4, router_many_kernel<T, V, true>);
+    cudaError_t e = init_all(kManyWarps<false> * kTileRows * many_pitch(128) * 4, router_many_kernel<T, V, false>);
+    if (e == cudaSuccess) e = init_all(kManyWarps<true> * kTileRows * many_pitch(kManyExperts) * 4, router_many_kernel<T, V, true>);
     if (e != cudaSuccess) return e;
     return init_all(0, router_kernel<T, 1, V>, router_kernel<T, 2, V>, router_kernel<T, 4, V>, router_kernel<T, 8, V>, router_grad_kernel<T, 4, 2, V>,
                     router_grad_kernel<T, 8, 4, V>, router_grad_kernel<T, 16, 4, V>, router_grad_kernel<T, 32, 4, V>,
