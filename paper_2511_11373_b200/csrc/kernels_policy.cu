@@ -5,7 +5,7 @@
 // weighted by 1 / live tokens, by 1 / (live sequences x the sequence's live tokens), or not at all, times `scale`.
 // Bound by HBM for long batches (16 to 24 bytes a token) and by latency for short ones.  No gradient may be written before
 // the tokens are counted, so a first kernel counts them (targets alone, which then lie in L2) with integer atomics, whose order
-// changes nothing, and its last block turns the counts into weights.  Terms are added in fp32 over the four tokens of a thread, in
+// changes nothing, and its last block turns the counts into weights.  Terms are added in fp32 over up to 32 tokens of a thread, in
 // fp64 beyond, and the blocks' sums in order by the last one to finish: the same call gives the same bits.  Which side of a border a
 // ratio is on is decided on logp - old against the borders' logarithms, in fp64 where fp32 is too near.  A warp finds the
 // sequences of its run of tokens together, 32 offsets a step.
@@ -55,11 +55,11 @@ __device__ __forceinline__ int find_here(const int32_t* seq_off, int lo, int hi,
 
 // The tokens of a warp: a piece [begin, end) of all, in whole runs.
 struct Piece { int begin, end; };
-__device__ __forceinline__ Piece warp_piece(int tokens, int warp, int warps) {
-    const int64_t runs = ((int64_t)tokens + kRun - 1) / kRun;
+__device__ __forceinline__ Piece warp_piece(int tokens, int run, int warp, int warps) {
+    const int64_t runs = ((int64_t)tokens + run - 1) / run;
     Piece p;
-    p.begin = (int)min((int64_t)tokens, runs * warp / warps * kRun);
-    p.end = (int)min((int64_t)tokens, runs * (warp + 1) / warps * kRun);
+    p.begin = (int)min((int64_t)tokens, runs * warp / warps * run);
+    p.end = (int)min((int64_t)tokens, runs * (warp + 1) / warps * run);
     return p;
 }
 // Moves first to the sequence of token t0 and returns that of token t1 (seqs: behind the last one).
@@ -73,51 +73,87 @@ __device__ __forceinline__ int advance(const PolicyArgs& a, int& first, int t0, 
 __device__ __forceinline__ void add_live(const PolicyArgs& a, int seq, int count, int& held) {
     if (count && seq < a.seqs) held += atomicAdd(a.seq_live + seq, count) == 0;
 }
-__device__ __forceinline__ void count_tokens(const PolicyArgs& a, int warp, int warps) {
-    const int lane = threadIdx.x & 31, begin = a.seq_off[0];
-    const Piece p = warp_piece(a.tokens, warp, warps);
+// live, held: what this warp found (held: sequences that nobody had found before).
+template <int QUADS>
+__device__ __forceinline__ void count_tokens(const PolicyArgs& a, int warp, int warps, int& live, int& held) {
+    constexpr int kLong = kRun * QUADS;                       // tokens whose loads are in flight together
+    const int lane = threadIdx.x & 31;
+    const Piece p = warp_piece(a.tokens, kLong, warp, warps);
+    live = held = 0;
     if (p.begin >= p.end) return;
-    int target[4], live = 0, held = 0;
-    load_quad(a.targets, p.begin + lane * 4, a.tokens, a.vector, -1, target);
-    int first = find_sequence(a.seq_off, 0, a.seqs, p.begin);
-    int pending = 0;                                          // live tokens of `first` that are not added yet
-    for (int t0 = p.begin; t0 < p.end; t0 += kRun) {
-        int next[4] = {-1, -1, -1, -1};
-        if (t0 + kRun < p.end) load_quad(a.targets, t0 + kRun + lane * 4, a.tokens, a.vector, -1, next);
-        const int before = first, t = t0 + lane * 4, last = advance(a, first, t0, min(a.tokens, t0 + kRun) - 1);
+    int pending = 0, first = -1, begin = 0;         // pending: live tokens of `first` that are not added yet
+    for (int t0 = p.begin; t0 < p.end; t0 += kLong) {
+        int target[QUADS][4];
+#pragma unroll
+        for (int q = 0; q < QUADS; ++q) load_quad(a.targets, t0 + q * kRun + lane * 4, a.tokens, a.vector, -1, target[q]);
+        if (first < 0) {
+            begin = a.seq_off[0];
+            first = find_sequence(a.seq_off, 0, a.seqs, t0);
+        }
+        const int before = first, last = advance(a, first, t0, min(a.tokens, t0 + kLong) - 1);
         if (first != before) {
             pending = __reduce_add_sync(0xffffffffu, pending);
-            if (lane == 0) add_live(a, before, pending, held);
+            if (lane == 0) {
+                add_live(a, before, pending, held);
+                live += before < a.seqs ? pending : 0;
+            }
             pending = 0;
         }
-        int count = 0, at = first, bound = at < a.seqs && first != last ? a.seq_off[1 + at] : INT32_MAX;
         if (first == last && t0 >= begin) {                   // one sequence
 #pragma unroll
-            for (int i = 0; i < 4; ++i) count += target[i] >= 0;
-        } else
+            for (int q = 0; q < QUADS; ++q)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (target[i] < 0 || t + i < begin) continue;
-            if (t + i >= bound) {
-                if (at == first) pending += count; else add_live(a, at, count, held);
-                live += at < a.seqs ? count : 0;
-                count = 0;
-                at = find_here(a.seq_off, at, last, t + i);
-                bound = at < a.seqs ? a.seq_off[1 + at] : INT32_MAX;
-            }
-            ++count;
+                for (int i = 0; i < 4; ++i) pending += target[q][i] >= 0;
+            continue;
         }
-        if (at == first) pending += count; else add_live(a, at, count, held);
-        live += at < a.seqs ? count : 0;
+        int count = 0, at = first, bound = at < a.seqs && first != last ? a.seq_off[1 + at] : INT32_MAX;
+        auto add = [&]() {
+            if (at == first) {
+                pending += count;
+            } else if (at < a.seqs) {
+                add_live(a, at, count, held);
+                live += count;
+            }
+            count = 0;
+        };
 #pragma unroll
-        for (int i = 0; i < 4; ++i) target[i] = next[i];
+        for (int q = 0; q < QUADS; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = t0 + q * kRun + lane * 4 + i;
+                if (target[q][i] < 0 || t < begin) continue;
+                if (t >= bound) {
+                    add();
+                    at = find_here(a.seq_off, at, last, t);
+                    bound = at < a.seqs ? a.seq_off[1 + at] : INT32_MAX;
+                }
+                ++count;
+            }
+        add();
     }
     pending = __reduce_add_sync(0xffffffffu, pending);
-    if (lane == 0) add_live(a, first, pending, held);
+    if (lane == 0) {
+        add_live(a, first, pending, held);
+        live += first < a.seqs ? pending : 0;
+    }
     live = __reduce_add_sync(0xffffffffu, live);
     held = __reduce_add_sync(0xffffffffu, held);
-    if (lane == 0 && live) atomicAdd(a.totals, live);
-    if (lane == 0 && held) atomicAdd(a.totals + 1, held);
+}
+// The block's counts into the totals: one addition each.
+template <int WARPS>
+__device__ __forceinline__ void add_totals(const PolicyArgs& a, int live, int held) {
+    __shared__ int sums[2][WARPS];
+    if ((threadIdx.x & 31) == 0) {
+        sums[0][threadIdx.x >> 5] = live;
+        sums[1][threadIdx.x >> 5] = held;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        int n = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) n += sums[threadIdx.x][w];
+        if (n) atomicAdd(a.totals + threadIdx.x, n);
+    }
 }
 
 // exp(x) - 1 and exp(x) - 1 - x without cancellation: the series below 1/2, where the differences would lose two bits and more.
@@ -184,10 +220,20 @@ struct Inputs {
 template <bool REF>
 __device__ __forceinline__ Inputs load_inputs(const PolicyArgs& a, int t) {
     Inputs v;
-    load_quad(a.targets, t, a.tokens, a.vector, -1, v.target);
-    load_quad(a.lp, t, a.tokens, a.vector, 0.f, v.lp);
-    load_quad(a.old_lp, t, a.tokens, a.vector, 0.f, v.old);
-    if (REF) load_quad(a.ref, t, a.tokens, a.vector, 0.f, v.ref);
+    if (a.vector && t + 4 <= a.tokens) {
+        const int4 g = *reinterpret_cast<const int4*>(a.targets + t);
+        const float4 l = *reinterpret_cast<const float4*>(a.lp + t), o = *reinterpret_cast<const float4*>(a.old_lp + t);
+        const float4 r = REF ? *reinterpret_cast<const float4*>(a.ref + t) : l;
+        v.target[0] = g.x; v.target[1] = g.y; v.target[2] = g.z; v.target[3] = g.w;
+        v.lp[0] = l.x; v.lp[1] = l.y; v.lp[2] = l.z; v.lp[3] = l.w;
+        v.old[0] = o.x; v.old[1] = o.y; v.old[2] = o.z; v.old[3] = o.w;
+        v.ref[0] = r.x; v.ref[1] = r.y; v.ref[2] = r.z; v.ref[3] = r.w;
+    } else {
+        load_quad(a.targets, t, a.tokens, 0, -1, v.target);
+        load_quad(a.lp, t, a.tokens, 0, 0.f, v.lp);
+        load_quad(a.old_lp, t, a.tokens, 0, 0.f, v.old);
+        if (REF) load_quad(a.ref, t, a.tokens, 0, 0.f, v.ref);
+    }
     return v;
 }
 
@@ -237,7 +283,7 @@ __device__ __forceinline__ double term_share(const PolicyArgs& a, int live, int 
 template <bool REF>
 __device__ __forceinline__ void loss_tokens(const PolicyArgs& a, int warp, int warps, double (&sums)[4]) {
     const int lane = threadIdx.x & 31, begin = a.seq_off[0];
-    const Piece p = warp_piece(a.tokens, warp, warps);
+    const Piece p = warp_piece(a.tokens, kRun, warp, warps);
     if (p.begin >= p.end) return;
     Inputs v = load_inputs<REF>(a, p.begin + lane * 4);
     const int live = __ldcg(a.totals), held = __ldcg(a.totals + 1);
@@ -322,7 +368,9 @@ __device__ __forceinline__ void write_stats(const PolicyArgs& a, double v) {
 }
 
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(const PolicyArgs a) {
-    count_tokens(a, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32));
+    int live, held;
+    count_tokens<4>(a, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32), live, held);
+    add_totals<kThreads / 32>(a, live, held);
 }
 
 template <bool REF>
@@ -359,7 +407,9 @@ __global__ void __launch_bounds__(kThreads, 3) policy_loss_kernel(const PolicyAr
 template <bool REF>
 __global__ void __launch_bounds__(kSmallThreads) policy_small_kernel(const PolicyArgs a) {
     __shared__ double reduce[kSmallThreads / 32][4];
-    count_tokens(a, threadIdx.x >> 5, kSmallThreads / 32);
+    int live, held;
+    count_tokens<1>(a, threadIdx.x >> 5, kSmallThreads / 32, live, held);
+    add_totals<kSmallThreads / 32>(a, live, held);
     __threadfence();
     __syncthreads();
     double sums[4] = {0., 0., 0., 0.};
@@ -380,7 +430,7 @@ cudaError_t launch_policy_loss(const PolicyArgs& a, int sms, cudaStream_t st) {
     if (a.tokens <= kSmallTokens)
         return launch_plain(a.has_ref ? policy_small_kernel<true> : policy_small_kernel<false>, dim3(1), dim3(kSmallThreads), 0, st, a);
     const int64_t need = ((int64_t)a.tokens + kThreads / 32 * kRun - 1) / (kThreads / 32 * kRun), most = policy_max_blocks(sms);
-    const int64_t counting = need < (int64_t)sms * 8 ? need : (int64_t)sms * 8;
+    const int64_t counting = (need + 3) / 4 < (int64_t)sms * 6 ? (need + 3) / 4 : (int64_t)sms * 6;
     const dim3 grid((unsigned)(need < most ? need : most)), block(kThreads);
     const cudaError_t e = launch_plain(policy_count_kernel, dim3((unsigned)counting), block, 0, st, a);
     if (e != cudaSuccess) return e;

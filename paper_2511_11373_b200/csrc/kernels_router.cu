@@ -125,89 +125,98 @@ constexpr uint32_t kKeyNegInf = 0x007fffffu;
 constexpr float kLog2e = 1.44269504f;
 
 // The end of a block: its sums and counts for all, and by the last block the call's totals.  sums, counts: [experts] in shared memory,
-// complete; z: the sum of lse^2 of lane 0 of each warp.
+// complete; z: the sum of lse^2 of lane 0 of each warp.  The last block has all its loads in flight together; a block that is alone has
+// none.
 template <int WARPS>
 __device__ __forceinline__ void router_finish(const RouterArgs& a, float* sums, int* counts, double z) {
     __shared__ double reduce[WARPS], part[WARPS * 32];
-    __shared__ int last, total_count, scan[WARPS];
+    __shared__ int last, scan[WARPS];
     constexpr int THREADS = WARPS * 32;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts, blocks = gridDim.x;
     if (lane == 0) reduce[warp] = z;
     __syncthreads();
-    for (int e = threadIdx.x; e < E; e += THREADS) {
-        a.parts[(int64_t)blockIdx.x * E + e] = sums[e];
-        if (counts[e]) atomicAdd(&a.work_counts[e], counts[e]);
-    }
-    if (threadIdx.x == 0) {
-        z = 0.;
-        for (int w = 0; w < WARPS; ++w) z += reduce[w];
-        a.z_parts[blockIdx.x] = z;
-    }
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    const int blocks = gridDim.x;
     z = 0.;
-    for (int b = threadIdx.x; b < blocks; b += THREADS) z += __ldcg(a.z_parts + b);
-    z = warp_sum_double(z);
-    // counts and their exclusive sums: every thread has a run of neighbouring experts
+    for (int w = 0; w < WARPS; ++w) z += reduce[w];
+    if (blocks > 1) {
+        for (int e = threadIdx.x; e < E; e += THREADS) {
+            a.parts[(int64_t)blockIdx.x * E + e] = sums[e];
+            if (counts[e]) atomicAdd(&a.work_counts[e], counts[e]);
+        }
+        if (threadIdx.x == 0) a.z_parts[blockIdx.x] = z;
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) last = atomicAdd(a.ticket, 1) == blocks - 1;
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+    }
+    // a thread's share of the columns' sums: as many threads for a column as there are for all columns at once, each with a run of blocks
+    const int slices = max(1, THREADS / E), here = min(E, THREADS), slice = threadIdx.x / here, column = threadIdx.x - slice * here;
+    auto column_sum = [&](int c) {
+        if (blocks == 1) return slice == 0 ? (double)sums[c] : 0.;
+        double v = 0.;
+#pragma unroll 16
+        for (int b = blocks * slice / slices; b < blocks * (slice + 1) / slices; ++b) v += __ldcg(a.parts + (int64_t)b * E + c);
+        return v;
+    };
+    // counts: every thread has a run of neighbouring experts
     const int each = (E + THREADS - 1) / THREADS;
     int run = 0;
     for (int i = 0; i < each; ++i) {
         const int e = threadIdx.x * each + i;
-        if (e < E) run += counts[e] = __ldcg(a.work_counts + e);
+        if (e < E) run += blocks > 1 ? __ldcg(a.work_counts + e) : counts[e];
     }
+    double v = slice < slices ? column_sum(column) : 0., zs = 0.;
+    if (blocks > 1)
+        for (int b = threadIdx.x; b < blocks; b += THREADS) zs += __ldcg(a.z_parts + b);
+    else if (threadIdx.x == 0)
+        zs = z;
     int before = run;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, before, o);
-        if (lane >= o) before += v;
+        const int up = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += up;
     }
-    __syncthreads();
-    if (lane == 0) reduce[warp] = z;
+    zs = warp_sum_double(zs);
+    __syncthreads();                                          // counts of this block and its z are read
     if (lane == 31) scan[warp] = before;
+    if (lane == 0) reduce[warp] = zs;
+    part[threadIdx.x] = v;
     __syncthreads();
-    int base = 0;
-    for (int w = 0; w < warp; ++w) base += scan[w];
+    int base = 0, total = 0;
+    z = 0.;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) base += scan[w];
+        total += scan[w];
+        z += reduce[w];
+    }
     int at = base + before - run;
     for (int i = 0; i < each; ++i) {
         const int e = threadIdx.x * each + i;
         if (e >= E) break;
+        const int n = blocks == 1 ? counts[e] : each == 1 ? run : __ldcg(a.work_counts + e);
         if (a.offsets) a.offsets[e] = at;
-        at += counts[e];
-        if (a.counts) a.counts[e] = counts[e];
-        a.work_counts[e] = 0;
+        at += n;
+        if (a.counts) a.counts[e] = n;
+        counts[e] = n;
+        if (blocks > 1) a.work_counts[e] = 0;
     }
-    if (threadIdx.x == THREADS - 1) {
-        total_count = base + before;
-        if (a.offsets) a.offsets[E] = total_count;
+    if (threadIdx.x == 0) {
+        if (a.offsets) a.offsets[E] = total;
         *a.ticket = 0;
     }
     __syncthreads();
-    // blocks' sums: as many threads for a column as there are for all columns at once, each with a run of blocks
     double balance = 0.;
-    const int slices = max(1, THREADS / E), here = min(E, THREADS);
     for (int c0 = 0; c0 < E; c0 += THREADS) {
-        const int s = threadIdx.x / here, c = c0 + threadIdx.x - s * here;
-        double v = 0.;
-        if (s < slices && c < E) {
-#pragma unroll 16
-            for (int b = blocks * s / slices; b < blocks * (s + 1) / slices; ++b) v += __ldcg(a.parts + (int64_t)b * E + c);
-        }
-        part[threadIdx.x] = v;
-        __syncthreads();
-        if (s == 0 && c < E) {
+        const int c = c0 + column;
+        if (c0 > 0) v = c < E ? column_sum(c) : 0.;           // more columns than threads
+        if (slice == 0 && c < E) {
             for (int i = 1; i < slices; ++i) v += part[i * here + threadIdx.x];
             if (a.prob_sums) a.prob_sums[c] = (float)v;
             balance += v * counts[c];
         }
-        __syncthreads();
     }
-    z = 0.;
-    for (int w = 0; w < WARPS; ++w) z += reduce[w];
     balance = warp_sum_double(balance);
     __syncthreads();
     if (lane == 0) reduce[warp] = balance;
@@ -215,7 +224,7 @@ __device__ __forceinline__ void router_finish(const RouterArgs& a, float* sums, 
     if (threadIdx.x == 0 && a.losses) {
         balance = 0.;
         for (int w = 0; w < WARPS; ++w) balance += reduce[w];
-        const double n = (double)total_count / a.top_k;
+        const double n = (double)total / a.top_k;
         a.losses[0] = n > 0. ? (float)(E * balance / (n * n * a.top_k)) : 0.f;
         a.losses[1] = n > 0. ? (float)(z / n) : 0.f;
     }
