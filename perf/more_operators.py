@@ -311,7 +311,8 @@ def _run_own(s):
             got.update(d_logits=s["d_logits"])
     else:
         st = binding.mars_policy_loss(u, s["lp"], s["old"], s["adv"], s["targets"], s["off"], s["stats"], s["d_lp"],
-                                      ref_logprobs=s["ref"], clip_low=CLIP_LOW, clip_high=CLIP_HIGH, kl_coef=c["kl"],
+                                      ref_logprobs=s["ref"], clip_low=CLIP_LOW, clip_high=CLIP_HIGH,
+                                      kl_coef=c["kl"] if c["ref"] else 0.0,
                                       reduce=c["reduce"], scale=s["scale"], per_token=c["per_token"])
         got.update(stats=s["stats"], d_lp=s["d_lp"])
     if st:
