@@ -243,7 +243,7 @@ __device__ __forceinline__ bool plain_terms(const PolicyArgs& a, float log_low, 
                                             float (&d)[4]) {
     // over the border: side * x - edge > 0
     const float side = A > 0.f ? 1.f : -1.f, edge = A > 0.f ? log_high : A < 0.f ? -log_low : INFINITY, limit = A > 0.f ? a.high : a.low;
-    const float near = 3e-7f * fabsf(edge);
+    const float near = fabsf(edge) < INFINITY ? 3e-7f * fabsf(edge) : 0.f;
     Terms s = sum;
     bool ok = true;
 #pragma unroll

@@ -151,7 +151,7 @@ __device__ __forceinline__ void router_finish(const RouterArgs& a, float* sums, 
         __threadfence();
     }
     // a thread's share of the columns' sums: as many threads for a column as there are for all columns at once, each with a run of blocks
-    const int slices = max(1, THREADS / E), here = min(E, THREADS), slice = threadIdx.x / here, column = threadIdx.x - slice * here;
+    const int slices = max(1, min(16, THREADS / E)), here = min(E, THREADS), slice = threadIdx.x / here, column = threadIdx.x - slice * here;
     auto column_sum = [&](int c) {
         if (blocks == 1) return slice == 0 ? (double)sums[c] : 0.;
         double v = 0.;
@@ -706,13 +706,16 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const
         }
         fetch(base + D * stride + sub, ahead[D - 1], ahead_lse[D - 1], ahead_dw[D - 1], ahead_idx[D - 1], ahead_first[D - 1]);
         if (a.has_d_weights) {
-            float w_sum = w_first, wdw = w_first != 0.f ? w_first * first_dw : 0.f;
+            // of renormalised weights' gradients only differences count: taken from that of the first choice, a weight next to 1 keeps the
+            // accuracy of what the others leave it
+            const float from = a.renormalise ? __shfl_sync(0xffffffffu, (unsigned)first_idx < (unsigned)E ? first_dw : 0.f, sub * L) : 0.f;
+            float w_sum = w_first, wdw = w_first != 0.f ? w_first * (first_dw - from) : 0.f;
             for (int i = l + L; i < k; i += L) {
                 const int e = on ? a.idx[row * k + i] : -1;
                 if ((unsigned)e < (unsigned)E) {
                     const float w = ex2((to_float(in[e]) - lse) * kLog2e);
                     w_sum += w;
-                    wdw = fmaf(w, a.d_weights[row * k + i], wdw);
+                    wdw = fmaf(w, a.d_weights[row * k + i] - from, wdw);
                 }
             }
 #pragma unroll
@@ -721,11 +724,11 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const
                 wdw += __shfl_xor_sync(0xffffffffu, wdw, o);
             }
             const float inv = a.renormalise ? 1.f / w_sum : 1.f, mean = a.renormalise ? wdw * inv : 0.f;
-            if (on && (unsigned)first_idx < (unsigned)E) atomicAdd(mine + first_idx, w_first * inv * (first_dw - mean));
+            if (on && (unsigned)first_idx < (unsigned)E) atomicAdd(mine + first_idx, w_first * inv * (first_dw - from - mean));
             for (int i = l + L; i < k; i += L) {
                 const int e = on ? a.idx[row * k + i] : -1;
                 if ((unsigned)e < (unsigned)E)
-                    atomicAdd(mine + e, ex2((to_float(in[e]) - lse) * kLog2e) * inv * (a.d_weights[row * k + i] - mean));
+                    atomicAdd(mine + e, ex2((to_float(in[e]) - lse) * kLog2e) * inv * (a.d_weights[row * k + i] - from - mean));
             }
             if (!a.renormalise) dot += wdw / L;
             __syncwarp();

@@ -644,6 +644,30 @@ def test_gradient_of_choices_that_are_not_the_routers():
     assert float((d.double() - want).abs().max()) <= 256 * V * float(dw.abs().max())
 
 
+@pytest.mark.parametrize("E,k", [(16, 1), (128, 2), (128, 8)])
+def test_weights_next_to_one_keep_their_gradients_accuracy(E, k):
+    """Renormalised weights: a first choice that leaves the others 1e-2 .. 1e-9, or that is the only one (no gradient at all)."""
+    n = 64
+    train = binding.Train(max_experts=E, device=DEV)
+    z = router_logits(n, E, F, seed=2, std=0.3)
+    z[torch.arange(n), torch.arange(n) % E] += torch.linspace(5.0, 20.0, n, device=DEV)
+    got = run_router(train, z, k)
+    dw = normal(gen(5), n, k, mean=3.0)
+    d = torch.empty_like(z)
+    assert binding.mars_router_grad(train, z, got["idx"], got["lse"], got["counts"], d, d_weights=dw) == 0
+    at = got["idx"].long()
+    sel = z.double().gather(1, at)
+    w = torch.softmax(sel, 1)
+    # w_i sum_j w_j (dw_i - dw_j): no difference of nearly equal numbers but those of the inputs
+    diff = dw.double()[:, :, None] - dw.double()[:, None, :]
+    push = w * (w[:, None, :] * diff).sum(2)
+    size = w * (w[:, None, :] * diff.abs()).sum(2)
+    want = torch.zeros(n, E, dtype=torch.float64, device=DEV).scatter_(1, at, push)
+    # exponentials of rounded arguments (up to 25), 8 of them added, products and differences of a few roundings
+    tol = torch.zeros_like(want).scatter_(1, at, size) * (64 + 4 * 25) * V
+    assert worst(d, want, tol + 1e-45) <= 1
+
+
 def test_counts_of_several_micro_batches():
     """counts added up: each call's gradient is its rows' share of the gradient over all rows."""
     train = binding.Train(max_experts=40, device=DEV)
@@ -779,6 +803,19 @@ def test_policy_loss_and_gradient_match_the_formula(lengths, reduce):
         c = policy_case(lengths, ref=ref, per_token=per_token, seed=len(lengths), before=before, behind=behind)
         kw = dict(kl=kl, reduce=reduce, scale=1.0 if reduce != "sum" else 0.01, per_token=per_token)
         check_policy(c, run_policy(train, c, **kw), **kw)
+
+
+@pytest.mark.parametrize("low,high", [(1.0, 0.2), (0.2, 1e6), (0.0, 0.0), (0.2, 0.28)])
+def test_policy_loss_of_zero_advantages_and_open_borders(low, high):
+    train = binding.Train(max_seqs=9, device=DEV)
+    for reduce, kl in (("sequences", 0.0), ("tokens", 0.3)):
+        c = policy_case([2000, 150, 1, 4000, 0, 700, 128, 128, 3000], masked=0.1, seed=4)
+        c["adv"][::2] = 0.0
+        c["adv"][1] = -1e-40
+        c["ref"] = c["lp"] + normal(gen(1), c["lp"].shape[0], std=1.0)           # many differences beyond 1/2
+        kw = dict(low=low, high=high, kl=kl, reduce=reduce)
+        ref = check_policy(c, run_policy(train, c, **kw), **kw)
+        assert float(ref["stats"][2]) > 0 or high > 1 or low == 1.0
 
 
 def test_policy_loss_without_live_tokens_and_without_tokens():
