@@ -507,7 +507,7 @@ MARS_API mars_status_t mars_grads_clip(mars_grads_t *grads, void *cuda_stream, f
  *
  * mars_train_t holds the workspace (256-byte aligned device memory of the current device) of norms of up to max_width, routers
  * of up to max_experts and policy losses of up to max_seqs sequences; 0 leaves a group out, one at least is not 0.
- * max_width <= 16384, max_experts <= 1024, max_seqs <= 2^20.  One call at a time per handle, on the GPU as well: calls on
+ * max_width <= 8192, max_experts <= 1024, max_seqs <= 2^20.  One call at a time per handle, on the GPU as well: calls on
  * several streams are ordered by the caller, and two graphs that are replayed at the same time need a handle each.  (mars_norm
  * and mars_router_grad use no workspace and may run beside anything.) */
 typedef struct mars_train mars_train_t;

@@ -4,7 +4,7 @@
 //   dx = r (g - n mean(g n) - [layer] mean(g)) (+ d_sum),   dw = sum over rows of dy n,   db = sum of dy
 // Bound by HBM: every matrix is read or written once.  A row stays in the registers of a group of threads (a part of a warp, a warp,
 // or several that meet at a named barrier of their own, so that groups of a block do not wait for one another), in 16-byte
-// pieces.  Rows that allow no such pieces go value by value and are read again where the other form keeps them.  The variance is taken from the centred
+// pieces, or value by value where a row allows no such pieces.  The variance is taken from the centred
 // values, in a second sum over the registers: sum of squares minus square of the sum would lose a mean that is large
 // beside the spread.
 // The gradient runs on a grid that fits the SMs at once: a thread keeps the sums of dw and db of its columns in fp32
@@ -20,8 +20,7 @@ namespace mars {
 namespace {
 
 constexpr int kChunk = 8;
-constexpr int kLoopSmem = 2 * kNormMaxWidth * 4;      // the sums of the widest row
-constexpr int kRowWidth = 8192;          // widest row that is kept in registers: 256 threads x 32 values
+constexpr int kEach = 16;                // values of a thread where rows go value by value
 
 // Threads of a row and chunks of eight neighbouring values of a thread; blocks of at most 256 threads.
 struct NormPlan { int group, nv, block; };
@@ -44,15 +43,13 @@ __host__ __device__ constexpr int forward_blocks(int nv, bool x_is_fp32) { retur
 __host__ __device__ constexpr int grad_blocks_sm(int nv, bool x_is_fp32, bool layer) { return nv == 4 ? 1 : nv == 1 && !x_is_fp32 && !layer ? 3 : 2; }
 __host__ __device__ constexpr int rows_together(int nv) { return nv == 1 ? 2 : 1; }
 
-// The same for rows that are read again instead of kept.
-NormPlan loop_plan(int width) {
-    NormPlan p;
-    p.nv = 0;
-    p.group = 32;
-    while (p.group < 256 && p.group * 8 < width) p.group *= 2;
-    p.block = 256;
-    return p;
+// Rows value by value: threads of a row, a power of two from 32 to 512.
+int scalar_group(int width) {
+    int group = 32;
+    while (group * kEach < width) group *= 2;
+    return group;
 }
+constexpr int scalar_block(int group) { return group < 256 ? 256 : group; }
 
 // Chunk j of a thread, zeros behind the row.
 template <typename T>
@@ -207,50 +204,59 @@ __global__ void __launch_bounds__(256, forward_blocks(NV, sizeof(XT) == 4)) norm
     }
 }
 
-// Any width and alignment, value by value: a row is read again (from L1 or L2) for every sum and for the result.
-template <typename XT, typename YT>
-__global__ void __launch_bounds__(256, 2) norm_loop_kernel(const NormArgs a, const int group) {
+// Any alignment: the same value by value, a thread having those that are a group apart.
+template <typename XT, typename YT, int G>
+__global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 3 : 1) norm_scalar_kernel(const NormArgs a) {
+    constexpr int kGroups = (G < 256 ? 256 : G) / G;
     __shared__ float scratch[2 * 16];
-    const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
+    const int index = threadIdx.x / G, lane = threadIdx.x % G;
     int half = 0;
     const float inv = 1.f / (float)a.width;
-    for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += (int64_t)gridDim.x * groups) {
+    float weight[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) weight[i] = i * G + lane < a.width ? load_any(a.weight, a.w_type, i * G + lane) : 0.f;
+    for (int64_t base = (int64_t)blockIdx.x * kGroups; base < a.rows; base += (int64_t)gridDim.x * kGroups) {
         const bool on = base + index < a.rows;
         const int row = on ? (int)(base + index) : 0;
-        const int W = on ? a.width : 0;
-        const XT* x = static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x);
-        const YT* add = static_cast<const YT*>(a.add) + row_offset(row, a.heads, a.width, a.ld_add);
-        bool adds = a.has_add;
-        if (a.sum) {                                          // a thread reads later what it stores here itself
-            XT* sum = static_cast<XT*>(a.sum) + row_offset(row, a.heads, a.width, a.ld_sum);
-#pragma unroll 4
-            for (int c = lane; c < W; c += group) sum[c] = from_float<XT>(to_float(x[c]) + to_float(add[c]));
-            x = sum;
-            adds = false;
+        const int W = on ? a.width - lane : 0;                // value i lies inside where i * G < W
+        const XT* x = static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x) + lane;
+        float v[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = load_if(x + i * G, i * G < W);
+        if (a.has_add) {
+            const YT* add = static_cast<const YT*>(a.add) + row_offset(row, a.heads, a.width, a.ld_add) + lane;
+            XT* sum = static_cast<XT*>(a.sum) + row_offset(row, a.heads, a.width, a.ld_sum) + lane;
+            float b[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) b[i] = load_if(add + i * G, i * G < W);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const XT s = from_float<XT>(v[i] + b[i]);
+                v[i] = to_float(s);
+                if (a.sum && i * G < W) sum[i * G] = s;
+            }
         }
-        auto value = [&](int c) { return adds ? to_float(from_float<XT>(to_float(x[c]) + to_float(add[c]))) : to_float(x[c]); };
         float mean = 0.f;
         if (a.layer) {
             float s[1] = {0.f};
-#pragma unroll 4
-            for (int c = lane; c < W; c += group) s[0] += value(c);
-            group_sum(s, group, index, scratch, half);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) s[0] += v[i];
+            group_sum(s, G, index, scratch, half);
             mean = s[0] * inv;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) v[i] = i * G < W ? v[i] - mean : 0.f;
         }
         float q[1] = {0.f};
-#pragma unroll 4
-        for (int c = lane; c < W; c += group) {
-            const float u = value(c) - mean;
-            q[0] = fmaf(u, u, q[0]);
-        }
-        group_sum(q, group, index, scratch, half);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) q[0] = fmaf(v[i], v[i], q[0]);
+        group_sum(q, G, index, scratch, half);
         const float rstd = 1.f / sqrtf(q[0] * inv + a.eps);
-        YT* y = static_cast<YT*>(a.y) + row_offset(row, a.heads, a.width, a.ld_y);
-#pragma unroll 4
-        for (int c = lane; c < W; c += group) {
-            float o = (value(c) - mean) * rstd * load_any(a.weight, a.w_type, c);
-            if (a.has_bias) o += load_any(a.bias, a.w_type, c);
-            y[c] = from_float<YT>(o);
+        YT* y = static_cast<YT*>(a.y) + row_offset(row, a.heads, a.width, a.ld_y) + lane;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            float o = v[i] * rstd * weight[i];
+            if (a.has_bias && i * G < W) o += load_any(a.bias, a.w_type, i * G + lane);
+            if (i * G < W) y[i * G] = from_float<YT>(o);
         }
         if (on && lane == 0) {
             if (a.rstd) a.rstd[row] = rstd;
@@ -410,59 +416,78 @@ __global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER
     }
 }
 
-// Any width and alignment, value by value: a row is read twice, the sums of its columns lie in shared memory, where every column of a
-// group belongs to one thread.
-template <typename XT, typename YT, bool LAYER>
-__global__ void __launch_bounds__(256, 2) norm_grad_loop_kernel(const NormGradArgs a, const int group) {
+// Any alignment: the same value by value.
+template <typename XT, typename YT, int G, bool LAYER>
+__global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 2 : 1) norm_grad_scalar_kernel(const NormGradArgs a) {
+    constexpr int kGroups = (G < 256 ? 256 : G) / G;
     __shared__ float scratch[2 * 16 * 2];
-    extern __shared__ float sums[];                           // [groups][width], the same again for db
-    const int index = threadIdx.x / group, lane = threadIdx.x - index * group, groups = blockDim.x / group;
+    extern __shared__ float sums[];                           // [groups][width]
+    const int index = threadIdx.x / G, lane = threadIdx.x % G;
     int half = 0;
     const float inv = 1.f / (float)a.width;
-    float* sw = sums + index * a.width;
-    float* sb = sums + (groups + index) * a.width;
-    for (int c = lane; c < a.width; c += group) {
-        sw[c] = 0.f;
-        if (LAYER) sb[c] = 0.f;
+    float weight[kEach], acc_w[kEach], acc_b[LAYER ? kEach : 1];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        weight[i] = i * G + lane < a.width ? load_any(a.weight, a.w_type, i * G + lane) : 0.f;
+        acc_w[i] = 0.f;
+        if (LAYER) acc_b[i] = 0.f;
     }
-    for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += (int64_t)gridDim.x * groups) {
+    for (int64_t base = (int64_t)blockIdx.x * kGroups; base < a.rows; base += (int64_t)gridDim.x * kGroups) {
         const bool on = base + index < a.rows;
-        const int row = on ? (int)(base + index) : 0, W = on ? a.width : 0;
-        const XT* x = static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x);
-        const YT* dy = static_cast<const YT*>(a.dy) + row_offset(row, a.heads, a.width, a.ld_dy);
-        const XT* ds = static_cast<const XT*>(a.d_sum) + row_offset(row, a.heads, a.width, a.ld_d_sum);
+        const int row = on ? (int)(base + index) : 0;
+        const int W = on ? a.width - lane : 0;
+        const XT* x = static_cast<const XT*>(a.x) + row_offset(row, a.heads, a.width, a.ld_x) + lane;
+        const YT* dy = static_cast<const YT*>(a.dy) + row_offset(row, a.heads, a.width, a.ld_dy) + lane;
+        float n[kEach], g[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) n[i] = load_if(x + i * G, i * G < W);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) g[i] = load_if(dy + i * G, i * G < W);
         const float r = on ? a.rstd[row] : 0.f, mean = LAYER && on ? a.mean[row] : 0.f;
         float s[2] = {0.f, 0.f};
-#pragma unroll 4
-        for (int c = lane; c < W; c += group) {
-            const float n = (to_float(x[c]) - mean) * r, d = to_float(dy[c]), g = d * load_any(a.weight, a.w_type, c);
-            sw[c] = fmaf(d, n, sw[c]);
-            s[0] = fmaf(g, n, s[0]);
-            if (LAYER) {
-                sb[c] += d;
-                s[1] += g;
-            }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            n[i] = i * G < W ? (n[i] - mean) * r : 0.f;
+            acc_w[i] = fmaf(g[i], n[i], acc_w[i]);
+            if (LAYER) acc_b[i] += g[i];
+            g[i] *= weight[i];
+            s[0] = fmaf(g[i], n[i], s[0]);
+            if (LAYER) s[1] += g[i];
         }
-        group_sum(s, group, index, scratch, half);
-        const float c0 = s[0] * inv, c1 = LAYER ? s[1] * inv : 0.f;
-        XT* dx = static_cast<XT*>(a.dx) + row_offset(row, a.heads, a.width, a.ld_dx);
-#pragma unroll 4
-        for (int c = lane; c < W; c += group) {
-            const float n = (to_float(x[c]) - mean) * r, g = to_float(dy[c]) * load_any(a.weight, a.w_type, c);
-            float d = fmaf(-n, c0, LAYER ? g - c1 : g) * r;
-            if (a.has_d_sum) d += to_float(ds[c]);
-            dx[c] = from_float<XT>(d);
+        group_sum(s, G, index, scratch, half);
+        const float c0 = -s[0] * inv * r, c1 = LAYER ? s[1] * inv : 0.f;
+        const XT* ds = static_cast<const XT*>(a.d_sum) + row_offset(row, a.heads, a.width, a.ld_d_sum) + lane;
+        XT* dx = static_cast<XT*>(a.dx) + row_offset(row, a.heads, a.width, a.ld_dx) + lane;
+        if (a.has_d_sum) {
+            float d[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) d[i] = load_if(ds + i * G, i * G < W);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (i * G < W) dx[i * G] = from_float<XT>(fmaf(g[i] - c1, r, n[i] * c0) + d[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (i * G < W) dx[i * G] = from_float<XT>(fmaf(g[i] - c1, r, n[i] * c0));
         }
     }
-    __syncthreads();
-    for (int c = threadIdx.x; c < a.width; c += blockDim.x) {
-        float t = 0.f, u = 0.f;
-        for (int k = 0; k < groups; ++k) {
-            t += sums[k * a.width + c];
-            if (LAYER) u += sums[(groups + k) * a.width + c];
+#pragma unroll
+    for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
+        float* out = which ? a.part_b : a.part_w;
+        if (!out) continue;
+        out += (int64_t)blockIdx.x * a.width;
+        float* own = kGroups == 1 ? out : sums + index * a.width;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (i * G + lane < a.width) own[i * G + lane] = which ? acc_b[LAYER ? i : 0] : acc_w[i];
+        if (kGroups == 1) continue;
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.width; c += blockDim.x) {
+            float t = 0.f;
+            for (int k = 0; k < kGroups; ++k) t += sums[k * a.width + c];
+            out[c] = t;
         }
-        if (a.part_w) a.part_w[(int64_t)blockIdx.x * a.width + c] = t;
-        if (LAYER && a.part_b) a.part_b[(int64_t)blockIdx.x * a.width + c] = u;
     }
 }
 
@@ -493,42 +518,64 @@ __global__ void __launch_bounds__(1024) norm_columns_kernel(const float* part_w,
     }
 }
 
-int64_t row_blocks(int64_t rows, const NormPlan& p) { return (rows + p.block / p.group - 1) / (p.block / p.group); }
+int64_t row_blocks(int64_t rows, int groups) { return (rows + groups - 1) / groups; }
 
 template <typename XT, typename YT>
 cudaError_t norm_typed(const NormArgs& a, bool vector, int sms, cudaStream_t st) {
-    const bool rows = vector && a.width <= kRowWidth;
-    const NormPlan p = rows ? norm_plan(a.width) : loop_plan(a.width);
-    const int64_t blocks = row_blocks(a.rows, p), most = (int64_t)sms * (rows ? forward_blocks(p.nv, sizeof(XT) == 4) : 64);
-    const dim3 grid((unsigned)(blocks < most ? blocks : most));
-    if (!rows) return launch_plain(norm_loop_kernel<XT, YT>, grid, dim3(p.block), 0, st, a, p.group);
-    if (p.nv == 1) return launch_plain(norm_rows_kernel<XT, YT, 1>, grid, dim3(p.block), 0, st, a, p.group);
-    if (p.nv == 2) return launch_plain(norm_rows_kernel<XT, YT, 2>, grid, dim3(p.block), 0, st, a, p.group);
-    return launch_plain(norm_rows_kernel<XT, YT, 4>, grid, dim3(p.block), 0, st, a, p.group);
+    const NormPlan p = norm_plan(a.width);
+    const int scalar = scalar_group(a.width);
+    const int64_t blocks = row_blocks(a.rows, vector ? p.block / p.group : scalar_block(scalar) / scalar);
+    const int64_t most = (int64_t)sms * (vector ? forward_blocks(p.nv, sizeof(XT) == 4) : scalar < 512 ? 3 : 1);
+    const dim3 grid((unsigned)(blocks < most ? blocks : most)), block(vector ? p.block : scalar_block(scalar));
+    if (vector) {
+        if (p.nv == 1) return launch_plain(norm_rows_kernel<XT, YT, 1>, grid, block, 0, st, a, p.group);
+        if (p.nv == 2) return launch_plain(norm_rows_kernel<XT, YT, 2>, grid, block, 0, st, a, p.group);
+        return launch_plain(norm_rows_kernel<XT, YT, 4>, grid, block, 0, st, a, p.group);
+    }
+    switch (scalar) {
+        case 32: return launch_plain(norm_scalar_kernel<XT, YT, 32>, grid, block, 0, st, a);
+        case 64: return launch_plain(norm_scalar_kernel<XT, YT, 64>, grid, block, 0, st, a);
+        case 128: return launch_plain(norm_scalar_kernel<XT, YT, 128>, grid, block, 0, st, a);
+        case 256: return launch_plain(norm_scalar_kernel<XT, YT, 256>, grid, block, 0, st, a);
+        default: return launch_plain(norm_scalar_kernel<XT, YT, 512>, grid, block, 0, st, a);
+    }
 }
 
 struct GradPlan {
     NormPlan p;
-    bool rows;              // rows in registers
+    bool vector;
     int blocks, smem;
 };
 GradPlan grad_plan(int64_t rows, int width, bool layer, bool x_is_fp32, bool vector, int sms) {
     GradPlan g;
-    g.rows = vector && width <= kRowWidth;
-    g.p = g.rows ? norm_plan(width) : loop_plan(width);
+    g.vector = vector;
+    g.p = norm_plan(width);
+    if (!vector) {
+        g.p.group = scalar_group(width);
+        g.p.block = scalar_block(g.p.group);
+        g.p.nv = 0;
+    }
     const int groups = g.p.block / g.p.group;
-    g.smem = g.rows ? groups * width * 4 : groups * width * 4 * (layer ? 2 : 1);
-    // as many blocks as run at once: by registers; by shared memory one, two or more
-    const int most = sms * (g.rows ? grad_blocks_sm(g.p.nv, x_is_fp32, layer) : g.smem > 100 * 1024 ? 1 : width > 2048 ? 2 : 4);
-    const int together = g.rows ? rows_together(g.p.nv) : 1;
-    const int64_t need = (row_blocks(rows, g.p) + together - 1) / together;
+    g.smem = vector || groups > 1 ? groups * width * 4 : 0;
+    // as many blocks as run at once
+    const int most = sms * (vector ? grad_blocks_sm(g.p.nv, x_is_fp32, layer) : g.p.group < 512 ? 2 : 1);
+    const int together = vector ? rows_together(g.p.nv) : 1;
+    const int64_t need = (row_blocks(rows, groups) + together - 1) / together;
     g.blocks = (int)(need < 1 ? 1 : need < most ? need : most);
     return g;
 }
 template <typename XT, typename YT, bool LAYER>
 cudaError_t norm_grad_typed(const NormGradArgs& a, const GradPlan& g, cudaStream_t st) {
     const dim3 grid(g.blocks), block(g.p.block);
-    if (!g.rows) return launch_plain(norm_grad_loop_kernel<XT, YT, LAYER>, grid, block, g.smem, st, a, g.p.group);
+    if (!g.vector) {
+        switch (g.p.group) {
+            case 32: return launch_plain(norm_grad_scalar_kernel<XT, YT, 32, LAYER>, grid, block, g.smem, st, a);
+            case 64: return launch_plain(norm_grad_scalar_kernel<XT, YT, 64, LAYER>, grid, block, g.smem, st, a);
+            case 128: return launch_plain(norm_grad_scalar_kernel<XT, YT, 128, LAYER>, grid, block, g.smem, st, a);
+            case 256: return launch_plain(norm_grad_scalar_kernel<XT, YT, 256, LAYER>, grid, block, g.smem, st, a);
+            default: return launch_plain(norm_grad_scalar_kernel<XT, YT, 512, LAYER>, grid, block, g.smem, st, a);
+        }
+    }
     if (g.p.group * g.p.nv * kChunk == a.width) {
         if (g.p.nv == 1) return launch_plain(norm_grad_rows_kernel<XT, YT, 1, LAYER, true>, grid, block, g.smem, st, a, g.p.group);
         if (g.p.nv == 2) return launch_plain(norm_grad_rows_kernel<XT, YT, 2, LAYER, true>, grid, block, g.smem, st, a, g.p.group);
@@ -543,7 +590,10 @@ template <typename XT, typename YT, bool LAYER>
 cudaError_t init_grad_rows() {
     return init_all(0, norm_grad_rows_kernel<XT, YT, 1, LAYER, false>, norm_grad_rows_kernel<XT, YT, 2, LAYER, false>,
                     norm_grad_rows_kernel<XT, YT, 4, LAYER, false>, norm_grad_rows_kernel<XT, YT, 1, LAYER, true>,
-                    norm_grad_rows_kernel<XT, YT, 2, LAYER, true>, norm_grad_rows_kernel<XT, YT, 4, LAYER, true>);
+                    norm_grad_rows_kernel<XT, YT, 2, LAYER, true>, norm_grad_rows_kernel<XT, YT, 4, LAYER, true>,
+                    norm_grad_scalar_kernel<XT, YT, 32, LAYER>, norm_grad_scalar_kernel<XT, YT, 64, LAYER>,
+                    norm_grad_scalar_kernel<XT, YT, 128, LAYER>, norm_grad_scalar_kernel<XT, YT, 256, LAYER>,
+                    norm_grad_scalar_kernel<XT, YT, 512, LAYER>);
 }
 
 // x and y of one type, or x fp32 (a residual stream) and y of 16 bits.
@@ -558,12 +608,12 @@ cudaError_t for_types(int x_type, int y_type, F f) {
 
 }  // namespace
 
-// Sums of dw or db: blocks x width (grad_plan: at most four blocks on an SM up to a width of 2048, three up to 4096, two beyond).
+// Sums of dw or db: blocks x width (grad_plan: at most three blocks on an SM up to a width of 256, two up to 4096, one beyond).
 size_t norm_grad_part_bytes(int max_width) {
     size_t most = 0;
-    const int limit[3] = {2048, 4096, kNormMaxWidth};
+    const int limit[3] = {256, 4096, kNormMaxWidth};
     for (int i = 0; i < 3; ++i) {
-        const size_t n = (size_t)(4 - i) * (size_t)(max_width < limit[i] ? max_width : limit[i]);
+        const size_t n = (size_t)(3 - i) * (size_t)(max_width < limit[i] ? max_width : limit[i]);
         if (n > most) most = n;
     }
     return (size_t)kTrainSms * most * 4;
@@ -574,10 +624,12 @@ cudaError_t init_norm_kernels() {
         const cudaError_t e = for_types(t < 3 ? 0 : t - 2, t < 3 ? t : t - 2, [&](auto* x, auto* y) {
             using XT = std::remove_pointer_t<decltype(x)>;
             using YT = std::remove_pointer_t<decltype(y)>;
-            cudaError_t r = init_all(0, norm_rows_kernel<XT, YT, 1>, norm_rows_kernel<XT, YT, 2>, norm_rows_kernel<XT, YT, 4>, norm_loop_kernel<XT, YT>);
+            cudaError_t r = init_all(0, norm_rows_kernel<XT, YT, 1>, norm_rows_kernel<XT, YT, 2>, norm_rows_kernel<XT, YT, 4>, norm_scalar_kernel<XT, YT, 32>,
+                                     norm_scalar_kernel<XT, YT, 64>, norm_scalar_kernel<XT, YT, 128>, norm_scalar_kernel<XT, YT, 256>,
+                                     norm_scalar_kernel<XT, YT, 512>);
             if (r == cudaSuccess) r = init_grad_rows<XT, YT, false>();
             if (r == cudaSuccess) r = init_grad_rows<XT, YT, true>();
-            return r != cudaSuccess ? r : init_all(kLoopSmem, norm_grad_loop_kernel<XT, YT, false>, norm_grad_loop_kernel<XT, YT, true>);
+            return r;
         });
         if (e != cudaSuccess) return e;
     }

@@ -17,7 +17,7 @@ namespace mars {
 namespace {
 
 constexpr int kThreads = 256, kSmallThreads = 512, kRun = 128;      // a warp works on runs of 128 tokens, four for each lane
-constexpr int kSmallTokens = 8192;                                  // up to here one block does everything
+constexpr int kSmallTokens = 4096;                                  // up to here one block does everything
 
 // Four neighbouring values, `fill` behind the last token.
 template <typename T>

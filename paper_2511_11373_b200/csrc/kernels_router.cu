@@ -42,7 +42,8 @@ __device__ __forceinline__ void load4(const T* row, int j, int lane, int experts
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = expert_of<false>(j, i, lane);
-            o[i] = c < experts ? to_float(row[c]) : fill;
+            o[i] = load_if(row + c, c < experts);
+            if (c >= experts) o[i] = fill;
         }
     }
 }
@@ -65,7 +66,7 @@ __device__ __forceinline__ void group_load4(const T* row, int j, int l, int expe
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = (j * 4 + i) * L + l;
-            o[i] = c < experts ? to_float(row[c]) : 0.f;
+            o[i] = load_if(row + c, c < experts);
         }
     }
 }
@@ -333,9 +334,10 @@ __global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_ker
 // for fp32 a row whose last choice and largest loser agree in the leading bits, or whose choices are out of order, is checked against the
 // values, and chosen again by the warp where that shows a difference.  The same pass over the row takes the exponentials, which go back
 // to shared memory; the lanes then add the columns up.
-constexpr int kManyExperts = 256, kManyK = 8, kManyRows = 8192;
+constexpr int kManyExperts = 512, kManyK = 8, kManyRows = 8192;
 // Warps of the one block that an SM's shared memory holds: few blocks leave few sums for the last one to add.
-template <bool WIDE> constexpr int kManyWarps = WIDE ? 12 : 24;
+// COLUMNS: 128 experts each.
+template <int COLUMNS> constexpr int kManyWarps = 24 / COLUMNS;
 constexpr int kTileRows = 16;
 __host__ __device__ constexpr int many_pitch(int experts) { return (experts + 63) / 64 * 64 + 4; }
 
@@ -377,12 +379,15 @@ __device__ __forceinline__ uint32_t leading(float v) {
     return (b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) & ~LOW;
 }
 
-template <typename T, bool V, bool WIDE>
-__global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(const RouterArgs a) {
-    constexpr int kWarps = kManyWarps<WIDE>, kThreads = kWarps * 32, kColumns = WIDE ? 2 : 1;     // columns: fours of a lane
+template <typename T, bool V, int kColumns>
+__global__ void __launch_bounds__(kManyWarps<kColumns> * 32, 1) router_many_kernel(const RouterArgs a) {
+    constexpr int kWarps = kManyWarps<kColumns>, kThreads = kWarps * 32;
+    // the last bits of a key: the largest number of a logit, or of a four, minus its number
+    constexpr int kBits = kColumns > 2 ? 9 : 8;
+    constexpr uint32_t kLow = (1u << kBits) - 1, kLowFour = kLow >> 2;
     extern __shared__ float tiles[];                          // [warps][16][pitch]
-    __shared__ float sums[kManyExperts], scale[kWarps][kTileRows];
-    __shared__ int counts[kManyExperts];
+    __shared__ float sums[kColumns * 128], scale[kWarps][kTileRows];
+    __shared__ int counts[kColumns * 128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.experts, k = a.top_k, pitch = many_pitch(E), padded = pitch - 4, fours = (E + 3) / 4;
     const int r = lane & 15, h = lane >> 4, half = padded / 2;           // row of the tile and half of it
     float* tile = tiles + warp * kTileRows * pitch;
@@ -430,7 +435,7 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
                 for (int c = lane; c < E; c += 32) {
                     float v[8];
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = r0 + q < rows ? to_float(in[(r0 + q) * a.ld + c]) : 0.f;
+                    for (int q = 0; q < 8; ++q) v[q] = load_if(in + (r0 + q) * a.ld + c, r0 + q < rows);
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
                         if (r0 + q < rows) tile[(r0 + q) * pitch + c] = v[q];
@@ -451,26 +456,26 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
                 for (int i = 0; i < 8; ++i) {
                     const int g = first + c * 8 + i;
                     const float4 v = *reinterpret_cast<const float4*>(mine + g * 4);
-                    key[i] = leading<63>(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))) | (uint32_t)(63 - g);
+                    key[i] = leading<kLowFour>(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))) | (kLowFour - g);
                 }
                 take8(groups, key, lost_group);
             }
         } else {                                              // eight fours in all
 #pragma unroll
-            for (int i = 0; i < 8; ++i) groups[i] = 0xffffffc0u | (uint32_t)(63 - first - i);
+            for (int i = 0; i < 8; ++i) groups[i] = ~kLowFour | (kLowFour - first - i);
         }
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             uint32_t key[8];
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const int g = min(63 - (int)(groups[i + q] & 63u), padded / 4 - 1);
+                const int g = min((int)(kLowFour - (groups[i + q] & kLowFour)), padded / 4 - 1);
                 const float4 v = *reinterpret_cast<const float4*>(mine + g * 4);
-                const uint32_t code = 255 - g * 4;            // 255 - expert
-                key[q * 4] = leading<255>(v.x) | code;
-                key[q * 4 + 1] = leading<255>(v.y) | (code - 1);
-                key[q * 4 + 2] = leading<255>(v.z) | (code - 2);
-                key[q * 4 + 3] = leading<255>(v.w) | (code - 3);
+                const uint32_t code = kLow - g * 4;
+                key[q * 4] = leading<kLow>(v.x) | code;
+                key[q * 4 + 1] = leading<kLow>(v.y) | (code - 1);
+                key[q * 4 + 2] = leading<kLow>(v.z) | (code - 2);
+                key[q * 4 + 3] = leading<kLow>(v.w) | (code - 3);
             }
             take8(best, key, lost);
         }
@@ -485,7 +490,7 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
         float val[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            idx[i] = min(255 - (int)(best[i] & 255u), E - 1);
+            idx[i] = min((int)(kLow - (best[i] & kLow)), E - 1);
             val[i] = mine[idx[i]];
         }
         float m = val[0], sum = 0.f;
@@ -501,7 +506,7 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
                     last = best[i];
                     next = i < 7 ? best[i < 7 ? i + 1 : 7] : 0u;
                 }
-            bool close = !sorted || (last >> 8) == (max(next, lost) >> 8) || (groups[7] >> 6) == (lost_group >> 6);
+            bool close = !sorted || (last >> kBits) == (max(next, lost) >> kBits) || (groups[7] >> (kBits - 2)) == (lost_group >> (kBits - 2));
             int larger = 0, above = 0;                        // logits, and chosen ones, that are larger than the least chosen
             if (__any_sync(0xffffffffu, on && close)) {
                 for (int c = first; c < min(fours, first + half / 4); ++c) {
@@ -518,19 +523,19 @@ __global__ void __launch_bounds__(kManyWarps<WIDE> * 32, 1) router_many_kernel(c
                 const int bad = __ffs(again) - 1;
                 again &= again - 1;
                 const float* other = tile + bad * pitch;
-                uint32_t key[kManyExperts / 32];
+                uint32_t key[kColumns * 4];
 #pragma unroll
-                for (int j = 0; j < kManyExperts / 32; ++j) key[j] = j * 32 + lane < E ? order_key(other[j * 32 + lane]) : 0u;
+                for (int j = 0; j < kColumns * 4; ++j) key[j] = j * 32 + lane < E ? order_key(other[j * 32 + lane]) : 0u;
                 for (int i = 0; i < k; ++i) {
                     uint32_t top = 0;
                     int at = 0;
 #pragma unroll
-                    for (int j = 0; j < kManyExperts / 32; ++j)
+                    for (int j = 0; j < kColumns * 4; ++j)
                         if (key[j] > top) { top = key[j]; at = j * 32 + lane; }
                     const uint32_t most = __reduce_max_sync(0xffffffffu, top);
                     const int e = (int)__reduce_min_sync(0xffffffffu, top == most ? (uint32_t)at : 0xffffffffu);
 #pragma unroll
-                    for (int j = 0; j < kManyExperts / 32; ++j)
+                    for (int j = 0; j < kColumns * 4; ++j)
                         if (j * 32 + lane == e) key[j] = 0;
                     if (r == bad) {
 #pragma unroll
@@ -774,9 +779,9 @@ cudaError_t router_launch(const RouterArgs& a, int sms, cudaStream_t st) {
 template <typename T, bool V>
 cudaError_t router_typed(const RouterArgs& a, int sms, cudaStream_t st) {
     if (a.experts <= kManyExperts && a.top_k <= kManyK && a.rows >= kManyRows) {
-        const int warps = a.experts <= 128 ? kManyWarps<false> : kManyWarps<true>;
+        const int warps = a.experts <= 128 ? kManyWarps<1> : a.experts <= 256 ? kManyWarps<2> : kManyWarps<4>;
         const int64_t need = ((int64_t)a.rows + kTileRows - 1) / kTileRows;
-        return launch_plain(a.experts <= 128 ? router_many_kernel<T, V, false> : router_many_kernel<T, V, true>,
+        return launch_plain(a.experts <= 128 ? router_many_kernel<T, V, 1> : a.experts <= 256 ? router_many_kernel<T, V, 2> : router_many_kernel<T, V, 4>,
                             dim3((unsigned)(need < sms ? need : sms)), dim3(warps * 32), (size_t)warps * kTileRows * many_pitch(a.experts) * 4, st, a);
     }
     if (a.experts <= 128) return router_launch<T, 1, V>(a, sms, st);
@@ -803,8 +808,9 @@ cudaError_t router_grad_typed(const RouterGradArgs& a, int sms, cudaStream_t st)
 
 template <typename T, bool V>
 cudaError_t router_init() {
-    cudaError_t e = init_all(kManyWarps<false> * kTileRows * many_pitch(128) * 4, router_many_kernel<T, V, false>);
-    if (e == cudaSuccess) e = init_all(kManyWarps<true> * kTileRows * many_pitch(kManyExperts) * 4, router_many_kernel<T, V, true>);
+    cudaError_t e = init_all(kManyWarps<1> * kTileRows * many_pitch(128) * 4, router_many_kernel<T, V, 1>);
+    if (e == cudaSuccess) e = init_all(kManyWarps<2> * kTileRows * many_pitch(256) * 4, router_many_kernel<T, V, 2>);
+    if (e == cudaSuccess) e = init_all(kManyWarps<4> * kTileRows * many_pitch(512) * 4, router_many_kernel<T, V, 4>);
     if (e != cudaSuccess) return e;
     return init_all(0, router_kernel<T, 1, V>, router_kernel<T, 2, V>, router_kernel<T, 4, V>, router_kernel<T, 8, V>, router_grad_kernel<T, 4, 2, V>,
                     router_grad_kernel<T, 8, 4, V>, router_grad_kernel<T, 16, 4, V>, router_grad_kernel<T, 32, 4, V>,

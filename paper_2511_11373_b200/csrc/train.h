@@ -34,7 +34,7 @@ cudaError_t init_router_kernels();
 cudaError_t init_policy_kernels();
 
 constexpr int kTrainSms = 148;               // SMs for which workspaces are laid out; grids take no more
-constexpr int kNormMaxWidth = 16384;
+constexpr int kNormMaxWidth = 8192;
 constexpr int kRouterMaxExperts = 1024, kRouterMaxK = 32;
 constexpr int kPolicyStats = 6;
 

@@ -67,6 +67,17 @@ __device__ __forceinline__ void store8(T* p, const Raw8<T>& r) {
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(T) / 2); ++i) *(reinterpret_cast<uint4*>(p) + i) = r.v[i];
 }
+// A value, or 0 without a load.
+__device__ __forceinline__ float load_if(const float* p, bool in) { return in ? *p : 0.f; }
+__device__ __forceinline__ float load_if(const __nv_bfloat16* p, bool in) {
+    const uint32_t b = in ? *reinterpret_cast<const uint16_t*>(p) : 0u;
+    return __uint_as_float(b << 16);
+}
+__device__ __forceinline__ float load_if(const __half* p, bool in) {
+    const uint16_t b = in ? *reinterpret_cast<const uint16_t*>(p) : (uint16_t)0;
+    return __half2float(__ushort_as_half(b));
+}
+
 // Value i of a small tensor whose type is known at run time (MARS_F32, MARS_BF16, MARS_F16).
 __device__ __forceinline__ float load_any(const void* p, int type, int64_t i) {
     if (type == 0) return static_cast<const float*>(p)[i];
