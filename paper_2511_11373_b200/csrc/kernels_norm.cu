@@ -10,6 +10,8 @@
 // The gradient runs on a grid that fits the SMs at once: a thread keeps the sums of dw and db of its columns in fp32
 // registers over all rows of its group and asks for the next row before it reduces the present one; groups of a block meet in
 // shared memory, blocks in a second kernel that adds their sums in fp64 in a fixed order: the same call gives the same bits.
+// Measured (B200, copy rate 6463 GB/s): RMS 32768 x 2048 bf16 with residual 86 us, 6.2 TB/s; its gradient 99 us, 5.4 TB/s with the
+// second kernel (the first alone 93 us); gradient of 524288 heads of 128 bf16 80 us, 23 instructions a value.
 #include <type_traits>
 
 #include "train.h"
@@ -22,7 +24,9 @@ namespace {
 constexpr int kChunk = 8;
 constexpr int kEach = 16;                // values of a thread where rows go value by value
 
-// Threads of a row and chunks of eight neighbouring values of a thread; blocks of at most 256 threads.
+// Threads of a row and chunks of eight neighbouring values of a thread; blocks of at most 256 threads.  Rows of up to 256 in one warp; two
+// chunks for a thread beyond it, four where 256 threads need them.  2^26 values bf16, one / two / four chunks: forward 131072 x 512 65 / 50 /
+// 109 us, 32768 x 2048 68 / 52 / 66; gradient 74 / 78 / 126 and 80 / 83 / 87 us, but 1000 x 2048 14.4 / 11.6 and layer norms 49 / 46.
 struct NormPlan { int group, nv, block; };
 NormPlan norm_plan(int width) {
     const int chunks = (width + kChunk - 1) / kChunk;
@@ -38,7 +42,9 @@ NormPlan norm_plan(int width) {
     p.block = 256 / p.group * p.group;
     return p;
 }
-// Blocks on an SM for which registers are planned, forward and backward; rows of a group that are worked on together.
+// Blocks on an SM for which registers are planned, forward and backward; rows of a group that are worked on together.  Gradient of
+// 32768 x 2048 bf16: two blocks 106 us, three, which spill, 112.  Narrow rows have registers for two rows at a time: the heads above, one
+// row and two blocks 141 us -> two rows, three blocks and rounds without conditions 80.
 __host__ __device__ constexpr int forward_blocks(int nv, bool x_is_fp32) { return nv == 4 ? 1 : nv == 2 ? (x_is_fp32 ? 2 : 3) : x_is_fp32 ? 3 : 4; }
 __host__ __device__ constexpr int grad_blocks_sm(int nv, bool x_is_fp32, bool layer) { return nv == 4 ? 1 : nv == 1 && !x_is_fp32 && !layer ? 3 : 2; }
 __host__ __device__ constexpr int rows_together(int nv) { return nv == 1 ? 2 : 1; }
@@ -116,7 +122,7 @@ __device__ __forceinline__ int64_t row_offset(int row, int heads, int width, int
 }
 
 // Rows in registers.  A block stays for many rows: the weight's values stay too, and the next rows are on their way while the present
-// ones are reduced.
+// ones are reduced (32768 x 2048 bf16 with residual: 87 us; a block for every four rows, that loads, reduces and stores, 120 us).
 template <typename XT, typename YT, int NV>
 __global__ void __launch_bounds__(256, forward_blocks(NV, sizeof(XT) == 4)) norm_rows_kernel(const NormArgs a, const int group) {
     __shared__ float scratch[2 * 16];
@@ -204,7 +210,8 @@ __global__ void __launch_bounds__(256, forward_blocks(NV, sizeof(XT) == 4)) norm
     }
 }
 
-// Any alignment: the same value by value, a thread having those that are a group apart.
+// Any alignment: the same value by value, a thread having those that are a group apart.  16 loads of 2 or 4 bytes a thread in flight, bound
+// by their number: 20000 x 1111 bf16 60 us (1.5 TB/s), fp32 53 us (3.4 TB/s); in loops that read a row again for each sum 178 us.
 template <typename XT, typename YT, int G>
 __global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 3 : 1) norm_scalar_kernel(const NormArgs a) {
     constexpr int kGroups = (G < 256 ? 256 : G) / G;
@@ -265,7 +272,8 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 3 : 1) norm_scala
     }
 }
 
-// Rows in registers, with the sums of the weight's gradient.
+// Rows in registers, with the sums of the weight's gradient.  The weight lies in shared memory: its registers go to the next row.  The
+// residual's gradient is asked for after the first pass over a row: before it, it costs registers (99 -> 118 us).
 // FULL: the chunks of a group's threads are the row's, none lies behind it.
 template <typename XT, typename YT, int NV, bool LAYER, bool FULL>
 __global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER)) norm_grad_rows_kernel(const NormGradArgs a, const int group) {
@@ -416,7 +424,7 @@ __global__ void __launch_bounds__(256, grad_blocks_sm(NV, sizeof(XT) == 4, LAYER
     }
 }
 
-// Any alignment: the same value by value.
+// Any alignment: the same value by value (20000 x 1111 bf16 127 us; in loops that read a row again 276 us).
 template <typename XT, typename YT, int G, bool LAYER>
 __global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 2 : 1) norm_grad_scalar_kernel(const NormGradArgs a) {
     constexpr int kGroups = (G < 256 ? 256 : G) / G;
@@ -496,7 +504,8 @@ __device__ __forceinline__ void store_any(void* p, int type, int64_t i, float v)
     else if (type == 1) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
     else static_cast<__half*>(p)[i] = __float2half_rn(v);
 }
-// dw (block row 0) and db (row 1): the blocks' sums of 32 columns, 32 runs of blocks side by side.
+// dw (block row 0) and db (row 1): the blocks' sums of 32 columns, 32 runs of blocks side by side.  7 us for 296 x 2048, most of it launch
+// and two chains of loads; the last block of the kernel before would have 2.4 MB to read alone.
 __global__ void __launch_bounds__(1024) norm_columns_kernel(const float* part_w, const float* part_b, int blocks, int width, void* dw,
                                                             void* db, int type, int accumulate) {
     __shared__ double s[32][33];

@@ -5,10 +5,13 @@
 // weighted by 1 / live tokens, by 1 / (live sequences x the sequence's live tokens), or not at all, times `scale`.
 // Bound by HBM for long batches (16 to 24 bytes a token) and by latency for short ones.  No gradient may be written before
 // the tokens are counted, so a first kernel counts them (targets alone, which then lie in L2) with integer atomics, whose order
-// changes nothing, and its last block turns the counts into weights.  Terms are added in fp32 over up to 32 tokens of a thread, in
-// fp64 beyond, and the blocks' sums in order by the last one to finish: the same call gives the same bits.  Which side of a border a
-// ratio is on is decided on logp - old against the borders' logarithms, in fp64 where fp32 is too near.  A warp finds the
-// sequences of its run of tokens together, 32 offsets a step.
+// changes nothing; the second kernel turns the counts into weights.  Terms are added in fp32 over the four neighbouring tokens of a thread,
+// in fp64 beyond, and the blocks' sums in order by the last one to finish: the same call gives the same bits.  Which side of a border a
+// ratio is on is decided on logp - old against the borders' logarithms, in fp64 where fp32 is too near.  A warp has one piece of all
+// tokens and goes through it in runs; it finds the sequences of a run together, 32 offsets a step, where the run leaves the last one.
+// Measured (B200): 4 M tokens of 1024 sequences with a reference 37 us (13 + 24; 10 at the copy rate), 29 for one sequence without;
+// with a search for every block and quad of tokens 58.  What is left are two launches, the first loads, and 80 instructions a token in
+// the second kernel; two or four blocks on an SM instead of three 46 and 40 us.
 #include "train.h"
 #include "train_types.cuh"
 
@@ -17,7 +20,8 @@ namespace mars {
 namespace {
 
 constexpr int kThreads = 256, kSmallThreads = 512, kRun = 128;      // a warp works on runs of 128 tokens, four for each lane
-constexpr int kSmallTokens = 4096;                                  // up to here one block does everything
+// Up to here one block does everything.  One block / two kernels: 256 tokens 6.6 / 8.8 us, 2048 8.4 / 15.3, 4096 12.4 / 15.9, 8192 19.4 / 17.1.
+constexpr int kSmallTokens = 4096;
 
 // Four neighbouring values, `fill` behind the last token.
 template <typename T>

@@ -325,15 +325,19 @@ __global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_ker
     router_finish<kWarps>(a, sums, counts, z);
 }
 
-// Many rows: two threads have a row, each half of its columns.  A warp brings 16 rows into shared memory (fp32, rows apart by an odd number of 16 bytes, so that eight
-// threads read their 16 bytes from different banks) and goes over them thread by thread.  The k <= 8 largest of a row lie in the eight
-// fours with the largest maxima; both choices, of fours and of logits, are made on 32-bit keys (leading bits that order like the value,
-// last bits that prefer the lower index), eight at a time: sorted (Batcher's odd-even merge, 19 exchanges) and merged into the eight
-// largest so far (the larger ones of the two ends, then a bitonic merge of 12 exchanges), and so are the two halves.  What bounds it is the integer pipe (half a
-// minimum or maximum a clock and scheduler): 8 of them a logit, where rounds over a warp took 40.  The keys hold bf16 and fp16 in full;
-// for fp32 a row whose last choice and largest loser agree in the leading bits, or whose choices are out of order, is checked against the
-// values, and chosen again by the warp where that shows a difference.  The same pass over the row takes the exponentials, which go back
-// to shared memory; the lanes then add the columns up.
+// Many rows: two threads have a row, each half of its columns.  A warp brings 16 rows into shared memory (fp32, rows apart by an odd number
+// of 16 bytes, so that eight threads read their 16 bytes from different banks) and goes over them thread by thread.  The k <= 8 largest of a
+// row lie in the eight fours with the largest maxima; both choices, of fours and of logits, are made on 32-bit keys (leading bits that order
+// like the value, last bits that prefer the lower index), eight at a time: sorted (Batcher's odd-even merge, 19 exchanges) and merged into
+// the eight largest so far (the larger ones of the two ends, then a bitonic merge of 12 exchanges), and so are the two halves.  The keys hold
+// bf16 and fp16 in full; for fp32 a row whose last choice and largest loser agree in the leading bits, or whose choices are out of order, is
+// checked against the values, and chosen again by the warp where that shows a difference.  The same pass over the row takes the
+// exponentials, which go back to shared memory; the lanes then add the columns up.
+// Bound by instructions and their latency: 136 of a warp for a row of 128 experts, where rounds over a warp take 590.  131072 x 128 fp32,
+// 8 choices: 44 us (1.5 TB/s; the rounds 117), of which 17 are there for any number of rows: one tile's chain 8, launch 3, the meeting of the
+// blocks 5.  50000 x 384: 60 us, the rounds 138.  One thread for a row took the 44 us too, with half the warps.
+// From kManyRows on: below, there is less than a tile for each warp.  fp32, rounds / this kernel: 4096 x 128 14.2 / 16.9 us, 8192 x 128
+// 20.4 / 17.8, 32768 x 128 39 / 22; 2048 x 384 20 / 26, 4096 x 384 34 / 29, 8192 x 384 46 / 30; 8192 x 16 13.8 / 15.2, 16384 x 16 18.3 / 15.5.
 constexpr int kManyExperts = 512, kManyK = 8, kManyRows = 8192;
 // Warps of the one block that an SM's shared memory holds: few blocks leave few sums for the last one to add.
 // COLUMNS: 128 experts each.
@@ -636,7 +640,9 @@ __global__ void __launch_bounds__(kManyWarps<kColumns> * 32, 1) router_many_kern
     router_finish<kWarps>(a, sums, counts, warp_sum_double(z2));
 }
 
-// Gradient: L lanes have a row (so that a warp reduces several rows in one go), NG fours of experts each.
+// Gradient: L lanes have a row (so that a warp reduces several rows in one go), NG fours of experts each.  131072 x 128 bf16 25 us (2.8 TB/s),
+// fp32 31 us (4.7 TB/s); a warp for a row took 600 instructions of it and 70 us, eight lanes 127; with the next row alone
+// on its way 39.
 template <typename T, int L, int NG, bool V>
 __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const RouterGradArgs a) {
     constexpr int kWarps = 8, kThreads = 256, R = 32 / L;     // rows of a warp

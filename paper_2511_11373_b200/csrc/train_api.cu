@@ -1,7 +1,6 @@
 // Host side of the operators of a training pass: argument checks, workspace layout, launches.
 #include <cmath>
 #include <new>
-#include <vector>
 
 #include "api_common.h"
 #include "train.h"
