@@ -513,6 +513,7 @@ __global__ void __launch_bounds__(1024) norm_columns_kernel(const float* part_w,
     void* out = blockIdx.y ? db : dw;
     const int c = blockIdx.x * 32 + threadIdx.x;
     double t = 0.;
+    pdl_wait();
     if (out && c < width) {
 #pragma unroll 8
         for (int b = threadIdx.y; b < blocks; b += 32) t += part[(int64_t)b * width + c];
@@ -664,8 +665,10 @@ cudaError_t launch_norm_grad(const NormGradArgs& a, int x_type, int y_type, bool
         if (e != cudaSuccess) return e;
     }
     if (!dw && !db) return cudaSuccess;
-    return launch_plain(norm_columns_kernel, dim3((unsigned)((a.width + 31) / 32), db ? 2u : 1u), dim3(32, 32), 0, st,
-                        (const float*)a.part_w, (const float*)a.part_b, a.rows > 0 ? g.blocks : 0, a.width, dw, db, dw_type, accumulate);
+    const dim3 grid((unsigned)((a.width + 31) / 32), db ? 2u : 1u), block(32, 32);
+    const float *w = a.part_w, *b = a.part_b;
+    if (a.rows == 0) return launch_plain(norm_columns_kernel, grid, block, 0, st, w, b, 0, a.width, dw, db, dw_type, accumulate);
+    return launch_second(norm_columns_kernel, grid, block, 0, st, w, b, g.blocks, a.width, dw, db, dw_type, accumulate);
 }
 
 }  // namespace mars

@@ -9,9 +9,9 @@
 // in fp64 beyond, and the blocks' sums in order by the last one to finish: the same call gives the same bits.  Which side of a border a
 // ratio is on is decided on logp - old against the borders' logarithms, in fp64 where fp32 is too near.  A warp has one piece of all
 // tokens and goes through it in runs; it finds the sequences of a run together, 32 offsets a step, where the run leaves the last one.
-// Measured (B200): 4 M tokens of 1024 sequences with a reference 37 us (13 + 24; 10 at the copy rate), 29 for one sequence without;
+// Measured (B200): 4 M tokens of 1024 sequences with a reference 34 us (13 + 24 alone, 37 one after the other; 10 at the copy rate);
 // with a search for every block and quad of tokens 58.  What is left are two launches, the first loads, and 80 instructions a token in
-// the second kernel; two or four blocks on an SM instead of three 46 and 40 us.
+// the second kernel; two or four blocks on an SM instead of three 46 and 40 us; the first kernel asking for the second one's lines in L2 + 3.
 #include "train.h"
 #include "train_types.cuh"
 
@@ -284,15 +284,20 @@ __device__ __forceinline__ double term_share(const PolicyArgs& a, int live, int 
 }
 
 // Terms and derivatives of a warp's tokens; sums: loss, kl, cut ratios, ratios.
-template <bool REF>
+// SECOND: of the second kernel, which waits for the first one's counts.
+template <bool REF, bool SECOND>
 __device__ __forceinline__ void loss_tokens(const PolicyArgs& a, int warp, int warps, double (&sums)[4]) {
     const int lane = threadIdx.x & 31, begin = a.seq_off[0];
     const Piece p = warp_piece(a.tokens, kRun, warp, warps);
-    if (p.begin >= p.end) return;
+    if (p.begin >= p.end) {
+        if (SECOND) pdl_wait();
+        return;
+    }
     Inputs v = load_inputs<REF>(a, p.begin + lane * 4);
+    int first = find_sequence(a.seq_off, 0, a.seqs, p.begin), of = -1;      // of: the sequence of share and seq_adv
+    if (SECOND) pdl_wait();
     const int live = __ldcg(a.totals), held = __ldcg(a.totals + 1);
     const float log_low = (float)a.log_low, log_high = (float)a.log_high;
-    int first = find_sequence(a.seq_off, 0, a.seqs, p.begin), of = -1;      // of: the sequence of share and seq_adv
     double share = 0.;
     float seq_adv = 0.f;
     for (int t0 = p.begin; t0 < p.end; t0 += kRun) {
@@ -372,6 +377,7 @@ __device__ __forceinline__ void write_stats(const PolicyArgs& a, double v) {
 }
 
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(const PolicyArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;");        // all blocks have started: those of the second kernel come in as these end
     int live, held;
     count_tokens<4>(a, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32), live, held);
     add_totals<kThreads / 32>(a, live, held);
@@ -382,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 3) policy_loss_kernel(const PolicyAr
     __shared__ double reduce[kThreads / 32][4];
     __shared__ int last;
     double sums[4] = {0., 0., 0., 0.};
-    loss_tokens<REF>(a, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32), sums);
+    loss_tokens<REF, true>(a, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32), sums);
     double v = block_sums<kThreads / 32>(sums, reduce);
     if (threadIdx.x < 4) {
         a.parts[(int64_t)blockIdx.x * 4 + threadIdx.x] = v;
@@ -417,7 +423,7 @@ __global__ void __launch_bounds__(kSmallThreads) policy_small_kernel(const Polic
     __threadfence();
     __syncthreads();
     double sums[4] = {0., 0., 0., 0.};
-    loss_tokens<REF>(a, threadIdx.x >> 5, kSmallThreads / 32, sums);
+    loss_tokens<REF, false>(a, threadIdx.x >> 5, kSmallThreads / 32, sums);
     write_stats(a, block_sums<kSmallThreads / 32>(sums, reduce));
 }
 
@@ -438,7 +444,7 @@ cudaError_t launch_policy_loss(const PolicyArgs& a, int sms, cudaStream_t st) {
     const dim3 grid((unsigned)(need < most ? need : most)), block(kThreads);
     const cudaError_t e = launch_plain(policy_count_kernel, dim3((unsigned)counting), block, 0, st, a);
     if (e != cudaSuccess) return e;
-    return launch_plain(a.has_ref ? policy_loss_kernel<true> : policy_loss_kernel<false>, grid, block, 0, st, a);
+    return launch_second(a.has_ref ? policy_loss_kernel<true> : policy_loss_kernel<false>, grid, block, 0, st, a);
 }
 
 }  // namespace mars

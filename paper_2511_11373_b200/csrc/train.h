@@ -6,7 +6,7 @@
 
 namespace mars {
 
-// Launches of these operators are ordinary ones: a grid starts when the work before it on the stream is done.  Their kernels are loaded when
+// A call's first launch is an ordinary one: the grid starts when the work before it on the stream is done.  The kernels are loaded when
 // a handle is created (init_*_kernels), not at a first launch among other work.
 template <typename... Params, typename... Args>
 inline cudaError_t launch_plain(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
@@ -15,6 +15,22 @@ inline cudaError_t launch_plain(void (*kernel)(Params...), dim3 grid, dim3 block
     cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args&&>(args)...);
+}
+// Launch of the second kernel of a call: its blocks may start while the first one, an ordinary launch of the same call, drains.  All of its threads
+// pass pdl_wait() before they read what the first kernel writes, and before they write.
+template <typename... Params, typename... Args>
+inline cudaError_t launch_second(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args&&>(args)...);
 }
 // Loads kernels, and lets them use up to `smem` bytes of dynamic shared memory where that is more than they may anyway.
