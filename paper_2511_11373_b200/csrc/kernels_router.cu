@@ -73,27 +73,35 @@ __device__ __forceinline__ void group_load4(const T* row, int j, int l, int expe
 // Four values as they lie in memory.
 template <typename T> struct Four { uint2 v; };
 template <> struct Four<float> { float4 v; };
-__device__ __forceinline__ void unpack_four(const Four<float>& f, float (&o)[4]) { o[0] = f.v.x; o[1] = f.v.y; o[2] = f.v.z; o[3] = f.v.w; }
-template <typename T>
-__device__ __forceinline__ void unpack_four(const Four<T>& f, float (&o)[4]) {
-    unpack2(f.v.x, o[0], o[1], T());
-    unpack2(f.v.y, o[2], o[3], T());
+__device__ __forceinline__ void unpack_four(const Four<float>& f, float2 (&o)[2]) {
+    o[0] = make_float2(f.v.x, f.v.y);
+    o[1] = make_float2(f.v.z, f.v.w);
 }
+template <typename T>
+__device__ __forceinline__ void unpack_four(const Four<T>& f, float2 (&o)[2]) {
+    unpack2(f.v.x, o[0].x, o[0].y, T());
+    unpack2(f.v.y, o[1].x, o[1].y, T());
+}
+// -inf in all four
+__device__ __forceinline__ uint32_t two_neg_inf(__nv_bfloat16) { return 0xff80ff80u; }
+__device__ __forceinline__ uint32_t two_neg_inf(__half) { return 0xfc00fc00u; }
+__device__ __forceinline__ void clear_four(Four<float>& f) { f.v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY); }
+template <typename T>
+__device__ __forceinline__ void clear_four(Four<T>& f) { f.v = make_uint2(two_neg_inf(T()), two_neg_inf(T())); }
+// -inf behind the last expert
 template <typename T, int L, bool V>
 __device__ __forceinline__ Four<T> load_four(const T* row, int j, int l, int experts) {
     Four<T> f;
     if constexpr (V) {
         const int c = (j * L + l) * 4;
-        if (c < experts) {
-            f.v = *reinterpret_cast<const decltype(f.v)*>(row + c);
-        } else if constexpr (sizeof(T) == 4) {
-            f.v = make_float4(0.f, 0.f, 0.f, 0.f);
-        } else {
-            f.v = make_uint2(0u, 0u);
-        }
+        clear_four(f);
+        if (c < experts) f.v = *reinterpret_cast<const decltype(f.v)*>(row + c);
     } else {
         float o[4];
         group_load4<T, L, false>(row, j, l, experts, o);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if ((j * 4 + i) * L + l >= experts) o[i] = -INFINITY;
         if constexpr (sizeof(T) == 4) f.v = make_float4(o[0], o[1], o[2], o[3]);
         else f.v = make_uint2(pack2(o[0], o[1], T()), pack2(o[2], o[3], T()));
     }
@@ -640,11 +648,28 @@ __global__ void __launch_bounds__(kManyWarps<kColumns> * 32, 1) router_many_kern
     router_finish<kWarps>(a, sums, counts, warp_sum_double(z2));
 }
 
-// Gradient: L lanes have a row (so that a warp reduces several rows in one go), NG fours of experts each.  131072 x 128 bf16 25 us (2.8 TB/s),
-// fp32 31 us (4.7 TB/s); a warp for a row took 600 instructions of it and 70 us, eight lanes 127; with the next row alone
-// on its way 39.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* smem_dst, const void* gsrc) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(smem_dst)), "l"(gsrc), "n"(BYTES));
+}
+// Adds v to a place that holds 0 but for an expert that was chosen twice: an exchange is one instruction in shared memory, an addition a loop.
+__device__ __forceinline__ void put(float* place, float v) {
+    const float before = atomicExch(place, v);
+    if (before != 0.f) atomicAdd(place, before);
+}
+constexpr int kAhead = 4;
+// Blocks on an SM: three of 16-bit logits, two of fp32 (shared memory of the ring), one of more than 512 experts.
+template <typename T, int NG> constexpr int kGradBlocks = NG > 4 ? 1 : sizeof(T) == 2 ? 3 : 2;
 template <typename T, int L, int NG, bool V>
-__global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const RouterGradArgs a) {
+constexpr int grad_smem(int experts) {
+    return 8 * (32 / L) * ((experts + 3) / 4 * 4 + 4) * 4 + (V ? 8 * kAhead * 32 * (NG * 4 * (int)sizeof(T) + 12) : 0);
+}
+// Gradient: L lanes have a row (so that a warp reduces several rows in one go), NG fours of experts each.  Bound by the bytes
+// that are on their way and by instructions: 131072 x 128 bf16 22 us (3.4 TB/s), fp32 26 (5.5 TB/s); without d_weights 17 and 24.  A warp
+// for a row took 600 instructions of it and 70 us; eight lanes with the next two rows in registers, two blocks on an SM, 24 and 30; the
+// weights' part added up in shared memory instead of exchanged + 1.
+template <typename T, int L, int NG, bool V>
+__global__ void __launch_bounds__(256, (kGradBlocks<T, NG>)) router_grad_kernel(const RouterGradArgs a) {
     constexpr int kWarps = 8, kThreads = 256, R = 32 / L;     // rows of a warp
     extern __shared__ float smem[];                           // [rows of the block][pitch]: the weights' part of a row
     __shared__ double reduce[kWarps];
@@ -663,59 +688,101 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const
     const double n = total > 0. ? total / k : 1.;             // live rows
     const float unit = total > 0. ? (float)((double)a.balance * E / n / total) : 0.f, zc = (float)(2. * (double)a.z / n);
     auto expert = [&](int j, int i) { return V ? (j * L + l) * 4 + i : (j * 4 + i) * L + l; };
-    float g[NG][4];
+    float2 g[NG][2];
 #pragma unroll
     for (int j = 0; j < NG; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) g[j][i] = expert(j, i) < E ? unit * a.counts[expert(j, i)] : 0.f;
-    const int64_t stride = (int64_t)gridDim.x * kWarps * R;
-    // the logits, lse and choices (the first L of them) of the next rows are on their way while this row is worked on: of two of 16 bits,
-    // of one of fp32 (registers)
-    constexpr int D = sizeof(T) == 2 && NG <= 4 ? 2 : 1;
-    Four<T> ahead[D][NG];
-    float ahead_lse[D], ahead_dw[D];
-    int ahead_idx[D], ahead_first[D];
-    auto fetch = [&](int64_t row, Four<T> (&z)[NG], float& lse, float& dw, int& idx, int& first) {
+        for (int i = 0; i < 2; ++i)
+            g[j][i] = make_float2(expert(j, 2 * i) < E ? unit * a.counts[expert(j, 2 * i)] : 0.f,
+                                  expert(j, 2 * i + 1) < E ? unit * a.counts[expert(j, 2 * i + 1)] : 0.f);
+    // Logits, lse and the first L choices of a row, with the weights' gradients.  Rows that allow it come by asynchronous copies into a ring of
+    // kAhead stages, three of them on their way while a row is worked on; a thread copies what it will read.  Others come by loads, one row ahead.
+    Four<T> z[NG];
+    float row_lse = 0.f, row_dw = 0.f;
+    int row_idx = -1;
+    auto fetch = [&](int64_t row) {
         const bool in_range = row < a.rows;
         const int64_t r = in_range ? row : 0;
 #pragma unroll
         for (int j = 0; j < NG; ++j) z[j] = load_four<T, L, V>(static_cast<const T*>(a.logits) + r * a.ld, j, l, in_range ? E : 0);
-        lse = in_range ? a.lse[r] : 0.f;
-        first = in_range ? a.idx[r * k] : -1;
-        idx = in_range && l < k ? a.idx[r * k + l] : -1;
-        dw = in_range && l < k && a.has_d_weights ? a.d_weights[r * k + l] : 0.f;
+        row_lse = in_range ? a.lse[r] : 0.f;
+        row_idx = in_range && l < k ? a.idx[r * k + l] : -1;
+        row_dw = in_range && l < k && a.has_d_weights ? a.d_weights[r * k + l] : 0.f;
     };
-    int64_t base = ((int64_t)blockIdx.x * kWarps + warp) * R;
-    if (base < a.rows) {
+    Four<T>* ring = reinterpret_cast<Four<T>*>(smem + kWarps * R * pitch) + warp * kAhead * NG * 32;                 // [stage][NG][lane]
+    float* tail = smem + kWarps * R * pitch + kWarps * kAhead * NG * 32 * (int)sizeof(Four<T>) / 4 + warp * kAhead * 96;      // [stage][lse, dw, idx][lane]
+    auto request = [&](int64_t row, int stage) {
+        if (row < a.rows) {
+            const T* in = static_cast<const T*>(a.logits) + row * a.ld + l * 4;
 #pragma unroll
-        for (int d = 0; d < D; ++d) fetch(base + d * stride + sub, ahead[d], ahead_lse[d], ahead_dw[d], ahead_idx[d], ahead_first[d]);
+            for (int j = 0; j < NG; ++j)
+                if (expert(j, 0) < E) copy_async<sizeof(Four<T>)>(ring + (stage * NG + j) * 32 + lane, in + j * L * 4);
+            float* s = tail + stage * 96 + lane;
+            copy_async<4>(s, a.lse + row);
+            if (l < k) {
+                copy_async<4>(s + 64, a.idx + row * k + l);
+                if (a.has_d_weights) copy_async<4>(s + 32, a.d_weights + row * k + l);
+            }
+        }
+        cp_async_commit();
+    };
+    const int64_t stride = (int64_t)gridDim.x * kWarps * R;
+    int64_t base = ((int64_t)blockIdx.x * kWarps + warp) * R;
+    int stage = 0;
+    if constexpr (V) {
+#pragma unroll
+        for (int s = 0; s < kAhead - 1; ++s) request(base + s * stride + sub, s);
+    } else {
+        fetch(base + sub);
     }
     for (; base < a.rows; base += stride) {
-        const bool in_range = base + sub < a.rows, on = ahead_first[0] >= 0;      // a row that took no part may hold anything
+        const bool in_range = base + sub < a.rows;
         const int64_t row = in_range ? base + sub : 0;
         const T* in = static_cast<const T*>(a.logits) + row * a.ld;
         T* out = static_cast<T*>(a.d_logits) + row * a.ld_d;
-        const int W = on ? E : 0, first_idx = ahead_idx[0];
-        const float lse = ahead_lse[0], first_dw = ahead_dw[0];
-        float v[NG][4];
-        float dot = 0.f;                                      // sum of p g, plus that of the selected where weights are p
+        const int here = stage;
+        if constexpr (V) {
+            cp_async_wait<kAhead - 2>();
+            __syncwarp();                                     // all lanes have this stage, and are done with the one that is filled again
+            request(base + (kAhead - 1) * stride + sub, (stage + kAhead - 1) % kAhead);
+            stage = (stage + 1) % kAhead;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                clear_four(z[j]);
+                if (expert(j, 0) < E) z[j] = ring[(here * NG + j) * 32 + lane];
+            }
+            const float* s = tail + here * 96 + lane;
+            row_lse = s[0];
+            row_dw = s[32];
+            row_idx = in_range && l < k ? __float_as_int(s[64]) : -1;
+        }
+        auto logit = [&](int e) {
+            if constexpr (V) {
+                const int f = e / 4;
+                return to_float(reinterpret_cast<const T*>(ring + (here * NG + f / L) * 32 + sub * L + f % L)[e % 4]);
+            } else {
+                return to_float(in[e]);
+            }
+        };
+        const int first_idx = row_idx;
+        const bool on = __shfl_sync(0xffffffffu, row_idx, sub * L) >= 0;      // a row that took no part may hold anything
+        const float lse = on ? row_lse : 0.f, first_dw = row_dw;
+        float2 v[NG][2], dots = make_float2(0.f, 0.f);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            unpack_four(ahead[0][j], v[j]);
+            if (!on) clear_four(z[j]);                        // p = 0, and so is all that follows
+            unpack_four(z[j], v[j]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[j][i] = expert(j, i) < W ? ex2((v[j][i] - lse) * kLog2e) : 0.f;
-                dot = fmaf(v[j][i], g[j][i], dot);
+            for (int i = 0; i < 2; ++i) {
+                v[j][i] = mul2(add2(v[j][i], make_float2(-lse, -lse)), make_float2(kLog2e, kLog2e));
+                v[j][i] = make_float2(ex2(v[j][i].x), ex2(v[j][i].y));
+                dots = fma2(v[j][i], g[j][i], dots);
             }
         }
+        float dot = dots.x + dots.y;                          // sum of p g, plus that of the selected where weights are p
         float w_first = 0.f;                                  // p of this lane's first choice
-        if (a.has_d_weights && on && (unsigned)first_idx < (unsigned)E) w_first = ex2((to_float(in[first_idx]) - lse) * kLog2e);
-        if (D == 2) {
-#pragma unroll
-            for (int j = 0; j < NG; ++j) ahead[0][j] = ahead[D - 1][j];
-            ahead_lse[0] = ahead_lse[D - 1]; ahead_dw[0] = ahead_dw[D - 1]; ahead_idx[0] = ahead_idx[D - 1]; ahead_first[0] = ahead_first[D - 1];
-        }
-        fetch(base + D * stride + sub, ahead[D - 1], ahead_lse[D - 1], ahead_dw[D - 1], ahead_idx[D - 1], ahead_first[D - 1]);
+        if (a.has_d_weights && on && (unsigned)first_idx < (unsigned)E) w_first = ex2((logit(first_idx) - lse) * kLog2e);
+        if constexpr (!V) fetch(base + stride + sub);
         if (a.has_d_weights) {
             // of renormalised weights' gradients only differences count: taken from that of the first choice, a weight next to 1 keeps the
             // accuracy of what the others leave it
@@ -724,7 +791,7 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const
             for (int i = l + L; i < k; i += L) {
                 const int e = on ? a.idx[row * k + i] : -1;
                 if ((unsigned)e < (unsigned)E) {
-                    const float w = ex2((to_float(in[e]) - lse) * kLog2e);
+                    const float w = ex2((logit(e) - lse) * kLog2e);
                     w_sum += w;
                     wdw = fmaf(w, a.d_weights[row * k + i] - from, wdw);
                 }
@@ -734,12 +801,12 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const
                 w_sum += __shfl_xor_sync(0xffffffffu, w_sum, o);
                 wdw += __shfl_xor_sync(0xffffffffu, wdw, o);
             }
-            const float inv = a.renormalise ? 1.f / w_sum : 1.f, mean = a.renormalise ? wdw * inv : 0.f;
-            if (on && (unsigned)first_idx < (unsigned)E) atomicAdd(mine + first_idx, w_first * inv * (first_dw - from - mean));
+            const float inv = a.renormalise ? __fdividef(1.f, w_sum) : 1.f, mean = a.renormalise ? wdw * inv : 0.f;
+            if (on && (unsigned)first_idx < (unsigned)E) put(mine + first_idx, w_first * inv * (first_dw - from - mean));
             for (int i = l + L; i < k; i += L) {
                 const int e = on ? a.idx[row * k + i] : -1;
                 if ((unsigned)e < (unsigned)E)
-                    atomicAdd(mine + e, ex2((to_float(in[e]) - lse) * kLog2e) * inv * (a.d_weights[row * k + i] - from - mean));
+                    put(mine + e, ex2((logit(e) - lse) * kLog2e) * inv * (a.d_weights[row * k + i] - from - mean));
             }
             if (!a.renormalise) dot += wdw / L;
             __syncwarp();
@@ -749,26 +816,30 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 2 : 1) router_grad_kernel(const
         const float shift = zc * lse - dot;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            float d[4], m[4] = {0.f, 0.f, 0.f, 0.f};
+            float2 m[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             if (a.has_d_weights) {
                 if (V) {
                     if (expert(j, 0) < E) {
                         const float4 q = *reinterpret_cast<const float4*>(mine + expert(j, 0));
-                        m[0] = q.x; m[1] = q.y; m[2] = q.z; m[3] = q.w;
+                        m[0] = make_float2(q.x, q.y);
+                        m[1] = make_float2(q.z, q.w);
                         *reinterpret_cast<float4*>(mine + expert(j, 0)) = make_float4(0.f, 0.f, 0.f, 0.f);
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (expert(j, i) < E) { m[i] = mine[expert(j, i)]; mine[expert(j, i)] = 0.f; }
+                        if (expert(j, i) < E) {
+                            (i & 1 ? m[i / 2].y : m[i / 2].x) = mine[expert(j, i)];
+                            mine[expert(j, i)] = 0.f;
+                        }
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) d[i] = fmaf(v[j][i], g[j][i] + shift, m[i]);
-            if (!on) d[0] = d[1] = d[2] = d[3] = 0.f;
+            for (int i = 0; i < 2; ++i) m[i] = fma2(v[j][i], add2(g[j][i], make_float2(shift, shift)), m[i]);
+            const float d[4] = {m[0].x, m[0].y, m[1].x, m[1].y};
             if (in_range) group_store4<T, L, V>(out, j, l, E, d);
         }
-        __syncwarp();
+        if constexpr (!V) __syncwarp();
     }
 }
 
@@ -798,8 +869,8 @@ cudaError_t router_typed(const RouterArgs& a, int sms, cudaStream_t st) {
 template <typename T, int L, int NG, bool V>
 cudaError_t router_grad_launch(const RouterGradArgs& a, int sms, cudaStream_t st) {
     constexpr int R = 32 / L;
-    const int64_t need = ((int64_t)a.rows + 8 * R - 1) / (8 * R), most = (int64_t)sms * (NG <= 4 ? 2 : 1);
-    const size_t smem = (size_t)8 * R * ((a.experts + 3) / 4 * 4 + 4) * 4;
+    const int64_t need = ((int64_t)a.rows + 8 * R - 1) / (8 * R), most = (int64_t)sms * kGradBlocks<T, NG>;
+    const size_t smem = grad_smem<T, L, NG, V>(a.experts);
     return launch_plain(router_grad_kernel<T, L, NG, V>, dim3((unsigned)(need < most ? need : most)), dim3(256), smem, st, a);
 }
 // Sixteen experts for a lane where a row has as many; a row for a whole warp beyond 256.
@@ -818,9 +889,13 @@ cudaError_t router_init() {
     if (e == cudaSuccess) e = init_all(kManyWarps<2> * kTileRows * many_pitch(256) * 4, router_many_kernel<T, V, 2>);
     if (e == cudaSuccess) e = init_all(kManyWarps<4> * kTileRows * many_pitch(512) * 4, router_many_kernel<T, V, 4>);
     if (e != cudaSuccess) return e;
-    return init_all(0, router_kernel<T, 1, V>, router_kernel<T, 2, V>, router_kernel<T, 4, V>, router_kernel<T, 8, V>, router_grad_kernel<T, 4, 2, V>,
-                    router_grad_kernel<T, 8, 4, V>, router_grad_kernel<T, 16, 4, V>, router_grad_kernel<T, 32, 4, V>,
-                    router_grad_kernel<T, 32, 8, V>);
+    e = init_all(0, router_kernel<T, 1, V>, router_kernel<T, 2, V>, router_kernel<T, 4, V>, router_kernel<T, 8, V>);
+    if (e == cudaSuccess) e = init_all(grad_smem<T, 4, 2, V>(32), router_grad_kernel<T, 4, 2, V>);
+    if (e == cudaSuccess) e = init_all(grad_smem<T, 8, 4, V>(128), router_grad_kernel<T, 8, 4, V>);
+    if (e == cudaSuccess) e = init_all(grad_smem<T, 16, 4, V>(256), router_grad_kernel<T, 16, 4, V>);
+    if (e == cudaSuccess) e = init_all(grad_smem<T, 32, 4, V>(512), router_grad_kernel<T, 32, 4, V>);
+    if (e == cudaSuccess) e = init_all(grad_smem<T, 32, 8, V>(kRouterMaxExperts), router_grad_kernel<T, 32, 8, V>);
+    return e;
 }
 
 }  // namespace
