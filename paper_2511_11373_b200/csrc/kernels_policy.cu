@@ -294,9 +294,17 @@ __device__ __forceinline__ void loss_tokens(const PolicyArgs& a, int warp, int w
         return;
     }
     Inputs v = load_inputs<REF>(a, p.begin + lane * 4);
+    int live = 0, held = 0;
+    auto counts = [&]() {
+        live = __ldcg(a.totals);
+        held = __ldcg(a.totals + 1);
+    };
+    if (!SECOND) counts();                                    // on their way during the search
     int first = find_sequence(a.seq_off, 0, a.seqs, p.begin), of = -1;      // of: the sequence of share and seq_adv
-    if (SECOND) pdl_wait();
-    const int live = __ldcg(a.totals), held = __ldcg(a.totals + 1);
+    if (SECOND) {
+        pdl_wait();
+        counts();
+    }
     const float log_low = (float)a.log_low, log_high = (float)a.log_high;
     double share = 0.;
     float seq_adv = 0.f;
