@@ -345,6 +345,26 @@ def test_rotations_match_the_formula(n, hq, hk, dim, rotary, layout):
             assert binding.mars_rope(rope, positions, same, same, inverse=inverse) == 0 and torch.equal(same, o)
 
 
+@pytest.mark.parametrize("n,hq,hk,dim,t", [(9001, 32, 4, 128, B), (5003, 37, 3, 64, H), (3001, 20, 0, 90, F), (70001, 5, 1, 64, B)])
+def test_rotations_of_many_rows(n, hq, hk, dim, t):
+    """One, two and three rounds of heads for a thread, heads left over among them."""
+    for layout in ("half", "interleaved"):
+        g = gen(n)
+        rope = binding.Rope(dim // 2 * 2, theta=1e4, layout=layout, device=DEV)
+        positions = torch.randint(0, 1 << 15, (n,), generator=g, device=DEV, dtype=torch.int32)
+        for h in (hq, hk):
+            if h:
+                x = normal(g, n, h, dim).to(t)
+                o = torch.empty_like(x)
+                other = normal(g, n, hq + hk - h, dim).to(t) if hk else None
+                back = torch.empty_like(other) if hk else None
+                assert binding.mars_rope(rope, positions, x, o, other, back) == 0
+                for got, src in ((o, x), (back, other)):
+                    if src is not None:
+                        want, tol = rope_reference(src, positions, rope.frequencies(), dim // 2 * 2, layout, 1.0, False)
+                        assert worst(got, want, tol) <= 1
+
+
 @pytest.mark.parametrize("scaling", ["none", "linear", "base", "parts"])
 def test_far_positions_keep_their_angles(scaling):
     """The largest and smallest positions, against cosines of a reduced angle in whole-number arithmetic."""
@@ -643,6 +663,34 @@ def test_gradient_of_choices_that_are_not_the_routers():
     push = w * (dw.double() - (w * dw.double()).sum(1, keepdim=True))
     want = torch.zeros(3, 12, dtype=torch.float64, device=DEV).scatter_add_(1, idx.clamp(0, 11).long(), torch.where(keep, push, 0.0))
     assert float((d.double() - want).abs().max()) <= 256 * V * float(dw.abs().max())
+
+
+@pytest.mark.parametrize("E,k,t", [(20, 3, F), (32, 8, B), (61, 5, H), (128, 8, B), (128, 12, F), (200, 8, H), (384, 6, F), (600, 4, B), (602, 10, F)])
+def test_router_gradient_of_many_rows(E, k, t):
+    """More rows than are on their way at once, rows that take no part among them, in place of the logits as well."""
+    n = 60011
+    train = binding.Train(max_experts=E, device=DEV)
+    z = router_logits(n, E, t, seed=E, pad=4)
+    live = torch.rand(n, generator=gen(2), device=DEV) < 0.9
+    z[~live] = math.nan
+    got = run_router(train, z, k, live, True)
+    dw = normal(gen(5), n, k)
+    dw[~live] = math.nan
+    check_router_grad(train, z, k, got, dw, True, 0.7, 0.03)
+    d, same = torch.empty(n, E, dtype=t, device=DEV), z.clone()
+    assert binding.mars_router_grad(train, z, got["idx"], got["lse"], got["counts"], d, d_weights=dw, balance_coef=0.7) == 0
+    assert binding.mars_router_grad(train, same, got["idx"], got["lse"], got["counts"], same, d_weights=dw, balance_coef=0.7) == 0
+    assert torch.equal(same, d)
+    # one expert twice: as if it were chosen once with the mean of both gradients and twice the weight
+    twice, once = got["idx"][:, :1].repeat(1, 2), got["idx"][:, :1].contiguous()
+    pair, mean = dw[:, :2].contiguous(), dw[:, :2].double().sum(1, keepdim=True).float()
+    a, b = (torch.empty(n, E, dtype=t, device=DEV) for _ in range(2))
+    assert binding.mars_router_grad(train, z, twice, got["lse"], got["counts"], a, d_weights=pair, renormalise=False) == 0
+    assert binding.mars_router_grad(train, z, once, got["lse"], got["counts"], b, d_weights=mean, renormalise=False) == 0
+    # both are p_j ([chosen] sum of dw - p sum of dw) of the same exponentials: some ten roundings of terms of at most |dw1| + |dw2|, and
+    # each result's own
+    size = pair.double().abs().sum(1, keepdim=True).nan_to_num() * 16 * V
+    assert worst(a, b.double(), rounded(t, b.double(), size) + U[t] * b.double().abs() + 1e-45) <= 1
 
 
 @pytest.mark.parametrize("E,k", [(16, 1), (128, 2), (128, 8)])
