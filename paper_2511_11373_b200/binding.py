@@ -750,12 +750,13 @@ def _heads(t: torch.Tensor, name: str, dtype, train, shape, row: int) -> int:
 
 
 def _norm_form(train: Train, kind: int, x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor, eps: float, heads: int, width: int):
+    eps = float(eps)                                       # a tensor would be found again by what it is, not by what it holds
     key = (kind, width, heads, x.dtype, y.dtype, weight.dtype, eps)
     form = train._forms.get(key)
     if form is None:
         if len(train._forms) >= 256:
             train._forms.clear()
-        form = mars_norm_t(kind, width, heads, MARS_TYPES[x.dtype], MARS_TYPES[y.dtype], MARS_TYPES[weight.dtype], float(eps), 0)
+        form = mars_norm_t(kind, width, heads, MARS_TYPES[x.dtype], MARS_TYPES[y.dtype], MARS_TYPES[weight.dtype], eps, 0)
         form = train._forms[key] = (byref(form), form)
     return form[0]
 
@@ -975,12 +976,13 @@ def mars_policy_loss(train: Train, logprobs: torch.Tensor, old_logprobs: torch.T
     if reduce not in POLICY_REDUCE:
         raise ValueError(f"reduce: one of {tuple(POLICY_REDUCE)}")
     n, seqs, f32, i32 = logprobs.shape[0], seq_off.shape[0] - 1, torch.float32, torch.int32
+    clip_low, clip_high, kl_coef, scale, per_token = float(clip_low), float(clip_high), float(kl_coef), float(scale), bool(per_token)
     key = (clip_low, clip_high, kl_coef, scale, reduce, per_token)
     form = train._forms.get(key)
     if form is None:
         if len(train._forms) >= 256:
             train._forms.clear()
-        form = mars_policy_t(clip_low, clip_high, kl_coef, scale, POLICY_REDUCE[reduce], int(bool(per_token)))
+        form = mars_policy_t(clip_low, clip_high, kl_coef, scale, POLICY_REDUCE[reduce], int(per_token))
         form = train._forms[key] = (byref(form), form)
     return lib().mars_policy_loss(train.handle, train._stream(stream), form[0], n, seqs, _vector(seq_off, "seq_off", i32, train, seqs + 1),
                                   _vector(targets, "targets", i32, train, n), _vector(logprobs, "logprobs", f32, train, n),

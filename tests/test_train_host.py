@@ -241,3 +241,40 @@ def test_the_binding_refuses_tensors_of_another_kind():
         a = dict(ok, **bad)
         with pytest.raises(ValueError):
             binding.mars_policy_loss(f, a["lp"], a["old"], a["adv"], a["t"], a["off"], a["stats"], **kw)
+
+
+class Passed:                                             # stands for the library: what a call passes on
+    def __init__(self):
+        self.forms = []
+
+    def __getattr__(self, name):
+        def call(handle, stream, form, *rest):
+            self.forms.append({n: getattr(form._obj, n) for n, _ in form._obj._fields_})
+            return 0
+        return call
+
+
+@pytest.mark.parametrize("name", ["clip_low", "clip_high", "kl_coef", "scale"])
+def test_a_coefficient_that_changes_in_place_is_read_again(monkeypatch, name):
+    passed, f, z = Passed(), Fake(), torch.zeros
+    f._forms = {}
+    monkeypatch.setattr(binding, "lib", lambda: passed)
+    coef, lp = torch.tensor(0.25, dtype=torch.float64), z(4)
+    args = (lp, lp, z(2), z(4, dtype=torch.int32), z(3, dtype=torch.int32), z(6))
+    for value in (0.25, 0.5, 0.5, 0.125):
+        coef.fill_(value)
+        assert binding.mars_policy_loss(f, *args, ref_logprobs=lp, **{name: coef}) == 0
+        assert passed.forms[-1][name] == value
+    assert binding.mars_policy_loss(f, *args, ref_logprobs=lp, **{name: 0.125}) == 0
+    assert passed.forms[-1] == passed.forms[-2] and len(f._forms) == 3          # a number and a tensor of its value are one form
+
+
+def test_an_epsilon_that_changes_in_place_is_read_again(monkeypatch):
+    passed, f, z = Passed(), Fake(), torch.zeros
+    f._forms = {}
+    monkeypatch.setattr(binding, "lib", lambda: passed)
+    eps = torch.tensor(0.25)
+    for value in (0.25, 0.5, 0.125):
+        eps.fill_(value)
+        assert binding.mars_norm(f, 0, z(4, 8), z(8), eps, z(4, 8)) == 0
+        assert passed.forms[-1]["eps"] == value
