@@ -975,6 +975,8 @@ def mars_policy_loss(train: Train, logprobs: torch.Tensor, old_logprobs: torch.T
     "tokens", "sequences" or "sum".  Returns the status code."""
     if reduce not in POLICY_REDUCE:
         raise ValueError(f"reduce: one of {tuple(POLICY_REDUCE)}")
+    if not isinstance(logprobs, torch.Tensor) or logprobs.dim() != 1 or not isinstance(seq_off, torch.Tensor) or seq_off.dim() != 1:
+        raise ValueError("logprobs: expected [n]; seq_off: expected [n_seqs + 1]")
     n, seqs, f32, i32 = logprobs.shape[0], seq_off.shape[0] - 1, torch.float32, torch.int32
     clip_low, clip_high, kl_coef, scale, per_token = float(clip_low), float(clip_high), float(kl_coef), float(scale), bool(per_token)
     key = (clip_low, clip_high, kl_coef, scale, reduce, per_token)

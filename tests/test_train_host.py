@@ -278,3 +278,20 @@ def test_an_epsilon_that_changes_in_place_is_read_again(monkeypatch):
         eps.fill_(value)
         assert binding.mars_norm(f, 0, z(4, 8), z(8), eps, z(4, 8)) == 0
         assert passed.forms[-1]["eps"] == value
+
+
+@pytest.mark.parametrize("wrong", [None, [0.0, 0.0, 0.0, 0.0], 1.5, torch.tensor(0.0), torch.tensor(0, dtype=torch.int32)], ids=["none", "list", "number", "fp32", "int32"])
+def test_arguments_that_are_no_tensors_of_a_call(wrong):
+    """Whatever stands in a tensor's place, the refusal is the same."""
+    f, z = Fake(), torch.zeros
+    lp, i32 = z(4), torch.int32
+    calls = [(binding.mars_policy_loss, [f, lp, lp, z(2), z(4, dtype=i32), z(3, dtype=i32), z(6)], range(1, 7)),
+             (binding.mars_norm, [f, 0, z(4, 8), z(8), 1e-6, z(4, 8)], (2, 3, 5)),
+             (binding.mars_norm_grad, [f, 0, z(4, 8), z(4, 8), z(8), z(4), z(4, 8)], (2, 3, 4, 5, 6)),
+             (binding.mars_rope, [f, z(4, dtype=i32), z(4, 2, 8), z(4, 2, 8)], (1, 2, 3)),
+             (binding.mars_router, [f, z(4, 8), z(4, 2, dtype=i32), z(4, 2)], (1, 2, 3)),
+             (binding.mars_router_grad, [f, z(4, 8), z(4, 2, dtype=i32), z(4), z(8, dtype=i32), z(4, 8)], range(1, 6))]
+    for call, args, places in calls:
+        for at in places:
+            with pytest.raises(ValueError):
+                call(*args[:at], wrong, *args[at + 1:])
