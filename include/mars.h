@@ -551,7 +551,7 @@ MARS_API mars_status_t mars_norm_grad(mars_train_t *train, void *cuda_stream, co
  *   MARS_ROPE_BASE    with theta factor^(rotary / (rotary - 2)) for theta (rotary > 2)
  *   MARS_ROPE_PARTS   by how often a pair turns over trained_positions: from `fast` turns on unchanged, up to `slow` turns
  *                     divided by factor, between them blended linearly in the number of turns (0 <= slow < fast)
- * Angles are taken in fp64.  mars_rope_frequencies writes the rotary / 2 frequencies to HOST memory.  The handle keeps them
+ * Angles are taken in fp64, from frequencies that are rounded to it once.  mars_rope_frequencies writes the rotary / 2 frequencies to HOST memory.  The handle keeps them
  * in `workspace` (device memory, 256-byte aligned, mars_rope_bytes(form)); any number of calls may use it at once.
  * mars_rope turns q [n_tokens][q_heads][head_dim] and, where k_heads > 0, k [n_tokens][k_heads][head_dim] (row strides ld, heads
  * next to each other; q and k may be columns of one projection) by positions [n_tokens] (device, any int32); inverse != 0

@@ -1,5 +1,6 @@
 // Host side of the operators of a training pass: argument checks, workspace layout, launches.
 #include <cmath>
+#include <limits>
 #include <new>
 
 #include "api_common.h"
@@ -222,20 +223,30 @@ static bool rope_form_ok(const mars_rope_form_t* f) {
            f->fast > f->slow && std::isfinite(f->fast);
 }
 
-mars_status_t mars_rope_frequencies(const mars_rope_form_t* f, double* out) {
-    if (!rope_form_ok(f) || !out) return MARS_ERR_INVALID_ARG;
-    const double d = f->rotary;
-    const double theta = f->scaling == MARS_ROPE_BASE ? f->theta * std::pow(f->factor, d / (d - 2.)) : f->theta;
+// The frequencies in 64 bits of mantissa, so that what is kept of them (angles for one position, turns for one position) is rounded once: in
+// fp64 the exponent's rounding alone, times ln theta, is several steps.
+static constexpr long double kTwoPi = 6.283185307179586476925286766559L;
+static_assert(std::numeric_limits<long double>::digits >= 64, "frequencies need more bits than fp64 has");
+static void long_frequencies(const mars_rope_form_t* f, long double* out) {
+    const long double d = f->rotary, factor = f->factor;
+    const long double theta = f->scaling == MARS_ROPE_BASE ? f->theta * std::pow(factor, d / (d - 2)) : f->theta;
     for (int i = 0; i < f->rotary / 2; ++i) {
-        double v = std::pow(theta, -2. * i / d);
-        if (f->scaling == MARS_ROPE_LINEAR) v /= f->factor;
+        long double v = std::pow(theta, -2 * i / d);
+        if (f->scaling == MARS_ROPE_LINEAR) v /= factor;
         if (f->scaling == MARS_ROPE_PARTS) {
-            const double turns = f->trained_positions * v / 6.283185307179586477;
-            const double keep = std::fmin(1., std::fmax(0., (turns - f->slow) / (f->fast - f->slow)));
-            v *= keep + (1. - keep) / f->factor;
+            const long double turns = f->trained_positions * v / kTwoPi;
+            const long double keep = std::fmin(1.L, std::fmax(0.L, (turns - f->slow) / ((long double)f->fast - f->slow)));
+            v *= keep + (1 - keep) / factor;
         }
         out[i] = v;
     }
+}
+
+mars_status_t mars_rope_frequencies(const mars_rope_form_t* f, double* out) {
+    if (!rope_form_ok(f) || !out) return MARS_ERR_INVALID_ARG;
+    long double table[256];
+    long_frequencies(f, table);
+    for (int i = 0; i < f->rotary / 2; ++i) out[i] = (double)table[i];
     return MARS_OK;
 }
 
@@ -243,10 +254,11 @@ size_t mars_rope_bytes(const mars_rope_form_t* f) { return rope_form_ok(f) ? ali
 
 mars_status_t mars_rope_create(const mars_rope_form_t* f, void* workspace, size_t workspace_bytes, mars_rope_t** out) {
     if (!rope_form_ok(f) || !workspace || !out || (uintptr_t)workspace % 256 || workspace_bytes < mars_rope_bytes(f)) return MARS_ERR_INVALID_ARG;
+    long double frequency[256];
     double table[256];
-    RUN(mars_rope_frequencies(f, table));
+    long_frequencies(f, frequency);
     for (int i = 0; i < f->rotary / 2; ++i) {
-        table[i] /= 6.283185307179586477;
+        table[i] = (double)(frequency[i] / kTwoPi);
         if (!std::isfinite(table[i])) return MARS_ERR_INVALID_ARG;
     }
     int dev = 0, sms = 0;

@@ -1,4 +1,7 @@
-"""Shared test helpers: small model shapes and an oracle-side runner (CPU only)."""
+"""Shared test helpers: small model shapes and an oracle-side runner (CPU only); the rotation's
+frequencies with 60 digits."""
+from decimal import Decimal, localcontext
+
 import torch
 
 import oracle
@@ -23,3 +26,25 @@ def fresh_cache(model, n_pages, page_size, seed=0, fill=True):
 def rel_l2(a: torch.Tensor, b: torch.Tensor) -> float:
     a, b = a.double(), b.double()
     return float((a - b).norm() / b.norm().clamp_min(1e-30))
+
+
+TWO_PI = Decimal("6.28318530717958647692528676655900576839433879875021164194988918")
+
+
+def exact_frequencies(rotary, scaling, theta, factor=8.0, trained=32768.0, fast=32.0, slow=1.0):
+    """The frequencies with 60 digits."""
+    with localcontext() as ctx:
+        ctx.prec = 60
+        d, theta, factor, trained, fast, slow = (Decimal(v) for v in (rotary, theta, factor, trained, fast, slow))
+        if scaling == 2:
+            theta *= factor ** (d / (d - 2))
+        out = []
+        for i in range(rotary // 2):
+            v = theta ** (-2 * i / d)
+            if scaling == 1:
+                v /= factor
+            if scaling == 3:
+                keep = min(Decimal(1), max(Decimal(0), (trained * v / TWO_PI - slow) / (fast - slow)))
+                v *= keep + (1 - keep) / factor
+            out.append(v)
+        return out

@@ -6,10 +6,12 @@ Tolerances are bounds from the arithmetic, evaluated on each test's own inputs. 
 c V times the sum of the absolute terms; chains here are 32 values of a thread and the 5 + 16 joins of its block at most.
 """
 import math
+from decimal import localcontext
 
 import pytest
 import torch
 
+from helpers import TWO_PI, exact_frequencies
 from paper_2511_11373_b200 import binding
 
 pytestmark = pytest.mark.gpu
@@ -1208,3 +1210,27 @@ def test_handles_refuse_what_they_were_not_made_for():
     rope = binding.Rope(64, device=DEV)
     q = torch.zeros(4, 1, 32, device=DEV)
     assert binding.mars_rope(rope, torch.zeros(4, device=DEV, dtype=torch.int32), q, q) == 1
+
+
+# ------------------------------------------------------------------------- what the tests above leave out
+
+@pytest.mark.parametrize("scaling", ["none", "linear", "base", "parts"])
+def test_far_angles_against_frequencies_of_60_digits(scaling):
+    """Neither the frequencies nor the turns of the library: both from theta, the exponent and the scaling."""
+    rotary, half = 96, 48
+    rope = binding.Rope(rotary, theta=5e5, scaling=scaling, factor=8.0, trained_positions=32768, device=DEV)
+    positions = [0, 1, -1, 40_000, 131_071, 1_000_003, 2 ** 31 - 1, -2 ** 31]
+    x = torch.zeros(len(positions), 1, rotary, device=DEV)
+    x[..., :half] = 1                                            # (1, 0) turns to (cos, sin)
+    out = torch.empty_like(x)
+    assert binding.mars_rope(rope, torch.tensor(positions, dtype=torch.int32, device=DEV), x, out) == 0
+    out = out[:, 0].cpu().tolist()
+    with localcontext() as ctx:
+        ctx.prec = 60
+        for j, f in enumerate(exact_frequencies(rotary, ["none", "linear", "base", "parts"].index(scaling), 5e5)):
+            for i, p in enumerate(positions):
+                turns = p * f / TWO_PI
+                angle = 2 * math.pi * float(turns - turns.to_integral_value())
+                # half a step of the table's entry (2^-58 for its chain) and of the product; the fraction in fp32 and the functions 2^-22
+                e = 2.0 ** -22 + 2 * math.pi * abs(float(turns)) * (2.0 ** -52 + 2.0 ** -58)
+                assert abs(out[i][j] - math.cos(angle)) <= e and abs(out[i][half + j] - math.sin(angle)) <= e, (p, j)

@@ -2,10 +2,12 @@
 rotation's frequencies and the binding's checks of tensors."""
 import ctypes
 import math
+from decimal import Decimal
 
 import pytest
 import torch
 
+from helpers import exact_frequencies
 from paper_2511_11373_b200 import binding
 
 A = 1 << 20                                              # a made-up address, aligned to everything
@@ -295,3 +297,16 @@ def test_arguments_that_are_no_tensors_of_a_call(wrong):
         for at in places:
             with pytest.raises(ValueError):
                 call(*args[:at], wrong, *args[at + 1:])
+
+
+@pytest.mark.parametrize("rotary", [2, 80, 96, 128, 510])
+@pytest.mark.parametrize("scaling", [0, 1, 2, 3])
+@pytest.mark.parametrize("theta", [1e4, 1e6, 5e5])
+def test_frequencies_are_rounded_once(lib, rotary, scaling, theta):
+    if scaling == 2 and rotary == 2:
+        return
+    got = binding.rope_frequencies(rope_form(rotary=rotary, scaling=scaling, theta=theta, factor=8.0, trained=32768.0))
+    for g, want in zip(got.tolist(), exact_frequencies(rotary, scaling, theta)):
+        # half a step of fp64 and, in steps of 2^-64 of the value: ln theta <= 17 for the rounded exponent, the power, a product and a
+        # quotient, some 24; by parts the blend has as much again from the turns, 64 in all
+        assert abs(Decimal(g) - want) <= want * (Decimal(2) ** -53 + Decimal(2) ** -58)
