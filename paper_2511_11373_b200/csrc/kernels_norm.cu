@@ -499,10 +499,11 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 2 : 1) norm_grad_
     }
 }
 
-__device__ __forceinline__ void store_any(void* p, int type, int64_t i, float v) {
-    if (type == 0) static_cast<float*>(p)[i] = v;
-    else if (type == 1) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
-    else static_cast<__half*>(p)[i] = __float2half_rn(v);
+// Rounded once: over fp32, a sum next to the middle between two numbers of 16 bits would lose what decides.
+__device__ __forceinline__ void store_any(void* p, int type, int64_t i, double v) {
+    if (type == 0) static_cast<float*>(p)[i] = (float)v;
+    else if (type == 1) static_cast<__nv_bfloat16*>(p)[i] = __double2bfloat16(v);
+    else static_cast<__half*>(p)[i] = __double2half(v);
 }
 // dw (block row 0) and db (row 1): the blocks' sums of 32 columns, 32 runs of blocks side by side.  7 us for 296 x 2048, most of it launch
 // and two chains of loads; the last block of the kernel before would have 2.4 MB to read alone.
@@ -524,7 +525,7 @@ __global__ void __launch_bounds__(1024) norm_columns_kernel(const float* part_w,
         t = 0.;
         for (int i = 0; i < 32; ++i) t += s[i][threadIdx.x];
         if (accumulate) t += (double)load_any(out, type, c);
-        store_any(out, type, c, (float)t);
+        store_any(out, type, c, t);
     }
 }
 

@@ -1234,3 +1234,24 @@ def test_far_angles_against_frequencies_of_60_digits(scaling):
                 # half a step of the table's entry (2^-58 for its chain) and of the product; the fraction in fp32 and the functions 2^-22
                 e = 2.0 ** -22 + 2 * math.pi * abs(float(turns)) * (2.0 ** -52 + 2.0 ** -58)
                 assert abs(out[i][j] - math.cos(angle)) <= e and abs(out[i][half + j] - math.sin(angle)) <= e, (p, j)
+
+
+@pytest.mark.parametrize("t", [B, H])
+@pytest.mark.parametrize("width", [128, 1111, 2048, 8192])
+@pytest.mark.parametrize("kind", [RMS, LAYER])
+def test_weight_gradients_are_rounded_once(kind, width, t):
+    """Sums next to the middle between two numbers of 16 bits: what decides is far below fp32's last bit."""
+    train = binding.Train(max_width=width, device=DEV)
+    n, u = 4096, U[t]                                            # the three rows that are not zeros lie in blocks of their own
+    x, w, ones = torch.ones(n, width, device=DEV), torch.ones(width, device=DEV), torch.ones(n, device=DEV)
+    mean = torch.zeros(n, device=DEV) if kind == LAYER else None
+    for sign, parts, want in ((1, (1.0, u, 2.0 ** -40), 1 + 2 * u), (-1, (1 + 2 * u, u, -2.0 ** -40), 1 + 2 * u)):
+        for accumulate in (False, True):
+            dy = torch.zeros(n, width, device=DEV)
+            dy[n // 2], dy[n - 1] = sign * parts[1], sign * parts[2]
+            dw = torch.full((width,), sign * parts[0], device=DEV, dtype=t) if accumulate else torch.full((width,), 77.0, device=DEV, dtype=t)
+            if not accumulate:
+                dy[0] = sign * parts[0]
+            db = dw.clone() if kind == LAYER else None
+            assert binding.mars_norm_grad(train, kind, dy, x, w, ones, torch.empty_like(x), dw, mean=mean, db=db, accumulate=accumulate) == 0
+            assert (dw.double() == sign * want).all() and (db is None or torch.equal(db, dw)), (dw[0], sign * want)
