@@ -558,6 +558,16 @@ __global__ void __launch_bounds__(kManyWarps<kColumns> * 32, 1) router_many_kern
             }
             m = val[0];
         }
+        // Nothing above -inf, or a NaN: the maxima of the fours pass over it, and with more than 64 experts its four need not be among the eight.
+        if (__any_sync(0xffffffffu, on && m == -INFINITY)) {
+            bool nan = false;
+            for (int c = first; c < min(fours, first + half / 4); ++c) {
+                const float4 v = *reinterpret_cast<const float4*>(mine + c * 4);
+                nan = nan || v.x != v.x || v.y != v.y || v.z != v.z || v.w != v.w;
+            }
+            nan = __shfl_xor_sync(0xffffffffu, nan, 16) || nan;
+            if (nan && m == -INFINITY) m = NAN;               // and so all that follows
+        }
         on = on && !(m == -INFINITY);                         // a row without a logit above -inf takes no part
         __syncwarp();                                         // a half's exponentials take the place of what the other may still look at
         const int end = min(fours, first + half / 4);

@@ -1255,3 +1255,24 @@ def test_weight_gradients_are_rounded_once(kind, width, t):
             db = dw.clone() if kind == LAYER else None
             assert binding.mars_norm_grad(train, kind, dy, x, w, ones, torch.empty_like(x), dw, mean=mean, db=db, accumulate=accumulate) == 0
             assert (dw.double() == sign * want).all() and (db is None or torch.equal(db, dw)), (dw[0], sign * want)
+
+
+@pytest.mark.parametrize("E,k", [(8, 8), (64, 4), (65, 8), (128, 8), (200, 3), (512, 8)])
+@pytest.mark.parametrize("t", [F, B, H])
+def test_a_nan_beside_nothing_but_minus_infinity(E, k, t):
+    """Neither of few nor of many rows is such a row one without logits: its weights and the sums are NaN, its choices different experts."""
+    train = binding.Train(max_experts=E, device=DEV)
+    for n in (70, 8200):
+        for at in (0, E // 2, E - 1):
+            for sign in (math.nan, -math.nan):
+                z = router_logits(n, E, t, seed=1)
+                want = run_router(train, z, k)
+                z[n - 3] = -math.inf
+                z[n - 3, at] = sign
+                got = run_router(train, z, k)
+                assert got["w"][n - 3].isnan().all() and got["lse"][n - 3].isnan() and got["sums"].isnan().all() and got["losses"].isnan().all()
+                chosen = got["idx"][n - 3].tolist()
+                assert len(set(chosen)) == k and 0 <= min(chosen) and max(chosen) < E
+                assert int(got["off"][-1]) == n * k and torch.equal(got["counts"].long(), torch.bincount(got["idx"].flatten().long(), minlength=E))
+                keep = torch.arange(n, device=DEV) != n - 3
+                assert all(torch.equal(got[name][keep], want[name][keep]) for name in ("idx", "w", "lse"))
