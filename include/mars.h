@@ -579,8 +579,8 @@ MARS_API mars_status_t mars_rope(mars_rope_t *rope, void *cuda_stream, int32_t n
  *   prob_sums [n_experts]: sum of p over the rows;  losses [2]: with N rows, f_e = counts_e / (N top_k),
  *     [0] balance = n_experts sum_e f_e prob_sums_e / N (1 when even),  [1] z = sum of lse^2 / N
  * lse, counts, offsets, prob_sums and losses may be NULL.  Rows that are not live, and rows without a logit above -inf, take no part:
- * idx -1, weights and lse 0.  Logits of -inf have p = 0 and are chosen last.  A NaN in a live row makes its weights NaN and the sums
- * with it; its choices are then any top_k different experts.  top_k <= 32.
+ * idx -1, weights and lse 0.  Logits of -inf have p = 0 and are chosen last.  A NaN in a live row, beside whatever else, makes its
+ * weights NaN and the sums with it; its choices are then any top_k different experts.  top_k <= 32.
  * mars_router_grad: d_logits [n_rows][ld_d] (the type of the logits) of
  *   sum of d_weights weights + balance_coef balance + z_coef z
  * given idx, lse and counts of mars_router; the choice itself has no gradient (f_e is constant).  d_weights may be NULL.  counts may be
