@@ -1276,3 +1276,63 @@ def test_a_nan_beside_nothing_but_minus_infinity(E, k, t):
                 assert int(got["off"][-1]) == n * k and torch.equal(got["counts"].long(), torch.bincount(got["idx"].flatten().long(), minlength=E))
                 keep = torch.arange(n, device=DEV) != n - 3
                 assert all(torch.equal(got[name][keep], want[name][keep]) for name in ("idx", "w", "lse"))
+
+
+@pytest.mark.parametrize("lengths", [[3, 0, 1500, 600, 1], [700, 6000, 31, 0, 900]], ids=["short", "long"])
+@pytest.mark.parametrize("per_token", [False, True])
+@pytest.mark.parametrize("reduce", ["tokens", "sequences"])
+def test_policy_tensors_that_start_off_16_bytes(lengths, per_token, reduce):
+    """Slices of a packed batch: the same bits as from the start of an allocation."""
+    train = binding.Train(max_seqs=len(lengths), device=DEV)
+    c = policy_case(lengths, per_token=per_token, seed=5, before=3, behind=2)
+    want = run_policy(train, c, kl=0.04, reduce=reduce, per_token=per_token)
+    check_policy(c, want, kl=0.04, reduce=reduce, per_token=per_token)
+
+    def moved(v, by):
+        buf = torch.full((v.shape[0] + by,), 3, device=DEV, dtype=v.dtype)
+        buf[by:] = v
+        return buf[by:]
+
+    names = ["lp", "old", "ref", "t", "off", "adv"]
+    for off_by in [{name: by} for name in names for by in (1, 2, 3)] + [dict.fromkeys(names, 1), dict(lp=1, old=2, ref=3)]:
+        a = {name: moved(v, off_by[name]) if name in off_by else v for name, v in c.items()}
+        assert (a["lp"].data_ptr() % 16 != 0) == ("lp" in off_by)
+        stats = torch.full((7,), 77.0, device=DEV)[1:]
+        for by in (0, 1, 2):
+            room = torch.full((len(c["lp"]) + 4,), 77.0, device=DEV)
+            d = room[by:by + len(c["lp"])]
+            assert binding.mars_policy_loss(train, a["lp"], a["old"], a["adv"], a["t"], a["off"], stats, d, ref_logprobs=a["ref"], clip_low=0.2,
+                                            clip_high=0.28, kl_coef=0.04, reduce=reduce, per_token=per_token) == 0
+            assert torch.equal(stats, want["stats"]) and torch.equal(d, want["d"])
+            assert (room[:by] == 77).all() and (room[by + len(d):] == 77).all()
+
+
+@pytest.mark.parametrize("kind", [RMS, LAYER])
+@pytest.mark.parametrize("xt,yt,wt", [(B, B, B), (F, B, F), (F, F, B), (H, H, F)])
+def test_norm_weights_that_start_off_16_bytes(kind, xt, yt, wt):
+    """Rows in whole 16-byte pieces, weight and bias not."""
+    train = binding.Train(max_width=2048, device=DEV)
+    for shape in ((300, 256), (70, 2048), (40, 6, 128)):
+        c = norm_case(kind, shape, xt, yt, wt, add=True, bias=kind == LAYER)
+        for names in (("w",), ("b",), ("w", "b")):
+            a = dict(c)
+            for name in names:
+                if a[name] is not None:
+                    a[name] = torch.cat([a[name].new_full((1,), math.nan), a[name]])[1:]
+            got = run_norm(train, a, yt)
+            check_norm(a, got, yt, 0)
+            back = run_norm_grad(train, a, got["s"], got["rstd"], got["mean"])
+            check_norm_grad(a, back, got["s"], got["rstd"], got["mean"], 0)
+
+
+@pytest.mark.parametrize("n,E,k", [(8192, 8, 2), (20000, 60, 4), (40000, 128, 8), (12345, 384, 8), (9000, 128, 12), (5000, 600, 8)])
+@pytest.mark.parametrize("t", [F, B])
+def test_router_of_many_rows_gives_the_same_bits_in_every_output(n, E, k, t):
+    train = binding.Train(max_experts=E, device=DEV)
+    z = router_logits(n, E, t, seed=3)
+    live = torch.rand(n, generator=gen(2), device=DEV) < 0.9
+    want = run_router(train, z, k, live)
+    assert all(torch.isfinite(v).all() for v in want.values())
+    for _ in range(12):
+        got = run_router(train, z, k, live)
+        assert all(torch.equal(got[name], want[name]) for name in want)
