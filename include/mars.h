@@ -585,7 +585,8 @@ MARS_API mars_status_t mars_rope(mars_rope_t *rope, void *cuda_stream, int32_t n
  *   sum of d_weights weights + balance_coef balance + z_coef z
  * given idx, lse and counts of mars_router; the choice itself has no gradient (f_e is constant).  d_weights may be NULL.  counts may be
  * those of several calls added up (micro-batches): N is then that of all of them.  Rows that took no part get 0; their logits and
- * d_weights are not used.  An idx outside the experts is left out.  d_logits may take the place of logits. */
+ * d_weights are not used.  lse's rounding to fp32 does not enter the probabilities (a common offset of a row's logits changes nothing), but where lse^2
+ * passes fp32 the z loss is infinite and its gradient means nothing.  An idx outside the experts is left out.  d_logits may take the place of logits. */
 MARS_API mars_status_t mars_router(mars_train_t *train, void *cuda_stream, int32_t n_rows, int32_t n_experts, int32_t top_k,
                                    const void *logits, int64_t ld, int32_t type, const uint8_t *live, int32_t renormalise, int32_t *idx,
                                    float *weights, float *lse, int32_t *counts, int32_t *offsets, float *prob_sums, float *losses);

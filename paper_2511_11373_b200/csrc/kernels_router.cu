@@ -668,6 +668,7 @@ __device__ __forceinline__ void put(float* place, float v) {
     if (before != 0.f) atomicAdd(place, before);
 }
 constexpr int kAhead = 4;
+constexpr float kNearLse = 8.f;                              // the gradient's probabilities beyond it: below
 // Blocks on an SM: three of 16-bit logits, two of fp32 (shared memory of the ring), one of more than 512 experts.
 template <typename T, int NG> constexpr int kGradBlocks = NG > 4 ? 1 : sizeof(T) == 2 ? 3 : 2;
 template <typename T, int L, int NG, bool V>
@@ -793,6 +794,20 @@ __global__ void __launch_bounds__(256, (kGradBlocks<T, NG>)) router_grad_kernel(
         float w_first = 0.f;                                  // p of this lane's first choice
         if (a.has_d_weights && on && (unsigned)first_idx < (unsigned)E) w_first = ex2((logit(first_idx) - lse) * kLog2e);
         if constexpr (!V) fetch(base + stride + sub);
+        // p = v / sum of the row's v.  That is 1 but for lse's rounding to its last bit, by which every v is off alike: 2^-22 of itself at most where
+        // |lse| < kNearLse, as much as the exponential, but 3e-5 for logits around 1000 and a factor of E where all are the lowest number.  So
+        // rows farther out are divided by it; for all of them it costs 131072 x 128 bf16 1.6 us of 24.
+        const bool far = on && !(fabsf(lse) < kNearLse);
+        float unite = 1.f;
+        if (__any_sync(0xffffffffu, far)) {
+            float2 sums = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < NG; ++j) sums = add2(sums, add2(v[j][0], v[j][1]));
+            float sum = sums.x + sums.y;
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (far) unite = __fdividef(1.f, sum);
+        }
         if (a.has_d_weights) {
             // of renormalised weights' gradients only differences count: taken from that of the first choice, a weight next to 1 keeps the
             // accuracy of what the others leave it
@@ -811,7 +826,7 @@ __global__ void __launch_bounds__(256, (kGradBlocks<T, NG>)) router_grad_kernel(
                 w_sum += __shfl_xor_sync(0xffffffffu, w_sum, o);
                 wdw += __shfl_xor_sync(0xffffffffu, wdw, o);
             }
-            const float inv = a.renormalise ? __fdividef(1.f, w_sum) : 1.f, mean = a.renormalise ? wdw * inv : 0.f;
+            const float inv = a.renormalise ? __fdividef(1.f, w_sum) : unite, mean = a.renormalise ? wdw * inv : 0.f;
             if (on && (unsigned)first_idx < (unsigned)E) put(mine + first_idx, w_first * inv * (first_dw - from - mean));
             for (int i = l + L; i < k; i += L) {
                 const int e = on ? a.idx[row * k + i] : -1;
@@ -823,7 +838,8 @@ __global__ void __launch_bounds__(256, (kGradBlocks<T, NG>)) router_grad_kernel(
         }
 #pragma unroll
         for (int o = L / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-        const float shift = zc * lse - dot;
+        // where lse^2 passes fp32 the z loss is infinite, and its part stays v lse
+        const float shift = fmaf(zc * lse, fabsf(lse) < 0x1p64f ? unite : 1.f, -dot * unite * unite);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
             float2 m[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -845,7 +861,7 @@ __global__ void __launch_bounds__(256, (kGradBlocks<T, NG>)) router_grad_kernel(
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) m[i] = fma2(v[j][i], add2(g[j][i], make_float2(shift, shift)), m[i]);
+            for (int i = 0; i < 2; ++i) m[i] = fma2(v[j][i], fma2(g[j][i], make_float2(unite, unite), make_float2(shift, shift)), m[i]);
             const float d[4] = {m[0].x, m[0].y, m[1].x, m[1].y};
             if (in_range) group_store4<T, L, V>(out, j, l, E, d);
         }

@@ -1336,3 +1336,41 @@ def test_router_of_many_rows_gives_the_same_bits_in_every_output(n, E, k, t):
     for _ in range(12):
         got = run_router(train, z, k, live)
         assert all(torch.equal(got[name], want[name]) for name in want)
+
+
+@pytest.mark.parametrize("E,k,t", [(20, 3, F), (61, 5, F), (128, 8, F), (128, 8, B), (384, 6, F), (600, 4, F)])
+@pytest.mark.parametrize("renormalise", [True, False])
+def test_router_gradient_of_logits_far_from_zero(E, k, t, renormalise):
+    """A common offset changes no probability: lse is rounded to its own last bit, the gradient is not to inherit that."""
+    for n, middle, std in ((70, 1000.0, 1.0), (9000, -4096.0, 1.0), (300, 3e5, 1.0), (500, 0.0, 16.0), (40, 1e7, 0.0)):
+        train = binding.Train(max_experts=E, device=DEV)
+        z = (router_logits(n, E, F, seed=4, std=1.0) * std + middle).to(t)
+        got = run_router(train, z, k, renormalise=renormalise)
+        dw = normal(gen(5), n, k, mean=0.5)
+        d = torch.empty_like(z)
+        cb, cz = 0.01 * n, 1e-3 * n / max(1.0, abs(middle))
+        assert binding.mars_router_grad(train, z, got["idx"], got["lse"], got["counts"], d, d_weights=dw, balance_coef=cb, z_coef=cz,
+                                        renormalise=renormalise) == 0
+        # the reference that takes lse as it is given, with the exact one in its place
+        exact = dict(got, lse=torch.logsumexp(z.double(), 1))
+        want, tol = router_grad_reference(z, k, exact, dw, renormalise, cb, cz)
+        # exponentials below the normal numbers are 0: 2^-126 times what multiplies them, |dw| <= 6 and as much of the losses
+        assert worst(d, want, rounded(t, want, tol) + 12 * 2.0 ** -126) <= 1, (n, middle, std)
+
+
+@pytest.mark.parametrize("E,k,t", [(16, 6, F), (61, 5, B), (128, 8, F), (128, 8, H), (600, 4, B)])
+@pytest.mark.parametrize("renormalise", [True, False])
+def test_router_gradient_of_rows_at_the_lowest_number(E, k, t, renormalise):
+    """All logits alike, whatever they are: every expert has a probability of 1 / E."""
+    train = binding.Train(max_experts=E, device=DEV)
+    n = 50
+    z = router_logits(n, E, t, seed=6)
+    z[7:20] = torch.finfo(t).min
+    got = run_router(train, z, k, renormalise=renormalise)
+    dw = normal(gen(5), n, k, mean=0.5)
+    d = torch.empty_like(z)
+    assert binding.mars_router_grad(train, z, got["idx"], got["lse"], got["counts"], d, d_weights=dw, balance_coef=0.5, renormalise=renormalise) == 0
+    same = z.clone()
+    same[7:20] = 0.0                                             # the same rows by another offset: lse = log E
+    want, tol = router_grad_reference(same, k, dict(got, lse=torch.logsumexp(same.double(), 1)), dw, renormalise, 0.5, 0.0)
+    assert worst(d, want, rounded(t, want, tol)) <= 1
