@@ -545,7 +545,7 @@ MARS_API mars_status_t mars_norm_grad(mars_train_t *train, void *cuda_stream, co
 
 /* Rotation of heads by their positions.  Of every head the first `rotary` values (even, 2 .. 512) are turned in pairs, (i, i + rotary / 2)
  * (MARS_ROPE_HALF, the layout of the model above) or (2i, 2i + 1) (MARS_ROPE_INTERLEAVED), by the angle position x frequency_i,
- * and multiplied by `scale`; the others pass.  frequency_i = theta^(-2i / rotary), stretched for contexts longer than those of
+ * and multiplied by `scale` (above 0 in fp32); the others pass.  frequency_i = theta^(-2i / rotary), stretched for contexts longer than those of
  * the training:
  *   MARS_ROPE_LINEAR  divided by factor
  *   MARS_ROPE_BASE    with theta factor^(rotary / (rotary - 2)) for theta (rotary > 2)

@@ -214,7 +214,7 @@ mars_status_t mars_norm_grad(mars_train_t* t, void* cuda_stream, const mars_norm
 static bool rope_form_ok(const mars_rope_form_t* f) {
     if (!f || f->rotary < 2 || f->rotary > 512 || f->rotary % 2 || (f->layout != MARS_ROPE_HALF && f->layout != MARS_ROPE_INTERLEAVED))
         return false;
-    if (!(f->theta > 0.) || !std::isfinite(f->theta) || !(f->scale > 0.) || !std::isfinite((float)f->scale)) return false;
+    if (!(f->theta > 0.) || !std::isfinite(f->theta) || !((float)f->scale > 0.f) || !std::isfinite((float)f->scale)) return false;
     if (f->scaling == MARS_ROPE_PLAIN) return true;
     if (!(f->factor > 0.) || !std::isfinite(f->factor)) return false;
     if (f->scaling == MARS_ROPE_LINEAR) return true;

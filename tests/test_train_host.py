@@ -310,3 +310,9 @@ def test_frequencies_are_rounded_once(lib, rotary, scaling, theta):
         # half a step of fp64 and, in steps of 2^-64 of the value: ln theta <= 17 for the rounded exponent, the power, a product and a
         # quotient, some 24; by parts the blend has as much again from the turns, 64 in all
         assert abs(Decimal(g) - want) <= want * (Decimal(2) ** -53 + Decimal(2) ** -58)
+
+
+def test_a_rotation_scaled_by_what_fp32_takes_for_zero_is_refused(lib):
+    for scale, ok in ((1e-50, False), (7e-46, False), (2e-45, True), (1e-30, True)):         # fp32 goes down to 1.4e-45, halves are rounded up
+        f, table = rope_form(scale=scale), (ctypes.c_double * 512)()
+        assert (lib.mars_rope_bytes(ctypes.byref(f)) > 0) == ok and (lib.mars_rope_frequencies(ctypes.byref(f), table) == 0) == ok
