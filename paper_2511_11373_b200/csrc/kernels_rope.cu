@@ -7,9 +7,9 @@
 // all heads it passes over.  Angles are in turns: position x turns in fp64 minus the nearest whole number.  The table's entries are rounded
 // once, from 64 bits, and so is the product: together they are off by 2^-52 of the number of turns (4e-11 of a turn at position 10^6, 8e-8 at
 // 2^31).  The fraction is rounded to fp32 for sincospif: 1.5e-8 of a turn, 9.4e-8 of a radian, about the error of the functions themselves.
-// Measured (B200, copy rate 6463 GB/s): 65536 tokens x 36 heads x 128 bf16 183 us, at the copy rate; 2048 tokens 10.5 us, of which the data
+// Measured (B200, copy rate 6463 GB/s): 65536 tokens x 36 heads x 128 bf16 187 us, at the copy rate; 2048 tokens 10.3 us, of which the data
 // would take 6: launch, the chain position - sines - loads, and the store.  Asking for the first heads before the sines are taken costs
-// registers: 183 -> 206 us.
+// registers, 183 -> 206 us for 65536 tokens; whether it would gain in one wave of blocks is not measured.
 #include "train.h"
 #include "train_types.cuh"
 

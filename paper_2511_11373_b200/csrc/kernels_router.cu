@@ -344,8 +344,12 @@ __global__ void __launch_bounds__(kWarpsOf<NG> * 32, NG <= 2 ? 2 : 1) router_ker
 // Bound by instructions and their latency: 136 of a warp for a row of 128 experts, where rounds over a warp take 590.  131072 x 128 fp32,
 // 8 choices: 44 us (1.5 TB/s; the rounds 117), of which 17 are there for any number of rows: one tile's chain 8, launch 3, the meeting of the
 // blocks 5.  50000 x 384: 60 us, the rounds 138.  One thread for a row took the 44 us too, with half the warps.
-// From kManyRows on: below, there is less than a tile for each warp.  fp32, rounds / this kernel: 4096 x 128 14.2 / 16.9 us, 8192 x 128
-// 20.4 / 17.8, 32768 x 128 39 / 22; 2048 x 384 20 / 26, 4096 x 384 34 / 29, 8192 x 384 46 / 30; 8192 x 16 13.8 / 15.2, 16384 x 16 18.3 / 15.5.
+// From kManyRows on, one number for all widths and so a compromise: the two meet at some 6000 rows of 128 experts, 3000 of 384 and 10000 of 16.
+// fp32, rounds / this kernel: 4096 x 128 14.2 / 16.9 us, 8192 x 128 20.4 / 17.8, 32768 x 128 39 / 22; 2048 x 384 20 / 26, 4096 x 384 34 / 29,
+// 8192 x 384 46 / 30; 8192 x 16 13.8 / 15.2, 16384 x 16 18.3 / 15.5.
+// Exponentials are ex2.approx of a product that is rounded once: off by some (max - z) 2^-23 of themselves, where expf, which the rounds
+// take, has half of it for far logits (the argument z - max is rounded in both).  expf here: 44.4 -> 47.8 us, and the weights' error against 64
+// bits goes from 6.9e-8 to 6.7e-8 of their norm (spread 1; 7.9e-8 for both at 16).
 constexpr int kManyExperts = 512, kManyK = 8, kManyRows = 8192;
 // Warps of the one block that an SM's shared memory holds: few blocks leave few sums for the last one to add.
 // COLUMNS: 128 experts each.
@@ -668,7 +672,7 @@ __device__ __forceinline__ void put(float* place, float v) {
     if (before != 0.f) atomicAdd(place, before);
 }
 constexpr int kAhead = 4;
-constexpr float kNearLse = 8.f;                              // the gradient's probabilities beyond it: below
+constexpr float kNearLse = 8.f;
 // Blocks on an SM: three of 16-bit logits, two of fp32 (shared memory of the ring), one of more than 512 experts.
 template <typename T, int NG> constexpr int kGradBlocks = NG > 4 ? 1 : sizeof(T) == 2 ? 3 : 2;
 template <typename T, int L, int NG, bool V>
@@ -678,7 +682,8 @@ constexpr int grad_smem(int experts) {
 // Gradient: L lanes have a row (so that a warp reduces several rows in one go), NG fours of experts each.  Bound by the bytes
 // that are on their way and by instructions: 131072 x 128 bf16 22 us (3.4 TB/s), fp32 26 (5.5 TB/s); without d_weights 17 and 24.  A warp
 // for a row took 600 instructions of it and 70 us; eight lanes with the next two rows in registers, two blocks on an SM, 24 and 30; the
-// weights' part added up in shared memory instead of exchanged + 1.
+// weights' part added up in shared memory instead of exchanged + 1.  Exponentials as above, and the quotients by the approximate reciprocal (two
+// steps): with expf and true quotients 22.6 -> 25.9 us for an error of 1.15e-7 instead of 1.37e-7 of the gradient's norm.
 template <typename T, int L, int NG, bool V>
 __global__ void __launch_bounds__(256, (kGradBlocks<T, NG>)) router_grad_kernel(const RouterGradArgs a) {
     constexpr int kWarps = 8, kThreads = 256, R = 32 / L;     // rows of a warp
